@@ -237,6 +237,84 @@ pic_status pic_attn_decode_noalloc(const pic_config* cfg, const pic_batch_host* 
                                    const pic_rope_table* rope, const void* q, void* o, const void* k_pool,
                                    const void* v_pool, int32_t num_blocks, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Speculative decoding.  A step drafts a tree of tokens for each request and checks all of
+ * them at once: pic_kv_append (or pic_kv_write) stores their rows in the slots behind the
+ * request's context, pic_tree_mask turns the trees' parent indices into visibility bits,
+ * pic_attn_tree attends, and pic_kv_keep moves the rows of the accepted branch to the front.
+ * A tree's token i has the mask row and the slot of row cu_rows[tree] + i.
+ * ---------------------------------------------------------------------------------- */
+
+/* Store the rows of a projection in the paged pool, rotating on the way where the pool holds
+ * rotated keys.  Row i < n:
+ *   pool[s/16][h][s%16][:] <- R_p k_new[i][h] (K), v_new[i][h] (V) for every KV head, s = slot_mapping[i];
+ *   q_out[i][h] <- R_p q[i][h] for every query head, p = positions[i]
+ * with k_prerotated = 1 (the conventional path: keys are stored rotated, and attention takes a
+ * rotated q); with k_prerotated = 0 nothing is rotated (the method's pool), positions may be
+ * NULL, and q is packed as it is.  Slots below 0 or at num_blocks * 16 and above store nothing
+ * (padding rows; their q rows are still written).  Slots must be distinct otherwise.
+ *  k_new, v_new DEVICE rows of [Hkv][D] dense elements, row i at i * stride elements;
+ *  q            DEVICE rows of [Hq][D] likewise, or NULL together with q_out;
+ *  q_out        DEVICE [n][Hq][D], dense; may be q itself if that is dense, else it must not
+ *               overlap q, k_new or v_new.
+ * Strides are at least a row and multiples of 16 bytes: the three inputs may be slices of one
+ * fused output.  cos/sin come from the exact phase, computed once per row and pair for all
+ * heads in float32; results are rounded once to cfg->dtype.  n < 2^24 per call. */
+pic_status pic_kv_append(const pic_config* cfg, void* k_pool, void* v_pool, int32_t num_blocks, const void* q,
+                         int64_t q_stride, void* q_out, const void* k_new, int64_t k_stride, const void* v_new,
+                         int64_t v_stride, const int32_t* positions, const int32_t* slot_mapping, int32_t n,
+                         void* stream);
+
+/* Visibility bits of drafted trees.  parents DEVICE [total_rows]: per token the index of its
+ * parent within its tree, an earlier token (parents[i] < i); a value outside [0, i) makes
+ * token i a root.  Tree t owns rows cu_rows[t] .. cu_rows[t+1]-1 (DEVICE [n_trees + 1]) and
+ * has at most 64 * mask_words tokens (rows past that are left as they are).
+ *  tree_mask DEVICE [total_rows][mask_words]: bit j%64 of word j/64 of row i is set if j is i
+ *            or an ancestor of i;
+ *  depth     DEVICE [total_rows] or NULL: number of ancestors (a token's logical position is
+ *            its root's plus its depth).
+ * 1 <= mask_words <= 64, n_trees < 2^16. */
+pic_status pic_tree_mask(const int32_t* parents, const int32_t* cu_rows, int32_t n_trees, int32_t total_rows,
+                         uint64_t* tree_mask, int32_t mask_words, int32_t* depth, void* stream);
+
+/* Workspace bytes of pic_attn_tree for this batch: split-KV partial results and, for more than
+ * 64 query spans, the work-group table.  The partial results of float32 calls are optional (a
+ * smaller workspace makes the call slower).  As with pic_workspace_size, a workspace belongs
+ * to one call until its kernels have run. */
+pic_status pic_tree_workspace_size(const pic_config* cfg, const pic_batch_host* batch, size_t* bytes);
+
+/* Attention of drafted tokens.  The tokens of every PIC_QUERY span are the queries, as in
+ * pic_attn_prefill (same batch, q, o, pools, workspace and rope table); each such span is one
+ * tree.  Query token i of a span that starts at sequence index s sees
+ *   every key j with w <= j < s, w being the span's window start, and
+ *   key s + j of its own span if bit j%64 of tree_mask[row of token i][j/64] is set
+ * (its own bit included: a token sees itself only if its mask says so; bits past the span are
+ * ignored).  A token that sees nothing gets zeros.  Keys and values of tokens that a query
+ * does not see, infinities and NaN included, do not change its output.
+ *  tree_mask DEVICE [total_q][mask_words], 8-byte aligned; mask_words * 64 must be at least
+ *            every query span's length. */
+pic_status pic_attn_tree(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev,
+                         const pic_rope_table* rope, const uint64_t* tree_mask, int32_t mask_words, const void* q,
+                         void* o, const void* k_pool, const void* v_pool, int32_t num_blocks, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Keep the accepted branch of every tree: for i < path_len[t], the K and V rows in the slot of
+ * token path[t][i] move to the slot of token i (all heads, bit for bit; rows are read before
+ * they are overwritten).  Tree t's tokens have the slots slot_mapping[cu_rows[t] ..
+ * cu_rows[t+1]-1].  Keys keep their rotation, if they have one: the branch's token of depth i
+ * already stands at logical position i of the tree.
+ *  path     DEVICE [n_trees][max_path], ascending within a tree (entries below i or past the tree
+ *           move nothing);
+ *  path_len DEVICE [n_trees], taken as at most max_path and the tree's length.
+ * slot_mapping DEVICE [total_rows]; a move from or to a slot outside the pool is skipped. */
+pic_status pic_kv_keep(const pic_config* cfg, void* k_pool, void* v_pool, int32_t num_blocks,
+                       const int32_t* slot_mapping, const int32_t* cu_rows, int32_t n_trees, int32_t total_rows,
+                       const int32_t* path, int32_t max_path, const int32_t* path_len, void* stream);
+
+/* Test hook: pic_plan_debug of a pic_attn_tree call. */
+pic_status pic_tree_plan_debug(const pic_config* cfg, const pic_batch_host* batch, int32_t* items, int32_t capacity,
+                               int32_t* n_items);
+
 /* Test hook: the work decomposition the prefill/decode call would launch, as
  * rows of 8 int32 {request, kv_head, first query row (flattened token*G+head
  * offset within the span), end query row, key begin, key end, span first token,

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_float, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 from typing import Optional
 
 import numpy as np
@@ -76,6 +76,16 @@ _sig = {
     "pic_plan_shape": (c_int32, [_P(pic_config), _P(pic_batch_host), c_int32, _P(c_int32)]),
     "pic_attn_decode_noalloc": (c_int32, [_P(pic_config), _P(pic_batch_host), _P(pic_batch_dev), _P(pic_rope_table),
                                           c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p]),
+    # speculative decoding
+    "pic_kv_append": (c_int32, [_P(pic_config), c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_int64,
+                                c_void_p, c_int64, c_void_p, c_void_p, c_int32, c_void_p]),
+    "pic_tree_mask": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p]),
+    "pic_tree_workspace_size": (c_int32, [_P(pic_config), _P(pic_batch_host), _P(c_size_t)]),
+    "pic_attn_tree": (c_int32, [_P(pic_config), _P(pic_batch_host), _P(pic_batch_dev), _P(pic_rope_table), c_void_p, c_int32,
+                                c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_size_t, c_void_p]),
+    "pic_kv_keep": (c_int32, [_P(pic_config), c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
+                              c_int32, c_void_p, c_void_p]),
+    "pic_tree_plan_debug": (c_int32, [_P(pic_config), _P(pic_batch_host), _P(c_int32), c_int32, _P(c_int32)]),
     # span cache (include/pic_cache.h): host only
     "pic_sha256": (c_int32, [c_void_p, c_size_t, c_void_p]),
     "pic_block_hashes": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p]),
@@ -251,6 +261,70 @@ def pic_plan_shape(cfg: pic_config, batch: HostBatch, is_decode: bool) -> dict:
     _check(_lib.pic_plan_shape(ctypes.byref(cfg), ctypes.byref(batch.c), int(is_decode), out))
     return {"attention_blocks": out[0], "merge_blocks": out[1], "groups": out[2], "upload_launches": out[3],
             "partial_slots": out[4]}
+
+
+# ------------------------------------------------------------------------------------
+# speculative decoding: rows into the cache, the tree's visibility, its attention, and the
+# accepted rows
+# ------------------------------------------------------------------------------------
+
+def _rows(t, what: str):
+    """Address and row stride (elements) of a [n][heads][D] view whose rows are dense."""
+    if t is None:
+        return None, 0
+    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+        raise ValueError(f"{what} must be [n][heads][D] with dense rows")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def pic_kv_append(cfg: pic_config, k_pool, v_pool, k_new, v_new, positions, slot_mapping, q=None, q_out=None,
+                  stream=None) -> None:
+    """k_new, v_new [n][Hkv][D] and q [n][Hq][D] may be views of one projection's output (rows
+    dense, any row stride); q_out is dense.  positions may be None for an unrotated pool."""
+    n = int(k_new.shape[0])
+    (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k_new, "k_new"), _rows(v_new, "v_new")
+    if q_out is not None and not q_out.is_contiguous():
+        raise ValueError("q_out must be dense")
+    _check(_lib.pic_kv_append(ctypes.byref(cfg), _ptr(k_pool), _ptr(v_pool), int(k_pool.shape[0]), qp, qs, _ptr(q_out), kp, ks,
+                              vp, vs, _ptr(positions), _ptr(slot_mapping), n, _stream(stream)))
+
+
+def pic_tree_mask(parents, cu_rows, mask, depth=None, stream=None) -> None:
+    """parents: int32 [rows]; cu_rows: int32 [trees + 1]; mask: int64 [rows][words] (64 bits per
+    word), depth: int32 [rows] or None -- both written."""
+    _check(_lib.pic_tree_mask(_ptr(parents), _ptr(cu_rows), int(cu_rows.shape[0]) - 1, int(parents.shape[0]), _ptr(mask),
+                              int(mask.shape[1]), _ptr(depth), _stream(stream)))
+
+
+def pic_tree_workspace_size(cfg: pic_config, batch: HostBatch) -> int:
+    out = c_size_t(0)
+    _check(_lib.pic_tree_workspace_size(ctypes.byref(cfg), ctypes.byref(batch.c), ctypes.byref(out)))
+    return out.value
+
+
+def pic_attn_tree(cfg: pic_config, batch: HostBatch, block_tables, positions, mask, q, o, k_pool, v_pool, workspace=None,
+                  table=None, stream=None) -> None:
+    """Attention of the drafted tokens (the PIC_QUERY spans); mask: int64 [query rows][words]."""
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_lib.pic_attn_tree(ctypes.byref(cfg), ctypes.byref(batch.c), ctypes.byref(_dev(block_tables, positions)),
+                              ctypes.byref(_rope(table)), _ptr(mask), int(mask.shape[1]), _ptr(q), _ptr(o), _ptr(k_pool),
+                              _ptr(v_pool), int(k_pool.shape[0]), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pic_kv_keep(cfg: pic_config, k_pool, v_pool, slot_mapping, cu_rows, path, path_len, stream=None) -> None:
+    """slot_mapping: int32 [rows] of the drafted tokens; path: int32 [trees][max_path]; path_len: int32 [trees]."""
+    _check(_lib.pic_kv_keep(ctypes.byref(cfg), _ptr(k_pool), _ptr(v_pool), int(k_pool.shape[0]), _ptr(slot_mapping),
+                            _ptr(cu_rows), int(cu_rows.shape[0]) - 1, int(slot_mapping.shape[0]), _ptr(path),
+                            int(path.shape[1]), _ptr(path_len), _stream(stream)))
+
+
+def pic_tree_plan_debug(cfg: pic_config, batch: HostBatch) -> np.ndarray:
+    n = c_int32(0)
+    _check(_lib.pic_tree_plan_debug(ctypes.byref(cfg), ctypes.byref(batch.c), None, 0, ctypes.byref(n)))
+    out = np.zeros((max(n.value, 1), 8), dtype=np.int32)
+    _check(_lib.pic_tree_plan_debug(ctypes.byref(cfg), ctypes.byref(batch.c), out.ctypes.data_as(POINTER(c_int32)), n.value,
+                                    ctypes.byref(n)))
+    return out[: n.value]
 
 
 # ------------------------------------------------------------------------------------

@@ -27,6 +27,10 @@ namespace {
 static_assert(sizeof(pic::Plan) + sizeof(pic::Args) <= 4096, "kernel arguments must stay within 4 KB");
 static_assert(sizeof(pic::KeyPlan) + sizeof(pic::Args) <= 4096, "kernel arguments must stay within 4 KB");
 static_assert(sizeof(pic::PlanUpload) <= 4096, "kernel arguments must stay within 4 KB");
+static_assert(sizeof(pic::Plan) + sizeof(pic::TreeArgs) <= 4096, "kernel arguments must stay within 4 KB");
+
+// The attention calls: what a plan is made for.
+enum class Call { kPrefill, kDecode, kTree };
 
 thread_local std::string g_error;
 
@@ -122,9 +126,11 @@ struct HostPlan {
     int merge_ways = 1;        // most thread rows that share a query head's splits in the decode merge
     int f32_waves = 0;         // waves per workgroup of the float32 kernel (float32 only)
     bool short_items = false;  // prefill of rotated keys: without the alternating kernel
+    bool tree = false;         // attention of drafted tokens
+    int tree_cols = 0;         // its blocks of 16 query rows per workgroup (bf16 only)
     pic::KeyPlan keys{};       // the rotated key copy (n = 0: keys are rotated in the attention kernel)
     bool keys_from_table = true;   // whether the copy also pays where a cos/sin table makes rotation cheap
-    int tile_rows() const { return f32_waves ? 16 * f32_waves : pic::kTileRows; }
+    int tile_rows() const { return f32_waves ? 16 * f32_waves : tree_cols ? 16 * tree_cols : pic::kTileRows; }
 };
 
 int32_t round_up(int64_t x, int64_t m) { return (int32_t)((x + m - 1) / m * m); }
@@ -162,9 +168,11 @@ bool short_items(const pic_config* c, const HostPlan& hp) {
 // Groups, their split policy and bases.  Prefill and float32 groups hold (row tile,
 // KV head, split) items.  `lean` (for a workspace without room for the rest) keeps
 // float32 keys unsplit and gives every query head of a decode merge one thread row.
-pic_status make_plan(const pic_config* c, const pic_batch_host* b, bool decode, bool lean, HostPlan& hp) {
+pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bool lean, HostPlan& hp) {
+    const bool decode = call == Call::kDecode;
     hp.groups.clear();
     hp.n_parts = 0;
+    hp.tree = call == Call::kTree;
     const int G = c->num_q_heads / c->num_kv_heads;
     std::vector<int32_t> w;
     int64_t pos_off = 0, q_row = 0;
@@ -246,9 +254,10 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, bool decode, 
             const int32_t n_rt = pic::row_tiles(g, G, tr);
             base += (int64_t)n_rt * c->num_kv_heads;
             // a row tile sees the window up to its own last token
+            // (of drafted tokens: up to the span's last)
             for (int64_t rt = 0; rt < n_rt; ++rt)
-                tiles_total += ((int64_t)g.tok0 + (std::min((rt + 1) * tr, (int64_t)g.n_tok * G) - 1) / G - g.win + tk) / tk *
-                               c->num_kv_heads;
+                tiles_total += ((int64_t)g.tok0 + (hp.tree ? g.n_tok - 1 : (std::min((rt + 1) * tr, (int64_t)g.n_tok * G) - 1) / G) -
+                                g.win + tk) / tk * c->num_kv_heads;
         }
         const int64_t chunk = !lean && base < 2 * target ? std::max<int64_t>(128 / tk, (tiles_total + target - 1) / target)
                                                        : (int64_t)INT32_MAX;
@@ -257,6 +266,26 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, bool decode, 
             const int64_t n_split = (tiles + chunk - 1) / chunk, each = (tiles + n_split - 1) / n_split;
             // no split past the end: its first key would overflow near 2^31 keys
             g.n_split = (int32_t)((tiles + each - 1) / each);
+            g.split_keys = (int32_t)std::min<int64_t>(each * tk, INT32_MAX);
+        }
+        std::stable_sort(hp.groups.begin(), hp.groups.end(), [](const pic::Group& x, const pic::Group& y) {
+            return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
+        });
+    } else if (hp.tree) {
+        // Drafted tokens: a workgroup's four waves take 64 keys at a time.  Key splits in
+        // chunks of the average work per compute unit, at least two rounds of the waves.
+        const int64_t tk = pic::kTreeWaves * pic::kBlock;
+        int64_t max_rows = 0;
+        for (auto& g : hp.groups) max_rows = std::max<int64_t>(max_rows, (int64_t)g.n_tok * G);
+        hp.tree_cols = pic::tree_cols(max_rows);
+        int64_t tiles_total = 0;
+        for (auto& g : hp.groups)
+            tiles_total += pic::row_tiles(g, G, hp.tile_rows()) * (((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk) * c->num_kv_heads;
+        const int64_t chunk = std::max<int64_t>(2, (tiles_total + pic::kTargetCUs - 1) / pic::kTargetCUs);
+        for (auto& g : hp.groups) {
+            const int64_t tiles = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
+            const int64_t n_split = (tiles + chunk - 1) / chunk, each = (tiles + n_split - 1) / n_split;
+            g.n_split = (int32_t)((tiles + each - 1) / each);   // none of them is empty
             g.split_keys = (int32_t)std::min<int64_t>(each * tk, INT32_MAX);
         }
         std::stable_sort(hp.groups.begin(), hp.groups.end(), [](const pic::Group& x, const pic::Group& y) {
@@ -396,7 +425,7 @@ WsLayout ws_layout(const pic_config* c, const HostPlan& hp) {
 // over 131,072 keys, the most: 2,271 against 1,853 us).
 void plan_keys(const pic_config* c, HostPlan& hp) {
     hp.keys.n = 0;
-    if (c->dtype != PIC_BF16 || c->k_prerotated || hp.dec_kernel) return;
+    if (c->dtype != PIC_BF16 || c->k_prerotated || hp.dec_kernel || hp.tree) return;
     const int G = c->num_q_heads / c->num_kv_heads;
     struct Run {
         int32_t req, lo, hi, pos_off;
@@ -441,8 +470,8 @@ void plan_keys(const pic_config* c, HostPlan& hp) {
 }
 
 // The plan of a call: groups with their split policy, then their bases.
-pic_status build_plan(const pic_config* c, const pic_batch_host* b, bool decode, HostPlan& hp, bool lean = false) {
-    pic_status st = make_plan(c, b, decode, lean, hp);
+pic_status build_plan(const pic_config* c, const pic_batch_host* b, Call call, HostPlan& hp, bool lean = false) {
+    pic_status st = make_plan(c, b, call, lean, hp);
     if (st) return st;
     plan_keys(c, hp);
     return assign_bases(c, hp);
@@ -451,11 +480,11 @@ pic_status build_plan(const pic_config* c, const pic_batch_host* b, bool decode,
 // The plan of a call with ws_bytes of workspace.  What a call can do without is left out
 // where it does not fit: float32 key splits (their partials) and the wider decode merges
 // (a merge block per query head, and in a large batch a map entry for each).
-pic_status build_plan_within(const pic_config* c, const pic_batch_host* b, bool decode, size_t ws_bytes, HostPlan& hp) {
-    pic_status st = build_plan(c, b, decode, hp);
+pic_status build_plan_within(const pic_config* c, const pic_batch_host* b, Call call, size_t ws_bytes, HostPlan& hp) {
+    pic_status st = build_plan(c, b, call, hp);
     if (st == PIC_OK && (c->dtype == PIC_F32 || hp.dec_kernel) && hp.n_parts > 0 && ws_layout(c, hp).need > ws_bytes) {
         hp = HostPlan{};
-        st = build_plan(c, b, decode, hp, true);
+        st = build_plan(c, b, call, hp, true);
     }
     return st;
 }
@@ -517,7 +546,8 @@ pic_status hip_status(int e, const char* what) {
 
 pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic_batch_dev* dv,
                          const pic_rope_table* rope, const void* q, void* o, const void* k_pool, const void* v_pool,
-                         int32_t num_blocks, void* ws, size_t ws_bytes, void* stream, bool decode) {
+                         int32_t num_blocks, void* ws, size_t ws_bytes, void* stream, Call call,
+                         const uint64_t* tree_mask = nullptr, int32_t mask_words = 0) {
     pic_status st = check_config(c);
     if (st) return st;
     if ((st = check_batch(b))) return st;
@@ -537,16 +567,23 @@ pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic
         return fail(PIC_EINVAL, "block tables and positions must be 4-byte aligned");
 
     HostPlan hp;
-    if ((st = build_plan_within(c, b, decode, ws == nullptr ? 0 : ws_bytes, hp))) return st;
+    if ((st = build_plan_within(c, b, call, ws == nullptr ? 0 : ws_bytes, hp))) return st;
     int64_t rows = 0;
     for (auto& g : hp.groups) rows += g.n_tok;
     if (rows == 0) return PIC_OK;
     if (!q || !o) return fail(PIC_EINVAL, "q and o must not be NULL");
+    if (hp.tree) {
+        if (tree_mask == nullptr) return fail(PIC_EINVAL, "tree_mask must not be NULL");
+        if (misaligned(tree_mask, 8)) return fail(PIC_EINVAL, "tree_mask must be 8-byte aligned");
+        for (auto& g : hp.groups)
+            if (((int64_t)g.n_tok + 63) / 64 > mask_words)
+                return fail(PIC_EINVAL, "mask_words too small for a span of " + std::to_string(g.n_tok) + " drafted tokens");
+    }
     const WsLayout wl = ws_layout(c, hp);
     if (wl.need > 0 && (ws == nullptr || ws_bytes < wl.need))
         return fail(PIC_EWORKSPACE, "workspace needs " + std::to_string(wl.need) + " bytes");
 
-    pic::Args a{};
+    pic::TreeArgs a{};
     phase_steps(c, a.fstep);
     a.chunk_map = chunk_map(c);
     a.q = q;
@@ -571,6 +608,9 @@ pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic
     a.hq = c->num_q_heads;
     a.hkv = c->num_kv_heads;
     a.group = c->num_q_heads / c->num_kv_heads;
+    a.mask = reinterpret_cast<const uint32_t*>(tree_mask);
+    a.words = 2 * mask_words;
+    a.tile_rows = hp.tile_rows();
 
     pic::Plan p;
     std::memset(&p, 0, sizeof(p));
@@ -610,6 +650,10 @@ pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic
         (st = hip_status(pic::launch_rope_keys(c->rope_style, c->head_dim, hp.keys, a, stream), "key rotation launch")))
         return st;
     const bool rope_on = c->k_prerotated == 0;
+    if (hp.tree)
+        return hip_status(c->dtype == PIC_F32 ? pic::launch_tree_f32(hp.f32_waves, c->rope_style, c->head_dim, rope_on, p, a, stream)
+                                              : pic::launch_tree(c->rope_style, c->head_dim, rope_on, p, a, stream),
+                          "tree attention launch");
     const int e = hp.dec_kernel ? pic::launch_decode(c->rope_style, c->head_dim, rope_on, p, a, stream)
                                 : pic::launch_attention(c->dtype, hp.f32_waves, hp.short_items, c->rope_style, c->head_dim, rope_on, p, a, stream);
     return hip_status(e, "attention launch");
@@ -750,7 +794,7 @@ pic_status pic_workspace_size(const pic_config* cfg, const pic_batch_host* batch
     if ((st = check_batch(batch))) return st;
     if (bytes == nullptr) return fail(PIC_EINVAL, "bytes is NULL");
     HostPlan hp;
-    if ((st = build_plan(cfg, batch, is_decode != 0, hp))) return st;
+    if ((st = build_plan(cfg, batch, is_decode != 0 ? Call::kDecode : Call::kPrefill, hp))) return st;
     *bytes = ws_layout(cfg, hp).total;
     return PIC_OK;
 }
@@ -759,14 +803,14 @@ pic_status pic_attn_prefill(const pic_config* cfg, const pic_batch_host* batch, 
                             const pic_rope_table* rope, const void* q, void* o, const void* k_pool, const void* v_pool,
                             int32_t num_blocks, void* workspace, size_t workspace_bytes, void* stream) {
     return run_attention(cfg, batch, dev, rope, q, o, k_pool, v_pool, num_blocks, workspace, workspace_bytes, stream,
-                         false);
+                         Call::kPrefill);
 }
 
 pic_status pic_attn_decode(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev,
                            const pic_rope_table* rope, const void* q, void* o, const void* k_pool, const void* v_pool,
                            int32_t num_blocks, void* workspace, size_t workspace_bytes, void* stream) {
     return run_attention(cfg, batch, dev, rope, q, o, k_pool, v_pool, num_blocks, workspace, workspace_bytes, stream,
-                         true);
+                         Call::kDecode);
 }
 
 pic_status pic_attn_decode_noalloc(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev,
@@ -776,7 +820,7 @@ pic_status pic_attn_decode_noalloc(const pic_config* cfg, const pic_batch_host* 
     if (st) return st;
     if ((st = check_batch(batch))) return st;
     HostPlan hp;
-    if ((st = build_plan_within(cfg, batch, true, pic::kScratchBytes, hp))) return st;
+    if ((st = build_plan_within(cfg, batch, Call::kDecode, pic::kScratchBytes, hp))) return st;
     const size_t need = ws_layout(cfg, hp).need;
     if (need > pic::kScratchBytes)
         return fail(PIC_EWORKSPACE, "batch needs " + std::to_string(need) + " bytes of scratch; the no-allocation "
@@ -784,18 +828,145 @@ pic_status pic_attn_decode_noalloc(const pic_config* cfg, const pic_batch_host* 
     void* ws = nullptr;
     if ((st = hip_status(pic::scratch_region(&ws), "scratch address"))) return st;
     return run_attention(cfg, batch, dev, rope, q, o, k_pool, v_pool, num_blocks, ws, pic::kScratchBytes, stream,
-                         true);
+                         Call::kDecode);
+}
+
+static pic_status plan_items(const pic_config* cfg, const pic_batch_host* batch, Call call, int32_t* items,
+                             int32_t capacity, int32_t* n_items);
+
+pic_status pic_tree_workspace_size(const pic_config* cfg, const pic_batch_host* batch, size_t* bytes) {
+    pic_status st = check_config(cfg);
+    if (st) return st;
+    if ((st = check_batch(batch))) return st;
+    if (bytes == nullptr) return fail(PIC_EINVAL, "bytes is NULL");
+    HostPlan hp;
+    if ((st = build_plan(cfg, batch, Call::kTree, hp))) return st;
+    *bytes = ws_layout(cfg, hp).total;
+    return PIC_OK;
+}
+
+pic_status pic_attn_tree(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev,
+                         const pic_rope_table* rope, const uint64_t* tree_mask, int32_t mask_words, const void* q, void* o,
+                         const void* k_pool, const void* v_pool, int32_t num_blocks, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+    if (mask_words < 0 || mask_words > INT32_MAX / 2) return fail(PIC_EINVAL, "mask_words out of range");
+    return run_attention(cfg, batch, dev, rope, q, o, k_pool, v_pool, num_blocks, workspace, workspace_bytes, stream,
+                         Call::kTree, tree_mask, mask_words);
+}
+
+pic_status pic_tree_mask(const int32_t* parents, const int32_t* cu_rows, int32_t n_trees, int32_t total_rows,
+                         uint64_t* tree_mask, int32_t mask_words, int32_t* depth, void* stream) {
+    if (n_trees < 0 || total_rows < 0) return fail(PIC_EINVAL, "n_trees and total_rows must be >= 0");
+    if (mask_words < 1 || mask_words > 64) return fail(PIC_EINVAL, "mask_words must be in [1, 64]");
+    if (n_trees > 65535) return fail(PIC_EINVAL, "n_trees must be < 2^16 per call");
+    if (n_trees == 0 || total_rows == 0) return PIC_OK;
+    if (!parents || !cu_rows || !tree_mask) return fail(PIC_EINVAL, "NULL buffer");
+    if (misaligned(tree_mask, 8)) return fail(PIC_EINVAL, "tree_mask must be 8-byte aligned");
+    if (misaligned(parents, 4) || misaligned(cu_rows, 4) || misaligned(depth, 4))
+        return fail(PIC_EINVAL, "parents, cu_rows and depth must be 4-byte aligned");
+    return hip_status(pic::launch_tree_mask(parents, cu_rows, n_trees, total_rows, tree_mask, mask_words, depth, stream),
+                      "tree mask launch");
+}
+
+// Bytes [p, p + n) and [q, q + m) share some byte.
+static bool overlap(const void* p, int64_t n, const void* q, int64_t m) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + (uintptr_t)m && b < a + (uintptr_t)n;
+}
+
+pic_status pic_kv_append(const pic_config* cfg, void* k_pool, void* v_pool, int32_t num_blocks, const void* q, int64_t q_stride,
+                         void* q_out, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                         const int32_t* positions, const int32_t* slot_mapping, int32_t n, void* stream) {
+    pic_status st = check_config(cfg);
+    if (st) return st;
+    if (n < 0 || num_blocks < 0) return fail(PIC_EINVAL, "n and num_blocks must be >= 0");
+    if (n == 0) return PIC_OK;
+    if (!k_pool || !v_pool || !k_new || !v_new || !slot_mapping) return fail(PIC_EINVAL, "NULL buffer");
+    if ((q == nullptr) != (q_out == nullptr)) return fail(PIC_EINVAL, "q and q_out must both be given or both be NULL");
+    if (cfg->k_prerotated && positions == nullptr) return fail(PIC_EINVAL, "positions must not be NULL");
+    if (num_blocks == 0) return fail(PIC_EINVAL, "empty pool");
+    const int64_t es = cfg->dtype == PIC_F32 ? 4 : 2, kv_row = (int64_t)cfg->num_kv_heads * cfg->head_dim,
+                  q_row = q ? (int64_t)cfg->num_q_heads * cfg->head_dim : 0;
+    if (n >= (1 << 24)) return fail(PIC_EINVAL, "n must be < 2^24 rows per call");
+    const int64_t most = INT64_MAX / 2 / es / n;   // elements per row whose byte offsets stay in range
+    if (k_stride < kv_row || v_stride < kv_row || (q && q_stride < q_row) || k_stride > most || v_stride > most ||
+        (q && q_stride > most))
+        return fail(PIC_EINVAL, "row strides must hold a row (and its offsets 64 bits)");
+    if (misaligned(k_pool, 16) || misaligned(v_pool, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) || misaligned(q, 16) ||
+        misaligned(q_out, 16) || misaligned(slot_mapping, 4) || misaligned(positions, 4) || k_stride * es % 16 ||
+        v_stride * es % 16 || (q && q_stride * es % 16))
+        return fail(PIC_EINVAL, "pools and rows must be 16-byte aligned, slot_mapping and positions 4-byte aligned");
+    if (q) {
+        // a row's queries may be replaced in place; anything else that shares memory would be a race
+        const int64_t out_bytes = n * q_row * es;
+        const bool in_place = q == q_out && q_stride == q_row;
+        if ((!in_place && overlap(q_out, out_bytes, q, ((n - 1) * q_stride + q_row) * es)) ||
+            overlap(q_out, out_bytes, k_new, ((n - 1) * k_stride + kv_row) * es) ||
+            overlap(q_out, out_bytes, v_new, ((n - 1) * v_stride + kv_row) * es))
+            return fail(PIC_EINVAL, "q_out overlaps an input (only a dense q may be its own q_out)");
+    }
+    pic::AppendArgs a{};
+    if (cfg->k_prerotated) {
+        phase_steps(cfg, a.fstep);
+        a.rot_half = (cfg->rotary_dim ? cfg->rotary_dim : cfg->head_dim) / 2;
+    }
+    a.q = q;
+    a.k = k_new;
+    a.v = v_new;
+    a.q_out = q_out;
+    a.k_pool = k_pool;
+    a.v_pool = v_pool;
+    a.positions = positions;
+    a.slots = slot_mapping;
+    a.q_stride = q ? q_stride * es / 16 : 0;
+    a.k_stride = k_stride * es / 16;
+    a.v_stride = v_stride * es / 16;
+    a.n_slots = (int64_t)num_blocks * pic::kBlock;
+    a.hq = q ? cfg->num_q_heads : 0;
+    a.hkv = cfg->num_kv_heads;
+    return hip_status(pic::launch_kv_append(cfg->dtype, cfg->rope_style, cfg->head_dim, n, a, stream), "kv_append launch");
+}
+
+pic_status pic_kv_keep(const pic_config* cfg, void* k_pool, void* v_pool, int32_t num_blocks, const int32_t* slot_mapping,
+                       const int32_t* cu_rows, int32_t n_trees, int32_t total_rows, const int32_t* path, int32_t max_path,
+                       const int32_t* path_len, void* stream) {
+    pic_status st = check_config(cfg);
+    if (st) return st;
+    if (num_blocks < 0 || n_trees < 0 || total_rows < 0 || max_path < 0)
+        return fail(PIC_EINVAL, "num_blocks, n_trees, total_rows and max_path must be >= 0");
+    if (n_trees == 0 || total_rows == 0 || max_path == 0) return PIC_OK;
+    if (!k_pool || !v_pool || !slot_mapping || !cu_rows || !path || !path_len) return fail(PIC_EINVAL, "NULL buffer");
+    if (num_blocks == 0) return fail(PIC_EINVAL, "empty pool");
+    if (n_trees >= (1 << 23)) return fail(PIC_EINVAL, "n_trees must be < 2^23 per call");
+    if (cfg->num_kv_heads > 65535) return fail(PIC_EUNSUPPORTED, "more than 65535 KV heads");
+    if (misaligned(k_pool, 16) || misaligned(v_pool, 16)) return fail(PIC_EINVAL, "pools must be 16-byte aligned");
+    for (const int32_t* p : {slot_mapping, cu_rows, path, path_len})
+        if (misaligned(p, 4)) return fail(PIC_EINVAL, "slot_mapping, cu_rows, path and path_len must be 4-byte aligned");
+    return hip_status(pic::launch_kv_keep(cfg->dtype, cfg->num_kv_heads, cfg->head_dim, k_pool, v_pool,
+                                          (int64_t)num_blocks * pic::kBlock, slot_mapping, cu_rows, path, path_len, n_trees,
+                                          max_path, total_rows, stream),
+                      "kv_keep launch");
 }
 
 pic_status pic_plan_debug(const pic_config* cfg, const pic_batch_host* batch, int32_t is_decode, int32_t* items,
                           int32_t capacity, int32_t* n_items) {
+    return plan_items(cfg, batch, is_decode != 0 ? Call::kDecode : Call::kPrefill, items, capacity, n_items);
+}
+
+pic_status pic_tree_plan_debug(const pic_config* cfg, const pic_batch_host* batch, int32_t* items, int32_t capacity,
+                               int32_t* n_items) {
+    return plan_items(cfg, batch, Call::kTree, items, capacity, n_items);
+}
+
+static pic_status plan_items(const pic_config* cfg, const pic_batch_host* batch, Call call, int32_t* items,
+                             int32_t capacity, int32_t* n_items) {
     pic_status st = check_config(cfg);
     if (st) return st;
     if ((st = check_batch(batch))) return st;
     if (n_items == nullptr || capacity < 0 || (capacity > 0 && items == nullptr))
         return fail(PIC_EINVAL, "bad output arguments");
     HostPlan hp;
-    if ((st = build_plan(cfg, batch, is_decode != 0, hp))) return st;
+    if ((st = build_plan(cfg, batch, call, hp))) return st;
     const int G = cfg->num_q_heads / cfg->num_kv_heads;
     int64_t n = 0;
     auto emit = [&](int32_t r, int32_t h, int32_t rl, int32_t rh, int32_t kl, int32_t kh, int32_t t0, int32_t slot) {
@@ -828,7 +999,7 @@ pic_status pic_plan_debug(const pic_config* cfg, const pic_batch_host* batch, in
                     for (int rt = 0; rt < n_rt; ++rt) {
                         const int32_t rl = rt * hp.tile_rows();
                         const int32_t rh = std::min(rl + hp.tile_rows(), g.n_tok * G);
-                        const int32_t t_last = g.tok0 + (rh - 1) / G;
+                        const int32_t t_last = hp.tree ? g.tok0 + g.n_tok - 1 : g.tok0 + (rh - 1) / G;
                         const int32_t kl = g.win + s * g.split_keys;
                         const int32_t kh = (int32_t)std::min<int64_t>((int64_t)kl + g.split_keys, t_last + 1);
                         if (kl >= kh) continue;
@@ -848,7 +1019,7 @@ pic_status pic_plan_shape(const pic_config* cfg, const pic_batch_host* batch, in
     if ((st = check_batch(batch))) return st;
     if (shape == nullptr) return fail(PIC_EINVAL, "shape is NULL");
     HostPlan hp;
-    if ((st = build_plan(cfg, batch, is_decode != 0, hp))) return st;
+    if ((st = build_plan(cfg, batch, is_decode != 0 ? Call::kDecode : Call::kPrefill, hp))) return st;
     const int64_t n = (int64_t)hp.groups.size();
     shape[0] = (int32_t)hp.n_items;
     shape[1] = (int32_t)hp.n_merge;

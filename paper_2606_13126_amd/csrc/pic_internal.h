@@ -188,6 +188,38 @@ struct Args {
     const void* k_rot;
 };
 
+// Arguments of the attention of drafted tokens: row i of the queries sees key k of its span
+// (the span's first token being key 0) if bit k of mask row i is set, and every key of
+// its window before the span.
+struct TreeArgs : Args {
+    const uint32_t* mask;     // [query rows][words], 32 keys per word
+    int32_t words;
+    int32_t tile_rows;        // query rows per workgroup
+};
+
+// bf16 attention of drafted tokens: waves of a workgroup, which take every fourth 16-key tile of
+// its key range, and column blocks of 16 query rows that each wave holds (1, 2 or 4).
+constexpr int kTreeWaves = 4;
+constexpr int tree_cols(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+
+// Rows of kv_append: strides in 16-byte chunks
+struct AppendArgs {
+    uint64_t fstep[64];
+    const void* q;
+    const void* k;
+    const void* v;
+    void* q_out;
+    void* k_pool;
+    void* v_pool;
+    const int32_t* positions;
+    const int32_t* slots;
+    int64_t q_stride, k_stride, v_stride;
+    int64_t n_slots;
+    int32_t hq;          // 0: no queries
+    int32_t hkv;
+    int32_t rot_half;    // pairs that turn (0: none)
+};
+
 // Records msg as the thread's last error (pic_last_error) and returns st.
 int32_t host_fail(int32_t st, const char* msg);
 
@@ -203,6 +235,15 @@ int launch_attention(int dtype, int f32_waves, bool short_items, int style, int 
 int launch_decode(int style, int d, bool rope, const Plan& plan, const Args& args, void* stream);
 int launch_rope_keys(int style, int d, const KeyPlan& plan, const Args& args, void* stream);
 int launch_plan_upload(const PlanUpload& up, void* stream);
+int launch_tree_f32(int f32_waves, int style, int d, bool rope, const Plan& plan, const TreeArgs& args, void* stream);
+// Launchers implemented in pic_tree.hip
+int launch_tree(int style, int d, bool rope, const Plan& plan, const TreeArgs& args, void* stream);
+int launch_tree_mask(const int32_t* parents, const int32_t* cu_rows, int n_trees, int total_rows, uint64_t* mask, int words,
+                     int32_t* depth, void* stream);
+int launch_kv_append(int dtype, int style, int d, int n, const AppendArgs& args, void* stream);
+int launch_kv_keep(int dtype, int hkv, int d, void* k_pool, void* v_pool, int64_t n_slots, const int32_t* slots,
+                   const int32_t* cu_rows, const int32_t* path, const int32_t* path_len, int n_trees, int max_path, int total_rows,
+                   void* stream);
 
 // Device scratch of the no-allocation entry point: kScratchBytes on each device,
 // shared by every call on that device.  scratch_region returns the current
