@@ -127,10 +127,10 @@ struct HostPlan {
     int f32_waves = 0;         // waves per workgroup of the float32 kernel (float32 only)
     bool short_items = false;  // prefill of rotated keys: without the alternating kernel
     bool tree = false;         // attention of drafted tokens
-    int tree_cols = 0;         // its blocks of 16 query rows per workgroup (bf16 only)
+    int tree_rows = 0;         // its query rows per workgroup (bf16 only)
     pic::KeyPlan keys{};       // the rotated key copy (n = 0: keys are rotated in the attention kernel)
     bool keys_from_table = true;   // whether the copy also pays where a cos/sin table makes rotation cheap
-    int tile_rows() const { return f32_waves ? 16 * f32_waves : tree_cols ? 16 * tree_cols : pic::kTileRows; }
+    int tile_rows() const { return f32_waves ? 16 * f32_waves : tree_rows ? tree_rows : pic::kTileRows; }
 };
 
 int32_t round_up(int64_t x, int64_t m) { return (int32_t)((x + m - 1) / m * m); }
@@ -272,16 +272,17 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
             return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
         });
     } else if (hp.tree) {
-        // Drafted tokens: a workgroup's four waves take 64 keys at a time.  Key splits in
-        // chunks of the average work per compute unit, at least two rounds of the waves.
-        const int64_t tk = pic::kTreeWaves * pic::kBlock;
+        // Drafted tokens: key splits in chunks of the average work per compute unit, at least
+        // 128 keys.
         int64_t max_rows = 0;
         for (auto& g : hp.groups) max_rows = std::max<int64_t>(max_rows, (int64_t)g.n_tok * G);
-        hp.tree_cols = pic::tree_cols(max_rows);
+        hp.tree_rows = pic::tree_rows(max_rows);
+        const int64_t tk = pic::tree_keys(hp.tree_rows);
         int64_t tiles_total = 0;
         for (auto& g : hp.groups)
             tiles_total += pic::row_tiles(g, G, hp.tile_rows()) * (((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk) * c->num_kv_heads;
-        const int64_t chunk = std::max<int64_t>(2, (tiles_total + pic::kTargetCUs - 1) / pic::kTargetCUs);
+        const int64_t chunk = std::min<int64_t>(std::max<int64_t>(128 / tk, (tiles_total + pic::kTargetCUs - 1) / pic::kTargetCUs),
+                                                (1 << 30) / tk);   // (keys of a split, counted from its start, stay in 31 bits)
         for (auto& g : hp.groups) {
             const int64_t tiles = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
             const int64_t n_split = (tiles + chunk - 1) / chunk, each = (tiles + n_split - 1) / n_split;

@@ -197,10 +197,12 @@ struct TreeArgs : Args {
     int32_t tile_rows;        // query rows per workgroup
 };
 
-// bf16 attention of drafted tokens: waves of a workgroup, which take every fourth 16-key tile of
-// its key range, and column blocks of 16 query rows that each wave holds (1, 2 or 4).
-constexpr int kTreeWaves = 4;
-constexpr int tree_cols(int64_t rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+// bf16 attention of drafted tokens: waves of a workgroup and its query rows for spans of at
+// most `rows` of them.  Up to 32 rows the waves all hold the same ones and take different cache
+// blocks; beyond, they are 2, 4 or 8 groups of 32 rows that share keys, 64 at a time.
+constexpr int kTreeWaves = 8;
+constexpr int tree_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+constexpr int tree_keys(int rows) { return rows <= 32 ? kTreeWaves * kBlock : 64; }   // keys that they take at a time
 
 // Rows of kv_append: strides in 16-byte chunks
 struct AppendArgs {

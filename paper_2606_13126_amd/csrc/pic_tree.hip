@@ -15,6 +15,7 @@ namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 // ---------------------------------------------------------------------------------
 // kv_append: one workgroup per row.  A unit is two 16-byte chunks of a head: NeoX the two
@@ -194,8 +195,8 @@ __global__ void __launch_bounds__(256) kv_keep_kernel(u32x4_t* __restrict__ k_po
     }
 }
 
-// cos/sin for bf16 entries: the hardware's sine of a fraction of a revolution (its error, about
-// 2^-20, is far below the rounding to 8 bits)
+// cos/sin by the hardware's sine of a fraction of a revolution (its error, about 2^-20, is far
+// below the 2^-12 to which the attention rounds what they turn)
 __device__ __forceinline__ void rope_cs_fast(int32_t pos, uint64_t step, float& c, float& s) {
     const uint64_t ph = (uint64_t)(int64_t)pos * step;
     const float r = (float)(int32_t)(ph >> 32) * 0x1p-32f;
@@ -203,141 +204,164 @@ __device__ __forceinline__ void rope_cs_fast(int32_t pos, uint64_t step, float& 
     s = __builtin_amdgcn_sinf(r);
 }
 
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)lo, (_Float16)hi});
+}
+
 // ---------------------------------------------------------------------------------
 // tree_bf16
 //
-// Workgroup: up to 16 CB query rows (drafted token x query head of one KV head's group) over
-// one key range.  Its four waves hold the same rows and take every fourth 16-key tile (one
-// cache block) of the range each, so that a wave reads, turns and multiplies its keys
-// without waiting for another; their results meet in LDS at the end.
-// Every read of the key loop goes straight to LDS, NST - 1 tiles ahead: K as stored, V, the
-// cos/sin rows of the tile's keys, and the positions of a later tile.  The wave turns its K
-// operand in registers and uses it for the CB column blocks:
-//   S^T (16 keys x 16 rows) = K Q^T       v_mfma_f32_16x16x32_bf16
-//   O^T (16 dims x 16 rows) += V^T P^T    v_mfma_f32_16x16x16_bf16, V^T by ds_read_b64_tr_b16
+// Workgroup: eight waves (two per SIMD, so that one's products run under the other's vector
+// work) over up to 16 CB WR query rows (drafted token x query head of one KV head's group) and
+// one key range.  The waves are WR row groups of KG = 8 / WR; a wave holds 16 CB rows.
+//   Few rows (WR = 1): a wave takes every eighth 16-key tile (one cache block) of the range, which
+//     it copies, turns and multiplies without waiting for another wave.
+//   More rows: steps of 64 keys.  Each wave copies and turns eight keys of a step, in place, one
+//     step before the row groups multiply them; one barrier per step.
+// K, V and the keys' positions go straight to LDS.  The results of a row group's KG waves meet
+// in LDS at the end.
+//   S^T (16 keys x 16 rows) = K Q^T       v_mfma_f32_16x16x32_f16 (bf16 without rotation)
+//   O^T (16 dims x 16 rows) += V^T P^T    v_mfma_f32_16x16x32_bf16, V^T by ds_read_b64_tr_b16
 // After the scores lane l holds row l%16 of each block and keys 4 (l/16) + {0..3}, the B
 // operand of the output product.
+//
+// Precision: a rotated key or query is rounded to 11 bits (float16), its size held by a power
+// of two where it does not fit: as bf16, 8 bits, each of the two alone would put outputs as
+// far from 64 bits as their own rounding does.  Without rotation q and k are exact.  A
+// probability enters the product as two bf16 numbers, its upper 8 bits and the rest: the 32
+// contraction steps of the instruction hold 16 keys twice, at the time of one.
+//
+// RoPE: a lane turns PL pairs of one key of a tile and holds their cos/sin.  Its next key is
+// STEP keys further; where the positions are too, the angles advance by a constant rotation (4
+// operations a pair, renewed every kRenew tiles), else they are computed.
 // ---------------------------------------------------------------------------------
-template <int D, bool ROPE>
-constexpr int tree_stages() { return ROPE ? 3 : 4; }
+constexpr int kRenew = 32;
 
-template <int D, int STYLE, bool ROPE, bool TABLE, int CB>
-__global__ void __launch_bounds__(kTreeWaves * 64, D == 64 ? 2 : 1) tree_bf16(const Plan plan, const TreeArgs a) {
+// max over the 8 lanes l & ~7 .. l | 7
+__device__ __forceinline__ float max_of8(float x) {
+    auto dpp = [&](auto ctrl) {
+        return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(x), __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    x = dpp(Idx<0xB1>{});    // lane ^ 1
+    x = dpp(Idx<0x4E>{});    // lane ^ 2
+    return dpp(Idx<0x141>{});   // lane ^ 7 (half rows mirrored)
+}
+
+template <int D, int STYLE, bool ROPE, int CB, int WR>
+__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan, const TreeArgs a) {
+    constexpr bool SHARED = WR > 1;        // the waves share their keys
     constexpr int KD = D / 32;             // 16x16x32 contraction steps of QK^T
     constexpr int DB = D / 16;             // 16-dim blocks of O^T
     constexpr int CH = D / 8;              // 16-byte chunks per K/V row
     constexpr int HALF = D / 2;
     constexpr int TK = kBlock;
-    constexpr int NW = kTreeWaves;
-    constexpr int NST = tree_stages<D, ROPE>();
-    constexpr int DPL = TK * CH / 64;      // 16-byte copies per lane per tile, each of K and V
-    constexpr int TROW = HALF / 4;         // 16-byte chunks (4 entries) per cos/sin row
-    constexpr int TPL = TK * TROW / 64;    // chunks of the tile's cos/sin rows per lane
-    constexpr int LPS = 2 * DPL + (TABLE ? TPL : 0);   // copies per lane per tile
-    constexpr int KV = TK * D;             // elements of a K or V tile
-    constexpr int SE = 2 * KV + (ROPE ? TK * HALF * 2 : 0);   // 2-byte elements of a stage
+    constexpr int NW = kTreeWaves, KG = NW / WR;
+    constexpr int STEP = SHARED ? 64 : NW * TK;    // keys of all waves
+    constexpr int OWNK = SHARED ? STEP / NW : TK;  // keys that a wave copies and turns
+    constexpr int PL = OWNK * HALF / 64;   // pairs that a lane turns
+    constexpr int NST = SHARED || D == 64 ? 4 : 2;
+    constexpr int DPL = OWNK * CH / 64;    // 16-byte copies per lane per step, each of K and V
+    constexpr int LPS = 2 * DPL + (ROPE ? 1 : 0);
+    constexpr int KV = STEP * D;           // elements of K or V in a stage
+    constexpr int SE = 2 * KV;             // elements of a stage: K of every tile, then V
+    constexpr int OWN = CB > KG ? CB / KG : 1;     // column blocks whose queries a wave turns
+    constexpr int SPARE = SHARED ? 2 : 1;  // stages that the queries pass through
+    constexpr int PER = SPARE * SE / NW;   // elements of them per wave
     static_assert((NST - 2) * LPS < 64, "vmcnt range");
-    static_assert(NW * NST * SE * 2 >= NW * CB * DB * 64 * 16, "the outputs meet in the stages");
+    static_assert(NST * SE * 2 >= NW * CB * DB * 64 * 16, "the outputs meet in the stages");
+    static_assert(PER * 2 >= 16 * HALF * 8 && PER * 2 >= OWN * KD * 64 * 16, "queries pass through the stages");
 
-    __shared__ __attribute__((aligned(16))) uint16_t stages[NW * NST * SE];
-    __shared__ int32_t ps[NW][NST][TK];
+    __shared__ __attribute__((aligned(16))) uint16_t stages[NST * SE];
+    __shared__ int32_t ps[NW][NST][OWNK];
+    __shared__ float ksc[NST][STEP];       // powers of two held back from a step's keys
+    __shared__ int32_t kbig[NST][NW];      // whether some key of a wave has one
     __shared__ float2 mls[NW][16 * CB];
+    __shared__ float qsl[NW][16 * CB];
     __shared__ __attribute__((aligned(4))) uint8_t infs[NW][CB][DB][64];   // infinities of V that a lane's rows see: +, 4 dims, and -, 4 dims
     __shared__ uint64_t fstep[HALF];
+    __shared__ __attribute__((aligned(16))) float2 stride_cs[HALF];        // cos/sin of STEP positions
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rg = wave / KG, kg = wave % KG;
     const int c16 = lane & 15, q4 = lane >> 4;
     const Group g = group_of<false>(plan, blockIdx.x);
     const int G = a.group, n_rt = g.n_rt;
     const int li = blockIdx.x - g.item_base;
     if (li >= a.hkv * g.n_split * n_rt) return;
     const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
-    const int rows_total = g.n_tok * G, row_lo = ic.rt * 16 * CB;
+    const int rows_total = g.n_tok * G, row_lo = (ic.rt * WR + rg) * 16 * CB;
     const int kv_lo = g.win + ic.split * g.split_keys, end = g.tok0 + g.n_tok;
     // (no sum below passes the last key: a request may have 2^31 - 1 of them)
     const int kv_hi = g.split_keys < end - kv_lo ? kv_lo + g.split_keys : end;
-    const int kt0 = kv_lo & ~(TK - 1);
-    const int n_tiles = (kv_hi - 1 - kt0) / TK + 1;
-    const int nt = n_tiles > wave ? (n_tiles - wave - 1) / NW + 1 : 0;   // this wave's
-    auto tile_key = [&](int u) { return kt0 + (u * NW + wave) * TK; };
+    // keys relative to kt0, the start of the first tile's block
+    const int kt0 = kv_lo & ~(TK - 1), k_lo = kv_lo - kt0, k_hi = kv_hi - kt0, k_tok = g.tok0 - kt0;
+    const int n_tiles = (k_hi - 1) / TK + 1;
+    // steps in which this wave copies keys
+    const int nt = SHARED ? (k_hi - 1) / STEP + 1 : n_tiles > wave ? (n_tiles - wave - 1) / NW + 1 : 0;
 
     if (ROPE)
-        for (int i = tid; i < HALF; i += NW * 64) fstep[i] = a.fstep[i];
+        for (int i = tid; i < HALF; i += NW * 64) {
+            fstep[i] = a.fstep[i];
+            rope_cs_fast(STEP, a.fstep[i], stride_cs[i].x, stride_cs[i].y);
+        }
     for (int i = tid; i < NW * CB * DB * 16; i += NW * 64) reinterpret_cast<uint32_t*>(infs)[i] = 0;
 
-    const int32_t* btab = a.block_tables + (size_t)g.req * a.max_blocks;
+    const int32_t* btab = a.block_tables + (size_t)g.req * a.max_blocks + (kt0 >> 4);
+    const int32_t* posv = a.positions + g.pos_off + kt0;
     const size_t blk_stride = (size_t)a.hkv * kBlock * D;
     const uint16_t* kpool = static_cast<const uint16_t*>(a.k_pool) + (size_t)ic.kvh * kBlock * D;
     const uint16_t* vpool = static_cast<const uint16_t*>(a.v_pool) + (size_t)ic.kvh * kBlock * D;
-    uint16_t* my = stages + wave * NST * SE;
 
-    // a key outside [kv_lo, kv_hi) stands for the tile's first key inside, so that nothing
-    // outside the range is read (its score is masked)
-    auto clamp_key = [&](int kt, int j) { return (j >= kv_lo && j < kv_hi) ? j : max(kt, kv_lo); };
-    auto copy_positions = [&](int u, int slot) {
-        if (!ROPE || u >= nt) return;
-        const int kt = tile_key(u);
-        if (lane < TK) dma_lds4(a.positions + g.pos_off + clamp_key(kt, kt + lane), &ps[wave][slot][0]);
-    };
-    // this lane's copies of a tile: byte offset within one head's page of a block
+    // The i-th copy of a step moves 64 chunks, 64 / CH keys from copy_key(i) on.  A key outside
+    // [k_lo, k_hi) stands for the nearest one inside, so that nothing outside the range is
+    // read (its score is masked).
+    constexpr int KPC = 64 / CH;           // keys per copy
+    auto copy_key = [&](int i) { return SHARED ? (i * NW + wave) * KPC : wave * TK + i * KPC; };
+    auto near_key = [&](int k) { return min(max(k, k_lo), k_hi - 1); };
+    // this lane's byte offset within one head's page of a block, but for the row
     uint32_t lane_off[DPL];
 #pragma unroll
     for (int i = 0; i < DPL; ++i) {
-        const int kk = (i * 64 + lane) / CH, pc = (i * 64 + lane) % CH;
-        lane_off[i] = (uint32_t)(kk * D + ((pc ^ dswz<D>(kk)) << 3)) * 2;
+        const int row = (copy_key(i) + lane / CH) & (TK - 1);
+        lane_off[i] = (uint32_t)(row * D + (((lane % CH) ^ dswz<D>(row)) << 3)) * 2;
     }
-    int odd_tile = -1;   // last tile with fewer than LPS copies
-    auto issue = [&](int u, int st, int blk) {
-        uint16_t* sg = my + st * SE;
-        const int kt = tile_key(u);
+    // own key j (0 .. OWNK - 1) of a step: its place in the step
+    auto own_key = [&](int j) { return copy_key(j / KPC) + j % KPC; };
+    struct Blocks {
+        int b[SHARED ? DPL : 1];           // (without sharing a step's copies are of one block)
+    };
+    auto blocks_of = [&](int u) {
+        Blocks r;
+#pragma unroll
+        for (int i = 0; i < (SHARED ? DPL : 1); ++i) r.b[i] = scalar_load(btab, min(u * STEP + copy_key(i), k_hi - 1) >> 4);
+        return r;
+    };
+    auto issue = [&](int u, int st, const Blocks& blk) {
+        uint16_t* sg = stages + st * SE;
         __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));   // the stage's last reads have returned (lgkmcnt 0)
-        copy_positions(u + NST - 1, st == 0 ? NST - 1 : st - 1);
-        if (ROPE) {
-            uint32_t* tab = reinterpret_cast<uint32_t*>(sg + 2 * KV);
-#pragma unroll
-            for (int i = 0; i < TPL; ++i) {
-                const int c = i * 64 + lane;
-                const int tkey = c / TROW, lc = (c % TROW) ^ (tkey & (TROW - 1));
-                const int32_t pos = ps[wave][st][tkey];
-                const bool in_table = TABLE && (uint32_t)pos < (uint32_t)a.rope_len;
-                if (in_table)
-                    dma_lds16(reinterpret_cast<const uint32_t*>(a.rope_table) + (size_t)pos * HALF + 4 * lc, tab + i * 64 * 4);
-                if (!TABLE || __builtin_amdgcn_ballot_w64(!in_table) != 0) {
-                    if (TABLE) odd_tile = u;
-                    if (!in_table) {
-                        u32x4_t w;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float ce, se;
-                            rope_cs_fast(pos, fstep[4 * lc + e], ce, se);
-                            w[e] = bf16_entry(ce, se);
-                        }
-                        *reinterpret_cast<u32x4_t*>(tab + c * 4) = w;
-                    }
-                }
-            }
-        }
-        const uint16_t* kb = kpool + (size_t)(uint32_t)blk * blk_stride;
-        const uint16_t* vb = vpool + (size_t)(uint32_t)blk * blk_stride;
-        const bool whole = kt >= kv_lo && kv_hi - kt >= TK;
+        if (ROPE && lane < OWNK) dma_lds4(posv + near_key(u * STEP + own_key(lane)), &ps[wave][st][0]);
 #pragma unroll
         for (int i = 0; i < DPL; ++i) {
+            const int k0 = u * STEP + copy_key(i);
+            const size_t base = (size_t)(uint32_t)blk.b[SHARED ? i : 0] * blk_stride;
             uint32_t off = lane_off[i];
-            if (!whole) {
-                const int kk = (i * 64 + lane) / CH;
-                off += (clamp_key(kt, kt + kk) - kt - kk) * D * 2;
+            if (k0 < k_lo || k_hi - k0 < KPC) {
+                const int k = k0 + lane / CH, row = k & (TK - 1);
+                off += ((near_key(k) & (TK - 1)) - row) * D * 2;
             }
-            dma_lds16_s(kb, off, sg + i * 64 * 8);
-            dma_lds16_s(vb, off, sg + KV + i * 64 * 8);
+            dma_lds16_s(kpool + base, off, sg + copy_key(i) * D);
+            dma_lds16_s(vpool + base, off, sg + KV + copy_key(i) * D);
         }
     };
-
 #pragma unroll
-    for (int u = 0; u < NST - 1; ++u) copy_positions(u, u);
+    for (int u = 0; u < NST - SPARE; ++u)
+        if (u < nt) issue(u, u, blocks_of(u));
 
-    // ---- queries: rows 16 cb .. 16 cb + 15 are turned and scaled by wave cb and passed to the
-    // others through the stage that is filled last
+    // ---- queries: the KG waves of a row group turn its column blocks and pass them to each
+    // other through stages that are filled later.  The cos/sin of a block's tokens (a token's
+    // heads share them) go the same way before.
     int toff[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -345,65 +369,93 @@ __global__ void __launch_bounds__(kTreeWaves * 64, D == 64 ? 2 : 1) tree_bf16(co
         toff[cb] = row < rows_total ? row / G : 0;
     }
     bf16x8_t qb[CB][KD];
-    __syncthreads();   // phase steps staged
-    if (wave < CB) {
-        const int row = row_lo + 16 * wave + c16;
-        const bool valid = row < rows_total;
-        const int to = valid ? row / G : 0, hl = valid ? row - to * G : 0;
-        const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + to) * a.hq + (size_t)ic.kvh * G + hl) * D;
-        float xf[KD][8];
+    float qs[CB];     // scores are the products times this (log2 units)
+    __syncthreads();  // phase steps staged
+    {
+        u32x4_t mine[OWN][KD];
+        uint16_t* spare = stages + (NST - SPARE) * SE + wave * PER;
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) {
-            const u32x4_t raw = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, kd * 4 + q4) * 8);
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                xf[kd][2 * m] = valid ? bf_lo(raw[m]) : 0.f;
-                xf[kd][2 * m + 1] = valid ? bf_hi(raw[m]) : 0.f;
-            }
-        }
-        if (ROPE) {
-            const int32_t pos = a.positions[g.pos_off + g.tok0 + to];
+        for (int o = 0; o < OWN; ++o) {
+            const int cb = kg + o * KG;
+            if (cb >= CB) break;
+            const int row0 = row_lo + 16 * cb, row = row0 + c16;
+            const bool valid = row < rows_total;
+            const int to = valid ? row / G : 0, hl = valid ? row - to * G : 0;
+            const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + to) * a.hq + (size_t)ic.kvh * G + hl) * D;
+            u32x4_t raw[KD];
 #pragma unroll
             for (int kd = 0; kd < KD; ++kd) {
-                if (STYLE == kNeox) {
-                    if (kd >= KD / 2) break;
+                raw[kd] = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, kd * 4 + q4) * 8);
+                if (!valid) raw[kd] = u32x4_t{0, 0, 0, 0};
+            }
+            float scale = a.scale_log2;
+            if (ROPE) {
+                const int t0 = min(row0, rows_total - 1) / G, t1 = min(row0 + 15, rows_total - 1) / G;
+                float2* cs = reinterpret_cast<float2*>(spare);
+                for (int i = lane; i < (t1 - t0 + 1) * HALF; i += 64) {
+                    float c, s;
+                    rope_cs_fast(a.positions[g.pos_off + g.tok0 + t0 + i / HALF], fstep[i % HALF], c, s);
+                    cs[i] = make_float2(c, s);
+                }
+                const float2* tc = cs + (valid ? to - t0 : 0) * HALF;
+                float xf[KD][8], big = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float c, s;
-                        rope_cs_fast(pos, fstep[kd * 32 + 8 * q4 + e], c, s);
-                        const float x = xf[kd][e], y = xf[kd + KD / 2][e];
-                        xf[kd][e] = x * c - y * s;
-                        xf[kd + KD / 2][e] = y * c + x * s;
-                    }
-                } else {
+                for (int kd = 0; kd < KD; ++kd)
 #pragma unroll
                     for (int m = 0; m < 4; ++m) {
-                        float c, s;
-                        rope_cs_fast(pos, fstep[kd * 16 + 4 * q4 + m], c, s);
-                        const float x = xf[kd][2 * m], y = xf[kd][2 * m + 1];
-                        xf[kd][2 * m] = x * c - y * s;
-                        xf[kd][2 * m + 1] = y * c + x * s;
+                        xf[kd][2 * m] = bf_lo(raw[kd][m]);
+                        xf[kd][2 * m + 1] = bf_hi(raw[kd][m]);
                     }
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    // NeoX: pairs 32 kd + 8 q4 + e, elements e of chunks kd and kd + KD / 2; GPT-J:
+                    // 16 kd + 4 q4 + m, elements 2 m and 2 m + 1 of chunk kd
+                    const int kd = STYLE == kNeox ? i / 8 : i / 4, e = STYLE == kNeox ? i % 8 : i % 4;
+                    const float2 t = tc[STYLE == kNeox ? kd * 32 + 8 * q4 + e : kd * 16 + 4 * q4 + e];
+                    float& x = STYLE == kNeox ? xf[kd][e] : xf[kd][2 * e];
+                    float& y = STYLE == kNeox ? xf[kd + KD / 2][e] : xf[kd][2 * e + 1];
+                    const float x0 = x, y0 = y;
+                    x = x0 * t.x - y0 * t.y;
+                    y = y0 * t.x + x0 * t.y;
+                    big = fmaxf(big, fmaxf(fabsf(x), fabsf(y)));
                 }
+                big = max_xor32(max_xor16(big));
+                // the row times 2^-ex lies in [-1, 1]
+                const int ex = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
+                scale = ldexpf(scale, ex);
+#pragma unroll
+                for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) raw[kd][m] = pack_f16(ldexpf(xf[kd][2 * m], -ex), ldexpf(xf[kd][2 * m + 1], -ex));
+            }
+#pragma unroll
+            for (int kd = 0; kd < KD; ++kd) mine[o][kd] = raw[kd];
+            if (KG == 1) {
+#pragma unroll
+                for (int kd = 0; kd < KD; ++kd) qb[o][kd] = __builtin_bit_cast(bf16x8_t, raw[kd]);
+                qs[o] = scale;
+            } else if (q4 == 0) {
+                qsl[rg * KG][16 * cb + c16] = scale;
             }
         }
-        u32x4_t* out = reinterpret_cast<u32x4_t*>(my + (NST - 1) * SE);
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);   // the last block's cos/sin have been read
+        if constexpr (KG > 1) {
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) {
-            u32x4_t w;
+            for (int o = 0; o < OWN; ++o)
+                if (kg + o * KG < CB)
 #pragma unroll
-            for (int m = 0; m < 4; ++m) w[m] = pack_bf16(xf[kd][2 * m] * a.scale_log2, xf[kd][2 * m + 1] * a.scale_log2);
-            out[kd * 64 + lane] = w;
+                    for (int kd = 0; kd < KD; ++kd) reinterpret_cast<u32x4_t*>(spare)[(o * KD + kd) * 64 + lane] = mine[o][kd];
+            barrier_keep_vmem();
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const uint16_t* from = stages + (NST - SPARE) * SE + (rg * KG + cb % KG) * PER + (cb / KG) * KD * 64 * 8;
+#pragma unroll
+                for (int kd = 0; kd < KD; ++kd) qb[cb][kd] = *reinterpret_cast<const bf16x8_t*>(from + (kd * 64 + lane) * 8);
+                qs[cb] = qsl[rg * KG][16 * cb + c16];
+            }
         }
+        barrier_keep_vmem();   // every wave has its rows: the stages may be filled
     }
-    wait_vmem();       // the first positions have landed
-    __syncthreads();
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-        for (int kd = 0; kd < KD; ++kd)
-            qb[cb][kd] = *reinterpret_cast<const bf16x8_t*>(stages + (cb * NST + NST - 1) * SE + (kd * 64 + lane) * 8);
-    __syncthreads();   // every wave has its rows: the stages may be filled
 
     f32x4_t acc[CB][DB];
     float m_run[CB], l_run[CB];
@@ -415,99 +467,147 @@ __global__ void __launch_bounds__(kTreeWaves * 64, D == 64 ? 2 : 1) tree_bf16(co
         for (int db = 0; db < DB; ++db) acc[cb][db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
-    // per-lane element offsets within a stage: K operand rows, cos/sin chunks, V^T operand rows
-    int k_off[KD], t_off[KD], v_off[DB];
+    // per-lane element offsets within a tile: K operand rows and V^T operand rows
+    int k_off[KD], v_off[DB];
 #pragma unroll
-    for (int kd = 0; kd < KD; ++kd) {
-        k_off[kd] = c16 * D + ((model_chunk(a.chunk_map, kd * 4 + q4) ^ dswz<D>(c16)) << 3);
-        // NeoX: 2 chunks for each of the KD / 2 steps of a half; GPT-J: 1 for each step
-        const int lc = STYLE == kNeox ? (kd / 2) * 8 + 2 * q4 + (kd % 2) : kd * 4 + q4;
-        t_off[kd] = 2 * KV + (c16 * HALF + 4 * (lc ^ (c16 & (TROW - 1)))) * 2;
-    }
+    for (int kd = 0; kd < KD; ++kd) k_off[kd] = c16 * D + ((model_chunk(a.chunk_map, kd * 4 + q4) ^ dswz<D>(c16)) << 3);
     {
         const int key = 4 * q4 + (c16 >> 2);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             const int d = db * 16 + 4 * (lane & 3);
-            v_off[db] = KV + key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7);
+            v_off[db] = key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7);
         }
     }
 
-    int blk_next = 0;
-    auto block_of = [&](int u) { return scalar_load(btab, min(tile_key(u), kv_hi - 1) >> 4); };
+    // ---- turning keys.  Without sharing a lane has the operand's elements of key c16: runs of 8
+    // (NeoX pairs 32 kd + 8 q4 + e of chunks kd and kd + KD / 2; GPT-J pairs 16 kd + 4 q4 + m).
+    // With sharing 8 lanes have one key, PL pairs (lane % 8) * PL + i each.
+    constexpr int RUN = SHARED ? PL : STYLE == kNeox ? 8 : 4;   // pairs in a row
+    const int own_j = SHARED ? lane >> 3 : c16;
+    const int pair0 = SHARED ? (lane & 7) * PL : RUN * q4;
+    auto pair_of = [&](int i) { return pair0 + (SHARED ? i : i / RUN * 4 * RUN + i % RUN); };
+    const int sh_row = SHARED ? own_key(own_j) : 0;
+    // SHARED: element offsets of the lane's two runs (NeoX) or of its 2 PL neighbours (GPT-J)
+    int s_off[2];
+    if (SHARED) {
+        const int e0 = STYLE == kNeox ? pair0 : 2 * pair0, e1 = STYLE == kNeox ? pair0 + HALF : e0 + PL;
+        const int row = sh_row & (TK - 1);
+        s_off[0] = sh_row * D + ((model_chunk(a.chunk_map, e0 >> 3) ^ dswz<D>(row)) << 3) + (e0 & 7);
+        s_off[1] = sh_row * D + ((model_chunk(a.chunk_map, e1 >> 3) ^ dswz<D>(row)) << 3) + (e1 & 7);
+    }
+    float rc[PL], rs[PL];   // cos/sin at position cs_pos
+    uint32_t cs_pos = 0;
+    int fresh = 0;          // steps until the angles are computed again
+    // turns 2 PL elements, words w[0 .. PL): NeoX x in the first half and y in the second; returns
+    // whether some key of the wave got a power of two
+    auto turn = [&](int st, uint32_t (&w)[PL]) {
+        const uint32_t pos = (uint32_t)ps[wave][st][own_j];
+        if (fresh == 0 || __builtin_amdgcn_ballot_w64(pos != cs_pos + STEP) != 0) {
 #pragma unroll
-    for (int u = 0; u < NST - 1; ++u)
-        if (u < nt) issue(u, u, block_of(u));
-    if (NST - 1 < nt) blk_next = block_of(NST - 1);
-    int st = 0;
-    for (int t = 0; t < nt; ++t) {
-        // tile t has landed once no more than the later tiles' copies are outstanding
-        if (t + NST - 2 < nt && odd_tile <= t) wait_vmem_n<(NST - 2) * LPS>();
-        else wait_vmem();
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);
-        const uint16_t* sg = my + st * SE;
-        const int kt = tile_key(t);
-        if (t + NST - 1 < nt) {
-            issue(t + NST - 1, st == 0 ? NST - 1 : st - 1, blk_next);
-            if (t + NST < nt) blk_next = block_of(t + NST);
-        }
-        u32x4_t kf[KD];
+            for (int i = 0; i < PL; ++i) rope_cs_fast((int32_t)pos, fstep[pair_of(i)], rc[i], rs[i]);
+            fresh = kRenew;
+        } else {
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) kf[kd] = *reinterpret_cast<const u32x4_t*>(sg + k_off[kd]);
-        if (ROPE) {
-            u32x4_t te[KD];
-#pragma unroll
-            for (int kd = 0; kd < KD; ++kd) te[kd] = *reinterpret_cast<const u32x4_t*>(sg + t_off[kd]);
-            if (STYLE == kNeox) {
-#pragma unroll
-                for (int kd = 0; kd < KD / 2; ++kd)
-#pragma unroll
-                    for (int m = 0; m < 4; m += 2) {
-                        const u32x4_t ee = te[2 * kd + m / 2];
-                        const Words4 o = rot4_neox(kf[kd][m], kf[kd + KD / 2][m], kf[kd][m + 1], kf[kd + KD / 2][m + 1],
-                                                   ee[0], ee[1], ee[2], ee[3]);
-                        kf[kd][m] = o.w[0];
-                        kf[kd + KD / 2][m] = o.w[1];
-                        kf[kd][m + 1] = o.w[2];
-                        kf[kd + KD / 2][m + 1] = o.w[3];
-                    }
-            } else {
-#pragma unroll
-                for (int kd = 0; kd < KD; ++kd) {
-                    const u32x4_t ee = te[kd];
-                    const Words4 o = rot4_gptj(kf[kd][0], kf[kd][1], kf[kd][2], kf[kd][3], ee[0], ee[1], ee[2], ee[3]);
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) kf[kd][m] = o.w[m];
-                }
+            for (int i = 0; i < PL; ++i) {
+                const float2 d = stride_cs[pair_of(i)];
+                const float c = rc[i], s = rs[i];
+                rc[i] = c * d.x - s * d.y;
+                rs[i] = s * d.x + c * d.y;
             }
         }
-        f32x4_t sc[CB];
+        --fresh;
+        cs_pos = pos;
+        float big = 0.f;
+        uint32_t out[PL];
+        auto rotate = [&](auto scaled, int ex) {
+#pragma unroll
+            for (int i = 0; i < PL; i += 2) {
+                const uint32_t A = STYLE == kNeox ? w[i / 2] : w[i], B = STYLE == kNeox ? w[PL / 2 + i / 2] : w[i + 1];
+                const float x0 = bf_lo(A), y0 = STYLE == kNeox ? bf_lo(B) : bf_hi(A);
+                const float x1 = STYLE == kNeox ? bf_hi(A) : bf_lo(B), y1 = bf_hi(B);
+                float p0 = x0 * rc[i] - y0 * rs[i], r0 = y0 * rc[i] + x0 * rs[i];
+                float p1 = x1 * rc[i + 1] - y1 * rs[i + 1], r1 = y1 * rc[i + 1] + x1 * rs[i + 1];
+                if (decltype(scaled)::value) {
+                    p0 = ldexpf(p0, -ex); r0 = ldexpf(r0, -ex); p1 = ldexpf(p1, -ex); r1 = ldexpf(r1, -ex);
+                } else {
+                    big = fmaxf(fmaxf(big, fabsf(p0)), fabsf(r0));
+                    big = fmaxf(fmaxf(big, fabsf(p1)), fabsf(r1));
+                }
+                out[STYLE == kNeox ? i / 2 : i] = STYLE == kNeox ? pack_f16(p0, p1) : pack_f16(p0, r0);
+                out[STYLE == kNeox ? PL / 2 + i / 2 : i + 1] = STYLE == kNeox ? pack_f16(r0, r1) : pack_f16(p1, r1);
+            }
+        };
+        rotate(std::false_type{}, 0);
+        // a key whose largest element lies outside 2^-8 .. 2^15 goes in times a power of two
+        big = SHARED ? max_of8(big) : max_xor32(max_xor16(big));
+        const bool odd = big >= 0x1p15f || (big < 0x1p-8f && big > 0.f);
+        const bool any = __builtin_amdgcn_ballot_w64(odd) != 0;
+        int ex = 0;
+        if (any) {
+            ex = odd && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
+            rotate(std::true_type{}, ex);
+        }
+        if (SHARED) {
+            if ((lane & 7) == 0) ksc[st][sh_row] = ldexpf(1.f, ex);
+            if (lane == 0) kbig[st][wave] = any;
+        } else if (any && q4 == 0) {
+            ksc[st][wave * TK + c16] = ldexpf(1.f, ex);
+        }
+#pragma unroll
+        for (int i = 0; i < PL; ++i) w[i] = out[i];
+        return any;
+    };
+
+    // ---- NT tiles: their K operands, V tiles, first key, and whether their keys have powers of two
+    // to give back (kscale, in tile order)
+    auto tiles = [&](auto ntc, const u32x4_t (*kf)[KD], const uint16_t* vt, int k0, bool powers, const float* kscale) {
+        constexpr int NT = decltype(ntc)::value;
+        f32x4_t sc[NT][CB];
 #pragma unroll
         for (int kd = 0; kd < KD; ++kd)
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-                sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[kd]), qb[cb][kd],
-                                                                 kd == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[cb], 0, 0, 0);
-        const bool masked = kt < kv_lo || kv_hi - kt < TK || g.tok0 - kt < TK;
-        uint32_t seen[CB];   // masked tiles: the row's bits of the tile's keys
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    const f32x4_t from = kd == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[n][cb];
+                    if (ROPE)
+                        sc[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kf[n][kd]), __builtin_bit_cast(f16x8_t, qb[cb][kd]), from, 0, 0, 0);
+                    else
+                        sc[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[n][kd]), qb[cb][kd], from, 0, 0, 0);
+                }
+        if (ROPE && powers) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sc[n][cb][r] *= kscale[n * TK + 4 * q4 + r];
+        }
+        const bool masked = k0 < k_lo || k_hi - k0 < NT * TK || k_tok - k0 < NT * TK;
+        uint32_t seen[CB];   // masked tiles: the row's bits of the tiles' keys
         if (masked) {
-            // keys [kv_lo, kv_hi) of the tile
-            const int lo = max(kv_lo - kt, 0), hi = min(kv_hi - kt, TK);
-            const uint32_t inside = ((1u << hi) - 1u) & ~((1u << lo) - 1u);
+            // keys [k_lo, k_hi) of the tiles (k0 < k_hi)
+            const int lo = max(k_lo - k0, 0), hi = min(k_hi - k0, NT * TK);
+            const uint32_t inside = (hi < 32 ? (1u << hi) - 1u : ~0u) & ~((1u << lo) - 1u);
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                seen[cb] = inside & tree_bits(a.mask + (size_t)(g.q_row0 + toff[cb]) * a.words, a.words, kt - g.tok0);
+                seen[cb] = inside & tree_bits(a.mask + (size_t)(g.q_row0 + toff[cb]) * a.words, a.words, k0 - k_tok);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (!((seen[cb] >> (4 * q4 + r)) & 1)) sc[cb][r] = -INFINITY;
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (!((seen[cb] >> (16 * n + 4 * q4 + r)) & 1)) sc[n][cb][r] = -INFINITY;
             }
         }
         float mx[CB];
         bool moves = false;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            mx[cb] = fmaxf(fmaxf(sc[cb][0], sc[cb][1]), fmaxf(sc[cb][2], sc[cb][3]));
-            mx[cb] = max_xor32(max_xor16(mx[cb]));
+            mx[cb] = fmaxf(fmaxf(sc[0][cb][0], sc[0][cb][1]), fmaxf(sc[0][cb][2], sc[0][cb][3]));
+#pragma unroll
+            for (int n = 1; n < NT; ++n) mx[cb] = fmaxf(fmaxf(fmaxf(mx[cb], sc[n][cb][0]), sc[n][cb][1]), fmaxf(sc[n][cb][2], sc[n][cb][3]));
+            mx[cb] = max_xor32(max_xor16(mx[cb])) * qs[cb];
             moves |= mx[cb] > m_run[cb] + 8.f;
         }
         // the reference maximum only moves when some row's maximum grows by more than 8
@@ -523,97 +623,203 @@ __global__ void __launch_bounds__(kTreeWaves * 64, D == 64 ? 2 : 1) tree_bf16(co
                 m_run[cb] = m_new;
             }
         }
-        // probabilities rounded to bf16 for P V; the row sum adds exactly those
-        u32x2_t pw[CB];
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            float p[4];
+        for (int n = 0; n < NT; ++n) {
+            u32x2_t af[DB];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(sc[cb][r] - m_run[cb]);
-            pw[cb] = u32x2_t{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])};
-            l_run[cb] = sum2_bf16(pw[cb][1], sum2_bf16(pw[cb][0], l_run[cb]));
-        }
-        lds_u16_t* vb = as_lds(sg);
-        bf16x4_t af[DB];
-        uint32_t huge = 0;   // masked tiles: whether V holds an infinity or NaN
+            for (int db = 0; db < DB; ++db) af[db] = __builtin_bit_cast(u32x2_t, lds_read_tr(as_lds(vt + n * TK * D) + v_off[db]));
+            uint32_t huge = 0;   // masked tiles: whether V holds an infinity or NaN
+            if (masked) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) af[db] = __builtin_bit_cast(bf16x4_t, lds_read_tr(vb + v_off[db]));
-        if (masked) {
+                for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const u32x2_t w = __builtin_bit_cast(u32x2_t, af[db]);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) huge |= (uint32_t)((w[e] & 0x7f80u) == 0x7f80u) | (uint32_t)((w[e] & 0x7f800000u) == 0x7f800000u);
+                    for (int e = 0; e < 2; ++e)
+                        huge |= (uint32_t)((af[db][e] & 0x7f80u) == 0x7f80u) | (uint32_t)((af[db][e] & 0x7f800000u) == 0x7f800000u);
             }
-        }
-        if (masked && __builtin_amdgcn_ballot_w64(huge != 0) != 0) {
-            // An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in
-            // the product below): the product takes the finite elements, and two more count
-            // the seen infinities of either sign (a NaN as one of each) per row and dimension,
-            // which join the outputs at the end.
+            if (masked && __builtin_amdgcn_ballot_w64(huge != 0) != 0) {
+                // An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in
+                // the product below): the product takes the finite elements, and two more count
+                // the seen infinities of either sign (a NaN as one of each) per row and
+                // dimension, which join the outputs at the end.
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const u32x2_t w = __builtin_bit_cast(u32x2_t, af[db]);
-                u32x2_t fin, up, down;
+                for (int db = 0; db < DB; ++db) {
+                    u32x2_t fin, up, down;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    fin[e] = up[e] = down[e] = 0;
+                    for (int e = 0; e < 2; ++e) {
+                        fin[e] = up[e] = down[e] = 0;
 #pragma unroll
-                    for (int h = 0; h < 32; h += 16) {
-                        const uint32_t x = (w[e] >> h) & 0xffffu, mag = x & 0x7fffu;
-                        if (mag < 0x7f80u) fin[e] |= x << h;
-                        else {
-                            if (x != 0xff80u) up[e] |= 0x3f80u << h;
-                            if (x != 0x7f80u) down[e] |= 0x3f80u << h;
+                        for (int h = 0; h < 32; h += 16) {
+                            const uint32_t x = (af[db][e] >> h) & 0xffffu, mag = x & 0x7fffu;
+                            if (mag < 0x7f80u) fin[e] |= x << h;
+                            else {
+                                if (x != 0xff80u) up[e] |= 0x3f80u << h;
+                                if (x != 0x7f80u) down[e] |= 0x3f80u << h;
+                            }
                         }
                     }
-                }
-                af[db] = __builtin_bit_cast(bf16x4_t, fin);
+                    af[db] = fin;
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-                    const uint32_t k4 = seen[cb] >> (4 * q4);
-                    const u32x2_t one = {(k4 & 1u) * 0x3f80u | ((k4 >> 1) & 1u) * 0x3f800000u,
-                                         ((k4 >> 2) & 1u) * 0x3f80u | ((k4 >> 3) & 1u) * 0x3f800000u};
-                    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
-                    const f32x4_t u = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4_t, up), __builtin_bit_cast(bf16x4_t, one), zero, 0, 0, 0);
-                    const f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4_t, down), __builtin_bit_cast(bf16x4_t, one), zero, 0, 0, 0);
-                    uint32_t f = 0;
+                    for (int cb = 0; cb < CB; ++cb) {
+                        const uint32_t k4 = seen[cb] >> (16 * n + 4 * q4);
+                        const u32x2_t one = {(k4 & 1u) * 0x3f80u | ((k4 >> 1) & 1u) * 0x3f800000u,
+                                             ((k4 >> 2) & 1u) * 0x3f80u | ((k4 >> 3) & 1u) * 0x3f800000u};
+                        const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+                        const f32x4_t u = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4_t, up), __builtin_bit_cast(bf16x4_t, one), zero, 0, 0, 0);
+                        const f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4_t, down), __builtin_bit_cast(bf16x4_t, one), zero, 0, 0, 0);
+                        uint32_t f = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) f |= (u[i] > 0.f ? 1u << i : 0u) | (d[i] > 0.f ? 16u << i : 0u);
-                    infs[wave][cb][db][lane] |= (uint8_t)f;
+                        for (int i = 0; i < 4; ++i) f |= (u[i] > 0.f ? 1u << i : 0u) | (d[i] > 0.f ? 16u << i : 0u);
+                        infs[wave][cb][db][lane] |= (uint8_t)f;
+                    }
                 }
             }
+            u32x4_t pw[CB];   // upper and lower parts of the probabilities
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                float p[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][cb][r], qs[cb], -m_run[cb]));
+                l_run[cb] += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    pw[cb][h] = pack_bf16(p[2 * h], p[2 * h + 1]);
+                    pw[cb][2 + h] = pack_bf16(p[2 * h] - bf_lo(pw[cb][h]), p[2 * h + 1] - bf_hi(pw[cb][h]));
+                }
+            }
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                const u32x4_t twice = {af[db][0], af[db][1], af[db][0], af[db][1]};
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb)
+                    acc[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, twice), __builtin_bit_cast(bf16x8_t, pw[cb]), acc[cb][db], 0, 0, 0);
+            }
         }
+    };
+    // a step's copies have landed once no more than those of the `later` next ones are outstanding
+    auto wait_step = [&](int u, auto later) {
+        constexpr int L = decltype(later)::value;
+        if (L > 0 && u + L < nt) wait_vmem_n<L * LPS>();
+        else wait_vmem();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    };
+    auto load_k = [&](u32x4_t (&kf)[KD], const uint16_t* kt) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+        for (int kd = 0; kd < KD; ++kd) kf[kd] = *reinterpret_cast<const u32x4_t*>(kt + k_off[kd]);
+    };
+
+    int st = 0;
+    auto next = [](int x) { return x + 1 == NST ? 0 : x + 1; };
+    auto prev = [](int x) { return x == 0 ? NST - 1 : x - 1; };
+    Blocks blk{};
+    if constexpr (!SHARED) {
+        if (NST - 1 < nt) blk = blocks_of(NST - 1);
+        for (int t = 0; t < nt; ++t) {
+            wait_step(t, Idx<NST - 2>{});
+            if (t + NST - 1 < nt) {
+                issue(t + NST - 1, prev(st), blk);
+                if (t + NST < nt) blk = blocks_of(t + NST);
+            }
+            const uint16_t* kt = stages + st * SE + wave * TK * D;
+            u32x4_t kf[1][KD];
+            load_k(kf[0], kt);
+            bool powers = false;
+            if constexpr (ROPE) {
+                uint32_t w[PL];   // runs in pair order, NeoX: all x, then all y
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-                acc[cb][db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(af[db], __builtin_bit_cast(bf16x4_t, pw[cb]), acc[cb][db], 0, 0, 0);
-        st = st + 1 == NST ? 0 : st + 1;
+                for (int i = 0; i < PL; ++i) w[i] = kf[0][i / 4][i % 4];
+                powers = turn(st, w);
+#pragma unroll
+                for (int i = 0; i < PL; ++i) kf[0][i / 4][i % 4] = w[i];
+            }
+            tiles(Idx<1>{}, kf, kt + KV, t * STEP + wave * TK, powers, &ksc[st][wave * TK]);
+            st = next(st);
+        }
+    } else {
+        typedef uint32_t run_t __attribute__((ext_vector_type(PL / 2)));
+        // step u has landed; its keys are turned in place
+        auto prepare = [&](int u, int sl) {
+            if (u >= nt) return;
+            wait_step(u, Idx<NST - 2>{});
+            if constexpr (ROPE) {
+                uint16_t* kt = stages + sl * SE;
+                uint32_t w[PL];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const run_t x = *reinterpret_cast<const run_t*>(kt + s_off[h]);
+#pragma unroll
+                    for (int i = 0; i < PL / 2; ++i) w[h * PL / 2 + i] = x[i];
+                }
+                turn(sl, w);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    run_t x;
+#pragma unroll
+                    for (int i = 0; i < PL / 2; ++i) x[i] = w[h * PL / 2 + i];
+                    *reinterpret_cast<run_t*>(kt + s_off[h]) = x;
+                }
+            }
+        };
+#pragma unroll
+        for (int u = NST - SPARE; u < NST - 1; ++u)
+            if (u < nt) issue(u, u, blocks_of(u));
+        if (NST - 1 < nt) blk = blocks_of(NST - 1);
+        prepare(0, 0);
+        barrier_keep_vmem();
+        constexpr int NT = KG == 4 ? 1 : 2;    // tiles at a time
+        const bool live = row_lo < rows_total;
+        for (int s = 0; s < nt; ++s) {
+            // step s + NST - 1 goes where step s - 1 was
+            if (s + NST - 1 < nt) {
+                issue(s + NST - 1, prev(st), blk);
+                if (s + NST < nt) blk = blocks_of(s + NST);
+            }
+            prepare(s + 1, next(st));
+            if (live) {
+                uint32_t flags = 0;
+                if (ROPE) flags = (uint32_t)kbig[st][lane % NW];
+                const bool powers = ROPE && __builtin_amdgcn_ballot_w64(flags != 0) != 0;
+#pragma unroll 1
+                for (int n = 0; n < 4 / KG; n += NT) {
+                    const int k0 = s * STEP + (kg * (4 / KG) + n) * TK;
+                    if (k0 >= k_hi) break;
+                    const uint16_t* kt = stages + st * SE + (kg * (4 / KG) + n) * TK * D;
+                    u32x4_t kf[NT][KD];
+#pragma unroll
+                    for (int m = 0; m < NT; ++m) load_k(kf[m], kt + m * TK * D);
+                    tiles(Idx<NT>{}, kf, kt + KV, k0, powers, &ksc[st][(kg * (4 / KG) + n) * TK]);
+                }
+            }
+            barrier_keep_vmem();
+            st = next(st);
+        }
     }
 
-    // ---- the waves' results meet: rows by their common maximum, outputs through the stages
+    // ---- the results of a row group's waves meet: rows by their common maximum, outputs through
+    // the stages
+    float M[CB], den[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-        const float l = sum_xor32(sum_xor16(l_run[cb]));
-        if (q4 == 0) mls[wave][16 * cb + c16] = make_float2(m_run[cb], l);
+        den[cb] = sum_xor32(sum_xor16(l_run[cb]));
+        M[cb] = m_run[cb];
+        if (KG > 1 && q4 == 0) mls[wave][16 * cb + c16] = make_float2(m_run[cb], den[cb]);
     }
-    __syncthreads();   // (every wave's copies have landed and been read)
-    float M[CB], den[CB];
+    if (KG > 1) __syncthreads();   // (every wave's copies have landed and been read)
     f32x4_t* meet = reinterpret_cast<f32x4_t*>(stages);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-        float2 w[NW];
-        M[cb] = kNegBig;
+        float mine = 1.f;
+        if (KG > 1) {
+            float2 w[KG];
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            w[i] = mls[i][16 * cb + c16];
-            M[cb] = fmaxf(M[cb], w[i].x);
+            for (int i = 0; i < KG; ++i) {
+                w[i] = mls[rg * KG + i][16 * cb + c16];
+                M[cb] = fmaxf(M[cb], w[i].x);
+            }
+            den[cb] = 0.f;
+#pragma unroll
+            for (int i = 0; i < KG; ++i) den[cb] += w[i].y * __builtin_amdgcn_exp2f(w[i].x - M[cb]);
+            mine = __builtin_amdgcn_exp2f(m_run[cb] - M[cb]);
         }
-        den[cb] = 0.f;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) den[cb] += w[i].y * __builtin_amdgcn_exp2f(w[i].x - M[cb]);
-        const float mine = __builtin_amdgcn_exp2f(m_run[cb] - M[cb]);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             f32x4_t x = acc[cb][db] * mine;
@@ -621,22 +827,29 @@ __global__ void __launch_bounds__(kTreeWaves * 64, D == 64 ? 2 : 1) tree_bf16(co
             if (f != 0)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] += ((f >> i) & 1 ? INFINITY : 0.f) - ((f >> (4 + i)) & 1 ? INFINITY : 0.f);
-            meet[((wave * CB + cb) * DB + db) * 64 + lane] = x;
+            if (KG > 1) meet[((wave * CB + cb) * DB + db) * 64 + lane] = x;
+            else acc[cb][db] = x;
         }
     }
-    __syncthreads();
-    const size_t prow0 = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (16 * CB);
+    if (KG > 1) __syncthreads();
+    const size_t prow0 = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (16 * CB * WR) + rg * 16 * CB;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
         const int row = row_lo + 16 * cb + c16;
         if (row >= rows_total) continue;
         const float inv = den[cb] == 0.f ? 0.f : 1.f / den[cb];   // (a drafted token may see nothing: its output is 0)
 #pragma unroll
-        for (int i = 0; i < DB / NW; ++i) {
-            const int db = i * NW + wave;
-            f32x4_t x = meet[(cb * DB + db) * 64 + lane];
+        for (int i = 0; i < (DB + KG - 1) / KG; ++i) {
+            const int db = i * KG + kg;
+            if (db >= DB) break;
+            f32x4_t x;
+            if (KG > 1) {
+                x = meet[((rg * KG * CB + cb) * DB + db) * 64 + lane];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) x += meet[((w * CB + cb) * DB + db) * 64 + lane];
+                for (int w = 1; w < KG; ++w) x += meet[(((rg * KG + w) * CB + cb) * DB + db) * 64 + lane];
+            } else {
+                x = acc[cb][i];
+            }
             if (g.n_split > 1) {
                 *reinterpret_cast<f32x4_t*>(a.part_o + (prow0 + 16 * cb + c16) * D + db * 16 + 4 * q4) = x;
             } else {
@@ -645,7 +858,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, D == 64 ? 2 : 1) tree_bf16(co
                 *reinterpret_cast<u32x2_t*>(op + db * 16 + 4 * q4) = u32x2_t{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
             }
         }
-        if (g.n_split > 1 && wave == 0 && q4 == 0)
+        if (g.n_split > 1 && kg == 0 && q4 == 0)
             *reinterpret_cast<float2*>(a.part_ml + (prow0 + 16 * cb + c16) * 2) = make_float2(M[cb], den[cb]);
     }
 }
@@ -693,12 +906,16 @@ __global__ void __launch_bounds__(kMergeRows * D / 4) tree_merge(const Plan plan
     *reinterpret_cast<u32x2_t*>(op) = u32x2_t{pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv)};
 }
 
-template <int D, int STYLE, bool ROPE, bool TABLE>
+template <int D, int STYLE, bool ROPE>
 hipError_t launch_tree_t(const Plan& plan, const TreeArgs& a, hipStream_t st) {
     const dim3 grid(plan.n_items), block(kTreeWaves * 64);
-    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, TABLE, 1>), grid, block, 0, st, plan, a);
-    else if (a.tile_rows == 32) hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, TABLE, 2>), grid, block, 0, st, plan, a);
-    else hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, TABLE, 4>), grid, block, 0, st, plan, a);
+    switch (a.tile_rows) {
+    case 16: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 1, 1>), grid, block, 0, st, plan, a); break;
+    case 32: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 1>), grid, block, 0, st, plan, a); break;
+    case 64: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 2>), grid, block, 0, st, plan, a); break;
+    case 128: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 4>), grid, block, 0, st, plan, a); break;
+    default: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 8>), grid, block, 0, st, plan, a); break;
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.n_merge == 0) return e;
     hipLaunchKernelGGL((tree_merge<D>), dim3(plan.n_merge), dim3(kMergeRows * D / 4), 0, st, plan, a);
@@ -707,10 +924,8 @@ hipError_t launch_tree_t(const Plan& plan, const TreeArgs& a, hipStream_t st) {
 
 template <int D>
 hipError_t launch_tree_d(int style, bool rope, const Plan& plan, const TreeArgs& a, hipStream_t st) {
-    const bool table = a.rope_table != nullptr && a.rope_len > 0;
-    if (!rope) return launch_tree_t<D, 0, false, false>(plan, a, st);   // (without rotation the pairing makes no difference)
-    if (style == kNeox) return table ? launch_tree_t<D, 0, true, true>(plan, a, st) : launch_tree_t<D, 0, true, false>(plan, a, st);
-    return table ? launch_tree_t<D, 1, true, true>(plan, a, st) : launch_tree_t<D, 1, true, false>(plan, a, st);
+    if (!rope) return launch_tree_t<D, 0, false>(plan, a, st);   // (without rotation the pairing makes no difference)
+    return style == kNeox ? launch_tree_t<D, 0, true>(plan, a, st) : launch_tree_t<D, 1, true>(plan, a, st);
 }
 
 template <typename T, int D>
