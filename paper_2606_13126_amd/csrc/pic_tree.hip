@@ -248,6 +248,14 @@ __device__ __forceinline__ float max_of8(float x) {
     return dpp(Idx<0x141>{});   // lane ^ 7 (half rows mirrored)
 }
 
+// Global -> LDS copies (dma_lds4, dma_lds16_s) to a wave-uniform LDS byte address
+__device__ __forceinline__ void copy_lds4(const void* src, uint32_t to) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(to) : "memory");
+}
+__device__ __forceinline__ void copy_lds16(const void* base, uint32_t off, uint32_t to) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(to) : "memory");
+}
+
 template <int D, int STYLE, bool ROPE, int CB, int WR>
 __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan, const TreeArgs a) {
     constexpr bool SHARED = WR > 1;        // the waves share their keys
@@ -276,6 +284,10 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
     __shared__ int32_t ps[NW][NST][OWNK];
     __shared__ float ksc[NST][STEP];       // powers of two held back from a step's keys
     __shared__ int32_t kbig[NST][NW];      // whether some key of a wave has one
+    // Steps in which rows differ in what they see: infinities of V (bits 0-7: +, 8-15: -, of a
+    // chunk's dimensions, a NaN both), and whether a wave's keys have some
+    __shared__ uint16_t vinf[NST][STEP][CH];
+    __shared__ int32_t vbad[NST][NW];
     __shared__ float2 mls[NW][16 * CB];
     __shared__ float qsl[NW][16 * CB];
     __shared__ __attribute__((aligned(4))) uint8_t infs[NW][CB][DB][64];   // infinities of V that a lane's rows see: +, 4 dims, and -, 4 dims
@@ -338,10 +350,11 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
         for (int i = 0; i < (SHARED ? DPL : 1); ++i) r.b[i] = scalar_load(btab, min(u * STEP + copy_key(i), k_hi - 1) >> 4);
         return r;
     };
+    const uint32_t stages_at = lds_offset(stages), ps_at = lds_offset(&ps[wave][0][0]);
     auto issue = [&](int u, int st, const Blocks& blk) {
-        uint16_t* sg = stages + st * SE;
+        const uint32_t sg = stages_at + (uint32_t)st * SE * 2;
         __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));   // the stage's last reads have returned (lgkmcnt 0)
-        if (ROPE && lane < OWNK) dma_lds4(posv + near_key(u * STEP + own_key(lane)), &ps[wave][st][0]);
+        if (ROPE && lane < OWNK) copy_lds4(posv + near_key(u * STEP + own_key(lane)), ps_at + (uint32_t)st * OWNK * 4);
 #pragma unroll
         for (int i = 0; i < DPL; ++i) {
             const int k0 = u * STEP + copy_key(i);
@@ -351,8 +364,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
                 const int k = k0 + lane / CH, row = k & (TK - 1);
                 off += ((near_key(k) & (TK - 1)) - row) * D * 2;
             }
-            dma_lds16_s(kpool + base, off, sg + copy_key(i) * D);
-            dma_lds16_s(vpool + base, off, sg + KV + copy_key(i) * D);
+            copy_lds16(kpool + base, off, sg + copy_key(i) * D * 2);
+            copy_lds16(vpool + base, off, sg + KV * 2 + copy_key(i) * D * 2);
         }
     };
 #pragma unroll
@@ -505,16 +518,15 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
         const uint32_t pos = (uint32_t)ps[wave][st][own_j];
         if (fresh == 0 || __builtin_amdgcn_ballot_w64(pos != cs_pos + STEP) != 0) {
 #pragma unroll
-            for (int i = 0; i < PL; ++i) rope_cs_fast((int32_t)pos, fstep[pair_of(i)], rc[i], rs[i]);
+            for (int i = 0; i < PL; ++i) rope_cs_fast((int32_t)(pos - STEP), fstep[pair_of(i)], rc[i], rs[i]);
             fresh = kRenew;
-        } else {
+        }
 #pragma unroll
-            for (int i = 0; i < PL; ++i) {
-                const float2 d = stride_cs[pair_of(i)];
-                const float c = rc[i], s = rs[i];
-                rc[i] = c * d.x - s * d.y;
-                rs[i] = s * d.x + c * d.y;
-            }
+        for (int i = 0; i < PL; ++i) {
+            const float2 d = stride_cs[pair_of(i)];
+            const float c = rc[i], s = rs[i];
+            rc[i] = c * d.x - s * d.y;
+            rs[i] = s * d.x + c * d.y;
         }
         --fresh;
         cs_pos = pos;
@@ -559,9 +571,37 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
         return any;
     };
 
-    // ---- NT tiles: their K operands, V tiles, first key, and whether their keys have powers of two
-    // to give back (kscale, in tile order)
-    auto tiles = [&](auto ntc, const u32x4_t (*kf)[KD], const uint16_t* vt, int k0, bool powers, const float* kscale) {
+    // ---- An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in the product):
+    // where a step has keys that not every row sees, the wave that copied them puts zeros in
+    // their place and notes them; what rows see of them joins their outputs at the end.
+    auto clean = [&](int u, int st) {
+        if (u * STEP >= k_lo && (u + 1) * STEP <= min(k_hi, k_tok)) return;
+        uint32_t found = 0;
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) {
+            const int key = copy_key(i) + lane / CH;
+            u32x4_t* at = reinterpret_cast<u32x4_t*>(stages + st * SE + KV + copy_key(i) * D + lane * 8);
+            u32x4_t v = *at;
+            uint32_t f = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t x = (v[e / 2] >> (16 * (e % 2))) & 0xffffu;
+                if ((x & 0x7f80u) == 0x7f80u) {
+                    f |= (x != 0xff80u ? 1u << e : 0u) | (x != 0x7f80u ? 0x100u << e : 0u);
+                    v[e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
+                }
+            }
+            vinf[st][key][(lane % CH) ^ dswz<D>(key & (TK - 1))] = (uint16_t)f;
+            if (f != 0) *at = v;
+            found |= f;
+        }
+        const bool any = __builtin_amdgcn_ballot_w64(found != 0) != 0;
+        if (lane == 0) vbad[st][wave] = any;
+    };
+
+    // ---- NT tiles: their K operands, V tiles, first key, stage and place in it, and whether their
+    // keys have powers of two to give back
+    auto tiles = [&](auto ntc, const u32x4_t (*kf)[KD], const uint16_t* vt, int k0, int st, int tile0, bool powers) {
         constexpr int NT = decltype(ntc)::value;
         f32x4_t sc[NT][CB];
 #pragma unroll
@@ -582,7 +622,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[n][cb][r] *= kscale[n * TK + 4 * q4 + r];
+                    for (int r = 0; r < 4; ++r) sc[n][cb][r] *= ksc[st][tile0 + n * TK + 4 * q4 + r];
         }
         const bool masked = k0 < k_lo || k_hi - k0 < NT * TK || k_tok - k0 < NT * TK;
         uint32_t seen[CB];   // masked tiles: the row's bits of the tiles' keys
@@ -598,6 +638,19 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (!((seen[cb] >> (16 * n + 4 * q4 + r)) & 1)) sc[n][cb][r] = -INFINITY;
+            }
+            if (__builtin_amdgcn_ballot_w64(vbad[st][lane % NW] != 0) != 0) {
+                // which of this lane's outputs the seen infinities reach
+#pragma unroll 1
+                for (int k = 0; k < NT * TK; ++k)
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb)
+                        if ((seen[cb] >> k) & 1)
+#pragma unroll 1
+                            for (int db = 0; db < DB; ++db) {
+                                const uint32_t both = vinf[st][tile0 + k][2 * db + (q4 >> 1)] >> (4 * (q4 & 1));
+                                infs[wave][cb][db][lane] |= (uint8_t)((both & 15u) | ((both >> 4) & 0xf0u));
+                            }
             }
         }
         float mx[CB];
@@ -628,51 +681,6 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
             u32x2_t af[DB];
 #pragma unroll
             for (int db = 0; db < DB; ++db) af[db] = __builtin_bit_cast(u32x2_t, lds_read_tr(as_lds(vt + n * TK * D) + v_off[db]));
-            uint32_t huge = 0;   // masked tiles: whether V holds an infinity or NaN
-            if (masked) {
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        huge |= (uint32_t)((af[db][e] & 0x7f80u) == 0x7f80u) | (uint32_t)((af[db][e] & 0x7f800000u) == 0x7f800000u);
-            }
-            if (masked && __builtin_amdgcn_ballot_w64(huge != 0) != 0) {
-                // An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in
-                // the product below): the product takes the finite elements, and two more count
-                // the seen infinities of either sign (a NaN as one of each) per row and
-                // dimension, which join the outputs at the end.
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    u32x2_t fin, up, down;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        fin[e] = up[e] = down[e] = 0;
-#pragma unroll
-                        for (int h = 0; h < 32; h += 16) {
-                            const uint32_t x = (af[db][e] >> h) & 0xffffu, mag = x & 0x7fffu;
-                            if (mag < 0x7f80u) fin[e] |= x << h;
-                            else {
-                                if (x != 0xff80u) up[e] |= 0x3f80u << h;
-                                if (x != 0x7f80u) down[e] |= 0x3f80u << h;
-                            }
-                        }
-                    }
-                    af[db] = fin;
-#pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) {
-                        const uint32_t k4 = seen[cb] >> (16 * n + 4 * q4);
-                        const u32x2_t one = {(k4 & 1u) * 0x3f80u | ((k4 >> 1) & 1u) * 0x3f800000u,
-                                             ((k4 >> 2) & 1u) * 0x3f80u | ((k4 >> 3) & 1u) * 0x3f800000u};
-                        const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
-                        const f32x4_t u = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4_t, up), __builtin_bit_cast(bf16x4_t, one), zero, 0, 0, 0);
-                        const f32x4_t d = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bf16x4_t, down), __builtin_bit_cast(bf16x4_t, one), zero, 0, 0, 0);
-                        uint32_t f = 0;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) f |= (u[i] > 0.f ? 1u << i : 0u) | (d[i] > 0.f ? 16u << i : 0u);
-                        infs[wave][cb][db][lane] |= (uint8_t)f;
-                    }
-                }
-            }
             u32x4_t pw[CB];   // upper and lower parts of the probabilities
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
@@ -720,6 +728,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
                 if (t + NST < nt) blk = blocks_of(t + NST);
             }
             const uint16_t* kt = stages + st * SE + wave * TK * D;
+            clean(t, st);
             u32x4_t kf[1][KD];
             load_k(kf[0], kt);
             bool powers = false;
@@ -731,7 +740,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
 #pragma unroll
                 for (int i = 0; i < PL; ++i) kf[0][i / 4][i % 4] = w[i];
             }
-            tiles(Idx<1>{}, kf, kt + KV, t * STEP + wave * TK, powers, &ksc[st][wave * TK]);
+            tiles(Idx<1>{}, kf, kt + KV, t * STEP + wave * TK, st, wave * TK, powers);
             st = next(st);
         }
     } else {
@@ -740,6 +749,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
         auto prepare = [&](int u, int sl) {
             if (u >= nt) return;
             wait_step(u, Idx<NST - 2>{});
+            clean(u, sl);
             if constexpr (ROPE) {
                 uint16_t* kt = stages + sl * SE;
                 uint32_t w[PL];
@@ -786,7 +796,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
                     u32x4_t kf[NT][KD];
 #pragma unroll
                     for (int m = 0; m < NT; ++m) load_k(kf[m], kt + m * TK * D);
-                    tiles(Idx<NT>{}, kf, kt + KV, k0, powers, &ksc[st][(kg * (4 / KG) + n) * TK]);
+                    tiles(Idx<NT>{}, kf, kt + KV, k0, st, (kg * (4 / KG) + n) * TK, powers);
                 }
             }
             barrier_keep_vmem();
