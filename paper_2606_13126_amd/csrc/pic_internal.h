@@ -199,9 +199,9 @@ struct TreeArgs : Args {
 
 // bf16 attention of drafted tokens: waves of a workgroup and its query rows for spans of at
 // most `rows` of them.  Up to 32 rows the waves all hold the same ones and take different cache
-// blocks; beyond, they are 2, 4 or 8 groups of 32 rows that share keys, 64 at a time.
+// blocks; beyond, they hold 32 each and share keys, 64 at a time.
 constexpr int kTreeWaves = 8;
-constexpr int tree_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+constexpr int tree_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256; }
 constexpr int tree_keys(int rows) { return rows <= 32 ? kTreeWaves * kBlock : 64; }   // keys that they take at a time
 
 // Rows of kv_append: strides in 16-byte chunks

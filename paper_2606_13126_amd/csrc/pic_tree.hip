@@ -3,8 +3,8 @@
 //  * kv_append  rows of a projection: k and v into the pool's slots, q packed; k and q
 //               turned at their positions on the way where the pool holds turned keys.
 //  * tree_mask  ancestor bits and depths of drafted trees.
-//  * tree_bf16  attention of the drafted tokens, bf16 MFMA; tree_merge joins its key splits.
-//               (float32: attn_f32 over TreeArgs, in pic_kernels.hip)
+//  * tree_few, tree_many  attention of the drafted tokens in bf16; tree_merge joins their key
+//               splits.  (float32: attn_f32 over TreeArgs, in pic_kernels.hip)
 //  * kv_keep    the accepted rows of every tree move to the front of its slots.
 #include <type_traits>
 
@@ -16,6 +16,7 @@ namespace {
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
 
 // ---------------------------------------------------------------------------------
 // kv_append: one workgroup per row.  A unit is two 16-byte chunks of a head: NeoX the two
@@ -210,31 +211,26 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 }
 
 // ---------------------------------------------------------------------------------
-// tree_bf16
+// Attention of drafted tokens in bf16: tree_few and tree_many
 //
 // Workgroup: eight waves (two per SIMD, so that one's products run under the other's vector
-// work) over up to 16 CB WR query rows (drafted token x query head of one KV head's group) and
-// one key range.  The waves are WR row groups of KG = 8 / WR; a wave holds 16 CB rows.
-//   Few rows (WR = 1): a wave takes every eighth 16-key tile (one cache block) of the range, which
-//     it copies, turns and multiplies without waiting for another wave.
-//   More rows: steps of 64 keys.  Each wave copies and turns eight keys of a step, in place, one
-//     step before the row groups multiply them; one barrier per step.
-// K, V and the keys' positions go straight to LDS.  The results of a row group's KG waves meet
-// in LDS at the end.
-//   S^T (16 keys x 16 rows) = K Q^T       v_mfma_f32_16x16x32_f16 (bf16 without rotation)
-//   O^T (16 dims x 16 rows) += V^T P^T    v_mfma_f32_16x16x32_bf16, V^T by ds_read_b64_tr_b16
-// After the scores lane l holds row l%16 of each block and keys 4 (l/16) + {0..3}, the B
-// operand of the output product.
+// work) over some query rows (drafted token x query head of one KV head's group) and one key
+// range.  K, V and the keys' positions go straight to LDS, some steps ahead.
+//   tree_few   up to 32 rows, held by every wave.  A wave takes every eighth 16-key tile (one
+//              cache block) of the range, which it copies, turns and multiplies without waiting
+//              for another wave; the eight results meet in LDS at the end.
+//   tree_many  128 or 256 rows, 32 of a wave, in steps of 64 keys that all waves share.  A wave
+//              copies and turns eight keys of a step, in place, one step before they are
+//              multiplied; one barrier per step.
 //
 // Precision: a rotated key or query is rounded to 11 bits (float16), its size held by a power
 // of two where it does not fit: as bf16, 8 bits, each of the two alone would put outputs as
 // far from 64 bits as their own rounding does.  Without rotation q and k are exact.  A
-// probability enters the product as two bf16 numbers, its upper 8 bits and the rest: the 32
-// contraction steps of the instruction hold 16 keys twice, at the time of one.
+// probability enters the product as two bf16 numbers, its upper 8 bits and the rest.
 //
-// RoPE: a lane turns PL pairs of one key of a tile and holds their cos/sin.  Its next key is
+// RoPE: a lane turns PL pairs of one key of a step and holds their cos/sin.  Its next key is
 // STEP keys further; where the positions are too, the angles advance by a constant rotation (4
-// operations a pair, renewed every kRenew tiles), else they are computed.
+// operations a pair, renewed every kRenew steps), else they are computed.
 // ---------------------------------------------------------------------------------
 constexpr int kRenew = 32;
 
@@ -256,102 +252,135 @@ __device__ __forceinline__ void copy_lds16(const void* base, uint32_t off, uint3
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(to) : "memory");
 }
 
-template <int D, int STYLE, bool ROPE, int CB, int WR>
-__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan, const TreeArgs a) {
-    constexpr bool SHARED = WR > 1;        // the waves share their keys
-    constexpr int KD = D / 32;             // 16x16x32 contraction steps of QK^T
-    constexpr int DB = D / 16;             // 16-dim blocks of O^T
-    constexpr int CH = D / 8;              // 16-byte chunks per K/V row
-    constexpr int HALF = D / 2;
-    constexpr int TK = kBlock;
-    constexpr int NW = kTreeWaves, KG = NW / WR;
-    constexpr int STEP = SHARED ? 64 : NW * TK;    // keys of all waves
-    constexpr int OWNK = SHARED ? STEP / NW : TK;  // keys that a wave copies and turns
-    constexpr int PL = OWNK * HALF / 64;   // pairs that a lane turns
-    constexpr int NST = SHARED || D == 64 ? 4 : 2;
-    constexpr int DPL = OWNK * CH / 64;    // 16-byte copies per lane per step, each of K and V
-    constexpr int LPS = 2 * DPL + (ROPE ? 1 : 0);
-    constexpr int KV = STEP * D;           // elements of K or V in a stage
-    constexpr int SE = 2 * KV;             // elements of a stage: K of every tile, then V
-    constexpr int OWN = CB > KG ? CB / KG : 1;     // column blocks whose queries a wave turns
-    constexpr int SPARE = SHARED ? 2 : 1;  // stages that the queries pass through
-    constexpr int PER = SPARE * SE / NW;   // elements of them per wave
-    static_assert((NST - 2) * LPS < 64, "vmcnt range");
-    static_assert(NST * SE * 2 >= NW * CB * DB * 64 * 16, "the outputs meet in the stages");
-    static_assert(PER * 2 >= 16 * HALF * 8 && PER * 2 >= OWN * KD * 64 * 16, "queries pass through the stages");
+// Sizes of the two kernels' steps (SHARED: tree_many)
+template <int D, bool SHARED>
+struct TreeShape {
+    static constexpr int CH = D / 8;             // 16-byte chunks per K/V row
+    static constexpr int HALF = D / 2;
+    static constexpr int NW = kTreeWaves;
+    static constexpr int STEP = SHARED ? 64 : NW * kBlock;   // keys of all waves
+    static constexpr int OWNK = STEP / NW;       // keys that a wave copies and turns
+    static constexpr int PL = OWNK * HALF / 64;  // pairs that a lane turns
+    static constexpr int NST = SHARED || D == 64 ? 4 : 2;    // steps in LDS
+    static constexpr int KPC = 64 / CH;          // keys per copy (64 chunks)
+    static constexpr int DPL = OWNK / KPC;       // copies per lane per step, each of K and V
+    static constexpr int KV = STEP * D;          // elements of K or V in a stage
+    static constexpr int SE = 2 * KV;            // elements of a stage: K of every tile, then V
+};
 
-    __shared__ __attribute__((aligned(16))) uint16_t stages[NST * SE];
-    __shared__ int32_t ps[NW][NST][OWNK];
-    __shared__ float ksc[NST][STEP];       // powers of two held back from a step's keys
-    __shared__ int32_t kbig[NST][NW];      // whether some key of a wave has one
+template <int D, bool SHARED>
+struct __attribute__((aligned(16))) TreeLds {
+    typedef TreeShape<D, SHARED> S;
+    uint16_t stages[S::NST * S::SE];
+    float2 stride_cs[S::HALF];           // cos/sin of STEP positions
+    uint64_t fstep[S::HALF];
+    int32_t ps[S::NW][S::NST][S::OWNK];  // positions
+    float ksc[S::NST][S::STEP];          // powers of two held back from a step's keys
+    int32_t kbig[S::NST][S::NW];         // whether some key of a wave has one
     // Steps in which rows differ in what they see: infinities of V (bits 0-7: +, 8-15: -, of a
     // chunk's dimensions, a NaN both), and whether a wave's keys have some
-    __shared__ uint16_t vinf[NST][STEP][CH];
-    __shared__ int32_t vbad[NST][NW];
-    __shared__ float2 mls[NW][16 * CB];
-    __shared__ float qsl[NW][16 * CB];
-    __shared__ __attribute__((aligned(4))) uint8_t infs[NW][CB][DB][64];   // infinities of V that a lane's rows see: +, 4 dims, and -, 4 dims
-    __shared__ uint64_t fstep[HALF];
-    __shared__ __attribute__((aligned(16))) float2 stride_cs[HALF];        // cos/sin of STEP positions
+    uint16_t vinf[S::NST][S::STEP][S::CH];
+    int32_t vbad[S::NST][S::NW];
+};
 
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int rg = wave / KG, kg = wave % KG;
-    const int c16 = lane & 15, q4 = lane >> 4;
-    const Group g = group_of<false>(plan, blockIdx.x);
-    const int G = a.group, n_rt = g.n_rt;
-    const int li = blockIdx.x - g.item_base;
-    if (li >= a.hkv * g.n_split * n_rt) return;
-    const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
-    const int rows_total = g.n_tok * G, row_lo = (ic.rt * WR + rg) * 16 * CB;
-    const int kv_lo = g.win + ic.split * g.split_keys, end = g.tok0 + g.n_tok;
-    // (no sum below passes the last key: a request may have 2^31 - 1 of them)
-    const int kv_hi = g.split_keys < end - kv_lo ? kv_lo + g.split_keys : end;
-    // keys relative to kt0, the start of the first tile's block
-    const int kt0 = kv_lo & ~(TK - 1), k_lo = kv_lo - kt0, k_hi = kv_hi - kt0, k_tok = g.tok0 - kt0;
-    const int n_tiles = (k_hi - 1) / TK + 1;
-    // steps in which this wave copies keys
-    const int nt = SHARED ? (k_hi - 1) / STEP + 1 : n_tiles > wave ? (n_tiles - wave - 1) / NW + 1 : 0;
+// A wave's share of the keys of a workgroup's range: copies into LDS, angles, turning.
+template <int D, int STYLE, bool ROPE, bool SHARED>
+struct TreeKeys : TreeShape<D, SHARED> {
+    typedef TreeShape<D, SHARED> S;
+    using S::CH; using S::HALF; using S::NW; using S::STEP; using S::OWNK; using S::PL; using S::NST; using S::KPC;
+    using S::DPL; using S::KV; using S::SE;
+    static constexpr int LPS = 2 * DPL + (ROPE ? 1 : 0);   // copies per lane per step
+    static constexpr int RUN = SHARED ? PL : STYLE == kNeox ? 8 : 4;   // pairs in a row
+    static_assert((NST - 2) * LPS < 64, "vmcnt range");
 
-    if (ROPE)
-        for (int i = tid; i < HALF; i += NW * 64) {
-            fstep[i] = a.fstep[i];
-            rope_cs_fast(STEP, a.fstep[i], stride_cs[i].x, stride_cs[i].y);
-        }
-    for (int i = tid; i < NW * CB * DB * 16; i += NW * 64) reinterpret_cast<uint32_t*>(infs)[i] = 0;
+    TreeLds<D, SHARED>& s;
+    int lane, wave;
+    int k_lo, k_hi, k_tok;     // first and last key + 1 of the range, and the span's start, from kt0, the start of the first block
+    int nt;                    // steps in which this wave copies keys
+    const int32_t* btab;
+    const int32_t* posv;
+    const uint16_t* kpool;
+    const uint16_t* vpool;
+    size_t blk_stride;
+    uint32_t stages_at, ps_at;
+    uint32_t lane_off[DPL];    // byte offset within one head's page of a block
+    int own_j, pair0, sh_row;  // the key that the lane turns (of the wave's, of the step), and its first pair
+    // SHARED: element offsets of the lane's two runs (NeoX) or of its 2 PL neighbours (GPT-J), as
+    // copied and (in the order of the kernel's chunks) as turned
+    int s_off[2], t_off[2];
+    float rc[PL], rs[PL];      // cos/sin at position cs_pos
+    uint32_t cs_pos = 0;
+    int fresh = 0;             // steps until the angles are computed again
 
-    const int32_t* btab = a.block_tables + (size_t)g.req * a.max_blocks + (kt0 >> 4);
-    const int32_t* posv = a.positions + g.pos_off + kt0;
-    const size_t blk_stride = (size_t)a.hkv * kBlock * D;
-    const uint16_t* kpool = static_cast<const uint16_t*>(a.k_pool) + (size_t)ic.kvh * kBlock * D;
-    const uint16_t* vpool = static_cast<const uint16_t*>(a.v_pool) + (size_t)ic.kvh * kBlock * D;
+    struct Blocks {
+        int b[SHARED ? DPL : 1];   // (without sharing a step's copies are of one block)
+    };
 
-    // The i-th copy of a step moves 64 chunks, 64 / CH keys from copy_key(i) on.  A key outside
+    // The i-th copy of a step moves 64 chunks, KPC keys from copy_key(i) on.  A key outside
     // [k_lo, k_hi) stands for the nearest one inside, so that nothing outside the range is
     // read (its score is masked).
-    constexpr int KPC = 64 / CH;           // keys per copy
-    auto copy_key = [&](int i) { return SHARED ? (i * NW + wave) * KPC : wave * TK + i * KPC; };
-    auto near_key = [&](int k) { return min(max(k, k_lo), k_hi - 1); };
-    // this lane's byte offset within one head's page of a block, but for the row
-    uint32_t lane_off[DPL];
-#pragma unroll
-    for (int i = 0; i < DPL; ++i) {
-        const int row = (copy_key(i) + lane / CH) & (TK - 1);
-        lane_off[i] = (uint32_t)(row * D + (((lane % CH) ^ dswz<D>(row)) << 3)) * 2;
-    }
+    __device__ __forceinline__ int copy_key(int i) const { return SHARED ? (i * NW + wave) * KPC : wave * kBlock + i * KPC; }
+    __device__ __forceinline__ int near_key(int k) const { return min(max(k, k_lo), k_hi - 1); }
     // own key j (0 .. OWNK - 1) of a step: its place in the step
-    auto own_key = [&](int j) { return copy_key(j / KPC) + j % KPC; };
-    struct Blocks {
-        int b[SHARED ? DPL : 1];           // (without sharing a step's copies are of one block)
-    };
-    auto blocks_of = [&](int u) {
+    __device__ __forceinline__ int own_key(int j) const { return copy_key(j / KPC) + j % KPC; }
+    __device__ __forceinline__ int pair_of(int i) const { return pair0 + (SHARED ? i : i / RUN * 4 * RUN + i % RUN); }
+
+    __device__ __forceinline__ TreeKeys(TreeLds<D, SHARED>& lds, const TreeArgs& a, const Group& g, const ItemCoords& ic)
+        : s(lds), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) {
+        const int kv_lo = g.win + ic.split * g.split_keys, end = g.tok0 + g.n_tok;
+        // (no sum below passes the last key: a request may have 2^31 - 1 of them)
+        const int kv_hi = g.split_keys < end - kv_lo ? kv_lo + g.split_keys : end;
+        const int kt0 = kv_lo & ~(kBlock - 1);
+        k_lo = kv_lo - kt0;
+        k_hi = kv_hi - kt0;
+        k_tok = g.tok0 - kt0;
+        const int n_tiles = (k_hi - 1) / kBlock + 1;
+        nt = SHARED ? (k_hi - 1) / STEP + 1 : n_tiles > wave ? (n_tiles - wave - 1) / NW + 1 : 0;
+        btab = a.block_tables + (size_t)g.req * a.max_blocks + (kt0 >> 4);
+        posv = a.positions + g.pos_off + kt0;
+        blk_stride = (size_t)a.hkv * kBlock * D;
+        kpool = static_cast<const uint16_t*>(a.k_pool) + (size_t)ic.kvh * kBlock * D;
+        vpool = static_cast<const uint16_t*>(a.v_pool) + (size_t)ic.kvh * kBlock * D;
+        stages_at = lds_offset(s.stages);
+        ps_at = lds_offset(&s.ps[wave][0][0]);
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) {
+            const int row = (copy_key(i) + lane / CH) & (kBlock - 1);
+            lane_off[i] = (uint32_t)(row * D + (((lane % CH) ^ dswz<D>(row)) << 3)) * 2;
+        }
+        // Without sharing a lane has the operand's elements of key lane % 16: runs of 8 (NeoX pairs
+        // 32 kd + 8 (lane / 16) + e of chunks kd and kd + KD / 2; GPT-J pairs 16 kd + 4 (lane / 16)
+        // + m).  With sharing 8 lanes have one key, PL pairs (lane % 8) * PL + i each.
+        own_j = SHARED ? lane >> 3 : lane & 15;
+        pair0 = SHARED ? (lane & 7) * PL : RUN * (lane >> 4);
+        sh_row = own_key(own_j);
+        if (SHARED) {
+            const int e0 = STYLE == kNeox ? pair0 : 2 * pair0, e1 = STYLE == kNeox ? pair0 + HALF : e0 + PL;
+            const int row = sh_row & (kBlock - 1);
+            for (int h = 0; h < 2; ++h) {
+                const int e = h == 0 ? e0 : e1;
+                s_off[h] = sh_row * D + ((model_chunk(a.chunk_map, e >> 3) ^ dswz<D>(row)) << 3) + (e & 7);
+                t_off[h] = sh_row * D + (((e >> 3) ^ dswz<D>(row)) << 3) + (e & 7);
+            }
+        }
+    }
+
+    // phase steps and the angles of STEP positions (all threads; a barrier follows)
+    __device__ __forceinline__ void fill_steps(const TreeArgs& a) {
+        if (ROPE)
+            for (int i = threadIdx.x; i < HALF; i += NW * 64) {
+                s.fstep[i] = a.fstep[i];
+                rope_cs_fast(STEP, a.fstep[i], s.stride_cs[i].x, s.stride_cs[i].y);
+            }
+    }
+    __device__ __forceinline__ Blocks blocks_of(int u) const {
         Blocks r;
 #pragma unroll
         for (int i = 0; i < (SHARED ? DPL : 1); ++i) r.b[i] = scalar_load(btab, min(u * STEP + copy_key(i), k_hi - 1) >> 4);
         return r;
-    };
-    const uint32_t stages_at = lds_offset(stages), ps_at = lds_offset(&ps[wave][0][0]);
-    auto issue = [&](int u, int st, const Blocks& blk) {
+    }
+    // the wave's copies of step u, into stage st
+    __device__ __forceinline__ void issue(int u, int st, const Blocks& blk) const {
         const uint32_t sg = stages_at + (uint32_t)st * SE * 2;
         __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));   // the stage's last reads have returned (lgkmcnt 0)
         if (ROPE && lane < OWNK) copy_lds4(posv + near_key(u * STEP + own_key(lane)), ps_at + (uint32_t)st * OWNK * 4);
@@ -361,172 +390,35 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
             const size_t base = (size_t)(uint32_t)blk.b[SHARED ? i : 0] * blk_stride;
             uint32_t off = lane_off[i];
             if (k0 < k_lo || k_hi - k0 < KPC) {
-                const int k = k0 + lane / CH, row = k & (TK - 1);
-                off += ((near_key(k) & (TK - 1)) - row) * D * 2;
+                const int k = k0 + lane / CH, row = k & (kBlock - 1);
+                off += ((near_key(k) & (kBlock - 1)) - row) * D * 2;
             }
             copy_lds16(kpool + base, off, sg + copy_key(i) * D * 2);
             copy_lds16(vpool + base, off, sg + KV * 2 + copy_key(i) * D * 2);
         }
-    };
-#pragma unroll
-    for (int u = 0; u < NST - SPARE; ++u)
-        if (u < nt) issue(u, u, blocks_of(u));
-
-    // ---- queries: the KG waves of a row group turn its column blocks and pass them to each
-    // other through stages that are filled later.  The cos/sin of a block's tokens (a token's
-    // heads share them) go the same way before.
-    int toff[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        const int row = row_lo + 16 * cb + c16;
-        toff[cb] = row < rows_total ? row / G : 0;
     }
-    bf16x8_t qb[CB][KD];
-    float qs[CB];     // scores are the products times this (log2 units)
-    __syncthreads();  // phase steps staged
-    {
-        u32x4_t mine[OWN][KD];
-        uint16_t* spare = stages + (NST - SPARE) * SE + wave * PER;
-#pragma unroll
-        for (int o = 0; o < OWN; ++o) {
-            const int cb = kg + o * KG;
-            if (cb >= CB) break;
-            const int row0 = row_lo + 16 * cb, row = row0 + c16;
-            const bool valid = row < rows_total;
-            const int to = valid ? row / G : 0, hl = valid ? row - to * G : 0;
-            const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + to) * a.hq + (size_t)ic.kvh * G + hl) * D;
-            u32x4_t raw[KD];
-#pragma unroll
-            for (int kd = 0; kd < KD; ++kd) {
-                raw[kd] = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, kd * 4 + q4) * 8);
-                if (!valid) raw[kd] = u32x4_t{0, 0, 0, 0};
-            }
-            float scale = a.scale_log2;
-            if (ROPE) {
-                const int t0 = min(row0, rows_total - 1) / G, t1 = min(row0 + 15, rows_total - 1) / G;
-                float2* cs = reinterpret_cast<float2*>(spare);
-                for (int i = lane; i < (t1 - t0 + 1) * HALF; i += 64) {
-                    float c, s;
-                    rope_cs_fast(a.positions[g.pos_off + g.tok0 + t0 + i / HALF], fstep[i % HALF], c, s);
-                    cs[i] = make_float2(c, s);
-                }
-                const float2* tc = cs + (valid ? to - t0 : 0) * HALF;
-                float xf[KD][8], big = 0.f;
-#pragma unroll
-                for (int kd = 0; kd < KD; ++kd)
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        xf[kd][2 * m] = bf_lo(raw[kd][m]);
-                        xf[kd][2 * m + 1] = bf_hi(raw[kd][m]);
-                    }
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    // NeoX: pairs 32 kd + 8 q4 + e, elements e of chunks kd and kd + KD / 2; GPT-J:
-                    // 16 kd + 4 q4 + m, elements 2 m and 2 m + 1 of chunk kd
-                    const int kd = STYLE == kNeox ? i / 8 : i / 4, e = STYLE == kNeox ? i % 8 : i % 4;
-                    const float2 t = tc[STYLE == kNeox ? kd * 32 + 8 * q4 + e : kd * 16 + 4 * q4 + e];
-                    float& x = STYLE == kNeox ? xf[kd][e] : xf[kd][2 * e];
-                    float& y = STYLE == kNeox ? xf[kd + KD / 2][e] : xf[kd][2 * e + 1];
-                    const float x0 = x, y0 = y;
-                    x = x0 * t.x - y0 * t.y;
-                    y = y0 * t.x + x0 * t.y;
-                    big = fmaxf(big, fmaxf(fabsf(x), fabsf(y)));
-                }
-                big = max_xor32(max_xor16(big));
-                // the row times 2^-ex lies in [-1, 1]
-                const int ex = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
-                scale = ldexpf(scale, ex);
-#pragma unroll
-                for (int kd = 0; kd < KD; ++kd)
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) raw[kd][m] = pack_f16(ldexpf(xf[kd][2 * m], -ex), ldexpf(xf[kd][2 * m + 1], -ex));
-            }
-#pragma unroll
-            for (int kd = 0; kd < KD; ++kd) mine[o][kd] = raw[kd];
-            if (KG == 1) {
-#pragma unroll
-                for (int kd = 0; kd < KD; ++kd) qb[o][kd] = __builtin_bit_cast(bf16x8_t, raw[kd]);
-                qs[o] = scale;
-            } else if (q4 == 0) {
-                qsl[rg * KG][16 * cb + c16] = scale;
-            }
-        }
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);   // the last block's cos/sin have been read
-        if constexpr (KG > 1) {
-#pragma unroll
-            for (int o = 0; o < OWN; ++o)
-                if (kg + o * KG < CB)
-#pragma unroll
-                    for (int kd = 0; kd < KD; ++kd) reinterpret_cast<u32x4_t*>(spare)[(o * KD + kd) * 64 + lane] = mine[o][kd];
-            barrier_keep_vmem();
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-                const uint16_t* from = stages + (NST - SPARE) * SE + (rg * KG + cb % KG) * PER + (cb / KG) * KD * 64 * 8;
-#pragma unroll
-                for (int kd = 0; kd < KD; ++kd) qb[cb][kd] = *reinterpret_cast<const bf16x8_t*>(from + (kd * 64 + lane) * 8);
-                qs[cb] = qsl[rg * KG][16 * cb + c16];
-            }
-        }
-        barrier_keep_vmem();   // every wave has its rows: the stages may be filled
+    // step u's copies have landed once no more than those of the LATER next ones are outstanding
+    template <int LATER>
+    __device__ __forceinline__ void wait_step(int u) const {
+        if (LATER > 0 && u + LATER < nt) wait_vmem_n<LATER * LPS>();
+        else wait_vmem();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
     }
-
-    f32x4_t acc[CB][DB];
-    float m_run[CB], l_run[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        m_run[cb] = kNegBig;
-        l_run[cb] = 0.f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) acc[cb][db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-
-    // per-lane element offsets within a tile: K operand rows and V^T operand rows
-    int k_off[KD], v_off[DB];
-#pragma unroll
-    for (int kd = 0; kd < KD; ++kd) k_off[kd] = c16 * D + ((model_chunk(a.chunk_map, kd * 4 + q4) ^ dswz<D>(c16)) << 3);
-    {
-        const int key = 4 * q4 + (c16 >> 2);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const int d = db * 16 + 4 * (lane & 3);
-            v_off[db] = key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7);
-        }
-    }
-
-    // ---- turning keys.  Without sharing a lane has the operand's elements of key c16: runs of 8
-    // (NeoX pairs 32 kd + 8 q4 + e of chunks kd and kd + KD / 2; GPT-J pairs 16 kd + 4 q4 + m).
-    // With sharing 8 lanes have one key, PL pairs (lane % 8) * PL + i each.
-    constexpr int RUN = SHARED ? PL : STYLE == kNeox ? 8 : 4;   // pairs in a row
-    const int own_j = SHARED ? lane >> 3 : c16;
-    const int pair0 = SHARED ? (lane & 7) * PL : RUN * q4;
-    auto pair_of = [&](int i) { return pair0 + (SHARED ? i : i / RUN * 4 * RUN + i % RUN); };
-    const int sh_row = SHARED ? own_key(own_j) : 0;
-    // SHARED: element offsets of the lane's two runs (NeoX) or of its 2 PL neighbours (GPT-J)
-    int s_off[2];
-    if (SHARED) {
-        const int e0 = STYLE == kNeox ? pair0 : 2 * pair0, e1 = STYLE == kNeox ? pair0 + HALF : e0 + PL;
-        const int row = sh_row & (TK - 1);
-        s_off[0] = sh_row * D + ((model_chunk(a.chunk_map, e0 >> 3) ^ dswz<D>(row)) << 3) + (e0 & 7);
-        s_off[1] = sh_row * D + ((model_chunk(a.chunk_map, e1 >> 3) ^ dswz<D>(row)) << 3) + (e1 & 7);
-    }
-    float rc[PL], rs[PL];   // cos/sin at position cs_pos
-    uint32_t cs_pos = 0;
-    int fresh = 0;          // steps until the angles are computed again
-    // turns 2 PL elements, words w[0 .. PL): NeoX x in the first half and y in the second; returns
-    // whether some key of the wave got a power of two
-    auto turn = [&](int st, uint32_t (&w)[PL]) {
-        const uint32_t pos = (uint32_t)ps[wave][st][own_j];
+    // Turns 2 PL elements, words w[0 .. PL): NeoX x in the first half and y in the second; returns
+    // whether some key of the wave got a power of two.
+    __device__ __forceinline__ bool turn(int st, uint32_t (&w)[PL]) {
+        const uint32_t pos = (uint32_t)s.ps[wave][st][own_j];
         if (fresh == 0 || __builtin_amdgcn_ballot_w64(pos != cs_pos + STEP) != 0) {
 #pragma unroll
-            for (int i = 0; i < PL; ++i) rope_cs_fast((int32_t)(pos - STEP), fstep[pair_of(i)], rc[i], rs[i]);
+            for (int i = 0; i < PL; ++i) rope_cs_fast((int32_t)(pos - STEP), s.fstep[pair_of(i)], rc[i], rs[i]);
             fresh = kRenew;
         }
 #pragma unroll
         for (int i = 0; i < PL; ++i) {
-            const float2 d = stride_cs[pair_of(i)];
-            const float c = rc[i], s = rs[i];
-            rc[i] = c * d.x - s * d.y;
-            rs[i] = s * d.x + c * d.y;
+            const float2 d = s.stride_cs[pair_of(i)];
+            const float c = rc[i], sn = rs[i];
+            rc[i] = c * d.x - sn * d.y;
+            rs[i] = sn * d.x + c * d.y;
         }
         --fresh;
         cs_pos = pos;
@@ -561,26 +453,25 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
             rotate(std::true_type{}, ex);
         }
         if (SHARED) {
-            if ((lane & 7) == 0) ksc[st][sh_row] = ldexpf(1.f, ex);
-            if (lane == 0) kbig[st][wave] = any;
-        } else if (any && q4 == 0) {
-            ksc[st][wave * TK + c16] = ldexpf(1.f, ex);
+            if ((lane & 7) == 0) s.ksc[st][sh_row] = ldexpf(1.f, ex);
+            if (lane == 0) s.kbig[st][wave] = any;
+        } else if (any && lane < 16) {
+            s.ksc[st][sh_row] = ldexpf(1.f, ex);
         }
 #pragma unroll
         for (int i = 0; i < PL; ++i) w[i] = out[i];
         return any;
-    };
-
-    // ---- An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in the product):
-    // where a step has keys that not every row sees, the wave that copied them puts zeros in
-    // their place and notes them; what rows see of them joins their outputs at the end.
-    auto clean = [&](int u, int st) {
+    }
+    // An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in the
+    // product): where a step has keys that not every row sees, the wave that copied them puts
+    // zeros in their place and notes them; what rows see of them joins their outputs at the end.
+    __device__ __forceinline__ void clean(int u, int st) {
         if (u * STEP >= k_lo && (u + 1) * STEP <= min(k_hi, k_tok)) return;
         uint32_t found = 0;
 #pragma unroll
         for (int i = 0; i < DPL; ++i) {
             const int key = copy_key(i) + lane / CH;
-            u32x4_t* at = reinterpret_cast<u32x4_t*>(stages + st * SE + KV + copy_key(i) * D + lane * 8);
+            u32x4_t* at = reinterpret_cast<u32x4_t*>(s.stages + st * SE + KV + copy_key(i) * D + lane * 8);
             u32x4_t v = *at;
             uint32_t f = 0;
 #pragma unroll
@@ -591,75 +482,257 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
                     v[e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
                 }
             }
-            vinf[st][key][(lane % CH) ^ dswz<D>(key & (TK - 1))] = (uint16_t)f;
+            s.vinf[st][key][(lane % CH) ^ dswz<D>(key & (kBlock - 1))] = (uint16_t)f;
             if (f != 0) *at = v;
             found |= f;
         }
         const bool any = __builtin_amdgcn_ballot_w64(found != 0) != 0;
-        if (lane == 0) vbad[st][wave] = any;
-    };
+        if (lane == 0) s.vbad[st][wave] = any;
+    }
+    // the infinities of V that 4 dimensions (half h of chunk c) have in key k of a step: +, 4 bits, and -, 4 bits
+    __device__ __forceinline__ uint32_t infs_of(int st, int k, int c, int h) const {
+        const uint32_t both = (uint32_t)s.vinf[st][k][c] >> (4 * h);
+        return (both & 15u) | ((both >> 4) & 0xf0u);
+    }
+    __device__ __forceinline__ bool wave_flag(const int32_t (&f)[NW]) const { return __builtin_amdgcn_ballot_w64(f[lane % NW] != 0) != 0; }
+    // keys [k_lo, k_hi) among the 32 from k0 on
+    __device__ __forceinline__ uint32_t inside(int k0, int n) const {
+        const int lo = min(max(k_lo - k0, 0), 31), hi = max(min(k_hi - k0, n), 0);
+        return (hi < 32 ? (1u << hi) - 1u : ~0u) & ~((1u << lo) - 1u);
+    }
+    // whether some row may not see one of n keys from k0 on
+    __device__ __forceinline__ bool masked(int k0, int n) const { return k0 < k_lo || k_hi - k0 < n || k_tok - k0 < n; }
+    static __device__ __forceinline__ int next(int st) { return st + 1 == NST ? 0 : st + 1; }
+    static __device__ __forceinline__ int prev(int st) { return st == 0 ? NST - 1 : st - 1; }
+};
 
-    // ---- NT tiles: their K operands, V tiles, first key, stage and place in it, and whether their
-    // keys have powers of two to give back
-    auto tiles = [&](auto ntc, const u32x4_t (*kf)[KD], const uint16_t* vt, int k0, int st, int tile0, bool powers) {
-        constexpr int NT = decltype(ntc)::value;
-        f32x4_t sc[NT][CB];
+// x with the infinities noted for its 4 dimensions
+__device__ __forceinline__ f32x4_t with_infs(f32x4_t x, uint32_t f) {
+    if (f != 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += ((f >> i) & 1 ? INFINITY : 0.f) - ((f >> (4 + i)) & 1 ? INFINITY : 0.f);
+    return x;
+}
+
+// cos/sin of a wave's tokens t0 .. t1 of the span (HALF pairs each) into cs
+template <int HALF>
+__device__ __forceinline__ void token_angles(const TreeArgs& a, const Group& g, const uint64_t* fstep, int lane, int t0, int t1, float2* cs) {
+    for (int i = lane; i < (t1 - t0 + 1) * HALF; i += 64) {
+        float c, s;
+        rope_cs_fast(a.positions[g.pos_off + g.tok0 + t0 + i / HALF], fstep[i % HALF], c, s);
+        cs[i] = make_float2(c, s);
+    }
+}
+
+// A query row's N chunks of 8 elements in xf turned by the angles tc (HALF pairs); the lane has
+// chunks c0 + i * dc (NeoX: the partners are N / 2 chunks on in xf).  Returns the largest size.
+template <int STYLE, int N>
+__device__ __forceinline__ float turn_row(float (&xf)[N][8], const float2* tc, int c0, int dc) {
+    float big = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) {
+        const int k = STYLE == kNeox ? i / 8 : i / 4, e = STYLE == kNeox ? i % 8 : i % 4;
+        const float2 t = tc[STYLE == kNeox ? (c0 + k * dc) * 8 + e : (c0 + k * dc) * 4 + e];
+        float& x = STYLE == kNeox ? xf[k][e] : xf[k][2 * e];
+        float& y = STYLE == kNeox ? xf[k + N / 2][e] : xf[k][2 * e + 1];
+        const float x0 = x, y0 = y;
+        x = x0 * t.x - y0 * t.y;
+        y = y0 * t.x + x0 * t.y;
+        big = fmaxf(big, fmaxf(fabsf(x), fabsf(y)));
+    }
+    return big;
+}
+
+// ---------------------------------------------------------------------------------
+// tree_few: up to 16 CB rows.
+//   S^T (16 keys x 16 rows) = K Q^T       v_mfma_f32_16x16x32_f16 (bf16 without rotation)
+//   O^T (16 dims x 16 rows) += V^T P^T    v_mfma_f32_16x16x32_bf16, V^T by ds_read_b64_tr_b16
+// After the scores lane l holds row l%16 of each block and keys 4 (l/16) + {0..3}, the B
+// operand of the output product.
+// ---------------------------------------------------------------------------------
+template <int D, int STYLE, bool ROPE, int CB>
+__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const Plan plan, const TreeArgs a) {
+    typedef TreeKeys<D, STYLE, ROPE, false> Keys;
+    constexpr int KD = D / 32;             // 16x16x32 contraction steps of QK^T
+    constexpr int DB = D / 16;             // 16-dim blocks of O^T
+    constexpr int TK = kBlock, NW = kTreeWaves, NST = Keys::NST, PL = Keys::PL, HALF = D / 2;
+    constexpr int PER = Keys::SE / NW;     // elements of a stage per wave
+    static_assert(NST * Keys::SE * 2 >= NW * CB * DB * 64 * 16, "the outputs meet in the stages");
+    static_assert(PER * 2 >= 16 * HALF * 8 && PER * 2 >= KD * 64 * 16, "queries pass through a stage");
+
+    __shared__ TreeLds<D, false> lds;
+    __shared__ float2 mls[NW][16 * CB];
+    __shared__ float qsl[16 * CB];
+    __shared__ __attribute__((aligned(4))) uint8_t infs[NW][CB][DB][64];   // infinities of V that a lane's rows see (Keys::infs_of)
+
+    const Group g = group_of<false>(plan, blockIdx.x);
+    const int G = a.group, n_rt = g.n_rt;
+    const int li = blockIdx.x - g.item_base;
+    if (li >= a.hkv * g.n_split * n_rt) return;
+    const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
+    const int rows_total = g.n_tok * G, row_lo = ic.rt * 16 * CB;
+    Keys keys(lds, a, g, ic);
+    const int lane = keys.lane, wave = keys.wave, nt = keys.nt;
+    const int c16 = lane & 15, q4 = lane >> 4;
+    keys.fill_steps(a);
+    for (int i = threadIdx.x; i < NW * CB * DB * 16; i += NW * 64) reinterpret_cast<uint32_t*>(infs)[i] = 0;
+#pragma unroll
+    for (int u = 0; u < NST - 1; ++u)
+        if (u < nt) keys.issue(u, u, keys.blocks_of(u));
+
+    // ---- queries: wave cb turns rows 16 cb .. 16 cb + 15 and passes them to the others through
+    // the stage that is filled last.  The cos/sin of their tokens (a token's heads share them) go
+    // the same way before.
+    int toff[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        const int row = row_lo + 16 * cb + c16;
+        toff[cb] = row < rows_total ? row / G : 0;
+    }
+    __syncthreads();  // phase steps staged
+    if (wave < CB) {
+        uint16_t* spare = lds.stages + (NST - 1) * Keys::SE + wave * PER;
+        const int row0 = row_lo + 16 * wave, row = row0 + c16;
+        const bool valid = row < rows_total;
+        const int to = valid ? row / G : 0, hl = valid ? row - to * G : 0;
+        const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + to) * a.hq + (size_t)ic.kvh * G + hl) * D;
+        u32x4_t raw[KD];
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) {
+            raw[kd] = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, kd * 4 + q4) * 8);
+            if (!valid) raw[kd] = u32x4_t{0, 0, 0, 0};
+        }
+        float scale = a.scale_log2;
+        if (ROPE) {
+            const int t0 = min(row0, rows_total - 1) / G, t1 = min(row0 + 15, rows_total - 1) / G;
+            float2* cs = reinterpret_cast<float2*>(spare);
+            token_angles<HALF>(a, g, lds.fstep, lane, t0, t1, cs);
+            float xf[KD][8];
+#pragma unroll
+            for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    xf[kd][2 * m] = bf_lo(raw[kd][m]);
+                    xf[kd][2 * m + 1] = bf_hi(raw[kd][m]);
+                }
+            float big = turn_row<STYLE, KD>(xf, cs + (valid ? to - t0 : 0) * HALF, q4, 4);
+            big = max_xor32(max_xor16(big));
+            // the row times 2^-ex lies in [-1, 1]
+            const int ex = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
+            scale = ldexpf(scale, ex);
+#pragma unroll
+            for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) raw[kd][m] = pack_f16(ldexpf(xf[kd][2 * m], -ex), ldexpf(xf[kd][2 * m + 1], -ex));
+        }
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);   // the cos/sin have been read
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) reinterpret_cast<u32x4_t*>(spare)[kd * 64 + lane] = raw[kd];
+        if (q4 == 0) qsl[16 * wave + c16] = scale;
+    }
+    barrier_keep_vmem();
+    bf16x8_t qb[CB][KD];
+    float qs[CB];     // scores are the products times this (log2 units)
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        const uint16_t* from = lds.stages + (NST - 1) * Keys::SE + cb * PER;
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) qb[cb][kd] = *reinterpret_cast<const bf16x8_t*>(from + (kd * 64 + lane) * 8);
+        qs[cb] = qsl[16 * cb + c16];
+    }
+    barrier_keep_vmem();   // every wave has its rows: the stage may be filled
+
+    f32x4_t acc[CB][DB];
+    float m_run[CB], l_run[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        m_run[cb] = kNegBig;
+        l_run[cb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[cb][db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // per-lane element offsets within a tile: K operand rows and V^T operand rows
+    int k_off[KD], v_off[DB];
+#pragma unroll
+    for (int kd = 0; kd < KD; ++kd) k_off[kd] = c16 * D + ((model_chunk(a.chunk_map, kd * 4 + q4) ^ dswz<D>(c16)) << 3);
+    {
+        const int key = 4 * q4 + (c16 >> 2);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            const int d = db * 16 + 4 * (lane & 3);
+            v_off[db] = key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7);
+        }
+    }
+
+    int st = 0;
+    typename Keys::Blocks blk{};
+    if (NST - 1 < nt) blk = keys.blocks_of(NST - 1);
+    for (int t = 0; t < nt; ++t) {
+        keys.template wait_step<NST - 2>(t);
+        if (t + NST - 1 < nt) {
+            keys.issue(t + NST - 1, keys.prev(st), blk);
+            if (t + NST < nt) blk = keys.blocks_of(t + NST);
+        }
+        const uint16_t* kt = lds.stages + st * Keys::SE + wave * TK * D;
+        const int k0 = t * Keys::STEP + wave * TK;
+        keys.clean(t, st);
+        u32x4_t kf[KD];
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) kf[kd] = *reinterpret_cast<const u32x4_t*>(kt + k_off[kd]);
+        bool powers = false;
+        if constexpr (ROPE) {
+            uint32_t w[PL];   // runs in pair order, NeoX: all x, then all y
+#pragma unroll
+            for (int i = 0; i < PL; ++i) w[i] = kf[i / 4][i % 4];
+            powers = keys.turn(st, w);
+#pragma unroll
+            for (int i = 0; i < PL; ++i) kf[i / 4][i % 4] = w[i];
+        }
+        f32x4_t sc[CB];
 #pragma unroll
         for (int kd = 0; kd < KD; ++kd)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-                    const f32x4_t from = kd == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[n][cb];
-                    if (ROPE)
-                        sc[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kf[n][kd]), __builtin_bit_cast(f16x8_t, qb[cb][kd]), from, 0, 0, 0);
-                    else
-                        sc[n][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[n][kd]), qb[cb][kd], from, 0, 0, 0);
-                }
+            for (int cb = 0; cb < CB; ++cb) {
+                const f32x4_t from = kd == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[cb];
+                if (ROPE)
+                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kf[kd]), __builtin_bit_cast(f16x8_t, qb[cb][kd]), from, 0, 0, 0);
+                else
+                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[kd]), qb[cb][kd], from, 0, 0, 0);
+            }
         if (ROPE && powers) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[n][cb][r] *= ksc[st][tile0 + n * TK + 4 * q4 + r];
+                for (int r = 0; r < 4; ++r) sc[cb][r] *= lds.ksc[st][wave * TK + 4 * q4 + r];
         }
-        const bool masked = k0 < k_lo || k_hi - k0 < NT * TK || k_tok - k0 < NT * TK;
-        uint32_t seen[CB];   // masked tiles: the row's bits of the tiles' keys
-        if (masked) {
-            // keys [k_lo, k_hi) of the tiles (k0 < k_hi)
-            const int lo = max(k_lo - k0, 0), hi = min(k_hi - k0, NT * TK);
-            const uint32_t inside = (hi < 32 ? (1u << hi) - 1u : ~0u) & ~((1u << lo) - 1u);
+        if (keys.masked(k0, TK)) {
+            const uint32_t inside = keys.inside(k0, TK);
+            uint32_t seen[CB];   // the row's bits of the tile's keys
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                seen[cb] = inside & tree_bits(a.mask + (size_t)(g.q_row0 + toff[cb]) * a.words, a.words, k0 - k_tok);
+                seen[cb] = inside & tree_bits(a.mask + (size_t)(g.q_row0 + toff[cb]) * a.words, a.words, k0 - keys.k_tok);
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (!((seen[cb] >> (16 * n + 4 * q4 + r)) & 1)) sc[n][cb][r] = -INFINITY;
+                for (int r = 0; r < 4; ++r)
+                    if (!((seen[cb] >> (4 * q4 + r)) & 1)) sc[cb][r] = -INFINITY;
             }
-            if (__builtin_amdgcn_ballot_w64(vbad[st][lane % NW] != 0) != 0) {
+            if (__builtin_amdgcn_readfirstlane(lds.vbad[st][wave]) != 0) {
                 // which of this lane's outputs the seen infinities reach
 #pragma unroll 1
-                for (int k = 0; k < NT * TK; ++k)
+                for (int k = 0; k < TK; ++k)
 #pragma unroll
                     for (int cb = 0; cb < CB; ++cb)
                         if ((seen[cb] >> k) & 1)
 #pragma unroll 1
-                            for (int db = 0; db < DB; ++db) {
-                                const uint32_t both = vinf[st][tile0 + k][2 * db + (q4 >> 1)] >> (4 * (q4 & 1));
-                                infs[wave][cb][db][lane] |= (uint8_t)((both & 15u) | ((both >> 4) & 0xf0u));
-                            }
+                            for (int db = 0; db < DB; ++db)
+                                infs[wave][cb][db][lane] |= (uint8_t)keys.infs_of(st, wave * TK + k, 2 * db + (q4 >> 1), q4 & 1);
             }
         }
         float mx[CB];
         bool moves = false;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
-            mx[cb] = fmaxf(fmaxf(sc[0][cb][0], sc[0][cb][1]), fmaxf(sc[0][cb][2], sc[0][cb][3]));
-#pragma unroll
-            for (int n = 1; n < NT; ++n) mx[cb] = fmaxf(fmaxf(fmaxf(mx[cb], sc[n][cb][0]), sc[n][cb][1]), fmaxf(sc[n][cb][2], sc[n][cb][3]));
+            mx[cb] = fmaxf(fmaxf(sc[cb][0], sc[cb][1]), fmaxf(sc[cb][2], sc[cb][3]));
             mx[cb] = max_xor32(max_xor16(mx[cb])) * qs[cb];
             moves |= mx[cb] > m_run[cb] + 8.f;
         }
@@ -676,204 +749,363 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_bf16(const Plan plan,
                 m_run[cb] = m_new;
             }
         }
+        u32x4_t pw[CB];   // upper and lower parts of the probabilities
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            u32x2_t af[DB];
+        for (int cb = 0; cb < CB; ++cb) {
+            float p[4];
 #pragma unroll
-            for (int db = 0; db < DB; ++db) af[db] = __builtin_bit_cast(u32x2_t, lds_read_tr(as_lds(vt + n * TK * D) + v_off[db]));
-            u32x4_t pw[CB];   // upper and lower parts of the probabilities
+            for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[cb][r], qs[cb], -m_run[cb]));
+            l_run[cb] += (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-                float p[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][cb][r], qs[cb], -m_run[cb]));
-                l_run[cb] += (p[0] + p[1]) + (p[2] + p[3]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    pw[cb][h] = pack_bf16(p[2 * h], p[2 * h + 1]);
-                    pw[cb][2 + h] = pack_bf16(p[2 * h] - bf_lo(pw[cb][h]), p[2 * h + 1] - bf_hi(pw[cb][h]));
-                }
+            for (int h = 0; h < 2; ++h) {
+                pw[cb][h] = pack_bf16(p[2 * h], p[2 * h + 1]);
+                pw[cb][2 + h] = pack_bf16(p[2 * h] - bf_lo(pw[cb][h]), p[2 * h + 1] - bf_hi(pw[cb][h]));
             }
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const u32x4_t twice = {af[db][0], af[db][1], af[db][0], af[db][1]};
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb)
-                    acc[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, twice), __builtin_bit_cast(bf16x8_t, pw[cb]), acc[cb][db], 0, 0, 0);
-            }
-        }
-    };
-    // a step's copies have landed once no more than those of the `later` next ones are outstanding
-    auto wait_step = [&](int u, auto later) {
-        constexpr int L = decltype(later)::value;
-        if (L > 0 && u + L < nt) wait_vmem_n<L * LPS>();
-        else wait_vmem();
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    };
-    auto load_k = [&](u32x4_t (&kf)[KD], const uint16_t* kt) {
-#pragma unroll
-        for (int kd = 0; kd < KD; ++kd) kf[kd] = *reinterpret_cast<const u32x4_t*>(kt + k_off[kd]);
-    };
-
-    int st = 0;
-    auto next = [](int x) { return x + 1 == NST ? 0 : x + 1; };
-    auto prev = [](int x) { return x == 0 ? NST - 1 : x - 1; };
-    Blocks blk{};
-    if constexpr (!SHARED) {
-        if (NST - 1 < nt) blk = blocks_of(NST - 1);
-        for (int t = 0; t < nt; ++t) {
-            wait_step(t, Idx<NST - 2>{});
-            if (t + NST - 1 < nt) {
-                issue(t + NST - 1, prev(st), blk);
-                if (t + NST < nt) blk = blocks_of(t + NST);
-            }
-            const uint16_t* kt = stages + st * SE + wave * TK * D;
-            clean(t, st);
-            u32x4_t kf[1][KD];
-            load_k(kf[0], kt);
-            bool powers = false;
-            if constexpr (ROPE) {
-                uint32_t w[PL];   // runs in pair order, NeoX: all x, then all y
-#pragma unroll
-                for (int i = 0; i < PL; ++i) w[i] = kf[0][i / 4][i % 4];
-                powers = turn(st, w);
-#pragma unroll
-                for (int i = 0; i < PL; ++i) kf[0][i / 4][i % 4] = w[i];
-            }
-            tiles(Idx<1>{}, kf, kt + KV, t * STEP + wave * TK, st, wave * TK, powers);
-            st = next(st);
-        }
-    } else {
-        typedef uint32_t run_t __attribute__((ext_vector_type(PL / 2)));
-        // step u has landed; its keys are turned in place
-        auto prepare = [&](int u, int sl) {
-            if (u >= nt) return;
-            wait_step(u, Idx<NST - 2>{});
-            clean(u, sl);
-            if constexpr (ROPE) {
-                uint16_t* kt = stages + sl * SE;
-                uint32_t w[PL];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const run_t x = *reinterpret_cast<const run_t*>(kt + s_off[h]);
-#pragma unroll
-                    for (int i = 0; i < PL / 2; ++i) w[h * PL / 2 + i] = x[i];
-                }
-                turn(sl, w);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    run_t x;
-#pragma unroll
-                    for (int i = 0; i < PL / 2; ++i) x[i] = w[h * PL / 2 + i];
-                    *reinterpret_cast<run_t*>(kt + s_off[h]) = x;
-                }
-            }
-        };
-#pragma unroll
-        for (int u = NST - SPARE; u < NST - 1; ++u)
-            if (u < nt) issue(u, u, blocks_of(u));
-        if (NST - 1 < nt) blk = blocks_of(NST - 1);
-        prepare(0, 0);
-        barrier_keep_vmem();
-        constexpr int NT = KG == 4 ? 1 : 2;    // tiles at a time
-        const bool live = row_lo < rows_total;
-        for (int s = 0; s < nt; ++s) {
-            // step s + NST - 1 goes where step s - 1 was
-            if (s + NST - 1 < nt) {
-                issue(s + NST - 1, prev(st), blk);
-                if (s + NST < nt) blk = blocks_of(s + NST);
-            }
-            prepare(s + 1, next(st));
-            if (live) {
-                uint32_t flags = 0;
-                if (ROPE) flags = (uint32_t)kbig[st][lane % NW];
-                const bool powers = ROPE && __builtin_amdgcn_ballot_w64(flags != 0) != 0;
-#pragma unroll 1
-                for (int n = 0; n < 4 / KG; n += NT) {
-                    const int k0 = s * STEP + (kg * (4 / KG) + n) * TK;
-                    if (k0 >= k_hi) break;
-                    const uint16_t* kt = stages + st * SE + (kg * (4 / KG) + n) * TK * D;
-                    u32x4_t kf[NT][KD];
-#pragma unroll
-                    for (int m = 0; m < NT; ++m) load_k(kf[m], kt + m * TK * D);
-                    tiles(Idx<NT>{}, kf, kt + KV, k0, st, (kg * (4 / KG) + n) * TK, powers);
-                }
-            }
-            barrier_keep_vmem();
-            st = next(st);
-        }
-    }
-
-    // ---- the results of a row group's waves meet: rows by their common maximum, outputs through
-    // the stages
-    float M[CB], den[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        den[cb] = sum_xor32(sum_xor16(l_run[cb]));
-        M[cb] = m_run[cb];
-        if (KG > 1 && q4 == 0) mls[wave][16 * cb + c16] = make_float2(m_run[cb], den[cb]);
-    }
-    if (KG > 1) __syncthreads();   // (every wave's copies have landed and been read)
-    f32x4_t* meet = reinterpret_cast<f32x4_t*>(stages);
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        float mine = 1.f;
-        if (KG > 1) {
-            float2 w[KG];
-#pragma unroll
-            for (int i = 0; i < KG; ++i) {
-                w[i] = mls[rg * KG + i][16 * cb + c16];
-                M[cb] = fmaxf(M[cb], w[i].x);
-            }
-            den[cb] = 0.f;
-#pragma unroll
-            for (int i = 0; i < KG; ++i) den[cb] += w[i].y * __builtin_amdgcn_exp2f(w[i].x - M[cb]);
-            mine = __builtin_amdgcn_exp2f(m_run[cb] - M[cb]);
         }
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-            f32x4_t x = acc[cb][db] * mine;
-            const uint32_t f = infs[wave][cb][db][lane];
-            if (f != 0)
+            const u32x2_t af = __builtin_bit_cast(u32x2_t, lds_read_tr(as_lds(kt + Keys::KV) + v_off[db]));
+            const u32x4_t twice = {af[0], af[1], af[0], af[1]};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] += ((f >> i) & 1 ? INFINITY : 0.f) - ((f >> (4 + i)) & 1 ? INFINITY : 0.f);
-            if (KG > 1) meet[((wave * CB + cb) * DB + db) * 64 + lane] = x;
-            else acc[cb][db] = x;
+            for (int cb = 0; cb < CB; ++cb)
+                acc[cb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, twice), __builtin_bit_cast(bf16x8_t, pw[cb]), acc[cb][db], 0, 0, 0);
         }
+        st = keys.next(st);
     }
-    if (KG > 1) __syncthreads();
-    const size_t prow0 = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (16 * CB * WR) + rg * 16 * CB;
+
+    // ---- the waves' results meet: rows by their common maximum, outputs through the stages
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-        const int row = row_lo + 16 * cb + c16;
-        if (row >= rows_total) continue;
-        const float inv = den[cb] == 0.f ? 0.f : 1.f / den[cb];   // (a drafted token may see nothing: its output is 0)
+        const float l = sum_xor32(sum_xor16(l_run[cb]));
+        if (q4 == 0) mls[wave][16 * cb + c16] = make_float2(m_run[cb], l);
+    }
+    __syncthreads();   // (every wave's copies have landed and been read)
+    float M[CB], den[CB];
+    f32x4_t* meet = reinterpret_cast<f32x4_t*>(lds.stages);
 #pragma unroll
-        for (int i = 0; i < (DB + KG - 1) / KG; ++i) {
-            const int db = i * KG + kg;
-            if (db >= DB) break;
-            f32x4_t x;
-            if (KG > 1) {
-                x = meet[((rg * KG * CB + cb) * DB + db) * 64 + lane];
+    for (int cb = 0; cb < CB; ++cb) {
+        float2 w[NW];
+        M[cb] = kNegBig;
 #pragma unroll
-                for (int w = 1; w < KG; ++w) x += meet[(((rg * KG + w) * CB + cb) * DB + db) * 64 + lane];
-            } else {
-                x = acc[cb][i];
-            }
-            if (g.n_split > 1) {
-                *reinterpret_cast<f32x4_t*>(a.part_o + (prow0 + 16 * cb + c16) * D + db * 16 + 4 * q4) = x;
-            } else {
-                const int hl = row - toff[cb] * G;
-                uint16_t* op = static_cast<uint16_t*>(a.o) + ((size_t)(g.q_row0 + toff[cb]) * a.hq + (size_t)ic.kvh * G + hl) * D;
-                *reinterpret_cast<u32x2_t*>(op + db * 16 + 4 * q4) = u32x2_t{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
-            }
+        for (int i = 0; i < NW; ++i) {
+            w[i] = mls[i][16 * cb + c16];
+            M[cb] = fmaxf(M[cb], w[i].x);
         }
-        if (g.n_split > 1 && kg == 0 && q4 == 0)
-            *reinterpret_cast<float2*>(a.part_ml + (prow0 + 16 * cb + c16) * 2) = make_float2(M[cb], den[cb]);
+        den[cb] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) den[cb] += w[i].y * __builtin_amdgcn_exp2f(w[i].x - M[cb]);
+        const float mine = __builtin_amdgcn_exp2f(m_run[cb] - M[cb]);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) meet[((wave * CB + cb) * DB + db) * 64 + lane] = with_infs(acc[cb][db] * mine, infs[wave][cb][db][lane]);
+    }
+    __syncthreads();
+    const size_t prow0 = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (16 * CB);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        const int row = row_lo + 16 * cb + c16, db = wave;
+        if (row >= rows_total || db >= DB) continue;
+        f32x4_t x = meet[(cb * DB + db) * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) x += meet[((w * CB + cb) * DB + db) * 64 + lane];
+        if (g.n_split > 1) {
+            *reinterpret_cast<f32x4_t*>(a.part_o + (prow0 + 16 * cb + c16) * D + db * 16 + 4 * q4) = x;
+            if (wave == 0 && q4 == 0) *reinterpret_cast<float2*>(a.part_ml + (prow0 + 16 * cb + c16) * 2) = make_float2(M[cb], den[cb]);
+        } else {
+            const float inv = den[cb] == 0.f ? 0.f : 1.f / den[cb];   // (a drafted token may see nothing: its output is 0)
+            const int hl = row - toff[cb] * G;
+            uint16_t* op = static_cast<uint16_t*>(a.o) + ((size_t)(g.q_row0 + toff[cb]) * a.hq + (size_t)ic.kvh * G + hl) * D;
+            *reinterpret_cast<u32x2_t*>(op + db * 16 + 4 * q4) = u32x2_t{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
+        }
     }
 }
 
-// Joins the key splits of tree_bf16: one block per kMergeRows rows of a (row tile, KV head),
+// ---------------------------------------------------------------------------------
+// tree_many: 32 WR rows, WR row groups of KG = 8 / WR waves, which take 32 keys of a step at a
+// time (every KG-th).
+//   S^T (32 keys x 32 rows) = K Q^T       v_mfma_f32_32x32x16_f16 (bf16 without rotation)
+//   O^T (32 dims x 32 rows) += V^T P^T    v_mfma_f32_32x32x16_bf16, V^T by
+//                                          ds_read_b64_tr_b16
+// After the scores lane l holds row l%32 and keys 8 (j/4) + 4 (l/32) + j%4, the B operand of
+// the output product, which takes 16 keys' upper parts and then the rest.  The two waves of a SIMD turn their keys of the next step at
+// different ends of a step, so that one's vector work lies beside the other's products.
+// ---------------------------------------------------------------------------------
+template <int D, int STYLE, bool ROPE, int WR>
+__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan, const TreeArgs a) {
+    typedef TreeKeys<D, STYLE, ROPE, true> Keys;
+    constexpr int KD = D / 16;             // 32x32x16 contraction steps of QK^T
+    constexpr int DB = D / 32;             // 32-dim blocks of O^T
+    constexpr int NW = kTreeWaves, KG = NW / WR, NST = Keys::NST, PL = Keys::PL, HALF = D / 2, SPARE = 2;
+    constexpr int PER = SPARE * Keys::SE / NW;     // elements of the stages filled last, per wave
+    static_assert(KG == 1 || KG == 2, "a step has two times 32 keys");
+    static_assert(NST * Keys::SE * 2 >= NW * DB * 4 * 64 * 16, "the outputs meet in the stages");
+    static_assert(PER * 2 >= 16 * HALF * 8, "the queries' angles pass through the stages");
+
+    __shared__ TreeLds<D, true> lds;
+    __shared__ float2 mls[NW][32];
+    __shared__ __attribute__((aligned(4))) uint8_t infs[NW][DB * 4][64];   // infinities of V that a lane's row sees (Keys::infs_of)
+
+    const Group g = group_of<false>(plan, blockIdx.x);
+    const int G = a.group, n_rt = g.n_rt;
+    const int li = blockIdx.x - g.item_base;
+    if (li >= a.hkv * g.n_split * n_rt) return;
+    const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
+    Keys keys(lds, a, g, ic);
+    const int lane = keys.lane, wave = keys.wave, nt = keys.nt;
+    const int rg = wave / KG, kg = wave % KG, l32 = lane & 31, hi = lane >> 5;
+    const int rows_total = g.n_tok * G, row_lo = (ic.rt * WR + rg) * 32;
+    keys.fill_steps(a);
+    for (int i = threadIdx.x; i < NW * DB * 4 * 16; i += NW * 64) reinterpret_cast<uint32_t*>(infs)[i] = 0;
+#pragma unroll
+    for (int u = 0; u < NST - SPARE; ++u)
+        if (u < nt) keys.issue(u, u, keys.blocks_of(u));
+
+    // ---- queries, 16 rows after the other, so that the cos/sin of their tokens (a token's heads
+    // share them) fit in the wave's part of the stages filled last
+    const int row = row_lo + l32;
+    const bool valid = row < rows_total;
+    const int toff = valid ? row / G : 0, hl = valid ? row - toff * G : 0;
+    bf16x8_t qb[KD];
+    float qs = a.scale_log2;   // the products times this are scores (log2 units)
+    __syncthreads();  // phase steps staged
+    {
+        const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + toff) * a.hq + (size_t)ic.kvh * G + hl) * D;
+        u32x4_t raw[KD];
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) {
+            raw[kd] = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, 2 * kd + hi) * 8);
+            if (!valid) raw[kd] = u32x4_t{0, 0, 0, 0};
+        }
+        if (ROPE) {
+            float2* cs = reinterpret_cast<float2*>(lds.stages + (NST - SPARE) * Keys::SE + wave * PER);
+            float xf[KD][8], big = 0.f;
+#pragma unroll
+            for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    xf[kd][2 * m] = bf_lo(raw[kd][m]);
+                    xf[kd][2 * m + 1] = bf_hi(raw[kd][m]);
+                }
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const int row0 = row_lo + 16 * h;
+                const int t0 = min(row0, rows_total - 1) / G, t1 = min(row0 + 15, rows_total - 1) / G;
+                token_angles<HALF>(a, g, lds.fstep, lane, t0, t1, cs);
+                if (l32 >> 4 == h) big = turn_row<STYLE, KD>(xf, cs + (valid ? toff - t0 : 0) * HALF, hi, 2);
+                __atomic_signal_fence(__ATOMIC_SEQ_CST);
+            }
+            // the row times 2^-ex lies in [-1, 1]
+            big = max_xor32(big);
+            const int ex = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
+            qs = ldexpf(qs, ex);
+#pragma unroll
+            for (int kd = 0; kd < KD; ++kd)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) raw[kd][m] = pack_f16(ldexpf(xf[kd][2 * m], -ex), ldexpf(xf[kd][2 * m + 1], -ex));
+        }
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) qb[kd] = __builtin_bit_cast(bf16x8_t, raw[kd]);
+    }
+    barrier_keep_vmem();   // the angles have been read: the stages may be filled
+
+    f32x16_t acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = f32x16_t{};
+    float m_run = kNegBig, l_run = 0.f;
+    // per-lane byte offsets: the K operand's row among 32 keys, the V^T operand's among 8 (chunk c,
+    // and the row 8 keys on, by xor)
+    constexpr int kSw8 = D == 128 ? 1 : 4;
+    uint32_t k_at = (uint32_t)(l32 * D + ((hi ^ dswz<D>(l32 & 15)) << 3)) * 2, v_at;
+    {
+        const int key = 4 * hi + ((lane & 15) >> 2), d = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+        v_at = (uint32_t)(Keys::KV + key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7)) * 2;
+    }
+
+    // ---- 32 keys from place p0 of the step in stage st on, the range's keys k0 ..
+    auto tile = [&](int st, int p0, int k0, bool powers) {
+        // (not kept apart for every chunk: registers are short)
+        asm volatile("" : "+v"(k_at), "+v"(v_at));
+        const uint32_t at = keys.stages_at + (uint32_t)(st * Keys::SE + p0 * D) * 2, kt = at + k_at, vt = at + v_at;
+        f32x16_t sc;
+#pragma unroll
+        for (int kd = 0; kd < KD; ++kd) {
+            const u32x4_t kf = *(lds_u32x4_t*)(uintptr_t)(kt ^ (32 * kd));
+            if (ROPE)
+                sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, kf), __builtin_bit_cast(f16x8_t, qb[kd]), kd == 0 ? f32x16_t{} : sc, 0, 0, 0);
+            else
+                sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), qb[kd], kd == 0 ? f32x16_t{} : sc, 0, 0, 0);
+        }
+        // keep the K reads kAhead ahead of their products (left alone, the compiler waits on each
+        // read right after issuing it)
+        constexpr int kAhead = KD < 6 ? KD : 6;
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);   // LDS reads
+#pragma unroll
+        for (int i = kAhead; i < KD; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);    // MFMA
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+        if (ROPE && powers) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sc[j] *= lds.ksc[st][p0 + 8 * (j >> 2) + 4 * hi + (j & 3)];
+        }
+        if (keys.masked(k0, 32)) {
+            // the row's bits of the keys
+            const uint32_t seen = keys.inside(k0, 32) & tree_bits(a.mask + (size_t)(g.q_row0 + toff) * a.words, a.words, k0 - keys.k_tok);
+            const uint32_t mine = seen >> (4 * hi);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) sc[j] = -INFINITY;
+            if (keys.wave_flag(lds.vbad[st])) {
+                // which of this lane's outputs the seen infinities reach
+#pragma unroll 1
+                for (int k = 0; k < 32; ++k)
+                    if ((seen >> k) & 1)
+#pragma unroll 1
+                        for (int c = 0; c < DB * 4; ++c) infs[wave][c][lane] |= (uint8_t)keys.infs_of(st, p0 + k, c, hi);
+            }
+        }
+        float mx = kNegBig;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[j]);
+        mx = max_xor32(mx) * qs;
+        // the reference maximum only moves when some row's maximum grows by more than 8
+        // (probabilities stay below 2^8), so most tiles skip rescaling
+        if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f) != 0) {
+            const float m_new = fmaxf(m_run, mx);
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+            m_run = m_new;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {   // keys 16 h .. 16 h + 15
+            float p[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * h + r], qs, -m_run));
+            l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+            u32x4_t up, down;   // upper parts (cut, not rounded) and the rest
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = __float_as_uint(p[2 * i]), y = __float_as_uint(p[2 * i + 1]);
+                up[i] = pair_hi(x, y);
+                down[i] = pack_bf16(p[2 * i] - __uint_as_float(x & 0xffff0000u), p[2 * i + 1] - __uint_as_float(y & 0xffff0000u));
+            }
+            u32x4_t af[DB];
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                const uint32_t off = (vt ^ (uint32_t)(64 * db)) + 32 * h * D, off8 = (vt ^ (uint32_t)(64 * db) ^ 16u * kSw8) + 32 * h * D + 16 * D;
+                const u32x2_t both[2] = {__builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off)),
+                                         __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off8))};
+                af[db] = __builtin_bit_cast(u32x4_t, both);
+            }
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, af[db]), __builtin_bit_cast(bf16x8_t, up), acc[db], 0, 0, 0);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, af[db]), __builtin_bit_cast(bf16x8_t, down), acc[db], 0, 0, 0);
+        }
+        // likewise the V reads of the second 16 keys
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, DB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 3 * DB, 0);
+    };
+    // step u has landed; this wave's keys of it are turned in place
+    typedef uint32_t run_t __attribute__((ext_vector_type(PL / 2)));
+    auto prepare = [&](int u, int sl) {
+        if (u >= nt) return;
+        keys.template wait_step<NST - 2>(u);
+        keys.clean(u, sl);
+        if constexpr (ROPE) {
+            uint16_t* kt = lds.stages + sl * Keys::SE;
+            uint32_t w[PL];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const run_t x = *reinterpret_cast<const run_t*>(kt + keys.s_off[h]);
+#pragma unroll
+                for (int i = 0; i < PL / 2; ++i) w[h * PL / 2 + i] = x[i];
+            }
+            keys.turn(sl, w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                run_t x;
+#pragma unroll
+                for (int i = 0; i < PL / 2; ++i) x[i] = w[h * PL / 2 + i];
+                *reinterpret_cast<run_t*>(kt + keys.t_off[h]) = x;
+            }
+        }
+    };
+#pragma unroll
+    for (int u = NST - SPARE; u < NST - 1; ++u)
+        if (u < nt) keys.issue(u, u, keys.blocks_of(u));
+    typename Keys::Blocks blk{};
+    if (NST - 1 < nt) blk = keys.blocks_of(NST - 1);
+    prepare(0, 0);
+    barrier_keep_vmem();
+    // (a loop for each role, so that no accumulator passes a branch.  A step's second 32 keys may
+    // lie past the range: they are masked.)
+    auto steps = [&](auto rows, auto turn_first) {
+        int st = 0;
+        for (int s = 0; s < nt; ++s) {
+            // step s + NST - 1 goes where step s - 1 was
+            if (s + NST - 1 < nt) {
+                keys.issue(s + NST - 1, keys.prev(st), blk);
+                if (s + NST < nt) blk = keys.blocks_of(s + NST);
+            }
+            if (decltype(turn_first)::value) prepare(s + 1, keys.next(st));
+            if (decltype(rows)::value) {
+                const bool powers = ROPE && keys.wave_flag(lds.kbig[st]);
+#pragma unroll 1
+                for (int p0 = 32 * kg; p0 < 64; p0 += 32 * KG) tile(st, p0, s * Keys::STEP + p0, powers);
+            }
+            if (!decltype(turn_first)::value) prepare(s + 1, keys.next(st));
+            barrier_keep_vmem();
+            st = keys.next(st);
+        }
+    };
+    if (row_lo >= rows_total) steps(std::false_type{}, std::true_type{});
+    else if (wave < NW / 2) steps(std::true_type{}, std::true_type{});
+    else steps(std::true_type{}, std::false_type{});
+
+    // ---- the results of a row group's waves meet: rows by their common maximum, outputs through
+    // the stages
+    float den = sum_xor32(l_run), M = m_run, mine = 1.f;
+    if constexpr (KG > 1) {
+        if (hi == 0) mls[wave][l32] = make_float2(m_run, den);
+        __syncthreads();   // (every wave's copies have landed and been read)
+        const float2 other = mls[wave ^ 1][l32];
+        M = fmaxf(m_run, other.x);
+        mine = __builtin_amdgcn_exp2f(m_run - M);
+        den = den * mine + other.y * __builtin_amdgcn_exp2f(other.x - M);
+    }
+    f32x4_t* meet = reinterpret_cast<f32x4_t*>(lds.stages);
+    f32x4_t out[DB * 4];   // dims 8 c + 4 (l/32) + {0..3}
+#pragma unroll
+    for (int c = 0; c < DB * 4; ++c) {
+        const f32x4_t x = {acc[c / 4][4 * (c % 4)], acc[c / 4][4 * (c % 4) + 1], acc[c / 4][4 * (c % 4) + 2], acc[c / 4][4 * (c % 4) + 3]};
+        out[c] = with_infs(x * mine, infs[wave][c][lane]);
+        if (KG > 1) meet[(wave * DB * 4 + c) * 64 + lane] = out[c];
+    }
+    if (KG > 1) __syncthreads();
+    if (row >= rows_total) return;
+    const size_t prow = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (32 * WR) + rg * 32 + l32;
+    const float inv = den == 0.f ? 0.f : 1.f / den;   // (a drafted token may see nothing: its output is 0)
+    uint16_t* op = static_cast<uint16_t*>(a.o) + ((size_t)(g.q_row0 + toff) * a.hq + (size_t)ic.kvh * G + hl) * D;
+#pragma unroll
+    for (int c = 0; c < DB * 4; ++c) {
+        if (KG > 1 && c % 2 != kg) continue;
+        f32x4_t x = out[c];
+        if (KG > 1) x += meet[((wave ^ 1) * DB * 4 + c) * 64 + lane];
+        const int d = 8 * c + 4 * hi;
+        if (g.n_split > 1) *reinterpret_cast<f32x4_t*>(a.part_o + prow * D + d) = x;
+        else *reinterpret_cast<u32x2_t*>(op + d) = u32x2_t{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
+    }
+    if (g.n_split > 1 && kg == 0 && hi == 0) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(M, den);
+}
+
+// Joins key splits: one block per kMergeRows rows of a (row tile, KV head),
 // one float4 of a row per thread, eight splits' loads in flight.
 template <int D>
 __global__ void __launch_bounds__(kMergeRows * D / 4) tree_merge(const Plan plan, const TreeArgs a) {
@@ -920,11 +1152,10 @@ template <int D, int STYLE, bool ROPE>
 hipError_t launch_tree_t(const Plan& plan, const TreeArgs& a, hipStream_t st) {
     const dim3 grid(plan.n_items), block(kTreeWaves * 64);
     switch (a.tile_rows) {
-    case 16: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 1, 1>), grid, block, 0, st, plan, a); break;
-    case 32: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 1>), grid, block, 0, st, plan, a); break;
-    case 64: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 2>), grid, block, 0, st, plan, a); break;
-    case 128: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 4>), grid, block, 0, st, plan, a); break;
-    default: hipLaunchKernelGGL((tree_bf16<D, STYLE, ROPE, 2, 8>), grid, block, 0, st, plan, a); break;
+    case 16: hipLaunchKernelGGL((tree_few<D, STYLE, ROPE, 1>), grid, block, 0, st, plan, a); break;
+    case 32: hipLaunchKernelGGL((tree_few<D, STYLE, ROPE, 2>), grid, block, 0, st, plan, a); break;
+    case 128: hipLaunchKernelGGL((tree_many<D, STYLE, ROPE, 4>), grid, block, 0, st, plan, a); break;
+    default: hipLaunchKernelGGL((tree_many<D, STYLE, ROPE, 8>), grid, block, 0, st, plan, a); break;
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.n_merge == 0) return e;
