@@ -404,53 +404,67 @@ struct TreeKeys : TreeShape<D, SHARED> {
         else wait_vmem();
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
     }
-    // Turns 2 PL elements, words w[0 .. PL): NeoX x in the first half and y in the second; returns
-    // whether some key of the wave got a power of two.
-    __device__ __forceinline__ bool turn(int st, uint32_t (&w)[PL]) {
+    // the angles of the lane's key of the step in stage st, computed where they cannot be advanced
+    __device__ __forceinline__ void find_angles(int st) {
         const uint32_t pos = (uint32_t)s.ps[wave][st][own_j];
         if (fresh == 0 || __builtin_amdgcn_ballot_w64(pos != cs_pos + STEP) != 0) {
 #pragma unroll
             for (int i = 0; i < PL; ++i) rope_cs_fast((int32_t)(pos - STEP), s.fstep[pair_of(i)], rc[i], rs[i]);
             fresh = kRenew;
         }
+        --fresh;
+        cs_pos = pos;
+    }
+    // pairs i and i + 1: their angles a step on, and 4 elements turned (times 2^-ex if SCALED; big
+    // takes in their sizes)
+    __device__ __forceinline__ void advance_pairs(int i0) {
 #pragma unroll
-        for (int i = 0; i < PL; ++i) {
+        for (int i = i0; i < i0 + 2; ++i) {
             const float2 d = s.stride_cs[pair_of(i)];
             const float c = rc[i], sn = rs[i];
             rc[i] = c * d.x - sn * d.y;
             rs[i] = sn * d.x + c * d.y;
         }
-        --fresh;
-        cs_pos = pos;
+    }
+    template <bool SCALED>
+    __device__ __forceinline__ void rotate_pairs(int i, const uint32_t (&w)[PL], uint32_t (&out)[PL], int ex, float& big) const {
+        const uint32_t A = STYLE == kNeox ? w[i / 2] : w[i], B = STYLE == kNeox ? w[PL / 2 + i / 2] : w[i + 1];
+        const float x0 = bf_lo(A), y0 = STYLE == kNeox ? bf_lo(B) : bf_hi(A);
+        const float x1 = STYLE == kNeox ? bf_hi(A) : bf_lo(B), y1 = bf_hi(B);
+        float p0 = x0 * rc[i] - y0 * rs[i], r0 = y0 * rc[i] + x0 * rs[i];
+        float p1 = x1 * rc[i + 1] - y1 * rs[i + 1], r1 = y1 * rc[i + 1] + x1 * rs[i + 1];
+        if (SCALED) {
+            p0 = ldexpf(p0, -ex); r0 = ldexpf(r0, -ex); p1 = ldexpf(p1, -ex); r1 = ldexpf(r1, -ex);
+        } else {
+            big = fmaxf(fmaxf(big, fabsf(p0)), fabsf(r0));
+            big = fmaxf(fmaxf(big, fabsf(p1)), fabsf(r1));
+        }
+        out[STYLE == kNeox ? i / 2 : i] = STYLE == kNeox ? pack_f16(p0, p1) : pack_f16(p0, r0);
+        out[STYLE == kNeox ? PL / 2 + i / 2 : i + 1] = STYLE == kNeox ? pack_f16(r0, r1) : pack_f16(p1, r1);
+    }
+    // Turns 2 PL elements, words w[0 .. PL): NeoX x in the first half and y in the second.  Returns
+    // the largest one's size (of the lane).
+    __device__ __forceinline__ float turn(const uint32_t (&w)[PL], uint32_t (&out)[PL]) {
         float big = 0.f;
-        uint32_t out[PL];
-        auto rotate = [&](auto scaled, int ex) {
 #pragma unroll
-            for (int i = 0; i < PL; i += 2) {
-                const uint32_t A = STYLE == kNeox ? w[i / 2] : w[i], B = STYLE == kNeox ? w[PL / 2 + i / 2] : w[i + 1];
-                const float x0 = bf_lo(A), y0 = STYLE == kNeox ? bf_lo(B) : bf_hi(A);
-                const float x1 = STYLE == kNeox ? bf_hi(A) : bf_lo(B), y1 = bf_hi(B);
-                float p0 = x0 * rc[i] - y0 * rs[i], r0 = y0 * rc[i] + x0 * rs[i];
-                float p1 = x1 * rc[i + 1] - y1 * rs[i + 1], r1 = y1 * rc[i + 1] + x1 * rs[i + 1];
-                if (decltype(scaled)::value) {
-                    p0 = ldexpf(p0, -ex); r0 = ldexpf(r0, -ex); p1 = ldexpf(p1, -ex); r1 = ldexpf(r1, -ex);
-                } else {
-                    big = fmaxf(fmaxf(big, fabsf(p0)), fabsf(r0));
-                    big = fmaxf(fmaxf(big, fabsf(p1)), fabsf(r1));
-                }
-                out[STYLE == kNeox ? i / 2 : i] = STYLE == kNeox ? pack_f16(p0, p1) : pack_f16(p0, r0);
-                out[STYLE == kNeox ? PL / 2 + i / 2 : i + 1] = STYLE == kNeox ? pack_f16(r0, r1) : pack_f16(p1, r1);
-            }
-        };
-        rotate(std::false_type{}, 0);
-        // a key whose largest element lies outside 2^-8 .. 2^15 goes in times a power of two
+        for (int i = 0; i < PL; i += 2) {
+            advance_pairs(i);
+            rotate_pairs<false>(i, w, out, 0, big);
+        }
+        return big;
+    }
+    // A key whose largest element lies outside 2^-8 .. 2^15 goes in times a power of two; returns
+    // whether some key of the wave does.
+    __device__ __forceinline__ bool fit(int st, const uint32_t (&w)[PL], uint32_t (&out)[PL], float big) {
         big = SHARED ? max_of8(big) : max_xor32(max_xor16(big));
         const bool odd = big >= 0x1p15f || (big < 0x1p-8f && big > 0.f);
         const bool any = __builtin_amdgcn_ballot_w64(odd) != 0;
         int ex = 0;
         if (any) {
             ex = odd && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
-            rotate(std::true_type{}, ex);
+            float none = 0.f;
+#pragma unroll
+            for (int i = 0; i < PL; i += 2) rotate_pairs<true>(i, w, out, ex, none);
         }
         if (SHARED) {
             if ((lane & 7) == 0) s.ksc[st][sh_row] = ldexpf(1.f, ex);
@@ -458,9 +472,26 @@ struct TreeKeys : TreeShape<D, SHARED> {
         } else if (any && lane < 16) {
             s.ksc[st][sh_row] = ldexpf(1.f, ex);
         }
-#pragma unroll
-        for (int i = 0; i < PL; ++i) w[i] = out[i];
         return any;
+    }
+    // SHARED: the lane's two runs of the step in stage st as copied, and as turned
+    typedef uint32_t run_t __attribute__((ext_vector_type(PL / 2)));
+    __device__ __forceinline__ void load_runs(int st, uint32_t (&w)[PL]) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const run_t x = *reinterpret_cast<const run_t*>(s.stages + st * SE + s_off[h]);
+#pragma unroll
+            for (int i = 0; i < PL / 2; ++i) w[h * PL / 2 + i] = x[i];
+        }
+    }
+    __device__ __forceinline__ void store_runs(int st, const uint32_t (&w)[PL]) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            run_t x;
+#pragma unroll
+            for (int i = 0; i < PL / 2; ++i) x[i] = w[h * PL / 2 + i];
+            *reinterpret_cast<run_t*>(s.stages + st * SE + t_off[h]) = x;
+        }
     }
     // An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in the
     // product): where a step has keys that not every row sees, the wave that copied them puts
@@ -685,9 +716,12 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const Plan plan, 
             uint32_t w[PL];   // runs in pair order, NeoX: all x, then all y
 #pragma unroll
             for (int i = 0; i < PL; ++i) w[i] = kf[i / 4][i % 4];
-            powers = keys.turn(st, w);
+            uint32_t out[PL];
+            keys.find_angles(st);
+            const float big = keys.turn(w, out);
+            powers = keys.fit(st, w, out, big);
 #pragma unroll
-            for (int i = 0; i < PL; ++i) kf[i / 4][i % 4] = w[i];
+            for (int i = 0; i < PL; ++i) kf[i / 4][i % 4] = out[i];
         }
         f32x4_t sc[CB];
 #pragma unroll
@@ -826,8 +860,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const Plan plan, 
 //   O^T (32 dims x 32 rows) += V^T P^T    v_mfma_f32_32x32x16_bf16, V^T by
 //                                          ds_read_b64_tr_b16
 // After the scores lane l holds row l%32 and keys 8 (j/4) + 4 (l/32) + j%4, the B operand of
-// the output product, which takes 16 keys' upper parts and then the rest.  The two waves of a SIMD turn their keys of the next step at
-// different ends of a step, so that one's vector work lies beside the other's products.
+// the output product, which takes 16 keys' upper parts and then the rest.  A wave turns its
+// keys of the next step beside the products of the scores.
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, bool ROPE, int WR>
 __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan, const TreeArgs a) {
@@ -920,56 +954,94 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
         v_at = (uint32_t)(Keys::KV + key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7)) * 2;
     }
 
-    // ---- 32 keys from place p0 of the step in stage st on, the range's keys k0 ..
-    auto tile = [&](int st, int p0, int k0, bool powers) {
-        // (not kept apart for every chunk: registers are short)
+    // step u has landed; this wave's keys of it are turned, but for the turning itself
+    auto landed = [&](int u, int sl) {
+        if (u >= nt) return;
+        keys.template wait_step<NST - 2>(u);
+        keys.clean(u, sl);
+        if (ROPE) keys.find_angles(sl);
+    };
+    constexpr int NT = 2 / KG;   // times 32 keys of a step
+    constexpr int TAKEN = KD * NT;
+    // ---- step s in stage st, and the turning of the next
+    auto step = [&](int s, int st) {
+        const int sl = keys.next(st);
+        landed(s + 1, sl);
+        const bool powers = ROPE && keys.wave_flag(lds.kbig[st]);
+        // ---- scores, with the next step's keys turned beside (past the last step: of nothing, into a
+        // stage that is not read again)
+        // (the offsets are not kept apart for every chunk: registers are short)
         asm volatile("" : "+v"(k_at), "+v"(v_at));
-        const uint32_t at = keys.stages_at + (uint32_t)(st * Keys::SE + p0 * D) * 2, kt = at + k_at, vt = at + v_at;
-        f32x16_t sc;
+        const uint32_t at = keys.stages_at + (uint32_t)(st * Keys::SE + 32 * kg * D) * 2, kt = at + k_at, vt = at + v_at;
+        // Every few vector instructions follow a product that they do not wait for, in the order written:
+        // left alone, the compiler puts the products side by side, and the vector unit idles.
+        f32x16_t sc[NT];
+        uint32_t w[PL], turned[PL];
+        float big = 0.f;
+        if constexpr (ROPE) keys.load_runs(sl, w);
+        constexpr int kAhead = 4;                 // K reads in flight
+        u32x4_t kf[TAKEN];
+        auto read_k = [&](int i) { kf[i] = *(lds_u32x4_t*)(uintptr_t)((kt ^ (32 * (i / NT))) + 64 * (i % NT) * D); };
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) {
-            const u32x4_t kf = *(lds_u32x4_t*)(uintptr_t)(kt ^ (32 * kd));
+        for (int i = 0; i < kAhead; ++i) read_k(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TAKEN; ++i) {
+            const int kd = i / NT, n = i % NT;
+            const f32x16_t from = kd == 0 ? f32x16_t{} : sc[n];
             if (ROPE)
-                sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, kf), __builtin_bit_cast(f16x8_t, qb[kd]), kd == 0 ? f32x16_t{} : sc, 0, 0, 0);
+                sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, kf[i]), __builtin_bit_cast(f16x8_t, qb[kd]), from, 0, 0, 0);
             else
-                sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), qb[kd], kd == 0 ? f32x16_t{} : sc, 0, 0, 0);
-        }
-        // keep the K reads kAhead ahead of their products (left alone, the compiler waits on each
-        // read right after issuing it)
-        constexpr int kAhead = KD < 6 ? KD : 6;
-        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);   // LDS reads
+                sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), qb[kd], from, 0, 0, 0);
+            if (i + kAhead < TAKEN) read_k(i + kAhead);
+            if constexpr (ROPE) {
+                // PL parts: the angles of two pairs, then their turning
 #pragma unroll
-        for (int i = kAhead; i < KD; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);    // MFMA
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                for (int part = i * PL / TAKEN; part < (i + 1) * PL / TAKEN; ++part) {
+                    if (part % 2 == 0) keys.advance_pairs(part);
+                    else keys.template rotate_pairs<false>(part - 1, w, turned, 0, big);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+        if constexpr (ROPE) {
+            keys.fit(sl, w, turned, big);
+            keys.store_runs(sl, turned);
+        }
         if (ROPE && powers) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) sc[j] *= lds.ksc[st][p0 + 8 * (j >> 2) + 4 * hi + (j & 3)];
-        }
-        if (keys.masked(k0, 32)) {
-            // the row's bits of the keys
-            const uint32_t seen = keys.inside(k0, 32) & tree_bits(a.mask + (size_t)(g.q_row0 + toff) * a.words, a.words, k0 - keys.k_tok);
-            const uint32_t mine = seen >> (4 * hi);
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) sc[j] = -INFINITY;
-            if (keys.wave_flag(lds.vbad[st])) {
-                // which of this lane's outputs the seen infinities reach
+                for (int j = 0; j < 16; ++j) sc[n][j] *= lds.ksc[st][32 * (kg + n) + 8 * (j >> 2) + 4 * hi + (j & 3)];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int p0 = 32 * (kg + n), k0 = s * Keys::STEP + p0;
+            if (keys.masked(k0, 32)) {
+                // the row's bits of the keys (the step's second 32 may all lie past the range)
+                const uint32_t seen = keys.inside(k0, 32) & tree_bits(a.mask + (size_t)(g.q_row0 + toff) * a.words, a.words, k0 - keys.k_tok);
+                const uint32_t mine = seen >> (4 * hi);
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) sc[n][j] = -INFINITY;
+                if (keys.wave_flag(lds.vbad[st])) {
+                    // which of this lane's outputs the seen infinities reach
 #pragma unroll 1
-                for (int k = 0; k < 32; ++k)
-                    if ((seen >> k) & 1)
+                    for (int k = 0; k < 32; ++k)
+                        if ((seen >> k) & 1)
 #pragma unroll 1
-                        for (int c = 0; c < DB * 4; ++c) infs[wave][c][lane] |= (uint8_t)keys.infs_of(st, p0 + k, c, hi);
+                            for (int c = 0; c < DB * 4; ++c) infs[wave][c][lane] |= (uint8_t)keys.infs_of(st, p0 + k, c, hi);
+                }
             }
         }
         float mx = kNegBig;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[j]);
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[n][j]);
         mx = max_xor32(mx) * qs;
         // the reference maximum only moves when some row's maximum grows by more than 8
-        // (probabilities stay below 2^8), so most tiles skip rescaling
+        // (probabilities stay below 2^8), so most steps skip rescaling
         if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f) != 0) {
             const float m_new = fmaxf(m_run, mx);
             const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -978,63 +1050,60 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
             for (int db = 0; db < DB; ++db) acc[db] *= alpha;
             m_run = m_new;
         }
+        // ---- outputs, 16 keys at a time, with the next 16's probabilities and V reads beside
+        constexpr int NH = 2 * NT, NM = 2 * DB;   // groups of keys, products of each
+        float p[2][8];
+        u32x4_t up[2], down[2];   // a probability's upper part (cut, not rounded) and the rest
+        u32x2_t af[2][NM];
+        // part i of NM of the probabilities of keys 16 h .. 16 h + 15
+        auto prob = [&](int h, int i) {
+            constexpr int E = 8 / NM;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {   // keys 16 h .. 16 h + 15
-            float p[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[8 * h + r], qs, -m_run));
-            l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-            u32x4_t up, down;   // upper parts (cut, not rounded) and the rest
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t x = __float_as_uint(p[2 * i]), y = __float_as_uint(p[2 * i + 1]);
-                up[i] = pair_hi(x, y);
-                down[i] = pack_bf16(p[2 * i] - __uint_as_float(x & 0xffff0000u), p[2 * i + 1] - __uint_as_float(y & 0xffff0000u));
+            for (int r = i * E; r < (i + 1) * E; ++r) {
+                p[h % 2][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h / 2][8 * (h % 2) + r], qs, -m_run));
+                l_run += p[h % 2][r];
+                if (r % 2 == 1) {
+                    const uint32_t x = __float_as_uint(p[h % 2][r - 1]), y = __float_as_uint(p[h % 2][r]);
+                    up[h % 2][r / 2] = pair_hi(x, y);
+                    down[h % 2][r / 2] = pack_bf16(p[h % 2][r - 1] - __uint_as_float(x & 0xffff0000u), p[h % 2][r] - __uint_as_float(y & 0xffff0000u));
+                }
             }
-            u32x4_t af[DB];
+        };
+        // V read i of NM: 8 keys of block i / 2
+        auto read_v = [&](int h, int i) {
+            const uint32_t off = (vt ^ (uint32_t)(64 * (i / 2)) ^ (i % 2 ? 16u * kSw8 : 0u)) + 32 * h * D + (i % 2 ? 16 * D : 0);
+            af[h % 2][i] = __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off));
+        };
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                const uint32_t off = (vt ^ (uint32_t)(64 * db)) + 32 * h * D, off8 = (vt ^ (uint32_t)(64 * db) ^ 16u * kSw8) + 32 * h * D + 16 * D;
-                const u32x2_t both[2] = {__builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off)),
-                                         __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off8))};
-                af[db] = __builtin_bit_cast(u32x4_t, both);
-            }
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, af[db]), __builtin_bit_cast(bf16x8_t, up), acc[db], 0, 0, 0);
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, af[db]), __builtin_bit_cast(bf16x8_t, down), acc[db], 0, 0, 0);
+        for (int i = 0; i < NM; ++i) {
+            read_v(0, i);
+            prob(0, i);
         }
-        // likewise the V reads of the second 16 keys
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, DB, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 3 * DB, 0);
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int i = 0; i < NM; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                const int db = i % DB;
+                const u32x4_t v = {af[h % 2][2 * db][0], af[h % 2][2 * db][1], af[h % 2][2 * db + 1][0], af[h % 2][2 * db + 1][1]};
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, i < DB ? up[h % 2] : down[h % 2]),
+                                                                  acc[db], 0, 0, 0);
+                if (h + 1 < NH) {
+                    read_v(h + 1, i);
+                    prob(h + 1, i);
+                }
+            }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    // step u has landed; this wave's keys of it are turned in place
-    typedef uint32_t run_t __attribute__((ext_vector_type(PL / 2)));
-    auto prepare = [&](int u, int sl) {
-        if (u >= nt) return;
-        keys.template wait_step<NST - 2>(u);
-        keys.clean(u, sl);
+    // a wave without rows copies and turns its keys only
+    auto turn_only = [&](int u, int sl) {
+        landed(u, sl);
         if constexpr (ROPE) {
-            uint16_t* kt = lds.stages + sl * Keys::SE;
-            uint32_t w[PL];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const run_t x = *reinterpret_cast<const run_t*>(kt + keys.s_off[h]);
-#pragma unroll
-                for (int i = 0; i < PL / 2; ++i) w[h * PL / 2 + i] = x[i];
-            }
-            keys.turn(sl, w);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                run_t x;
-#pragma unroll
-                for (int i = 0; i < PL / 2; ++i) x[i] = w[h * PL / 2 + i];
-                *reinterpret_cast<run_t*>(kt + keys.t_off[h]) = x;
-            }
+            uint32_t w[PL], turned[PL];
+            keys.load_runs(sl, w);
+            const float big = keys.turn(w, turned);
+            keys.fit(sl, w, turned, big);
+            keys.store_runs(sl, turned);
         }
     };
 #pragma unroll
@@ -1042,11 +1111,9 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
         if (u < nt) keys.issue(u, u, keys.blocks_of(u));
     typename Keys::Blocks blk{};
     if (NST - 1 < nt) blk = keys.blocks_of(NST - 1);
-    prepare(0, 0);
+    turn_only(0, 0);
     barrier_keep_vmem();
-    // (a loop for each role, so that no accumulator passes a branch.  A step's second 32 keys may
-    // lie past the range: they are masked.)
-    auto steps = [&](auto rows, auto turn_first) {
+    auto steps = [&](auto rows) {
         int st = 0;
         for (int s = 0; s < nt; ++s) {
             // step s + NST - 1 goes where step s - 1 was
@@ -1054,20 +1121,14 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
                 keys.issue(s + NST - 1, keys.prev(st), blk);
                 if (s + NST < nt) blk = keys.blocks_of(s + NST);
             }
-            if (decltype(turn_first)::value) prepare(s + 1, keys.next(st));
-            if (decltype(rows)::value) {
-                const bool powers = ROPE && keys.wave_flag(lds.kbig[st]);
-#pragma unroll 1
-                for (int p0 = 32 * kg; p0 < 64; p0 += 32 * KG) tile(st, p0, s * Keys::STEP + p0, powers);
-            }
-            if (!decltype(turn_first)::value) prepare(s + 1, keys.next(st));
+            if (decltype(rows)::value) step(s, st);
+            else turn_only(s + 1, keys.next(st));
             barrier_keep_vmem();
             st = keys.next(st);
         }
     };
-    if (row_lo >= rows_total) steps(std::false_type{}, std::true_type{});
-    else if (wave < NW / 2) steps(std::true_type{}, std::true_type{});
-    else steps(std::true_type{}, std::false_type{});
+    if (row_lo < rows_total) steps(std::true_type{});
+    else steps(std::false_type{});
 
     // ---- the results of a row group's waves meet: rows by their common maximum, outputs through
     // the stages
