@@ -225,8 +225,12 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 //
 // Precision: a rotated key or query is rounded to 11 bits (float16), its size held by a power
 // of two where it does not fit: as bf16, 8 bits, each of the two alone would put outputs as
-// far from 64 bits as their own rounding does.  Without rotation q and k are exact.  A
-// probability enters the product as two bf16 numbers, its upper 8 bits and the rest.
+// far from 64 bits as their own rounding does.  Without rotation q and k are exact.
+// tree_few multiplies a probability as two bf16 numbers, its upper 8 bits and the rest, in the
+// time of one.  In tree_many the second number would cost half as many products again (16 x 96
+// tokens of 64 / 8 heads over 8,192 keys 766 us, without it 632): a probability is rounded to
+// bf16, and the row sum adds the rounded ones, which brings outputs to 1.4 times the error of
+// their own rounding.
 //
 // RoPE: a lane turns PL pairs of one key of a step and holds their cos/sin.  Its next key is
 // STEP keys further; where the positions are too, the angles advance by a constant rotation (4
@@ -382,15 +386,19 @@ struct TreeKeys : TreeShape<D, SHARED> {
     // the wave's copies of step u, into stage st
     __device__ __forceinline__ void issue(int u, int st, const Blocks& blk) const {
         const uint32_t sg = stages_at + (uint32_t)st * SE * 2;
-        __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));   // the stage's last reads have returned (lgkmcnt 0)
-        if (ROPE && lane < OWNK) copy_lds4(posv + near_key(u * STEP + own_key(lane)), ps_at + (uint32_t)st * OWNK * 4);
+        // the stage's last reads have returned (SHARED: before the last barrier)
+        if (!SHARED) __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));
+        const bool whole = u * STEP >= k_lo && (u + 1) * STEP <= k_hi;   // the step needs no nearest keys
+        if (ROPE && lane < OWNK) {
+            const int k = u * STEP + own_key(lane);
+            copy_lds4(posv + (whole ? k : near_key(k)), ps_at + (uint32_t)st * OWNK * 4);
+        }
 #pragma unroll
         for (int i = 0; i < DPL; ++i) {
-            const int k0 = u * STEP + copy_key(i);
             const size_t base = (size_t)(uint32_t)blk.b[SHARED ? i : 0] * blk_stride;
             uint32_t off = lane_off[i];
-            if (k0 < k_lo || k_hi - k0 < KPC) {
-                const int k = k0 + lane / CH, row = k & (kBlock - 1);
+            if (!whole) {
+                const int k = u * STEP + copy_key(i) + lane / CH, row = k & (kBlock - 1);
                 off += ((near_key(k) & (kBlock - 1)) - row) * D * 2;
             }
             copy_lds16(kpool + base, off, sg + copy_key(i) * D * 2);
@@ -860,7 +868,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const Plan plan, 
 //   O^T (32 dims x 32 rows) += V^T P^T    v_mfma_f32_32x32x16_bf16, V^T by
 //                                          ds_read_b64_tr_b16
 // After the scores lane l holds row l%32 and keys 8 (j/4) + 4 (l/32) + j%4, the B operand of
-// the output product, which takes 16 keys' upper parts and then the rest.  A wave turns its
+// the output product.  A wave turns its
 // keys of the next step beside the products of the scores.
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, bool ROPE, int WR>
@@ -961,29 +969,35 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
         keys.clean(u, sl);
         if (ROPE) keys.find_angles(sl);
     };
+    typename Keys::Blocks blk{};
     constexpr int NT = 2 / KG;   // times 32 keys of a step
     constexpr int TAKEN = KD * NT;
     // ---- step s in stage st, and the turning of the next
     auto step = [&](int s, int st) {
         const int sl = keys.next(st);
-        landed(s + 1, sl);
-        const bool powers = ROPE && keys.wave_flag(lds.kbig[st]);
-        // ---- scores, with the next step's keys turned beside (past the last step: of nothing, into a
-        // stage that is not read again)
         // (the offsets are not kept apart for every chunk: registers are short)
         asm volatile("" : "+v"(k_at), "+v"(v_at));
         const uint32_t at = keys.stages_at + (uint32_t)(st * Keys::SE + 32 * kg * D) * 2, kt = at + k_at, vt = at + v_at;
+        constexpr int kAhead = 4;                 // K reads in flight
+        u32x4_t kf[TAKEN];
+        auto read_k = [&](int i) { kf[i] = *(lds_u32x4_t*)(uintptr_t)((kt ^ (32 * (i / NT))) + 64 * (i % NT) * D); };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read_k(i);
+        const int32_t flag = ROPE ? lds.kbig[st][lane % NW] : 0;
+        // step s + NST - 1 goes where step s - 1 was
+        if (s + NST - 1 < nt) {
+            keys.issue(s + NST - 1, keys.prev(st), blk);
+            if (s + NST < nt) blk = keys.blocks_of(s + NST);
+        }
+        landed(s + 1, sl);
+        // ---- scores, with the next step's keys turned beside (past the last step: of nothing, into a
+        // stage that is not read again)
         // Every few vector instructions follow a product that they do not wait for, in the order written:
         // left alone, the compiler puts the products side by side, and the vector unit idles.
         f32x16_t sc[NT];
         uint32_t w[PL], turned[PL];
         float big = 0.f;
         if constexpr (ROPE) keys.load_runs(sl, w);
-        constexpr int kAhead = 4;                 // K reads in flight
-        u32x4_t kf[TAKEN];
-        auto read_k = [&](int i) { kf[i] = *(lds_u32x4_t*)(uintptr_t)((kt ^ (32 * (i / NT))) + 64 * (i % NT) * D); };
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) read_k(i);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < TAKEN; ++i) {
@@ -1008,7 +1022,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
             keys.fit(sl, w, turned, big);
             keys.store_runs(sl, turned);
         }
-        if (ROPE && powers) {
+        if (ROPE && __builtin_amdgcn_ballot_w64(flag != 0) != 0) {   // some key of the step came in times a power of two
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -1051,43 +1065,40 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
             m_run = m_new;
         }
         // ---- outputs, 16 keys at a time, with the next 16's probabilities and V reads beside
-        constexpr int NH = 2 * NT, NM = 2 * DB;   // groups of keys, products of each
-        float p[2][8];
-        u32x4_t up[2], down[2];   // a probability's upper part (cut, not rounded) and the rest
-        u32x2_t af[2][NM];
-        // part i of NM of the probabilities of keys 16 h .. 16 h + 15
+        constexpr int NH = 2 * NT;   // groups of keys
+        u32x4_t pw[2];               // probabilities rounded to bf16; the row sum adds exactly those
+        u32x2_t af[2][2 * DB];
+        // part i of DB of the probabilities of keys 16 h .. 16 h + 15
         auto prob = [&](int h, int i) {
-            constexpr int E = 8 / NM;
+            constexpr int E = 8 / DB;
 #pragma unroll
-            for (int r = i * E; r < (i + 1) * E; ++r) {
-                p[h % 2][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h / 2][8 * (h % 2) + r], qs, -m_run));
-                l_run += p[h % 2][r];
-                if (r % 2 == 1) {
-                    const uint32_t x = __float_as_uint(p[h % 2][r - 1]), y = __float_as_uint(p[h % 2][r]);
-                    up[h % 2][r / 2] = pair_hi(x, y);
-                    down[h % 2][r / 2] = pack_bf16(p[h % 2][r - 1] - __uint_as_float(x & 0xffff0000u), p[h % 2][r] - __uint_as_float(y & 0xffff0000u));
-                }
+            for (int r = i * E; r < (i + 1) * E; r += 2) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h / 2][8 * (h % 2) + r], qs, -m_run));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h / 2][8 * (h % 2) + r + 1], qs, -m_run));
+                pw[h % 2][r / 2] = pack_bf16(x, y);
+                l_run = sum2_bf16(pw[h % 2][r / 2], l_run);
             }
         };
-        // V read i of NM: 8 keys of block i / 2
+        // V reads of block i
         auto read_v = [&](int h, int i) {
-            const uint32_t off = (vt ^ (uint32_t)(64 * (i / 2)) ^ (i % 2 ? 16u * kSw8 : 0u)) + 32 * h * D + (i % 2 ? 16 * D : 0);
-            af[h % 2][i] = __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {   // 8 keys each
+                const uint32_t off = (vt ^ (uint32_t)(64 * i) ^ (e ? 16u * kSw8 : 0u)) + 32 * h * D + (e ? 16 * D : 0);
+                af[h % 2][2 * i + e] = __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off));
+            }
         };
 #pragma unroll
-        for (int i = 0; i < NM; ++i) {
+        for (int i = 0; i < DB; ++i) {
             read_v(0, i);
             prob(0, i);
         }
 #pragma unroll
         for (int h = 0; h < NH; ++h)
 #pragma unroll
-            for (int i = 0; i < NM; ++i) {
+            for (int i = 0; i < DB; ++i) {
                 __builtin_amdgcn_sched_barrier(0);
-                const int db = i % DB;
-                const u32x4_t v = {af[h % 2][2 * db][0], af[h % 2][2 * db][1], af[h % 2][2 * db + 1][0], af[h % 2][2 * db + 1][1]};
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, i < DB ? up[h % 2] : down[h % 2]),
-                                                                  acc[db], 0, 0, 0);
+                const u32x4_t v = {af[h % 2][2 * i][0], af[h % 2][2 * i][1], af[h % 2][2 * i + 1][0], af[h % 2][2 * i + 1][1]};
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, pw[h % 2]), acc[i], 0, 0, 0);
                 if (h + 1 < NH) {
                     read_v(h + 1, i);
                     prob(h + 1, i);
@@ -1109,20 +1120,21 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
 #pragma unroll
     for (int u = NST - SPARE; u < NST - 1; ++u)
         if (u < nt) keys.issue(u, u, keys.blocks_of(u));
-    typename Keys::Blocks blk{};
     if (NST - 1 < nt) blk = keys.blocks_of(NST - 1);
     turn_only(0, 0);
     barrier_keep_vmem();
     auto steps = [&](auto rows) {
         int st = 0;
         for (int s = 0; s < nt; ++s) {
-            // step s + NST - 1 goes where step s - 1 was
-            if (s + NST - 1 < nt) {
-                keys.issue(s + NST - 1, keys.prev(st), blk);
-                if (s + NST < nt) blk = keys.blocks_of(s + NST);
+            if (decltype(rows)::value) {
+                step(s, st);
+            } else {
+                if (s + NST - 1 < nt) {
+                    keys.issue(s + NST - 1, keys.prev(st), blk);
+                    if (s + NST < nt) blk = keys.blocks_of(s + NST);
+                }
+                turn_only(s + 1, keys.next(st));
             }
-            if (decltype(rows)::value) step(s, st);
-            else turn_only(s + 1, keys.next(st));
             barrier_keep_vmem();
             st = keys.next(st);
         }
