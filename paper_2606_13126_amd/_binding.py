@@ -272,21 +272,22 @@ def _rows(t, what: str):
     """Address and row stride (elements) of a [n][heads][D] view whose rows are dense."""
     if t is None:
         return None, 0
-    if t.dim() != 3 or t.stride(2) != 1 or t.stride(1) != t.shape[2]:
+    n, heads, d = t.size()
+    row, head, one = t.stride()
+    if one != 1 or head != d:
         raise ValueError(f"{what} must be [n][heads][D] with dense rows")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return t.data_ptr(), row if n > 1 else heads * d
 
 
 def pic_kv_append(cfg: pic_config, k_pool, v_pool, k_new, v_new, positions, slot_mapping, q=None, q_out=None,
                   stream=None) -> None:
     """k_new, v_new [n][Hkv][D] and q [n][Hq][D] may be views of one projection's output (rows
     dense, any row stride); q_out is dense.  positions may be None for an unrotated pool."""
-    n = int(k_new.shape[0])
     (qp, qs), (kp, ks), (vp, vs) = _rows(q, "q"), _rows(k_new, "k_new"), _rows(v_new, "v_new")
     if q_out is not None and not q_out.is_contiguous():
         raise ValueError("q_out must be dense")
-    _check(_lib.pic_kv_append(ctypes.byref(cfg), _ptr(k_pool), _ptr(v_pool), int(k_pool.shape[0]), qp, qs, _ptr(q_out), kp, ks,
-                              vp, vs, _ptr(positions), _ptr(slot_mapping), n, _stream(stream)))
+    _check(_lib.pic_kv_append(ctypes.byref(cfg), k_pool.data_ptr(), v_pool.data_ptr(), k_pool.size(0), qp, qs, _ptr(q_out), kp,
+                              ks, vp, vs, _ptr(positions), slot_mapping.data_ptr(), k_new.size(0), _stream(stream)))
 
 
 def pic_tree_mask(parents, cu_rows, mask, depth=None, stream=None) -> None:

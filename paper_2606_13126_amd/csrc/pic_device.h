@@ -212,8 +212,8 @@ __device__ __forceinline__ int32_t scalar_load(const int32_t* p, int i) { return
 // Group of attention block `bid` (MERGE: of merge block `bid`): binary search over
 // the groups in the kernel arguments, or two scalar loads from the table the
 // plan-upload launches wrote for a large batch.
-template <bool MERGE>
-__device__ __forceinline__ Group group_of(const Plan& plan, int bid) {
+template <bool MERGE, int N>
+__device__ __forceinline__ Group group_of(const PlanOf<N>& plan, int bid) {
     if (plan.table != nullptr) {
         const int gi = scalar_load(MERGE ? plan.merge_map : plan.item_map, bid);
         const int32_t* src = reinterpret_cast<const int32_t*>(plan.table + gi);

@@ -490,6 +490,17 @@ pic_status build_plan_within(const pic_config* c, const pic_batch_host* b, Call 
     return st;
 }
 
+// The fraction of x (above its floor) as 64 binary digits, cut.  In signed conversions: clang's
+// floorl and unsigned conversion took 5 of the 7 us that the steps of 64 pairs cost a call.
+uint64_t fraction64(long double x) {
+    if (!(fabsl(x) < 9223372036854775808.0L)) return 0;   // no digits below 1 that far out
+    x -= (long double)(int64_t)x;
+    if (x < 0.0L) x += 1.0L;
+    const long double up = x * 4294967296.0L;
+    const int64_t hi = (int64_t)up;
+    return ((uint64_t)hi << 32) + (uint64_t)(int64_t)((up - (long double)hi) * 4294967296.0L);
+}
+
 // Phase step of RoPE pair i: omega_i / 2pi revolutions per position as a 64-bit
 // binary fraction, in long double so that the rounding of omega_i stays far below
 // the 2^-64 step.  omega_i = theta^(-2i/R) or the given inv_freq[i] for i < R/2,
@@ -507,10 +518,9 @@ void phase_steps(const pic_config* c, uint64_t* out) {
         out[i] = 0;
         if (i >= rd / 2) continue;
         if (c->inv_freq) om = (long double)c->inv_freq[i];
-        else om = i % 16 == 0 || c->rope_theta < 1.0 ? powl((long double)c->rope_theta, -2.0L * i / rd) : om * ratio;
-        long double rev = om / two_pi;
-        rev -= floorl(rev);
-        out[i] = (uint64_t)(rev * 18446744073709551616.0L);
+        else if (i % 16 == 0 || c->rope_theta < 1.0) om = powl((long double)c->rope_theta, -2.0L * i / rd);
+        else om = om * ratio;
+        out[i] = fraction64(om / two_pi);
     }
 }
 

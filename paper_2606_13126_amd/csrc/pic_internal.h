@@ -101,7 +101,8 @@ __host__ __device__ inline int32_t row_tiles(const Group& g, int32_t group, int3
 // caller's workspace (`table`), written there by plan-upload launches on the same
 // stream, with the group index of every attention block in item_map and of every
 // merge block in merge_map.
-struct Plan {
+template <int N>
+struct PlanOf {
     int32_t n_groups;
     int32_t n_items;     // blocks of the attention launch
     int32_t n_merge;     // blocks of the merge launch
@@ -109,8 +110,12 @@ struct Plan {
     const Group* table;       // device [n_groups], or null when g[] holds the groups
     const int32_t* item_map;  // device [n_items]: group of each attention block
     const int32_t* merge_map; // device [n_merge]: group of each merge block
-    Group g[kMaxGroups];
+    Group g[N];
 };
+typedef PlanOf<kMaxGroups> Plan;
+// Few groups in short arguments: a launch whose arguments are 3.7 KB takes about 2 us longer on
+// the host than one of 1 KB, which a small call, bound by its launches, notices.
+constexpr int kFewGroups = 8;
 
 // A prefill whose keys are each seen by many row tiles rotates them once, into a copy
 // in the workspace: one segment per run of keys of a request that some query sees.
@@ -141,8 +146,8 @@ struct PlanUpload {
 };
 
 // last group whose `field` is <= b (the fields are non-decreasing over groups)
-template <int32_t Group::*field>
-__host__ __device__ inline int plan_search(const Plan& p, int b) {
+template <int32_t Group::*field, int N>
+__host__ __device__ inline int plan_search(const PlanOf<N>& p, int b) {
     int lo = 0, hi = p.n_groups - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -203,6 +208,14 @@ struct TreeArgs : Args {
 constexpr int kTreeWaves = 8;
 constexpr int tree_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256; }
 constexpr int tree_keys(int rows) { return rows <= 32 ? kTreeWaves * kBlock : 64; }   // keys that they take at a time
+
+// Arguments of the join of their key splits
+struct TreeMergeArgs {
+    const float* part_o;
+    const float* part_ml;
+    void* o;
+    int32_t tile_rows, hq, hkv, group;
+};
 
 // Rows of kv_append: strides in 16-byte chunks
 struct AppendArgs {

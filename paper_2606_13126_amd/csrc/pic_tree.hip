@@ -589,8 +589,8 @@ __device__ __forceinline__ float turn_row(float (&xf)[N][8], const float2* tc, i
 // After the scores lane l holds row l%16 of each block and keys 4 (l/16) + {0..3}, the B
 // operand of the output product.
 // ---------------------------------------------------------------------------------
-template <int D, int STYLE, bool ROPE, int CB>
-__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const Plan plan, const TreeArgs a) {
+template <int D, int STYLE, bool ROPE, int CB, int NG>
+__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> plan, const TreeArgs a) {
     typedef TreeKeys<D, STYLE, ROPE, false> Keys;
     constexpr int KD = D / 32;             // 16x16x32 contraction steps of QK^T
     constexpr int DB = D / 16;             // 16-dim blocks of O^T
@@ -871,8 +871,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const Plan plan, 
 // the output product.  A wave turns its
 // keys of the next step beside the products of the scores.
 // ---------------------------------------------------------------------------------
-template <int D, int STYLE, bool ROPE, int WR>
-__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan, const TreeArgs a) {
+template <int D, int STYLE, bool ROPE, int WR, int NG>
+__global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG> plan, const TreeArgs a) {
     typedef TreeKeys<D, STYLE, ROPE, true> Keys;
     constexpr int KD = D / 16;             // 32x32x16 contraction steps of QK^T
     constexpr int DB = D / 32;             // 32-dim blocks of O^T
@@ -1180,8 +1180,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const Plan plan,
 
 // Joins key splits: one block per kMergeRows rows of a (row tile, KV head),
 // one float4 of a row per thread, eight splits' loads in flight.
-template <int D>
-__global__ void __launch_bounds__(kMergeRows * D / 4) tree_merge(const Plan plan, const TreeArgs a) {
+template <int D, int NG>
+__global__ void __launch_bounds__(kMergeRows * D / 4) tree_merge(const PlanOf<NG> plan, const TreeMergeArgs a) {
     constexpr int TPR = D / 4, U = 8;
     const Group g = group_of<true>(plan, blockIdx.x);
     if (g.n_split <= 1) return;
@@ -1221,19 +1221,28 @@ __global__ void __launch_bounds__(kMergeRows * D / 4) tree_merge(const Plan plan
     *reinterpret_cast<u32x2_t*>(op) = u32x2_t{pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv)};
 }
 
-template <int D, int STYLE, bool ROPE>
-hipError_t launch_tree_t(const Plan& plan, const TreeArgs& a, hipStream_t st) {
+template <int D, int STYLE, bool ROPE, int NG>
+hipError_t launch_tree_n(const PlanOf<NG>& plan, const TreeArgs& a, hipStream_t st) {
     const dim3 grid(plan.n_items), block(kTreeWaves * 64);
     switch (a.tile_rows) {
-    case 16: hipLaunchKernelGGL((tree_few<D, STYLE, ROPE, 1>), grid, block, 0, st, plan, a); break;
-    case 32: hipLaunchKernelGGL((tree_few<D, STYLE, ROPE, 2>), grid, block, 0, st, plan, a); break;
-    case 128: hipLaunchKernelGGL((tree_many<D, STYLE, ROPE, 4>), grid, block, 0, st, plan, a); break;
-    default: hipLaunchKernelGGL((tree_many<D, STYLE, ROPE, 8>), grid, block, 0, st, plan, a); break;
+    case 16: hipLaunchKernelGGL((tree_few<D, STYLE, ROPE, 1, NG>), grid, block, 0, st, plan, a); break;
+    case 32: hipLaunchKernelGGL((tree_few<D, STYLE, ROPE, 2, NG>), grid, block, 0, st, plan, a); break;
+    case 128: hipLaunchKernelGGL((tree_many<D, STYLE, ROPE, 4, NG>), grid, block, 0, st, plan, a); break;
+    default: hipLaunchKernelGGL((tree_many<D, STYLE, ROPE, 8, NG>), grid, block, 0, st, plan, a); break;
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.n_merge == 0) return e;
-    hipLaunchKernelGGL((tree_merge<D>), dim3(plan.n_merge), dim3(kMergeRows * D / 4), 0, st, plan, a);
+    const TreeMergeArgs m = {a.part_o, a.part_ml, a.o, a.tile_rows, a.hq, a.hkv, a.group};
+    hipLaunchKernelGGL((tree_merge<D, NG>), dim3(plan.n_merge), dim3(kMergeRows * D / 4), 0, st, plan, m);
     return hipGetLastError();
+}
+
+template <int D, int STYLE, bool ROPE>
+hipError_t launch_tree_t(const Plan& plan, const TreeArgs& a, hipStream_t st) {
+    if (plan.n_groups > kFewGroups) return launch_tree_n<D, STYLE, ROPE, kMaxGroups>(plan, a, st);
+    PlanOf<kFewGroups> few = {plan.n_groups, plan.n_items, plan.n_merge, plan.merge_ways, plan.table, plan.item_map, plan.merge_map, {}};
+    for (int i = 0; i < plan.n_groups; ++i) few.g[i] = plan.g[i];
+    return launch_tree_n<D, STYLE, ROPE, kFewGroups>(few, a, st);
 }
 
 template <int D>
