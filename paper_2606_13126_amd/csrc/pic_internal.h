@@ -113,8 +113,8 @@ struct PlanOf {
     Group g[N];
 };
 typedef PlanOf<kMaxGroups> Plan;
-// Few groups in short arguments: a launch whose arguments are 3.7 KB takes about 2 us longer on
-// the host than one of 1 KB, which a small call, bound by its launches, notices.
+// Few groups in short arguments: the two launches of a small call take 12.2 us on the host, 13.8
+// with 3.7 KB of arguments each.
 constexpr int kFewGroups = 8;
 
 // A prefill whose keys are each seen by many row tiles rotates them once, into a copy

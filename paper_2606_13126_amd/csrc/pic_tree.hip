@@ -412,6 +412,13 @@ struct TreeKeys : TreeShape<D, SHARED> {
         else wait_vmem();
         __atomic_signal_fence(__ATOMIC_SEQ_CST);
     }
+    // the first of ISSUED steps' positions have landed
+    template <int ISSUED>
+    __device__ __forceinline__ void wait_first() const {
+        if (nt >= ISSUED) wait_vmem_n<ISSUED * LPS - 1>();
+        else wait_vmem();
+        __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    }
     // the angles of the lane's key of the step in stage st, computed where they cannot be advanced
     __device__ __forceinline__ void find_angles(int st) {
         const uint32_t pos = (uint32_t)s.ps[wave][st][own_j];
@@ -553,12 +560,14 @@ __device__ __forceinline__ f32x4_t with_infs(f32x4_t x, uint32_t f) {
     return x;
 }
 
-// cos/sin of a wave's tokens t0 .. t1 of the span (HALF pairs each) into cs
+// cos/sin of a wave's tokens t0 .. t1 of the span (at most 16; HALF pairs each) into cs
 template <int HALF>
 __device__ __forceinline__ void token_angles(const TreeArgs& a, const Group& g, const uint64_t* fstep, int lane, int t0, int t1, float2* cs) {
+    const int32_t pos = a.positions[g.pos_off + g.tok0 + min(t0 + (lane & 15), t1)];   // of token t0 + lane
+    const uint64_t step = fstep[lane % HALF];
     for (int i = lane; i < (t1 - t0 + 1) * HALF; i += 64) {
         float c, s;
-        rope_cs_fast(a.positions[g.pos_off + g.tok0 + t0 + i / HALF], fstep[i % HALF], c, s);
+        rope_cs_fast(__shfl(pos, i / HALF), step, c, s);
         cs[i] = make_float2(c, s);
     }
 }
@@ -602,7 +611,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
     __shared__ TreeLds<D, false> lds;
     __shared__ float2 mls[NW][16 * CB];
     __shared__ float qsl[16 * CB];
-    __shared__ __attribute__((aligned(4))) uint8_t infs[NW][CB][DB][64];   // infinities of V that a lane's rows see (Keys::infs_of)
+    __shared__ uint8_t infs[NW][CB * DB][64];   // infinities of V that a lane's rows see (Keys::infs_of), if `noted`
 
     const Group g = group_of<false>(plan, blockIdx.x);
     const int G = a.group, n_rt = g.n_rt;
@@ -613,11 +622,10 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
     Keys keys(lds, a, g, ic);
     const int lane = keys.lane, wave = keys.wave, nt = keys.nt;
     const int c16 = lane & 15, q4 = lane >> 4;
-    keys.fill_steps(a);
-    for (int i = threadIdx.x; i < NW * CB * DB * 16; i += NW * 64) reinterpret_cast<uint32_t*>(infs)[i] = 0;
 #pragma unroll
     for (int u = 0; u < NST - 1; ++u)
         if (u < nt) keys.issue(u, u, keys.blocks_of(u));
+    keys.fill_steps(a);
 
     // ---- queries: wave cb turns rows 16 cb .. 16 cb + 15 and passes them to the others through
     // the stage that is filled last.  The cos/sin of their tokens (a token's heads share them) go
@@ -669,6 +677,10 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
         for (int kd = 0; kd < KD; ++kd) reinterpret_cast<u32x4_t*>(spare)[kd * 64 + lane] = raw[kd];
         if (q4 == 0) qsl[16 * wave + c16] = scale;
     }
+    if (ROPE && nt > 0) {   // the first tile's angles, while its keys come
+        keys.template wait_first<NST - 1>();
+        keys.find_angles(0);
+    }
     barrier_keep_vmem();
     bf16x8_t qb[CB][KD];
     float qs[CB];     // scores are the products times this (log2 units)
@@ -705,6 +717,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
     }
 
     int st = 0;
+    bool noted = false;
     typename Keys::Blocks blk{};
     if (NST - 1 < nt) blk = keys.blocks_of(NST - 1);
     for (int t = 0; t < nt; ++t) {
@@ -725,7 +738,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
 #pragma unroll
             for (int i = 0; i < PL; ++i) w[i] = kf[i / 4][i % 4];
             uint32_t out[PL];
-            keys.find_angles(st);
+            if (t > 0) keys.find_angles(st);
             const float big = keys.turn(w, out);
             powers = keys.fit(st, w, out, big);
 #pragma unroll
@@ -761,13 +774,16 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
             if (__builtin_amdgcn_readfirstlane(lds.vbad[st][wave]) != 0) {
                 // which of this lane's outputs the seen infinities reach
 #pragma unroll 1
+                for (int i = 0; i < CB * DB && !noted; ++i) infs[wave][i][lane] = 0;
+                noted = true;
+#pragma unroll 1
                 for (int k = 0; k < TK; ++k)
 #pragma unroll
                     for (int cb = 0; cb < CB; ++cb)
                         if ((seen[cb] >> k) & 1)
 #pragma unroll 1
                             for (int db = 0; db < DB; ++db)
-                                infs[wave][cb][db][lane] |= (uint8_t)keys.infs_of(st, wave * TK + k, 2 * db + (q4 >> 1), q4 & 1);
+                                infs[wave][cb * DB + db][lane] |= (uint8_t)keys.infs_of(st, wave * TK + k, 2 * db + (q4 >> 1), q4 & 1);
             }
         }
         float mx[CB];
@@ -838,8 +854,14 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
         for (int i = 0; i < NW; ++i) den[cb] += w[i].y * __builtin_amdgcn_exp2f(w[i].x - M[cb]);
         const float mine = __builtin_amdgcn_exp2f(m_run[cb] - M[cb]);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) meet[((wave * CB + cb) * DB + db) * 64 + lane] = with_infs(acc[cb][db] * mine, infs[wave][cb][db][lane]);
+        for (int db = 0; db < DB; ++db) meet[((wave * CB + cb) * DB + db) * 64 + lane] = acc[cb][db] * mine;
     }
+    if (noted)
+#pragma unroll 1
+        for (int i = 0; i < CB * DB; ++i) {
+            f32x4_t* at = meet + (wave * CB * DB + i) * 64 + lane;
+            *at = with_infs(*at, infs[wave][i][lane]);
+        }
     __syncthreads();
     const size_t prow0 = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (16 * CB);
 #pragma unroll
@@ -884,7 +906,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
 
     __shared__ TreeLds<D, true> lds;
     __shared__ float2 mls[NW][32];
-    __shared__ __attribute__((aligned(4))) uint8_t infs[NW][DB * 4][64];   // infinities of V that a lane's row sees (Keys::infs_of)
+    __shared__ uint8_t infs[NW][DB * 4][64];   // infinities of V that a lane's row sees (Keys::infs_of), if `noted`
 
     const Group g = group_of<false>(plan, blockIdx.x);
     const int G = a.group, n_rt = g.n_rt;
@@ -895,11 +917,10 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
     const int lane = keys.lane, wave = keys.wave, nt = keys.nt;
     const int rg = wave / KG, kg = wave % KG, l32 = lane & 31, hi = lane >> 5;
     const int rows_total = g.n_tok * G, row_lo = (ic.rt * WR + rg) * 32;
-    keys.fill_steps(a);
-    for (int i = threadIdx.x; i < NW * DB * 4 * 16; i += NW * 64) reinterpret_cast<uint32_t*>(infs)[i] = 0;
 #pragma unroll
     for (int u = 0; u < NST - SPARE; ++u)
         if (u < nt) keys.issue(u, u, keys.blocks_of(u));
+    keys.fill_steps(a);
 
     // ---- queries, 16 rows after the other, so that the cos/sin of their tokens (a token's heads
     // share them) fit in the wave's part of the stages filled last
@@ -953,6 +974,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[db] = f32x16_t{};
     float m_run = kNegBig, l_run = 0.f;
+    bool noted = false;
     // per-lane byte offsets: the K operand's row among 32 keys, the V^T operand's among 8 (chunk c,
     // and the row 8 keys on, by xor)
     constexpr int kSw8 = D == 128 ? 1 : 4;
@@ -1040,6 +1062,9 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
                     if (!((mine >> (8 * (j >> 2) + (j & 3))) & 1)) sc[n][j] = -INFINITY;
                 if (keys.wave_flag(lds.vbad[st])) {
                     // which of this lane's outputs the seen infinities reach
+#pragma unroll 1
+                    for (int c = 0; c < DB * 4 && !noted; ++c) infs[wave][c][lane] = 0;
+                    noted = true;
 #pragma unroll 1
                     for (int k = 0; k < 32; ++k)
                         if ((seen >> k) & 1)
@@ -1158,9 +1183,14 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
 #pragma unroll
     for (int c = 0; c < DB * 4; ++c) {
         const f32x4_t x = {acc[c / 4][4 * (c % 4)], acc[c / 4][4 * (c % 4) + 1], acc[c / 4][4 * (c % 4) + 2], acc[c / 4][4 * (c % 4) + 3]};
-        out[c] = with_infs(x * mine, infs[wave][c][lane]);
-        if (KG > 1) meet[(wave * DB * 4 + c) * 64 + lane] = out[c];
+        out[c] = x * mine;
     }
+    if (noted)
+#pragma unroll
+        for (int c = 0; c < DB * 4; ++c) out[c] = with_infs(out[c], infs[wave][c][lane]);
+    if (KG > 1)
+#pragma unroll
+        for (int c = 0; c < DB * 4; ++c) meet[(wave * DB * 4 + c) * 64 + lane] = out[c];
     if (KG > 1) __syncthreads();
     if (row >= rows_total) return;
     const size_t prow = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (32 * WR) + rg * 32 + l32;
