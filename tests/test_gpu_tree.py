@@ -1,0 +1,698 @@
+"""Speculative decoding on the GPU against plain float64: kv_append, tree_mask, attn_tree and
+kv_keep at the sizes and masks where they can go wrong, and a step of all four."""
+import numpy as np
+import pytest
+import torch
+
+from tests import tree_util as T
+from tests.gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+B = pytest.importorskip("paper_2606_13126_amd._binding")
+HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}   # of a rounding, relative
+# cos/sin in float32: the phase rounded to 24 bits (pi 2^-24), the sine of it to a few units, and in
+# the bf16 attention 32 advances of at most 2^-22 each
+ANGLE, ANGLE_ADVANCED = 2.0 ** -21, 2.0 ** -17
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def cfg_of(hq, hkv, d, dtype, style=0, rot=0, prerotated=0, theta=1e4, scale=0.0, inv_freq=None):
+    return B.make_config(hq, hkv, d, dtype=B.PIC_F32 if dtype == torch.float32 else B.PIC_BF16, rope_theta=theta, rope_style=style,
+                         rotary_dim=rot, k_prerotated=prerotated, softmax_scale=scale, inv_freq=inv_freq)
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Drafts:
+    """Requests of (context, drafted tokens, window start) over a pool of blocks in random order, their
+    queries, keys, values and masks."""
+
+    def __init__(self, lens, hq=8, hkv=2, d=128, dtype=torch.bfloat16, style=0, rot=0, prerotated=0, seed=0, see=None, positions=None,
+                 words=None, inv_freq=None, kscale=1.0, qscale=1.0, theta=1e4):
+        rng = self.rng = np.random.default_rng(seed)
+        self.lens = [(l + (0,))[:3] for l in lens]
+        self.hq, self.hkv, self.d, self.dtype, self.style, self.rot = hq, hkv, d, dtype, style, rot
+        self.prerotated, self.inv_freq, self.theta = prerotated, inv_freq, theta
+        self.cfg = cfg_of(hq, hkv, d, dtype, style, rot, prerotated, theta, inv_freq=inv_freq)
+        seq, cu, start, flags, win = [], [0], [], [], []
+        for ctx, n, w in self.lens:
+            if ctx:
+                start.append(0), flags.append(B.PIC_PDEP), win.append(-1)
+            if n:
+                start.append(ctx), flags.append(B.PIC_PDEP | B.PIC_QUERY), win.append(w)
+            seq.append(ctx + n)
+            cu.append(len(start))
+        self.host = B.HostBatch(seq, cu, start, flags, win)
+        need = [-(-s // 16) for s in seq]
+        self.nb = sum(need) + 2
+        table = np.zeros((len(seq), max(need)), np.int32)
+        ids = rng.permutation(self.nb)
+        for r, k in enumerate(need):
+            table[r, :k], ids = ids[:k], ids[k:]
+        self.table = table
+        self.see, depth = [], []
+        for r, (ctx, n, w) in enumerate(self.lens):
+            s, dep = T.ancestors(T.random_parents(rng, n))
+            self.see.append(s if see is None else see(rng, n))
+            depth.append(dep)
+        self.words = words or max(1, max(-(-n // 64) for _, n, _ in self.lens))
+        self.pos = (np.concatenate([np.concatenate([np.arange(c), c + dp]) for (c, n, w), dp in zip(self.lens, depth)])
+                    if positions is None else positions(rng, sum(seq))).astype(np.int32)
+        rows = sum(n for _, n, _ in self.lens)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        r = lambda *s: torch.randn(*s, generator=g, device="cuda")   # noqa: E731
+        self.q = (r(rows, hq, d) * qscale).to(dtype)
+        self.k_pool, self.v_pool = (r(self.nb, hkv, 16, d) * kscale).to(dtype), r(self.nb, hkv, 16, d).to(dtype)
+        self.mask = dev(np.concatenate([T.pack(s, self.words) for s in self.see]))
+        self.block_tables, self.positions = dev(table), dev(self.pos)
+        self.ws = torch.empty(max(1, B.pic_tree_workspace_size(self.cfg, self.host)), dtype=torch.uint8, device="cuda")
+
+    def run(self, table=None, o=None, stream=None, ws=None):
+        o = torch.full_like(self.q, float("nan")) if o is None else o
+        B.pic_attn_tree(self.cfg, self.host, self.block_tables, self.positions, self.mask, self.q, o, self.k_pool, self.v_pool,
+                        workspace=self.ws if ws is None else ws, table=table, stream=stream)
+        return o
+
+    def rope_table(self, n):
+        t = torch.empty((n, self.d // 2) + ((2,) if self.dtype == torch.float32 else ()), dtype=torch.float32, device="cuda")
+        B.pic_rope_table_build(self.cfg, t)
+        return t
+
+    def slot(self, r, j):
+        return int(self.table[r, j // 16]) * 16 + j % 16
+
+    def check(self, got, what="", k_pool=None, v_pool=None):
+        """Every output within what its roundings can do (derived below)."""
+        rot = self.rot or self.d
+        kp, vp, q = f64(self.k_pool if k_pool is None else k_pool), f64(self.v_pool if v_pool is None else v_pool), f64(self.q)
+        got = f64(got)
+        row, off, worst = 0, 0, 0.0
+        scale = self.d ** -0.5
+        for r, (ctx, n, w) in enumerate(self.lens):
+            L = ctx + n
+            if n == 0:
+                off += L
+                continue
+            j = np.arange(w, L)
+            k, v = (p[self.table[r, j // 16], :, j % 16] for p in (kp, vp))
+            qq = q[row:row + n]
+            if not self.prerotated:
+                k = T.rotate(k, self.pos[off + w:off + L], rot, self.theta, self.style, self.inv_freq)
+                qq = T.rotate(qq, self.pos[off + ctx:off + L], rot, self.theta, self.style, self.inv_freq)
+            see = np.concatenate([np.ones((n, ctx - w), bool), self.see[r]], 1)
+            o, spread = T.attention(qq, k, v, see, scale)
+            # A score q.k is off by at most |q||k| scale times the relative errors of q and k: float32
+            # angles, and for bf16 a rounding of either to 11 bits (without rotation to none); its
+            # sum of D products by D 2^-24 of the same.  A relative error e of every probability moves
+            # an output by at most e / (1 - e) sum p |v - o|.  Probabilities are rounded to bf16 (the
+            # sum adds the rounded ones), outputs to their type; exp2, sums and joins stay in 32 bits.
+            bf = self.dtype == torch.bfloat16
+            each = 0.0 if self.prerotated else (2.0 ** -11 if bf else 2.0 ** -24) + (ANGLE_ADVANCED if bf else ANGLE)
+            nq, nk = np.linalg.norm(qq, axis=-1).max(), np.linalg.norm(k, axis=-1).max()
+            ds = nq * nk * scale * (2 * each + each * each + self.d * 2.0 ** -24)
+            e = np.expm1(ds) + (2.0 ** -8 if bf else 0.0) + 2.0 ** -20
+            assert e < 0.5, "inputs too large for the bound"
+            mean = np.abs(o) + spread
+            tol = e / (1 - e) * spread + (HALF_STEP[self.dtype] * 1.01 + 2.0 ** -20) * mean + 1e-30
+            d = np.abs(got[row:row + n] - o)
+            assert np.isfinite(got[row:row + n]).all(), (what, r)
+            worst = max(worst, float((d / tol).max()))
+            assert (d <= tol).all(), (what, r, float((d / tol).max()), float(d.max()))
+            row, off = row + n, off + L
+        say(f"  {what}: at most {worst:.2f} of the bound")
+
+
+# ------------------------------------------------------------------------------------
+# attn_tree
+# ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 64), (16, 1, 128), (7, 1, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ctx", [0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 700])
+def test_attn_tree_lengths(hq, hkv, d, dtype, ctx):
+    g = hq // hkv
+    # rows that fill, overfill and underfill every size of row tile
+    nodes = sorted({1, 2, max(1, 16 // g), 16 // g + 1, max(1, 32 // g), 32 // g + 1, max(1, 128 // g), 128 // g + 1})
+    for n in nodes:
+        b = Drafts([(ctx, n)], hq, hkv, d, dtype, style=n % 2, seed=ctx * 131 + n)
+        b.check(b.run(), f"ctx {ctx} nodes {n}")
+
+
+@pytest.mark.parametrize("n", [255, 257, 513])
+def test_attn_tree_of_many_tokens(n):
+    for hq, hkv, dtype in ((2, 1, torch.bfloat16), (4, 4, torch.bfloat16), (2, 2, torch.float32)):
+        b = Drafts([(100, n), (37, 64), (0, n // 2)], hq, hkv, 64, dtype, seed=n)
+        b.check(b.run(), f"{n} tokens")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("style,rot,prerotated", [(0, 0, 0), (1, 0, 0), (0, 32, 0), (0, 16, 0), (1, 34, 0), (1, 2, 0), (0, 0, 1), (0, 64, 1)])
+@pytest.mark.parametrize("d,nodes", [(128, 5), (128, 40), (64, 9), (64, 70)])
+def test_attn_tree_rotations(dtype, style, rot, prerotated, d, nodes):
+    b = Drafts([(150, nodes), (290, 3), (16, 1)], 8, 2, d, dtype, style, rot, prerotated, seed=nodes)
+    b.check(b.run(), "no table")
+    if not prerotated:
+        # a table, also one that ends inside the context
+        for n in (500, 100):
+            b.check(b.run(table=b.rope_table(n)), f"table of {n}")
+
+
+def test_attn_tree_scaled_frequencies():
+    freq = 5e5 ** (-2.0 * np.arange(32) / 64) / np.linspace(1, 8, 32)
+    for n in (4, 50):
+        b = Drafts([(200, n)], 8, 2, 128, rot=64, inv_freq=freq, seed=n)
+        b.check(b.run(), "frequencies")
+
+
+@pytest.mark.parametrize("kind", ["far", "negative", "scattered", "jumps"])
+@pytest.mark.parametrize("nodes", [6, 60])
+def test_attn_tree_positions(kind, nodes):
+    """Logical positions of any kind: the angles that advance from tile to tile are computed anew
+    where positions do not."""
+    def positions(rng, n):
+        p = np.arange(n)
+        if kind == "far":
+            return p + (1 << 30)
+        if kind == "negative":
+            return p - 5000
+        if kind == "scattered":
+            return rng.integers(-(1 << 31), 1 << 31, n)
+        return p + 1000 * (p // 150)
+    # 5,000 keys: the angles of a lane are renewed on the way
+    b = Drafts([(5000, nodes), (333, nodes)], 8, 2, 128, positions=positions, seed=nodes)
+    b.check(b.run(), kind)
+
+
+def test_attn_tree_windows():
+    for w in (0, 1, 15, 16, 100, 333):
+        for n in (3, 33):
+            for dtype in (torch.bfloat16, torch.float32):
+                b = Drafts([(333, n, w), (400, 2, 399)], 8, 2, 64, dtype, seed=w)
+                b.check(b.run(), f"window {w}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nodes", [1, 5, 20, 70])
+def test_attn_tree_any_mask(dtype, nodes):
+    """Masks need not be trees: rows that see nothing, later tokens, not themselves; bits past the
+    span are ignored."""
+    def see(rng, n):
+        s = rng.random((n, n)) < 0.3
+        s[::3] = False
+        return s
+    for ctx in (0, 40):
+        b = Drafts([(ctx, nodes), (ctx, 3)], 8, 2, 128, dtype, see=see, words=3, seed=nodes)
+        words = b.mask.cpu().numpy().view(np.uint64).copy()
+        row = 0
+        for c, n, w in b.lens:
+            for j in range(n, 192):
+                words[row:row + n, j // 64] |= np.uint64(1) << np.uint64(j % 64)
+            row += n
+        b.mask = dev(words.view(np.int64))
+        o = b.run()
+        b.check(o, f"ctx {ctx}")
+        if ctx == 0:
+            empty = np.concatenate([~s.any(1) for s in b.see])
+            assert empty.any() and (f64(o)[empty] == 0).all()
+
+
+def poison(b, r, j, value):
+    blk, off = b.slot(r, j) // 16, b.slot(r, j) % 16
+    for p, x in ((b.k_pool, value[0]), (b.v_pool, value[1])):
+        if x is not None:
+            p[blk, :, off] = x
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("nodes,hq,d,prerotated", [(3, 8, 128, 0), (7, 8, 128, 1), (30, 8, 128, 0), (30, 8, 64, 0), (70, 16, 64, 1), (70, 8, 128, 0)])
+def test_attn_tree_unseen_tokens_do_not_matter(dtype, nodes, hq, d, prerotated):
+    """Infinities and NaN in keys and values of tokens that a row does not see leave it bit for bit;
+    infinities that it sees arrive in their own dimensions."""
+    b = Drafts([(77, nodes), (300, nodes)], hq, 2, d, dtype, prerotated=prerotated, seed=nodes)
+    bad = nodes // 2
+    for r in range(2):
+        poison(b, r, b.lens[r][0] + bad, (0.0, 0.0))
+    ref = b.run()
+    sees = np.concatenate([s[:, bad] for s in b.see])
+    for kv in ((float("nan"), float("inf")), (float("inf"), float("nan")), (None, -float("inf")), (float("nan"), None)):
+        for r in range(2):
+            poison(b, r, b.lens[r][0] + bad, kv)
+        o = b.run()
+        assert torch.equal(o[dev(~sees)], ref[dev(~sees)])
+        assert not torch.isfinite(o[dev(sees)]).all()
+    v = torch.ones(d, device="cuda", dtype=dtype)
+    v[::4], v[1::4], v[2::4] = float("inf"), -float("inf"), float("nan")
+    for r in range(2):
+        poison(b, r, b.lens[r][0] + bad, (0.0, v))
+    o = b.run()
+    assert torch.isfinite(o[dev(~sees)]).all()
+    o = f64(o[dev(sees)])
+    assert (o[..., ::4] == np.inf).all() and (o[..., 1::4] == -np.inf).all() and np.isnan(o[..., 2::4]).all() and np.isfinite(o[..., 3::4]).all()
+
+
+def test_attn_tree_keys_outside_the_window_are_not_read():
+    for n in (4, 40):
+        for dtype in (torch.bfloat16, torch.float32):
+            b = Drafts([(200, n, 72)], 8, 2, 128, dtype, seed=n)
+            for j in range(72):
+                poison(b, 0, j, (float("nan"), float("nan")))
+            o = b.run()
+            assert torch.isfinite(o).all()
+            for j in range(72):
+                poison(b, 0, j, (0.0, 0.0))
+            b.check(o, "window")
+
+
+@pytest.mark.parametrize("nodes", [5, 40])
+@pytest.mark.parametrize("power", [-60, -20, 17, 60])
+def test_attn_tree_large_and_small_keys(nodes, power):
+    """Keys far from 1, queries as far the other way: float16 holds them by powers of two."""
+    for style in (0, 1):
+        b = Drafts([(130, nodes)], 8, 2, 128, style=style, seed=nodes, kscale=2.0 ** power, qscale=2.0 ** -power)
+        b.check(b.run(), f"2^{power}")
+    # some keys large, others small, others as usual, with queries to which the large ones matter
+    b = Drafts([(130, nodes)], 8, 2, 128, seed=nodes + 2, qscale=2.0 ** -20)
+    for j in (3, 64, 100, 131):
+        poison_key(b, j, 2.0 ** 20)
+    for j in (1, 65):
+        poison_key(b, j, 2.0 ** -power)
+    if abs(power) < 40:
+        b.check(b.run(), "mixed")
+    # Large keys that lie across the queries (in dimensions where those are 0, at position 0): their
+    # scores are 0 but for the sine of the angle, which is 0 up to its error of 2^-17, times a key of
+    # 2^40 sqrt(64) and a query of about 8, times the scale of 2^-3.5: up to 2^25.5, so that any of the
+    # three keys may win.  What remains is that outputs are means of values.
+    b = Drafts([(130, nodes)], 8, 2, 128, seed=nodes + 1, prerotated=0, positions=lambda rng, n: np.zeros(n))
+    b.q[..., :64] = 0
+    for j in (3, 64, 100):
+        blk, off = b.slot(0, j) // 16, b.slot(0, j) % 16
+        b.k_pool[blk, :, off, 64:] = 0
+        b.k_pool[blk, :, off, :64] = 2.0 ** 40
+    assert (b.run().abs() <= b.v_pool.abs().max()).all()
+
+
+def poison_key(b, j, times):
+    blk, off = b.slot(0, j) // 16, b.slot(0, j) % 16
+    b.k_pool[blk, :, off] *= times
+
+
+def test_attn_tree_batch_of_many_requests():
+    """More spans than the kernel arguments hold, some requests without a tree, small and large ones."""
+    rng = np.random.default_rng(5)
+    lens = [(int(rng.integers(0, 200)), int(rng.integers(0, 12))) for _ in range(90)]
+    lens = [(max(c, 1) if n == 0 else c, n) for c, n in lens]
+    for dtype in (torch.bfloat16, torch.float32):
+        b = Drafts(lens, 8, 2, 64, dtype, seed=9)
+        b.check(b.run(), "90 requests")
+    b = Drafts(lens[:70] + [(900, 100)], 8, 2, 128, seed=10)
+    b.check(b.run(), "a large tree among small ones")
+
+
+def test_attn_tree_several_trees_of_one_request():
+    """Each query span is a tree of its own: a later one sees all of an earlier one."""
+    b = Drafts([(64, 40)], 8, 2, 128, seed=3)
+    first, second = 17, 23
+    b.host = B.HostBatch([104], [0, 3], [0, 64, 81], [B.PIC_SSEP, B.PIC_PDEP | B.PIC_QUERY, B.PIC_PDEP | B.PIC_QUERY])
+    s1, s2 = T.ancestors(T.random_parents(b.rng, first))[0], T.ancestors(T.random_parents(b.rng, second))[0]
+    b.mask = dev(np.concatenate([T.pack(s1, 1), T.pack(s2, 1)]))
+    see = np.zeros((40, 40), bool)
+    see[:first, :first] = s1
+    see[first:, :first] = True
+    see[first:, first:] = s2
+    b.see = [see]
+    b.ws = torch.empty(max(1, B.pic_tree_workspace_size(b.cfg, b.host)), dtype=torch.uint8, device="cuda")
+    b.check(b.run(), "two trees")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_chain_is_prefill_and_one_token_is_decode(dtype):
+    for n in (1, 9, 50):
+        b = Drafts([(210, n), (35, n)], 8, 2, 128, dtype, see=lambda rng, m: np.tril(np.ones((m, m), bool)),
+                   positions=lambda rng, m: np.arange(m), seed=n)
+        tree = b.run()
+        o = torch.empty_like(b.q)
+        ws = torch.empty(max(1, B.pic_workspace_size(b.cfg, b.host, False)), dtype=torch.uint8, device="cuda")
+        B.pic_attn_prefill(b.cfg, b.host, b.block_tables, b.positions, b.q, o, b.k_pool, b.v_pool, workspace=ws)
+        b.check(tree, "chain")
+        assert (f64(tree) - f64(o)).max() < (5e-2 if dtype == torch.bfloat16 else 1e-4)
+        if n == 1:
+            ws = torch.empty(max(1, B.pic_workspace_size(b.cfg, b.host, True)), dtype=torch.uint8, device="cuda")
+            B.pic_attn_decode(b.cfg, b.host, b.block_tables, b.positions, b.q, o, b.k_pool, b.v_pool, workspace=ws)
+            assert (f64(tree) - f64(o)).max() < (5e-2 if dtype == torch.bfloat16 else 1e-4)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attn_tree_writes_its_rows_only(dtype):
+    for n in (3, 40):
+        b = Drafts([(500, n)], 8, 2, 128, dtype, seed=n)
+        pools = [b.k_pool.clone(), b.v_pool.clone()]
+        guarded = torch.full((n + 2, 8, 128), 7.0, dtype=dtype, device="cuda")
+        ws = torch.full((b.ws.numel() + 512,), 9, dtype=torch.uint8, device="cuda")
+        B.pic_attn_tree(b.cfg, b.host, b.block_tables, b.positions, b.mask, b.q, guarded[1:-1], b.k_pool, b.v_pool,
+                        workspace=ws[:b.ws.numel()])
+        assert (guarded[0] == 7).all() and (guarded[-1] == 7).all() and (ws[b.ws.numel():] == 9).all()
+        assert torch.equal(b.k_pool, pools[0]) and torch.equal(b.v_pool, pools[1])
+        assert torch.equal(guarded[1:-1], b.run())
+
+
+def test_attn_tree_pool_past_4_gib():
+    """Block ids whose byte offsets pass 32 bits."""
+    blocks = (5 << 30) // (8 * 16 * 128 * 2)
+    b = Drafts([(300, 6)], 32, 8, 128, seed=1)
+    small = b.run()
+    far = torch.zeros((2, blocks, 8, 16, 128), dtype=torch.bfloat16, device="cuda")
+    at = blocks - b.nb
+    far[0, at:], far[1, at:] = b.k_pool, b.v_pool
+    b.block_tables = b.block_tables + at
+    b.k_pool, b.v_pool = far[0], far[1]
+    assert torch.equal(b.run(), small)
+    # rows appended and kept out there
+    cfg = cfg_of(8, 8, 128, torch.bfloat16, prerotated=1)
+    rows = torch.randn(20, 8, 128, device="cuda").bfloat16()
+    slots = torch.arange(20, dtype=torch.int32, device="cuda") + (blocks - 2) * 16
+    near = far[:, -2:].clone()
+    pos = torch.arange(20, dtype=torch.int32, device="cuda")
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")   # noqa: E731
+    for k, v, s in ((near[0], near[1], slots - (blocks - 2) * 16), (far[0], far[1], slots)):
+        B.pic_kv_append(cfg, k, v, rows, rows, pos, s)
+        B.pic_kv_keep(cfg, k, v, s, ints(0, 20), ints(0, 7, 19).view(1, 3), ints(3))
+    assert torch.equal(far[:, -2:], near)
+
+
+# ------------------------------------------------------------------------------------
+# kv_append
+# ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hq,hkv,d,style,rot", [(32, 8, 128, 0, 0), (8, 2, 64, 1, 0), (7, 1, 128, 0, 64), (4, 4, 64, 1, 34), (6, 3, 128, 1, 2),
+                                                (12, 12, 64, 0, 16), (64, 8, 128, 0, 0), (1, 1, 64, 0, 48)])
+@pytest.mark.parametrize("n", [1, 2, 65])
+def test_kv_append_turns_and_stores(dtype, hq, hkv, d, style, rot, n):
+    rng = np.random.default_rng(n)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    fused = torch.randn(n + 1, hq + 2 * hkv + 1, d, generator=g, device="cuda").to(dtype)   # rows with a gap behind them
+    q, k, v = fused[:n, :hq], fused[:n, hq:hq + hkv], fused[:n, hq + hkv:-1]
+    nb = n // 16 + 3
+    slots = rng.permutation(nb * 16)[:n].astype(np.int32)
+    if n > 2:
+        slots[[3, 17, 40]] = -1, -5, nb * 16 + 9   # padding rows, and one outside the pool
+    pos = rng.integers(-(1 << 31), 1 << 31, n).astype(np.int32)
+    pos[0] = 0
+    pools = torch.randn(2, nb, hkv, 16, d, generator=g, device="cuda").to(dtype)
+    before = pools.clone()
+    out = torch.full((n + 2, hq, d), 5.0, dtype=dtype, device="cuda")
+    cfg = cfg_of(hq, hkv, d, dtype, style, rot, 1, theta=5e5)
+    B.pic_kv_append(cfg, pools[0], pools[1], k, v, dev(pos), dev(slots), q=q, q_out=out[1:-1])
+    assert (out[0] == 5).all() and (out[-1] == 5).all()
+    keep = [i for i in range(n) if 0 <= slots[i] < nb * 16]
+    want = before.clone()
+    for i in keep:
+        want[:, slots[i] // 16, :, slots[i] % 16] = pools[:, slots[i] // 16, :, slots[i] % 16]
+    assert torch.equal(pools, want)   # nothing else was written
+    r = rot or d
+    for name, x, got, rows in (("q", q, out[1:-1], range(n)),
+                               ("k", k, torch.stack([pools[0, slots[i] // 16, :, slots[i] % 16] for i in keep]), keep)):
+        x = f64(x)[list(rows)]
+        y = T.rotate(x, pos[list(rows)], r, 5e5, style)
+        partner = T.rotate(np.abs(x), np.zeros(len(x)), r, 5e5, style)
+        size = np.abs(x).copy()   # |x| + |y| of an element's pair
+        if style == 0:
+            s = partner[..., :r // 2] + partner[..., r // 2:r]
+            size[..., :r // 2] = size[..., r // 2:r] = s
+        else:
+            s = partner[..., 0:r:2] + partner[..., 1:r:2]
+            size[..., 0:r:2] = size[..., 1:r:2] = s
+        # float32 angles and products, then one rounding
+        tol = size * (ANGLE + 2.0 ** -23) * (1 + HALF_STEP[dtype]) + np.abs(y) * HALF_STEP[dtype] * 1.001
+        tol[..., r:] = 0   # past the rotary width: a copy
+        d_ = np.abs(f64(got) - y)
+        assert (d_ <= tol).all(), (name, float((d_ / np.maximum(tol, 1e-300)).max()))
+    for i in keep:
+        assert torch.equal(pools[1, slots[i] // 16, :, slots[i] % 16], v[i])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_kv_append_unrotated_in_place_and_without_queries(dtype):
+    n, hq, hkv, d = 37, 8, 2, 64
+    qkv = torch.randn(n, hq + 2 * hkv, d, device="cuda").to(dtype)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    slots = dev(np.random.default_rng(0).permutation(64)[:n].astype(np.int32))
+    a, b = torch.zeros(2, 4, hkv, 16, d, dtype=dtype, device="cuda"), torch.zeros(2, 4, hkv, 16, d, dtype=dtype, device="cuda")
+    plain = cfg_of(hq, hkv, d, dtype)
+    out = torch.empty(n, hq, d, dtype=dtype, device="cuda")
+    B.pic_kv_append(plain, a[0], a[1], k, v, None, slots, q=q, q_out=out)
+    B.pic_kv_write(plain, b[0], b[1], k.contiguous(), v.contiguous(), slots)
+    assert torch.equal(a, b) and torch.equal(out, q)                 # the unrotated pool: bit for bit
+    # infinities and NaN are copied too
+    odd = k.clone()
+    odd[0, 0, :3] = torch.tensor([float("inf"), float("nan"), -float("inf")])
+    B.pic_kv_append(plain, a[0], a[1], odd, v, None, slots)
+    s = int(slots[0])
+    assert torch.equal(a[0, s // 16, :, s % 16].view(torch.int16 if dtype == torch.bfloat16 else torch.int32),
+                       odd[0].contiguous().view(torch.int16 if dtype == torch.bfloat16 else torch.int32))
+    # the same queries in place, and keys without queries
+    cfg = cfg_of(hq, hkv, d, dtype, 1, 34, 1)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") * 1000
+    B.pic_kv_append(cfg, a[0], a[1], k, v, pos, slots, q=q, q_out=out)
+    dense = q.contiguous()
+    B.pic_kv_append(cfg, b[0], b[1], k, v, pos, slots, q=dense, q_out=dense)
+    assert torch.equal(dense, out) and torch.equal(a, b)
+    b.zero_()
+    B.pic_kv_append(cfg, b[0], b[1], k, v, pos, slots)
+    assert torch.equal(b[0].flatten()[a[0].flatten() != 0], a[0].flatten()[a[0].flatten() != 0])
+    # what rope_rotate and kv_write store in two calls (float32 roundings of the same angles)
+    turned = k.contiguous()
+    B.pic_rope_rotate(cfg, turned, pos)
+    B.pic_kv_write(cfg, b[0], b[1], turned, v.contiguous(), slots)
+    assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------------------------
+# tree_mask and kv_keep
+# ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sizes", [[1], [2, 64, 1, 63, 65], [0, 5, 0, 130], [1000, 3], [4096], [61] * 64])
+@pytest.mark.parametrize("shape", ["random", "chain", "star", "bad"])
+def test_tree_mask(sizes, shape):
+    rng = np.random.default_rng(len(sizes))
+    parents = []
+    for n in sizes:
+        p = T.random_parents(rng, n)
+        if shape == "chain":
+            p = np.arange(-1, n - 1, dtype=np.int32)
+        elif shape == "star":
+            p = np.where(np.arange(n) > 0, 0, -1).astype(np.int32)
+        elif shape == "bad" and n:   # parents that are not earlier tokens make roots
+            p[rng.random(n) < 0.3] = [1 << 30, -7, n][int(rng.integers(0, 3))]
+            p[-1] = n - 1
+        parents.append(p)
+    extra = 0 if max(sizes) > 4032 else 1
+    words = max(1, -(-max(sizes) // 64)) + extra
+    total = sum(sizes)
+    cu = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    mask = torch.full((total + 2, words), 77, dtype=torch.int64, device="cuda")
+    depth = torch.full((total + 2,), 77, dtype=torch.int32, device="cuda")
+    B.pic_tree_mask(dev(np.concatenate(parents)), dev(cu), mask[1:-1], depth=depth[1:-1])
+    other = torch.empty_like(mask)
+    B.pic_tree_mask(dev(np.concatenate(parents)), dev(cu), other[1:-1])
+    got, dep = mask.cpu().numpy(), depth.cpu().numpy()
+    assert (got[[0, -1]] == 77).all() and (dep[[0, -1]] == 77).all() and torch.equal(other[1:-1], mask[1:-1])
+    for t, n in enumerate(sizes):
+        see, d = T.ancestors(parents[t])
+        assert (got[1 + cu[t]:1 + cu[t + 1]] == T.pack(see, words)).all()
+        assert (dep[1 + cu[t]:1 + cu[t + 1]] == d).all()
+
+
+def test_tree_mask_stays_in_its_arrays():
+    """Row ranges that lie outside the arrays write nothing there."""
+    parents = torch.zeros(10, dtype=torch.int32, device="cuda")
+    mask = torch.full((14, 1), 5, dtype=torch.int64, device="cuda")
+    cu = torch.tensor([-3, 4, 2, 8, 400], dtype=torch.int32, device="cuda")   # negative, backwards, past the end
+    B.pic_tree_mask(parents, cu, mask[2:-2])
+    assert (mask[:2] == 5).all() and (mask[-2:] == 5).all()
+    assert mask[10:12].flatten().tolist() == [1, 3]   # the last range, as far as it lies inside
+
+
+def keep_rows(pools, slots, cu, path, length, n_slots):
+    """One row after the other, ascending."""
+    for t in range(len(cu) - 1):
+        n = cu[t + 1] - cu[t]
+        for i in range(max(0, min(int(length[t]), path.shape[1], n))):
+            p = int(path[t, i])
+            if i < p < n:
+                a, b = int(slots[cu[t] + p]), int(slots[cu[t] + i])
+                if 0 <= a < n_slots and 0 <= b < n_slots:
+                    for pool in pools:
+                        pool[b // 16, :, b % 16] = pool[a // 16, :, a % 16]
+
+
+@pytest.mark.parametrize("hkv,d,dtype", [(8, 128, torch.bfloat16), (2, 64, torch.bfloat16), (3, 128, torch.float32), (1, 64, torch.float32)])
+@pytest.mark.parametrize("sizes,most", [([1], 1), ([5, 64, 0, 17], 17), ([300, 40], 200), ([33] * 40, 9)])
+def test_kv_keep(hkv, d, dtype, sizes, most):
+    rng = np.random.default_rng(most)
+    total = sum(sizes)
+    cu = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32)
+    nb = -(-total // 16) + 2
+    slots = rng.permutation(nb * 16)[:total].astype(np.int32)
+    path = rng.integers(-2, 400, (len(sizes), most)).astype(np.int32)   # rows of no tree: rubbish that moves nothing
+    length = np.zeros(len(sizes), np.int32)
+    for t, n in enumerate(sizes):
+        m = int(rng.integers(0, min(n, most) + 1)) if n else 0
+        path[t, :m] = np.sort(rng.choice(n, m, replace=False)) if m else []
+        length[t] = m
+    pools = torch.randn(2, nb, hkv, 16, d, device="cuda").to(dtype)
+    want = pools.cpu().clone()
+    keep_rows(want, slots, cu, path, length, nb * 16)
+    B.pic_kv_keep(cfg_of(hkv, hkv, d, dtype), pools[0], pools[1], dev(slots), dev(cu), dev(path), dev(length))
+    assert torch.equal(pools.cpu(), want)
+
+
+def test_kv_keep_takes_no_bad_entry():
+    """Entries out of range, slots outside the pool and lengths past the path move nothing."""
+    pools = torch.randn(2, 4, 2, 16, 64, device="cuda").bfloat16()
+    want = pools.cpu().clone()
+    slots = np.array([0, 1, 2, -1, 64, 5, 6, 1 << 30], np.int32)
+    path = np.array([[1, 1, 3, 4, 5, 7, 8, -3]], np.int32)   # to a slot; none; from no slot; from outside; to outside; ...
+    for length in (8, 100, -5):
+        keep_rows(want, slots, [0, 8], path, [length], 64)
+        B.pic_kv_keep(cfg_of(2, 2, 64, torch.bfloat16), pools[0], pools[1], dev(slots), dev(np.array([0, 8], np.int32)), dev(path),
+                      dev(np.array([length], np.int32)))
+        assert torch.equal(pools.cpu(), want)
+    # row ranges outside the slots
+    for cu in ([-4, 8], [4, 2], [6, 300]):
+        B.pic_kv_keep(cfg_of(2, 2, 64, torch.bfloat16), pools[0], pools[1], dev(slots), dev(np.array(cu, np.int32)),
+                      dev(np.array([[1, 2]], np.int32)), dev(np.array([2], np.int32)))
+    assert torch.equal(pools.cpu(), want)
+
+
+# ------------------------------------------------------------------------------------
+# together
+# ------------------------------------------------------------------------------------
+
+class Step:
+    """A step of speculative decoding with fixed buffers: rows appended, mask, attention, rows kept."""
+
+    def __init__(self, prerotated, nodes, dtype=torch.bfloat16):
+        self.b = b = Drafts([(100, nodes), (37, nodes), (0, nodes)], 8, 2, 128, dtype, prerotated=prerotated, seed=nodes)
+        self.nodes, rows = nodes, 3 * nodes
+        self.qkv = torch.zeros(rows, 12, 128, dtype=dtype, device="cuda")
+        self.parents = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        self.cu = torch.arange(0, rows + 1, nodes, dtype=torch.int32, device="cuda")
+        self.slots = dev(np.array([b.slot(r, c + i) for r, (c, n, w) in enumerate(b.lens) for i in range(n)], np.int32))
+        self.row_pos = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        self.path = torch.zeros(3, 6, dtype=torch.int32, device="cuda")
+        self.length = torch.zeros(3, dtype=torch.int32, device="cuda")
+        self.o = torch.empty_like(b.q)
+
+    def draft(self, seed):
+        """New inputs in the same buffers."""
+        b, rng = self.b, np.random.default_rng(seed)
+        trees = [T.random_parents(rng, self.nodes) for _ in range(3)]
+        self.trees = [T.ancestors(t) for t in trees]
+        b.see = [s for s, _ in self.trees]
+        self.parents.copy_(dev(np.concatenate(trees)))
+        off, pos = 0, b.pos.copy()
+        row = []
+        for (c, n, w), (_, dep) in zip(b.lens, self.trees):
+            pos[off + c:off + c + n] = c + dep
+            row.append(c + dep)
+            off += c + n
+        b.pos = pos
+        b.positions.copy_(dev(pos))
+        self.row_pos.copy_(dev(np.concatenate(row).astype(np.int32)))
+        self.qkv.copy_(torch.randn(self.qkv.shape, generator=torch.Generator().manual_seed(seed)))
+        self.paths = []
+        for t, (see, dep) in enumerate(self.trees):
+            leaf = int(rng.integers(0, self.nodes))
+            p = np.nonzero(see[leaf])[0][:6]
+            self.paths.append(p)
+            self.path[t, :len(p)] = dev(p.astype(np.int32))
+            self.length[t] = len(p)
+
+    def run(self, stream=None):
+        b = self.b
+        B.pic_kv_append(b.cfg, b.k_pool, b.v_pool, self.qkv[:, 8:10], self.qkv[:, 10:], self.row_pos, self.slots, q=self.qkv[:, :8],
+                        q_out=b.q, stream=stream)
+        B.pic_tree_mask(self.parents, self.cu, b.mask, stream=stream)
+        b.run(o=self.o, stream=stream)
+        B.pic_kv_keep(b.cfg, b.k_pool, b.v_pool, self.slots, self.cu, self.path, self.length, stream=stream)
+
+
+@pytest.mark.parametrize("prerotated", [0, 1])
+@pytest.mark.parametrize("nodes", [7, 50])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_step_of_all_four(prerotated, nodes, dtype):
+    s = Step(prerotated, nodes, dtype)
+    s.draft(1)
+    b = s.b
+    k0, v0 = b.k_pool.clone(), b.v_pool.clone()
+    s.run()
+    # attention over the pools as they were before rows were kept
+    drafted_k, drafted_v = k0.clone(), v0.clone()
+    q = torch.empty_like(b.q)
+    B.pic_kv_append(b.cfg, drafted_k, drafted_v, s.qkv[:, 8:10], s.qkv[:, 10:], s.row_pos, s.slots, q=s.qkv[:, :8], q_out=q)
+    assert torch.equal(q, b.q)
+    b.check(s.o, "step", drafted_k, drafted_v)
+    # the accepted branch, decoded from the kept rows, sees what its last token saw in the tree
+    seq = [c + len(p) for (c, n, w), p in zip(b.lens, s.paths)]
+    host = B.HostBatch(seq, [0, 1, 2, 3], [0, 0, 0], [B.PIC_PDEP] * 3)
+    last = torch.tensor([t * nodes + int(p[-1]) for t, p in enumerate(s.paths)], device="cuda")
+    pos = dev(np.concatenate([np.arange(n) for n in seq]).astype(np.int32))
+    o = torch.empty(3, 8, 128, dtype=dtype, device="cuda")
+    ws = torch.empty(max(1, B.pic_workspace_size(b.cfg, host, True)), dtype=torch.uint8, device="cuda")
+    B.pic_attn_decode(b.cfg, host, b.block_tables, pos, b.q[last].contiguous(), o, b.k_pool, b.v_pool, workspace=ws)
+    err = (f64(o) - f64(s.o[last]))
+    assert np.linalg.norm(err) / np.linalg.norm(f64(o)) < (2e-2 if dtype == torch.bfloat16 else 1e-5)
+
+
+@pytest.mark.parametrize("nodes", [7, 50])
+@pytest.mark.parametrize("prerotated", [0, 1])
+def test_step_captured_and_replayed(nodes, prerotated):
+    """A captured step gives, on every replay, what the eager one gives on the same inputs."""
+    s, e = Step(prerotated, nodes), Step(prerotated, nodes)
+    s.draft(0)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        s.run(stream=stream)
+    torch.cuda.synchronize()
+    s.b.k_pool.copy_(e.b.k_pool), s.b.v_pool.copy_(e.b.v_pool)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        s.run(stream=torch.cuda.current_stream())
+    for seed in (1, 2, 3, 4):
+        s.draft(seed), e.draft(seed)
+        e.run()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(s.o, e.o) and torch.equal(s.b.k_pool, e.b.k_pool) and torch.equal(s.b.v_pool, e.b.v_pool)
+        assert torch.equal(s.b.mask, e.b.mask)
+
+
+def test_calls_on_two_streams_and_repeats_agree():
+    """Calls that overlap on two streams, each with its own workspace, and repeats: bit for bit."""
+    a, b = Drafts([(3000, 20)], 8, 2, 128, seed=1), Drafts([(2000, 9), (700, 70)], 8, 2, 128, seed=2)
+    ra, rb = a.run(), b.run()
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = [(torch.empty_like(ra), torch.empty_like(rb)) for _ in range(5)]
+    torch.cuda.synchronize()
+    for oa, ob in outs:
+        a.run(o=oa, stream=s)
+        b.run(o=ob, stream=t)
+    torch.cuda.synchronize()
+    for oa, ob in outs:
+        assert torch.equal(oa, ra) and torch.equal(ob, rb)
