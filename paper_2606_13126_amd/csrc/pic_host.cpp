@@ -165,6 +165,76 @@ bool short_items(const pic_config* c, const HostPlan& hp) {
     return tiles < items * (c->head_dim == 128 ? 5 : 8);
 }
 
+// Query rows per workgroup of a call with drafted tokens in bf16: the ones that take the least
+// time by what each costs per key.  Measured on 256 items of 4,096 keys that the L2 holds (D 128,
+// us): 16 rows 61; 32 rows 69; 128 rows 99 with up to 64 of them used, 131 with all; 256 rows 117
+// with up to 64, 127 with 128, 171 with 192, 199 with all.  64 rows in two tiles of 32 take 132,
+// 192 rows in two of 128 253, but a long span among many short ones is better cut than the short
+// ones given its tile.
+int tree_tile(const HostPlan& hp, int G) {
+    const auto cost = [](int tile, int64_t rows) -> int64_t {
+        if (tile <= 32) return tile == 16 ? 61 : 69;
+        if (rows <= 64) return tile == 128 ? 99 : 117;
+        return tile == 128 ? 131 : rows <= 128 ? 132 : rows <= 192 ? 171 : 199;
+    };
+    int best = 0;
+    int64_t least = 0;
+    for (int bits : {4, 5, 7, 8}) {
+        const int tile = 1 << bits;
+        int64_t sum = 0;
+        for (auto& g : hp.groups) {
+            const int64_t rows = (int64_t)g.n_tok * G, full = (rows - 1) >> bits;
+            sum += (((int64_t)g.tok0 + g.n_tok - g.win + 63) / 64) * (full * cost(tile, tile) + cost(tile, rows - full * tile));
+        }
+        if (best == 0 || sum < least) {
+            best = tile;
+            least = sum;
+        }
+    }
+    return best;
+}
+
+// Keys per split of drafted tokens, in steps of tk keys.  A compute unit holds one workgroup.  Looked
+// at are no splits, and the longest ones that make no more than 1, 2, 3.. items per compute unit;
+// taken is what ends first when an item costs its steps, 4 more for its start and, if split,
+// some for its partial rows, which the join reads back.  (Splits of the average work per compute
+// unit make a few items more than one each, and the last of them run alone: 10 trees of 3 to 12
+// tokens over 1,000 to 4,000 keys 54.8 us against 35.1, 5 trees of 16 over 30,000 222 against 148,
+// 64 trees of 17 to 70 tokens 294 against 296.)  At least 128 keys.
+// On return n_split and split_keys of the groups hold their items per split and their steps.
+int64_t tree_chunk(HostPlan& hp, int G, int hkv, int64_t tk) {
+    constexpr int64_t kStart = 4, kRounds = 6;
+    const int64_t join = hp.tree_rows <= 32 ? 1 : hp.tree_rows <= 128 ? 4 : 5;
+    int64_t total = 0, unsplit = 0, longest = 0, shortest = INT64_MAX;
+    for (auto& g : hp.groups) {
+        const int64_t tiles = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
+        g.split_keys = (int32_t)tiles;
+        g.n_split = (int32_t)std::min<int64_t>((int64_t)pic::row_tiles(g, G, hp.tree_rows) * hkv, 1 << 23);   // (more are refused)
+        total += g.n_split * tiles;
+        unsplit += g.n_split;
+        longest = std::max(longest, tiles);
+        shortest = std::min(shortest, tiles);
+    }
+    const int64_t least = 128 / tk, cus = pic::kTargetCUs;
+    // (items of several lengths, the long ones first, end close to the average)
+    int64_t best = longest, time = (unsplit + cus - 1) / cus * (longest + kStart);
+    if (unsplit > cus) time = std::min(time, (total + unsplit * kStart) / cus + shortest);
+    for (int64_t n = std::max<int64_t>(1, (unsplit + cus - 1) / cus); n <= kRounds; ++n) {
+        int64_t chunk = std::max(least, (total + n * cus - 1) / (n * cus));
+        for (; chunk < longest; chunk += 1 + chunk / 16) {
+            int64_t items = 0;
+            for (auto& g : hp.groups) items += (int64_t)g.n_split * ((uint32_t)(g.split_keys + chunk - 1) / (uint32_t)chunk);
+            if (items <= n * cus) break;
+        }
+        if (chunk < longest && n * (chunk + kStart + join) < time) {
+            time = n * (chunk + kStart + join);
+            best = chunk;
+        }
+        if (chunk <= least) break;
+    }
+    return std::min<int64_t>(best, (1 << 30) / tk);   // (keys of a split, counted from its start, stay in 31 bits)
+}
+
 // Groups, their split policy and bases.  Prefill and float32 groups hold (row tile,
 // KV head, split) items.  `lean` (for a workspace without room for the rest) keeps
 // float32 keys unsplit and gives every query head of a decode merge one thread row.
@@ -272,20 +342,10 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
             return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
         });
     } else if (hp.tree) {
-        // Drafted tokens: key splits in chunks of the average work per compute unit, at least
-        // 128 keys.
-        int64_t max_rows = 0;
-        for (auto& g : hp.groups) max_rows = std::max<int64_t>(max_rows, (int64_t)g.n_tok * G);
-        hp.tree_rows = pic::tree_rows(max_rows);
-        const int64_t tk = pic::tree_keys(hp.tree_rows);
-        int64_t tiles_total = 0;
-        for (auto& g : hp.groups)
-            tiles_total += pic::row_tiles(g, G, hp.tile_rows()) * (((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk) * c->num_kv_heads;
-        const int64_t chunk = std::min<int64_t>(std::max<int64_t>(128 / tk, (tiles_total + pic::kTargetCUs - 1) / pic::kTargetCUs),
-                                                (1 << 30) / tk);   // (keys of a split, counted from its start, stay in 31 bits)
+        hp.tree_rows = tree_tile(hp, G);
+        const int64_t tk = pic::tree_keys(hp.tree_rows), chunk = tree_chunk(hp, G, c->num_kv_heads, tk);
         for (auto& g : hp.groups) {
-            const int64_t tiles = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
-            const int64_t n_split = (tiles + chunk - 1) / chunk, each = (tiles + n_split - 1) / n_split;
+            const int64_t tiles = g.split_keys, n_split = (tiles + chunk - 1) / chunk, each = (tiles + n_split - 1) / n_split;
             g.n_split = (int32_t)((tiles + each - 1) / each);   // none of them is empty
             g.split_keys = (int32_t)std::min<int64_t>(each * tk, INT32_MAX);
         }

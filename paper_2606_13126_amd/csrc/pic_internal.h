@@ -202,11 +202,10 @@ struct TreeArgs : Args {
     int32_t tile_rows;        // query rows per workgroup
 };
 
-// bf16 attention of drafted tokens: waves of a workgroup and its query rows for spans of at
-// most `rows` of them.  Up to 32 rows the waves all hold the same ones and take different cache
-// blocks; beyond, they hold 32 each and share keys, 64 at a time.
+// bf16 attention of drafted tokens: waves of a workgroup.  With 16 or 32 query rows the waves all
+// hold the same ones and take different cache blocks; with 128 or 256 they hold 32 each and share
+// keys, 64 at a time.
 constexpr int kTreeWaves = 8;
-constexpr int tree_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256; }
 constexpr int tree_keys(int rows) { return rows <= 32 ? kTreeWaves * kBlock : 64; }   // keys that they take at a time
 
 // Arguments of the join of their key splits
