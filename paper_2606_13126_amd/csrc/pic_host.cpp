@@ -308,7 +308,10 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
         // Key splits when the unsplit items leave compute units idle (two workgroups of
         // four waves or eight of one wave share a CU): chunks of about the average
         // work per resident workgroup, at least 128 keys, below which a split's start
-        // and its partial rows cost more than the keys.
+        // and its partial rows cost more than the keys.  Drafted tokens are few, so that
+        // most calls have fewer items than compute units: at least 64 keys (128, 64 and 32: 3 trees
+        // of 13 tokens over 700 keys 16.9, 13.8, 13.9 us, 1 of 2 over 1,000 25.9, 18.7, 16.8, 1
+        // of 8 over 1,500 17.5, 14.9, 16.9, 1 of 30 over 4,000 41.6, 42.3, 42.9).
         int64_t max_rows = 0, token_heads = 0;
         for (auto& g : hp.groups) {
             max_rows = std::max<int64_t>(max_rows, (int64_t)g.n_tok * G);
@@ -329,7 +332,7 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
                 tiles_total += ((int64_t)g.tok0 + (hp.tree ? g.n_tok - 1 : (std::min((rt + 1) * tr, (int64_t)g.n_tok * G) - 1) / G) -
                                 g.win + tk) / tk * c->num_kv_heads;
         }
-        const int64_t chunk = !lean && base < 2 * target ? std::max<int64_t>(128 / tk, (tiles_total + target - 1) / target)
+        const int64_t chunk = !lean && base < 2 * target ? std::max<int64_t>((hp.tree ? 64 : 128) / tk, (tiles_total + target - 1) / target)
                                                        : (int64_t)INT32_MAX;
         for (auto& g : hp.groups) {
             const int64_t tiles = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
