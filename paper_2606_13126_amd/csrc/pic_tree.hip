@@ -468,15 +468,15 @@ struct TreeKeys : TreeShape<D, SHARED> {
         }
         return big;
     }
-    // A key whose largest element lies outside 2^-8 .. 2^15 goes in times a power of two; returns
-    // whether some key of the wave does.
+    // A key whose largest element lies outside 2^-8 .. 2^15 goes in times a power of two that puts it
+    // just below 2^15; returns whether some key of the wave does.
     __device__ __forceinline__ bool fit(int st, const uint32_t (&w)[PL], uint32_t (&out)[PL], float big) {
         big = SHARED ? max_of8(big) : max_xor32(max_xor16(big));
         const bool odd = big >= 0x1p15f || (big < 0x1p-8f && big > 0.f);
         const bool any = __builtin_amdgcn_ballot_w64(odd) != 0;
         int ex = 0;
         if (any) {
-            ex = odd && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
+            ex = odd && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) - 15 : 0;
             float none = 0.f;
 #pragma unroll
             for (int i = 0; i < PL; i += 2) rotate_pairs<true>(i, w, out, ex, none);
@@ -591,6 +591,15 @@ __device__ __forceinline__ float turn_row(float (&xf)[N][8], const float2* tc, i
     return big;
 }
 
+// A query row whose largest element is big goes in times 2^-ex, within 1.  A small row goes in
+// within 2^-7: with a key of up to 2^15 its products stay below 2^15, and times the largest
+// power of two of a key, 2^113, in range.  (Not a large one: its factor must stay in range too.)
+__device__ __forceinline__ int query_exponent(float big) {
+    return big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) + (big < 1.f ? 7 : 0) : 0;
+}
+// The products' factor with it: not 0, with which a masked -Inf would be NaN.
+__device__ __forceinline__ float back_scale(float scale, int ex) { return fmaxf(ldexpf(scale, ex), 0x1p-149f); }
+
 // ---------------------------------------------------------------------------------
 // tree_few: up to 16 CB rows.
 //   S^T (16 keys x 16 rows) = K Q^T       v_mfma_f32_16x16x32_f16 (bf16 without rotation)
@@ -664,9 +673,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
                 }
             float big = turn_row<STYLE, KD>(xf, cs + (valid ? to - t0 : 0) * HALF, q4, 4);
             big = max_xor32(max_xor16(big));
-            // the row times 2^-ex lies in [-1, 1]
-            const int ex = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
-            scale = ldexpf(scale, ex);
+            const int ex = query_exponent(big);
+            scale = back_scale(scale, ex);
 #pragma unroll
             for (int kd = 0; kd < KD; ++kd)
 #pragma unroll
@@ -956,10 +964,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
                 if (l32 >> 4 == h) big = turn_row<STYLE, KD>(xf, cs + (valid ? toff - t0 : 0) * HALF, hi, 2);
                 __atomic_signal_fence(__ATOMIC_SEQ_CST);
             }
-            // the row times 2^-ex lies in [-1, 1]
-            big = max_xor32(big);
-            const int ex = big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0;
-            qs = ldexpf(qs, ex);
+            const int ex = query_exponent(max_xor32(big));
+            qs = back_scale(qs, ex);
 #pragma unroll
             for (int kd = 0; kd < KD; ++kd)
 #pragma unroll

@@ -304,6 +304,34 @@ def test_attn_tree_large_and_small_keys(nodes, power):
     assert (b.run().abs() <= b.v_pool.abs().max()).all()
 
 
+def test_attn_tree_extreme_scales():
+    """Keys near the type's largest value with queries as small, a few large elements among many small
+    ones, and scores that underflow to 0."""
+    for nodes in (5, 40):
+        for power in (124, -124):
+            b = Drafts([(130, nodes)], 8, 2, 128, seed=4, kscale=2.0 ** power, qscale=2.0 ** -power)
+            b.check(b.run(), f"2^{power}")
+        b = Drafts([(130, nodes)], 8, 2, 128, seed=3)
+        for dim in range(128):
+            times = 2.0 ** 14
+            if dim % 64 == 0:   # the pair that the queries do not have
+                b.q[..., dim] = 0
+                b.k_pool[..., dim] = 2.0 ** -7
+            else:
+                b.q[..., dim] *= times
+                b.k_pool[..., dim] /= times
+        b.check(b.run(), "small beside large")
+        for prerotated in (0, 1):
+            b = Drafts([(0, nodes)], 8, 2, 128, seed=4, prerotated=prerotated, qscale=2.0 ** -125)
+            b.cfg = cfg_of(8, 2, 128, torch.bfloat16, prerotated=prerotated, scale=2.0 ** -40)
+            # equal probabilities to 2^-100: the mean of the values seen
+            o, v = f64(b.run()), f64(b.v_pool)[b.table[0, np.arange(nodes) // 16], :, np.arange(nodes) % 16]
+            for i in range(nodes):
+                seen = v[b.see[0][i]].repeat(4, 1)
+                # a rounding of the output, and of equal probabilities none
+                assert (np.abs(o[i] - seen.mean(0)) <= 2.0 ** -8 * np.abs(seen.mean(0)) + 2.0 ** -20 * np.abs(seen).mean(0) + 1e-30).all()
+
+
 def poison_key(b, j, times):
     blk, off = b.slot(0, j) // 16, b.slot(0, j) % 16
     b.k_pool[blk, :, off] *= times
