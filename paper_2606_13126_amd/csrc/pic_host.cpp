@@ -165,74 +165,88 @@ bool short_items(const pic_config* c, const HostPlan& hp) {
     return tiles < items * (c->head_dim == 128 ? 5 : 8);
 }
 
-// Query rows per workgroup of a call with drafted tokens in bf16: the ones that take the least
-// time by what each costs per key.  Measured on 256 items of 4,096 keys that the L2 holds (D 128,
-// us): 16 rows 61; 32 rows 69; 128 rows 99 with up to 64 of them used, 131 with all; 256 rows 117
-// with up to 64, 127 with 128, 171 with 192, 199 with all.  64 rows in two tiles of 32 take 132,
-// 192 rows in two of 128 253, but a long span among many short ones is better cut than the short
-// ones given its tile.
-int tree_tile(const HostPlan& hp, int G) {
-    const auto cost = [](int tile, int64_t rows) -> int64_t {
-        if (tile <= 32) return tile == 16 ? 61 : 69;
-        if (rows <= 64) return tile == 128 ? 99 : 117;
-        return tile == 128 ? 131 : rows <= 128 ? 132 : rows <= 192 ? 171 : 199;
-    };
-    int best = 0;
-    int64_t least = 0;
+// Row tiles and key splits of a call with drafted tokens in bf16.  A compute unit holds one
+// workgroup, and an item costs a start and its steps (of 128 keys with 16 or 32 query rows, of
+// 64 with 128 or 256).  Per tile, looked at are no splits and the longest splits that make no
+// more than 1, 2, 3 or 4 items per compute unit (at least 128 keys); taken is what ends first
+// by the costs below.  They were fitted to 78,000 calls of 2,720 batches (1 to 48 requests
+// of 1 to 100 tokens over 100 to 24,000 keys, equal and ragged, 1 to 8 KV heads of 4 to 16 query
+// heads, D 128), which they describe within 8%.  On these batches the choice takes 1.04 times
+// the best of all tiles and splits (1.10 at the 90th percentile).  Tiles by the number of rows alone
+// and splits of the average work per compute unit took 1.2 to 1.3 times (1.5): few tokens over
+// short contexts want small tiles, which fill the chip (a tree of 64 tokens, 256 rows, over 1,537
+// keys 19.9 us in tiles of 32, 30.9 in one), and a few items more than compute units end late (5
+// trees of 16 over 30,000 keys 148 us against 222).
+struct TreeSplit {
+    int tile = 0;
+    int64_t chunk = 0;    // steps per split
+    double us = 0;
+};
+
+double tree_step_us(int tile, int64_t rows) {
+    if (tile <= 32) return tile == 16 ? 1.5 : 1.7;
+    if (rows <= 64) return tile == 128 ? 1.3 : 1.6;
+    return rows <= 128 ? 1.7 : rows <= 192 ? 2.1 : 2.3;
+}
+
+TreeSplit tree_split(HostPlan& hp, int G, int hkv) {
+    constexpr int64_t kCUs = pic::kTargetCUs;
+    TreeSplit best;
     for (int bits : {4, 5, 7, 8}) {
         const int tile = 1 << bits;
-        int64_t sum = 0;
+        const int64_t tk = pic::tree_keys(tile), least = 128 / tk;
+        const double start = tile == 16 ? 6.5 : tile == 32 ? 7.5 : 9.2;
+        // per group: steps in split_keys, items per split in n_split (more than this are refused)
+        double work = 0;
+        int64_t unsplit = 0, longest = 0, total = 0;
         for (auto& g : hp.groups) {
-            const int64_t rows = (int64_t)g.n_tok * G, full = (rows - 1) >> bits;
-            sum += (((int64_t)g.tok0 + g.n_tok - g.win + 63) / 64) * (full * cost(tile, tile) + cost(tile, rows - full * tile));
+            const int64_t steps = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk, rows = (int64_t)g.n_tok * G, full = (rows - 1) >> bits;
+            g.split_keys = (int32_t)steps;
+            g.n_split = (int32_t)std::min<int64_t>((full + 1) * hkv, 1 << 23);
+            work += (double)(steps * hkv) * ((double)full * tree_step_us(tile, tile) + tree_step_us(tile, rows - (full << bits)));
+            unsplit += g.n_split;
+            total += g.n_split * steps;
+            longest = std::max(longest, steps);
         }
-        if (best == 0 || sum < least) {
-            best = tile;
-            least = sum;
+        if (best.tile != 0 && work / kCUs > best.us) continue;
+        const auto look = [&](int64_t chunk) {
+            double most = 0, last = 1e30, split_rows = 0;
+            int64_t items = 0;
+            uint32_t splits = 1;
+            for (auto& g : hp.groups) {
+                const uint32_t steps = (uint32_t)g.split_keys, n = (steps + (uint32_t)chunk - 1) / (uint32_t)chunk;
+                const double us = (n == 1 ? steps : (uint32_t)chunk) * tree_step_us(tile, std::min<int64_t>((int64_t)g.n_tok * G, tile));
+                most = std::max(most, us);
+                last = std::min(last, us);
+                items += (int64_t)g.n_split * n;
+                splits = std::max(splits, n);
+                if (n > 1) split_rows += (double)n * g.n_tok * G * hkv;
+            }
+            double us = start + most;
+            if (items > kCUs) {
+                // in rounds, or (items of several lengths, the long ones first) near the average
+                const double rounds = (double)((items + kCUs - 1) / kCUs) * us, average = (items * start + work) / kCUs + start + last;
+                us = std::max(us, std::min(rounds, average));
+            }
+            if (splits > 1) us += 4 + 0.1 * splits + 2e-4 * split_rows;   // the join, and the partial rows that it reads
+            if (best.tile == 0 || us < best.us) best = TreeSplit{tile, chunk, us};
+        };
+        look(longest);
+        for (int64_t n = 1; n <= 4; ++n) {
+            if (unsplit > n * kCUs) continue;
+            int64_t chunk = std::max(least, (total + n * kCUs - 1) / (n * kCUs));
+            for (; chunk < longest; chunk += 1 + chunk / 16) {
+                int64_t items = 0;
+                for (auto& g : hp.groups) items += (int64_t)g.n_split * ((uint32_t)(g.split_keys + chunk - 1) / (uint32_t)chunk);
+                if (items <= n * kCUs) break;
+            }
+            if (chunk >= longest) continue;
+            look(chunk);
+            if (n == 1 && chunk * 32 < longest) look((longest + 31) / 32);   // (the join reads a row's splits one after the other)
+            if (chunk <= least) break;
         }
     }
     return best;
-}
-
-// Keys per split of drafted tokens, in steps of tk keys.  A compute unit holds one workgroup.  Looked
-// at are no splits, and the longest ones that make no more than 1, 2, 3.. items per compute unit;
-// taken is what ends first when an item costs its steps, 4 more for its start and, if split,
-// some for its partial rows, which the join reads back.  (Splits of the average work per compute
-// unit make a few items more than one each, and the last of them run alone: 10 trees of 3 to 12
-// tokens over 1,000 to 4,000 keys 54.8 us against 35.1, 5 trees of 16 over 30,000 222 against 148,
-// 64 trees of 17 to 70 tokens 294 against 296.)  At least 128 keys.
-// On return n_split and split_keys of the groups hold their items per split and their steps.
-int64_t tree_chunk(HostPlan& hp, int G, int hkv, int64_t tk) {
-    constexpr int64_t kStart = 4, kRounds = 6;
-    const int64_t join = hp.tree_rows <= 32 ? 1 : hp.tree_rows <= 128 ? 4 : 5;
-    int64_t total = 0, unsplit = 0, longest = 0, shortest = INT64_MAX;
-    for (auto& g : hp.groups) {
-        const int64_t tiles = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
-        g.split_keys = (int32_t)tiles;
-        g.n_split = (int32_t)std::min<int64_t>((int64_t)pic::row_tiles(g, G, hp.tree_rows) * hkv, 1 << 23);   // (more are refused)
-        total += g.n_split * tiles;
-        unsplit += g.n_split;
-        longest = std::max(longest, tiles);
-        shortest = std::min(shortest, tiles);
-    }
-    const int64_t least = 128 / tk, cus = pic::kTargetCUs;
-    // (items of several lengths, the long ones first, end close to the average)
-    int64_t best = longest, time = (unsplit + cus - 1) / cus * (longest + kStart);
-    if (unsplit > cus) time = std::min(time, (total + unsplit * kStart) / cus + shortest);
-    for (int64_t n = std::max<int64_t>(1, (unsplit + cus - 1) / cus); n <= kRounds; ++n) {
-        int64_t chunk = std::max(least, (total + n * cus - 1) / (n * cus));
-        for (; chunk < longest; chunk += 1 + chunk / 16) {
-            int64_t items = 0;
-            for (auto& g : hp.groups) items += (int64_t)g.n_split * ((uint32_t)(g.split_keys + chunk - 1) / (uint32_t)chunk);
-            if (items <= n * cus) break;
-        }
-        if (chunk < longest && n * (chunk + kStart + join) < time) {
-            time = n * (chunk + kStart + join);
-            best = chunk;
-        }
-        if (chunk <= least) break;
-    }
-    return std::min<int64_t>(best, (1 << 30) / tk);   // (keys of a split, counted from its start, stay in 31 bits)
 }
 
 // Groups, their split policy and bases.  Prefill and float32 groups hold (row tile,
@@ -345,10 +359,12 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
             return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
         });
     } else if (hp.tree) {
-        hp.tree_rows = tree_tile(hp, G);
-        const int64_t tk = pic::tree_keys(hp.tree_rows), chunk = tree_chunk(hp, G, c->num_kv_heads, tk);
+        const TreeSplit sp = tree_split(hp, G, c->num_kv_heads);
+        hp.tree_rows = sp.tile;
+        const int64_t tk = pic::tree_keys(sp.tile), chunk = std::min<int64_t>(sp.chunk, (1 << 30) / tk);   // (keys of a split, counted from its start, stay in 31 bits)
         for (auto& g : hp.groups) {
-            const int64_t tiles = g.split_keys, n_split = (tiles + chunk - 1) / chunk, each = (tiles + n_split - 1) / n_split;
+            const int64_t tiles = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
+            const int64_t n_split = (tiles + chunk - 1) / chunk, each = (tiles + n_split - 1) / n_split;
             g.n_split = (int32_t)((tiles + each - 1) / each);   // none of them is empty
             g.split_keys = (int32_t)std::min<int64_t>(each * tk, INT32_MAX);
         }
@@ -401,7 +417,9 @@ pic_status assign_bases(const pic_config* c, HostPlan& hp) {
     int64_t item = 0, part = 0, merge = 0;
     for (auto& g : hp.groups) {
         const int64_t n = items_of(c, hp, g);
-        const int64_t n_pad = hp.dec_kernel ? n : round_up(n, 8);
+        // (drafted tokens: padding would leave compute units of the last XCDs idle, 44 trees of 4 KV
+        // heads without splits half of them)
+        const int64_t n_pad = hp.dec_kernel || hp.tree ? n : round_up(n, 8);
         g.item_base = (int32_t)item;
         g.part_base = (int32_t)part;
         g.merge_base = (int32_t)merge;

@@ -83,7 +83,7 @@ struct Group {
     };
     int32_t n_split;     // key splits per (row tile, KV head)
     int32_t split_keys;  // keys per split (a multiple of kTileKeys)
-    int32_t item_base;   // first item (block index) of the group; a multiple of 8 (prefill)
+    int32_t item_base;   // first item (block index) of the group; a multiple of 8 (prefill, but for drafted tokens)
     int32_t part_base;   // first partial slot (split groups)
     int32_t merge_base;  // first block of the merge launch (split groups)
 };
