@@ -291,6 +291,7 @@ pic_status pic_tree_workspace_size(const pic_config* cfg, const pic_batch_host* 
  * (its own bit included: a token sees itself only if its mask says so; bits past the span are
  * ignored).  A token that sees nothing gets zeros.  Keys and values of tokens that a query
  * does not see, infinities and NaN included, do not change its output.
+ *  rope      read in float32 only: in bf16 cos/sin are computed, whether a table is given or not;
  *  tree_mask DEVICE [total_q][mask_words], 8-byte aligned; mask_words * 64 must be at least
  *            every query span's length. */
 pic_status pic_attn_tree(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev,

@@ -612,6 +612,9 @@ __device__ __forceinline__ float back_scale(float scale, int ex) { return fmaxf(
 //   O^T (16 dims x 16 rows) += V^T P^T    v_mfma_f32_16x16x32_bf16, V^T by ds_read_b64_tr_b16
 // After the scores lane l holds row l%16 of each block and keys 4 (l/16) + {0..3}, the B
 // operand of the output product.
+// With keys of their own bound by memory (32 requests of 8 tokens over 8,192 keys, 8 KV heads of
+// 128: 198 us, 5.5 TB/s; the vector unit, which turns the keys, is busy 48%, the matrix cores
+// 11%), with few keys by an item's start: 6.4 us with 16 rows, 7.4 with 32, and 1.5 or 1.7 per step.
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, bool ROPE, int CB, int NG>
 __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> plan, const TreeArgs a) {
@@ -906,6 +909,10 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
 // After the scores lane l holds row l%32 and keys 8 (j/4) + 4 (l/32) + j%4, the B operand of
 // the output product.  A wave turns its
 // keys of the next step beside the products of the scores.
+// Bound by power: matrix cores busy 34%, vector unit 45%, at a clock of 1.75 to 1.95 GHz (32 requests
+// of 64 tokens of 32 heads over 8,192 keys 388 to 440 us, 625 to 708 TFLOP/s; keys turned already
+// 311 to 358).  Half a step between the two waves of a SIMD, so that one's products
+// run beside the other's softmax, changed nothing (387 against 388 us).
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, bool ROPE, int WR, int NG>
 __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG> plan, const TreeArgs a) {
