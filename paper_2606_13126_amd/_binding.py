@@ -274,7 +274,7 @@ def _rows(t, what: str):
         return None, 0
     n, heads, d = t.size()
     row, head, one = t.stride()
-    if one != 1 or head != d:
+    if one != 1 or (heads > 1 and head != d):
         raise ValueError(f"{what} must be [n][heads][D] with dense rows")
     return t.data_ptr(), row if n > 1 else heads * d
 

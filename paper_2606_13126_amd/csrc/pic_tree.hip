@@ -515,13 +515,16 @@ struct TreeKeys : TreeShape<D, SHARED> {
         }
     }
     // An infinity or NaN in V must not reach rows that do not see its key (0 x Inf in the
-    // product): where a step has keys that not every row sees, the wave that copied them puts
-    // zeros in their place and notes them; what rows see of them joins their outputs at the end.
+    // product): where keys that are scored together are not all seen by every row, the wave that
+    // copied them puts zeros in their place and notes them; what rows see of them joins their
+    // outputs at the end.
+    static constexpr int TOGETHER = SHARED ? 32 : kBlock;
     __device__ __forceinline__ void clean(int u, int st) {
-        if (u * STEP >= k_lo && (u + 1) * STEP <= min(k_hi, k_tok)) return;
+        if (!masked(u * STEP, STEP)) return;
         uint32_t found = 0;
 #pragma unroll
         for (int i = 0; i < DPL; ++i) {
+            if (!masked(u * STEP + (copy_key(i) & ~(TOGETHER - 1)), TOGETHER)) continue;
             const int key = copy_key(i) + lane / CH;
             u32x4_t* at = reinterpret_cast<u32x4_t*>(s.stages + st * SE + KV + copy_key(i) * D + lane * 8);
             u32x4_t v = *at;
@@ -778,7 +781,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sc[cb][r] *= lds.ksc[st][wave * TK + 4 * q4 + r];
         }
-        if (keys.masked(k0, TK)) {
+        if (keys.masked(k0, Keys::TOGETHER)) {
             const uint32_t inside = keys.inside(k0, TK);
             uint32_t seen[CB];   // the row's bits of the tile's keys
 #pragma unroll
@@ -824,7 +827,9 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
                 m_run[cb] = m_new;
             }
         }
-        u32x4_t pw[CB];   // upper and lower parts of the probabilities
+        // Upper and lower parts of the probabilities: the upper cut off, so that no part is negative, the
+        // lower of a probability above 0 never 0: an infinity that a row sees times them is that infinity.
+        u32x4_t pw[CB];
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             float p[4];
@@ -833,8 +838,9 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
             l_run[cb] += (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                pw[cb][h] = pack_bf16(p[2 * h], p[2 * h + 1]);
-                pw[cb][2 + h] = pack_bf16(p[2 * h] - bf_lo(pw[cb][h]), p[2 * h + 1] - bf_hi(pw[cb][h]));
+                pw[cb][h] = __builtin_amdgcn_perm(__float_as_uint(p[2 * h + 1]), __float_as_uint(p[2 * h]), 0x07060302u);
+                pw[cb][2 + h] = pack_bf16(__builtin_amdgcn_fmed3f(p[2 * h] - bf_lo(pw[cb][h]), p[2 * h], 0x1p-126f),
+                                          __builtin_amdgcn_fmed3f(p[2 * h + 1] - bf_hi(pw[cb][h]), p[2 * h + 1], 0x1p-126f));
             }
         }
 #pragma unroll
@@ -1072,7 +1078,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int p0 = 32 * (kg + n), k0 = s * Keys::STEP + p0;
-            if (keys.masked(k0, 32)) {
+            if (keys.masked(k0, Keys::TOGETHER)) {
                 // the row's bits of the keys (the step's second 32 may all lie past the range)
                 const uint32_t seen = keys.inside(k0, 32) & tree_bits(a.mask + (size_t)(g.q_row0 + toff) * a.words, a.words, k0 - keys.k_tok);
                 const uint32_t mine = seen >> (4 * hi);

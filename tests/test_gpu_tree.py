@@ -263,6 +263,24 @@ def test_attn_tree_unseen_tokens_do_not_matter(dtype, nodes, hq, d, prerotated):
     assert (o[..., ::4] == np.inf).all() and (o[..., 1::4] == -np.inf).all() and np.isnan(o[..., 2::4]).all() and np.isfinite(o[..., 3::4]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("nodes,ctx", [(3, 300), (7, 90), (20, 300), (70, 500), (70, 75), (40, 110)])
+def test_attn_tree_infinities_of_the_context(dtype, nodes, ctx, d):
+    """Infinities in values that every row sees, of one sign or both, arrive as they are."""
+    b = Drafts([(ctx, nodes)], 8, 2, d, dtype, seed=nodes)
+    v = torch.ones(d, device="cuda", dtype=dtype)
+    v[::4], v[1::4], v[2::4] = float("inf"), -float("inf"), float("nan")
+    poison(b, 0, 5, (None, v))
+    v[0] = 1
+    poison(b, 0, 70, (None, v))
+    v[4] = -float("inf")
+    poison(b, 0, 71, (None, v))
+    o = f64(b.run())
+    assert (o[..., 0] == np.inf).all() and np.isnan(o[..., 4]).all() and (o[..., 8::4] == np.inf).all()
+    assert (o[..., 1::4] == -np.inf).all() and np.isnan(o[..., 2::4]).all() and np.isfinite(o[..., 3::4]).all()
+
+
 def test_attn_tree_keys_outside_the_window_are_not_read():
     for n in (4, 40):
         for dtype in (torch.bfloat16, torch.float32):
