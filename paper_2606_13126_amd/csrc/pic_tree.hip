@@ -204,8 +204,8 @@ __global__ void __launch_bounds__(256) kv_keep_kernel(u32x4_t* __restrict__ k_po
 
 // cos/sin by the hardware's sine of a fraction of a revolution (its error, about 2^-20, is far
 // below the 2^-12 to which the attention rounds what they turn)
-__device__ __forceinline__ void rope_cs_fast(int32_t pos, uint64_t step, float& c, float& s) {
-    const uint64_t ph = (uint64_t)(int64_t)pos * step;
+__device__ __forceinline__ void rope_cs_fast(int64_t pos, uint64_t step, float& c, float& s) {
+    const uint64_t ph = (uint64_t)pos * step;
     const float r = (float)(int32_t)(ph >> 32) * 0x1p-32f;
     c = __builtin_amdgcn_cosf(r);
     s = __builtin_amdgcn_sinf(r);
@@ -319,7 +319,7 @@ struct TreeKeys : TreeShape<D, SHARED> {
     // copied and (in the order of the kernel's chunks) as turned
     int s_off[2], t_off[2];
     float rc[PL], rs[PL];      // cos/sin at position cs_pos
-    uint32_t cs_pos = 0;
+    int32_t cs_pos = 0;
     int fresh = 0;             // steps until the angles are computed again
 
     struct Blocks {
@@ -427,10 +427,11 @@ struct TreeKeys : TreeShape<D, SHARED> {
     }
     // the angles of the lane's key of the step in stage st, computed where they cannot be advanced
     __device__ __forceinline__ void find_angles(int st) {
-        const uint32_t pos = (uint32_t)s.ps[wave][st][own_j];
-        if (fresh == 0 || __builtin_amdgcn_ballot_w64(pos != cs_pos + STEP) != 0) {
+        const int32_t pos = s.ps[wave][st][own_j];
+        // (STEP on, and not past the type's end)
+        if (fresh == 0 || __builtin_amdgcn_ballot_w64((uint32_t)pos != (uint32_t)cs_pos + STEP || pos < cs_pos) != 0) {
 #pragma unroll
-            for (int i = 0; i < PL; ++i) rope_cs_fast((int32_t)(pos - STEP), s.fstep[pair_of(i)], rc[i], rs[i]);
+            for (int i = 0; i < PL; ++i) rope_cs_fast((int64_t)pos - STEP, s.fstep[pair_of(i)], rc[i], rs[i]);
             fresh = kRenew;
         }
         --fresh;

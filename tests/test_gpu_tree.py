@@ -177,7 +177,7 @@ def test_attn_tree_scaled_frequencies():
         b.check(b.run(), "frequencies")
 
 
-@pytest.mark.parametrize("kind", ["far", "negative", "scattered", "jumps"])
+@pytest.mark.parametrize("kind", ["far", "negative", "scattered", "jumps", "least", "around"])
 @pytest.mark.parametrize("nodes", [6, 60])
 def test_attn_tree_positions(kind, nodes):
     """Logical positions of any kind: the angles that advance from tile to tile are computed anew
@@ -190,6 +190,10 @@ def test_attn_tree_positions(kind, nodes):
             return p - 5000
         if kind == "scattered":
             return rng.integers(-(1 << 31), 1 << 31, n)
+        if kind == "least":
+            return p - (1 << 31)
+        if kind == "around":   # past the type's end to its start
+            return (p + (1 << 32) - 700) % (1 << 32) - (1 << 31)
         return p + 1000 * (p // 150)
     # 5,000 keys: the angles of a lane are renewed on the way
     b = Drafts([(5000, nodes), (333, nodes)], 8, 2, 128, positions=positions, seed=nodes)
