@@ -571,15 +571,21 @@ pic_status build_plan_within(const pic_config* c, const pic_batch_host* b, Call 
     return st;
 }
 
-// The fraction of x (above its floor) as 64 binary digits, cut.  In signed conversions: clang's
-// floorl and unsigned conversion took 5 of the 7 us that the steps of 64 pairs cost a call.
+// The fraction of x (above its floor) as 64 binary digits, cut.
 uint64_t fraction64(long double x) {
     if (!(fabsl(x) < 9223372036854775808.0L)) return 0;   // no digits below 1 that far out
-    x -= (long double)(int64_t)x;
-    if (x < 0.0L) x += 1.0L;
-    const long double up = x * 4294967296.0L;
-    const int64_t hi = (int64_t)up;
-    return ((uint64_t)hi << 32) + (uint64_t)(int64_t)((up - (long double)hi) * 4294967296.0L);
+    if (x < 0.0L) {
+        x -= (long double)(int64_t)x;
+        if (x < 0.0L) x += 1.0L;
+    }
+    // x = mantissa 2^(exponent - 16383 - 63): its bits below 1, without a conversion (which switches the
+    // rounding mode and back: three of them per pair took 2 to 10 us a call, by where the code lies)
+    uint64_t mantissa;
+    uint16_t exponent;
+    std::memcpy(&mantissa, &x, 8);
+    std::memcpy(&exponent, reinterpret_cast<const char*>(&x) + 8, 2);
+    const int up = (int)exponent - 16382;
+    return up >= 0 ? (up < 64 ? mantissa << up : 0) : up > -64 ? mantissa >> -up : 0;
 }
 
 // Phase step of RoPE pair i: omega_i / 2pi revolutions per position as a 64-bit
