@@ -628,7 +628,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
     constexpr int TK = kBlock, NW = kTreeWaves, NST = Keys::NST, PL = Keys::PL, HALF = D / 2;
     constexpr int PER = Keys::SE / NW;     // elements of a stage per wave
     static_assert(NST * Keys::SE * 2 >= NW * CB * DB * 64 * 16, "the outputs meet in the stages");
-    static_assert(PER * 2 >= 16 * HALF * 8 && PER * 2 >= KD * 64 * 16, "queries pass through a stage");
+    static_assert(PER * 2 >= KD * 64 * 16, "queries pass through a stage");
 
     __shared__ TreeLds<D, false> lds;
     __shared__ float2 mls[NW][16 * CB];
@@ -649,54 +649,62 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
         if (u < nt) keys.issue(u, u, keys.blocks_of(u));
     keys.fill_steps(a);
 
-    // ---- queries: wave cb turns rows 16 cb .. 16 cb + 15 and passes them to the others through
-    // the stage that is filled last.  The cos/sin of their tokens (a token's heads share them) go
-    // the same way before.
+    // ---- queries: a wave turns 2 CB rows, LPR lanes a row, and passes them to the others through the
+    // stage that is filled last
     int toff[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
         const int row = row_lo + 16 * cb + c16;
         toff[cb] = row < rows_total ? row / G : 0;
     }
-    __syncthreads();  // phase steps staged
-    if (wave < CB) {
-        uint16_t* spare = lds.stages + (NST - 1) * Keys::SE + wave * PER;
-        const int row0 = row_lo + 16 * wave, row = row0 + c16;
+    {
+        constexpr int LPR = 32 / CB, PP = HALF / LPR;   // lanes of a row, pairs of a lane
+        static_assert(NW * 64 == 16 * CB * LPR, "every lane has a part of a row");
+        typedef uint16_t part_t __attribute__((ext_vector_type(PP)));
+        const int r = (wave * 64 + lane) / LPR, p0 = lane % LPR * PP, row = row_lo + r;
         const bool valid = row < rows_total;
         const int to = valid ? row / G : 0, hl = valid ? row - to * G : 0;
+        // two runs of PP elements: NeoX the pairs' x and y, GPT-J one after the other
+        const int e[2] = {STYLE == kNeox ? p0 : 2 * p0, STYLE == kNeox ? p0 + HALF : 2 * p0 + PP};
         const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + to) * a.hq + (size_t)ic.kvh * G + hl) * D;
-        u32x4_t raw[KD];
+        part_t x[2];
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) {
-            raw[kd] = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, kd * 4 + q4) * 8);
-            if (!valid) raw[kd] = u32x4_t{0, 0, 0, 0};
-        }
+        for (int h = 0; h < 2; ++h) x[h] = *reinterpret_cast<const part_t*>(qp + model_chunk(a.chunk_map, e[h] >> 3) * 8 + (e[h] & 7));
+        const int32_t pos = ROPE ? a.positions[g.pos_off + g.tok0 + to] : 0;
+        __syncthreads();  // phase steps staged
+        float f[2 * PP];
+#pragma unroll
+        for (int i = 0; i < 2 * PP; ++i) f[i] = valid ? __uint_as_float((uint32_t)x[i / PP][i % PP] << 16) : 0.f;
         float scale = a.scale_log2;
         if (ROPE) {
-            const int t0 = min(row0, rows_total - 1) / G, t1 = min(row0 + 15, rows_total - 1) / G;
-            float2* cs = reinterpret_cast<float2*>(spare);
-            token_angles<HALF>(a, g, lds.fstep, lane, t0, t1, cs);
-            float xf[KD][8];
+            float big = 0.f;
 #pragma unroll
-            for (int kd = 0; kd < KD; ++kd)
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    xf[kd][2 * m] = bf_lo(raw[kd][m]);
-                    xf[kd][2 * m + 1] = bf_hi(raw[kd][m]);
-                }
-            float big = turn_row<STYLE, KD>(xf, cs + (valid ? to - t0 : 0) * HALF, q4, 4);
-            big = max_xor32(max_xor16(big));
+            for (int i = 0; i < PP; ++i) {
+                float c, s;
+                rope_cs_fast(pos, lds.fstep[p0 + i], c, s);
+                float& u = STYLE == kNeox ? f[i] : f[2 * i];
+                float& v = STYLE == kNeox ? f[PP + i] : f[2 * i + 1];
+                const float u0 = u, v0 = v;
+                u = u0 * c - v0 * s;
+                v = v0 * c + u0 * s;
+                big = fmaxf(big, fmaxf(fabsf(u), fabsf(v)));
+            }
+            big = max_of8(big);
+            big = fmaxf(big, __shfl_xor(big, 8));
+            if (LPR == 32) big = max_xor16(big);
             const int ex = query_exponent(big);
             scale = back_scale(scale, ex);
 #pragma unroll
-            for (int kd = 0; kd < KD; ++kd)
-#pragma unroll
-                for (int m = 0; m < 4; ++m) raw[kd][m] = pack_f16(ldexpf(xf[kd][2 * m], -ex), ldexpf(xf[kd][2 * m + 1], -ex));
+            for (int i = 0; i < 2 * PP; ++i) x[i / PP][i % PP] = __builtin_bit_cast(uint16_t, (_Float16)ldexpf(f[i], -ex));
+        } else if (!valid) {
+            x[0] = x[1] = part_t(0);
         }
-        __atomic_signal_fence(__ATOMIC_SEQ_CST);   // the cos/sin have been read
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) reinterpret_cast<u32x4_t*>(spare)[kd * 64 + lane] = raw[kd];
-        if (q4 == 0) qsl[16 * wave + c16] = scale;
+        for (int h = 0; h < 2; ++h) {
+            const int k = e[h] >> 3;   // chunk: of the lanes 16 (k % 4) + row of step k / 4
+            *reinterpret_cast<part_t*>(lds.stages + (NST - 1) * Keys::SE + (r >> 4) * PER + ((k >> 2) * 64 + (k & 3) * 16 + (r & 15)) * 8 + (e[h] & 7)) = x[h];
+        }
+        if (lane % LPR == 0) qsl[r] = scale;
     }
     if (ROPE && nt > 0) {   // the first tile's angles, while its keys come
         keys.template wait_first<NST - 1>();
