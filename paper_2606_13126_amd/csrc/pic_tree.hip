@@ -617,8 +617,8 @@ __device__ __forceinline__ float back_scale(float scale, int ex) { return fmaxf(
 // After the scores lane l holds row l%16 of each block and keys 4 (l/16) + {0..3}, the B
 // operand of the output product.
 // With keys of their own bound by memory (32 requests of 8 tokens over 8,192 keys, 8 KV heads of
-// 128: 198 us, 5.5 TB/s; the vector unit, which turns the keys, is busy 48%, the matrix cores
-// 11%), with few keys by an item's start: 6.4 us with 16 rows, 7.4 with 32, and 1.5 or 1.7 per step.
+// 128: 196 us, 5.5 TB/s; the vector unit, which turns the keys, is busy 48%, the matrix cores
+// 11%), with few keys by an item's start: about 6 us with 16 rows, 7 with 32, and 1.5 or 1.7 per step.
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, bool ROPE, int CB, int NG>
 __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> plan, const TreeArgs a) {
