@@ -746,3 +746,47 @@ def test_calls_on_two_streams_and_repeats_agree():
     torch.cuda.synchronize()
     for oa, ob in outs:
         assert torch.equal(oa, ra) and torch.equal(ob, rb)
+
+
+def test_attn_tree_float32_in_a_small_workspace():
+    """Without room for partial results float32 keys stay unsplit: the same sums in another order."""
+    for lens in ([(700, 5)], [(900, 30), (64, 3)]):
+        b = Drafts(lens, 8, 2, 64, torch.float32, seed=7)
+        for ws in (torch.empty(0, dtype=torch.uint8, device="cuda"), torch.empty(256, dtype=torch.uint8, device="cuda")):
+            assert b.ws.numel() > ws.numel()
+            b.check(b.run(ws=ws), "small workspace")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attn_tree_reads_no_table_entry_past_a_request(dtype):
+    """Entries behind a request's blocks may hold anything."""
+    for n in (3, 40):
+        b = Drafts([(333, n), (20, 2), (0, n)], 8, 2, 128, dtype, seed=n)
+        o = b.run()
+        table = b.table.copy()
+        for r, (ctx, m, w) in enumerate(b.lens):
+            table[r, -(-(ctx + m) // 16):] = [1 << 30, -1][r % 2]
+        wide = np.full((len(b.lens), table.shape[1] + 3), -5, np.int32)
+        wide[:, :table.shape[1]] = table
+        b.block_tables = dev(wide)
+        assert torch.equal(b.run(), o)
+
+
+def test_many_requests_captured_and_replayed():
+    """More spans than the kernel arguments hold: the captured call uploads its plan on every replay."""
+    rng = np.random.default_rng(11)
+    b = Drafts([(int(rng.integers(1, 300)), int(rng.integers(1, 20))) for _ in range(80)], 8, 2, 64, seed=12)
+    other = Drafts([(int(rng.integers(1, 300)), int(rng.integers(1, 9))) for _ in range(90)], 8, 2, 64, seed=13)
+    ref, ref_other = b.run(), other.run()
+    torch.cuda.synchronize()
+    o = torch.zeros_like(ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.run(o=o, stream=torch.cuda.current_stream())
+    for _ in range(4):
+        o.zero_()
+        b.ws.fill_(255)
+        graph.replay()
+        assert torch.equal(other.run(), ref_other)
+        torch.cuda.synchronize()
+        assert torch.equal(o, ref)
