@@ -958,8 +958,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
         if (u < nt) keys.issue(u, u, keys.blocks_of(u));
     keys.fill_steps(a);
 
-    // ---- queries, 16 rows after the other, so that the cos/sin of their tokens (a token's heads
-    // share them) fit in the wave's part of the stages filled last
+    // ---- queries.  The cos/sin of their tokens (a token's heads share them) go through the wave's
+    // part of the stages filled last, which holds 16 tokens: more take two times 16 rows.
     const int row = row_lo + l32;
     const bool valid = row < rows_total;
     const int toff = valid ? row / G : 0, hl = valid ? row - toff * G : 0;
@@ -984,12 +984,13 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
                     xf[kd][2 * m] = bf_lo(raw[kd][m]);
                     xf[kd][2 * m + 1] = bf_hi(raw[kd][m]);
                 }
+            const int each = min(row_lo + 31, rows_total - 1) / G - min(row_lo, rows_total - 1) / G < 16 ? 32 : 16;
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const int row0 = row_lo + 16 * h;
-                const int t0 = min(row0, rows_total - 1) / G, t1 = min(row0 + 15, rows_total - 1) / G;
+            for (int h = 0; h < 32; h += each) {
+                const int row0 = row_lo + h;
+                const int t0 = min(row0, rows_total - 1) / G, t1 = min(row0 + each - 1, rows_total - 1) / G;
                 token_angles<HALF>(a, g, lds.fstep, lane, t0, t1, cs);
-                if (l32 >> 4 == h) big = turn_row<STYLE, KD>(xf, cs + (valid ? toff - t0 : 0) * HALF, hi, 2);
+                if (l32 >= h && l32 < h + each) big = turn_row<STYLE, KD>(xf, cs + (valid ? toff - t0 : 0) * HALF, hi, 2);
                 __atomic_signal_fence(__ATOMIC_SEQ_CST);
             }
             const int ex = query_exponent(max_xor32(big));
