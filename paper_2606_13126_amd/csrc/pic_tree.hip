@@ -627,7 +627,8 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
     constexpr int DB = D / 16;             // 16-dim blocks of O^T
     constexpr int TK = kBlock, NW = kTreeWaves, NST = Keys::NST, PL = Keys::PL, HALF = D / 2;
     constexpr int PER = Keys::SE / NW;     // elements of a stage per wave
-    static_assert(NST * Keys::SE * 2 >= NW * CB * DB * 64 * 16, "the outputs meet in the stages");
+    constexpr int PPT = TK * D / 512;      // a wave's outputs of 16 x 16 in the place of a tile of K or V
+    static_assert(NST * 2 * PPT >= CB * DB, "the outputs meet in the stages");
     static_assert(PER * 2 >= KD * 64 * 16, "queries pass through a stage");
 
     __shared__ TreeLds<D, false> lds;
@@ -648,6 +649,19 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
     for (int u = 0; u < NST - 1; ++u)
         if (u < nt) keys.issue(u, u, keys.blocks_of(u));
     keys.fill_steps(a);
+
+    // per-lane element offsets within a tile: K operand rows and V^T operand rows
+    int k_off[KD], v_off[DB];
+#pragma unroll
+    for (int kd = 0; kd < KD; ++kd) k_off[kd] = c16 * D + ((model_chunk(a.chunk_map, kd * 4 + q4) ^ dswz<D>(c16)) << 3);
+    {
+        const int key = 4 * q4 + (c16 >> 2);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            const int d = db * 16 + 4 * (lane & 3);
+            v_off[db] = key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7);
+        }
+    }
 
     // ---- queries: a wave turns 2 CB rows, LPR lanes a row, and passes them to the others through the
     // stage that is filled last
@@ -730,19 +744,6 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
         l_run[cb] = 0.f;
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[cb][db] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    }
-
-    // per-lane element offsets within a tile: K operand rows and V^T operand rows
-    int k_off[KD], v_off[DB];
-#pragma unroll
-    for (int kd = 0; kd < KD; ++kd) k_off[kd] = c16 * D + ((model_chunk(a.chunk_map, kd * 4 + q4) ^ dswz<D>(c16)) << 3);
-    {
-        const int key = 4 * q4 + (c16 >> 2);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const int d = db * 16 + 4 * (lane & 3);
-            v_off[db] = key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7);
-        }
     }
 
     int st = 0;
@@ -863,51 +864,49 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
         st = keys.next(st);
     }
 
-    // ---- the waves' results meet: rows by their common maximum, outputs through the stages
+    // ---- the waves' results meet: a wave leaves its rows' maxima, sums and outputs (in its own part of
+    // the stages, which no other wave reads before), then wave db joins dims 16 db .. 16 db + 15
+    const auto piece = [&](int w, int i) {
+        const int r = i / PPT;   // K of stage 0, V of stage 0, K of stage 1 ..
+        return reinterpret_cast<f32x4_t*>(lds.stages + r / 2 * Keys::SE + r % 2 * Keys::KV + w * TK * D) + i % PPT * 64 + lane;
+    };
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
         const float l = sum_xor32(sum_xor16(l_run[cb]));
         if (q4 == 0) mls[wave][16 * cb + c16] = make_float2(m_run[cb], l);
-    }
-    __syncthreads();   // (every wave's copies have landed and been read)
-    float M[CB], den[CB];
-    f32x4_t* meet = reinterpret_cast<f32x4_t*>(lds.stages);
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        float2 w[NW];
-        M[cb] = kNegBig;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            w[i] = mls[i][16 * cb + c16];
-            M[cb] = fmaxf(M[cb], w[i].x);
-        }
-        den[cb] = 0.f;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) den[cb] += w[i].y * __builtin_amdgcn_exp2f(w[i].x - M[cb]);
-        const float mine = __builtin_amdgcn_exp2f(m_run[cb] - M[cb]);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) meet[((wave * CB + cb) * DB + db) * 64 + lane] = acc[cb][db] * mine;
+        for (int db = 0; db < DB; ++db) *piece(wave, cb * DB + db) = acc[cb][db];
     }
     if (noted)
 #pragma unroll 1
-        for (int i = 0; i < CB * DB; ++i) {
-            f32x4_t* at = meet + (wave * CB * DB + i) * 64 + lane;
-            *at = with_infs(*at, infs[wave][i][lane]);
-        }
+        for (int i = 0; i < CB * DB; ++i) *piece(wave, i) = with_infs(*piece(wave, i), infs[wave][i][lane]);
     __syncthreads();
     const size_t prow0 = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + ic.rt) * (16 * CB);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
         const int row = row_lo + 16 * cb + c16, db = wave;
         if (row >= rows_total || db >= DB) continue;
-        f32x4_t x = meet[(cb * DB + db) * 64 + lane];
+        float2 w[NW];
+        f32x4_t part[NW];
+        float M = kNegBig, den = 0.f;
 #pragma unroll
-        for (int w = 1; w < NW; ++w) x += meet[((w * CB + cb) * DB + db) * 64 + lane];
+        for (int i = 0; i < NW; ++i) {
+            w[i] = mls[i][16 * cb + c16];
+            part[i] = *piece(i, cb * DB + db);
+            M = fmaxf(M, w[i].x);
+        }
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const float f = __builtin_amdgcn_exp2f(w[i].x - M);
+            den += w[i].y * f;
+            x += part[i] * f;
+        }
         if (g.n_split > 1) {
             *reinterpret_cast<f32x4_t*>(a.part_o + (prow0 + 16 * cb + c16) * D + db * 16 + 4 * q4) = x;
-            if (wave == 0 && q4 == 0) *reinterpret_cast<float2*>(a.part_ml + (prow0 + 16 * cb + c16) * 2) = make_float2(M[cb], den[cb]);
+            if (wave == 0 && q4 == 0) *reinterpret_cast<float2*>(a.part_ml + (prow0 + 16 * cb + c16) * 2) = make_float2(M, den);
         } else {
-            const float inv = den[cb] == 0.f ? 0.f : 1.f / den[cb];   // (a drafted token may see nothing: its output is 0)
+            const float inv = den == 0.f ? 0.f : 1.f / den;   // (a drafted token may see nothing: its output is 0)
             const int hl = row - toff[cb] * G;
             uint16_t* op = static_cast<uint16_t*>(a.o) + ((size_t)(g.q_row0 + toff[cb]) * a.hq + (size_t)ic.kvh * G + hl) * D;
             *reinterpret_cast<u32x2_t*>(op + db * 16 + 4 * q4) = u32x2_t{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
