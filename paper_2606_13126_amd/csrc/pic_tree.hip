@@ -1243,10 +1243,13 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
 }
 
 // Joins key splits: one block per kMergeRows rows of a (row tile, KV head),
-// one float4 of a row per thread, eight splits' loads in flight.
-template <int D, int NG>
+// one float4 of a row per thread, U splits' loads in flight: 8 for row tiles of 16 or 32, of which
+// small calls have many splits, 4 for larger ones, many of 2 splits, for which the repeats of the
+// last count (U = 8 and 4: 8 tokens over 1,537 keys, 13 splits, 12.9 and 13.8 us, 1 over 20,000 20.2
+// and 21.9; 16 trees of 96 tokens of 64 heads, 2 splits, 593 and 584, 16 ragged trees 61.6 and 60.3).
+template <int D, int NG, int U>
 __global__ void __launch_bounds__(kMergeRows * D / 4) tree_merge(const PlanOf<NG> plan, const TreeMergeArgs a) {
-    constexpr int TPR = D / 4, U = 8;
+    constexpr int TPR = D / 4;
     const Group g = group_of<true>(plan, blockIdx.x);
     if (g.n_split <= 1) return;
     const int n_rt = g.n_rt, chunks = a.tile_rows / kMergeRows;
@@ -1297,7 +1300,9 @@ hipError_t launch_tree_n(const PlanOf<NG>& plan, const TreeArgs& a, hipStream_t 
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.n_merge == 0) return e;
     const TreeMergeArgs m = {a.part_o, a.part_ml, a.o, a.tile_rows, a.hq, a.hkv, a.group};
-    hipLaunchKernelGGL((tree_merge<D, NG>), dim3(plan.n_merge), dim3(kMergeRows * D / 4), 0, st, plan, m);
+    const dim3 merges(plan.n_merge), threads(kMergeRows * D / 4);
+    if (a.tile_rows <= 32) hipLaunchKernelGGL((tree_merge<D, NG, 8>), merges, threads, 0, st, plan, m);
+    else hipLaunchKernelGGL((tree_merge<D, NG, 4>), merges, threads, 0, st, plan, m);
     return hipGetLastError();
 }
 
