@@ -171,8 +171,8 @@ bool short_items(const pic_config* c, const HostPlan& hp) {
 // more than 1, 2, 3 or 4 items per compute unit (at least 128 keys); taken is what ends first
 // by the costs below.  They were fitted to 78,000 calls of 2,720 batches (1 to 48 requests
 // of 1 to 100 tokens over 100 to 24,000 keys, equal and ragged, 1 to 8 KV heads of 4 to 16 query
-// heads, D 128), which they describe within 8%.  On these batches the choice takes 1.04 times
-// the best of all tiles and splits (1.10 at the 90th percentile).  Tiles by the number of rows alone
+// heads, D 128), which they describe within 8%.  On 2,705 other batches the choice takes 1.03
+// times the best of all tiles and splits (1.10 at the 90th percentile).  Tiles by the number of rows alone
 // and splits of the average work per compute unit took 1.2 to 1.3 times (1.5): few tokens over
 // short contexts want small tiles, which fill the chip (a tree of 64 tokens, 256 rows, over 1,537
 // keys 19.9 us in tiles of 32, 30.9 in one), and a few items more than compute units end late (5
