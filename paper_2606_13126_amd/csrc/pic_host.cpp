@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <limits>
 #include <string>
 #include <vector>
 
@@ -571,7 +572,12 @@ pic_status build_plan_within(const pic_config* c, const pic_batch_host* b, Call 
     return st;
 }
 
-// The fraction of x (above its floor) as 64 binary digits, cut.
+// The fraction of x (above its floor) as 64 binary digits, cut.  The bytes of x are read: a 64-bit
+// mantissa, then 15 bits of exponent, as x86 keeps a long double.
+#ifndef __HIP_DEVICE_COMPILE__   // (the device's own is a double)
+static_assert(std::numeric_limits<long double>::digits == 64 && std::numeric_limits<long double>::max_exponent == 16384,
+              "phase steps need the 80-bit long double of x86");
+#endif
 uint64_t fraction64(long double x) {
     if (!(fabsl(x) < 9223372036854775808.0L)) return 0;   // no digits below 1 that far out
     if (x < 0.0L) {
