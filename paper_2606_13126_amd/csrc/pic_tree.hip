@@ -278,8 +278,10 @@ struct TreeShape {
     static constexpr int SE = 2 * KV;            // elements of a stage: K of every tile, then V
 };
 
+// (SHARED: stages begin at a multiple of a row, within which chunks are found by an exclusive or on
+// their addresses)
 template <int D, bool SHARED>
-struct __attribute__((aligned(16))) TreeLds {
+struct __attribute__((aligned(SHARED ? 2 * D : 16))) TreeLds {
     typedef TreeShape<D, SHARED> S;
     uint16_t stages[S::NST * S::SE];
     float2 stride_cs[S::HALF];           // cos/sin of STEP positions
