@@ -355,13 +355,18 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) {
 __device__ __forceinline__ void dma_lds16(const void* src, const void* lds_wave_base) {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds_offset(lds_wave_base)) : "memory");
 }
-// the same from a wave-uniform address plus a 32-bit byte offset per lane
+// from a wave-uniform address plus a 32-bit byte offset per lane, and four bytes a lane, to a
+// wave-uniform LDS byte address
+__device__ __forceinline__ void copy_lds16(const void* base, uint32_t off, uint32_t to) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(to) : "memory");
+}
+__device__ __forceinline__ void copy_lds4(const void* src, uint32_t to) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(to) : "memory");
+}
 __device__ __forceinline__ void dma_lds16_s(const void* base, uint32_t off, const void* lds_wave_base) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds_offset(lds_wave_base)) : "memory");
+    copy_lds16(base, off, lds_offset(lds_wave_base));
 }
-__device__ __forceinline__ void dma_lds4(const void* src, const void* lds_wave_base) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(lds_offset(lds_wave_base)) : "memory");
-}
+__device__ __forceinline__ void dma_lds4(const void* src, const void* lds_wave_base) { copy_lds4(src, lds_offset(lds_wave_base)); }
 
 // Workgroup barrier that leaves the vector-memory queue alone (__syncthreads
 // would also drain every outstanding global->LDS load): this wave's LDS writes are

@@ -254,14 +254,6 @@ __device__ __forceinline__ float max_of8(float x) {
     return dpp(Idx<0x141>{});   // lane ^ 7 (half rows mirrored)
 }
 
-// Global -> LDS copies (dma_lds4, dma_lds16_s) to a wave-uniform LDS byte address
-__device__ __forceinline__ void copy_lds4(const void* src, uint32_t to) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(to) : "memory");
-}
-__device__ __forceinline__ void copy_lds16(const void* base, uint32_t off, uint32_t to) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(to) : "memory");
-}
-
 // Sizes of the two kernels' steps (SHARED: tree_many)
 template <int D, bool SHARED>
 struct TreeShape {
