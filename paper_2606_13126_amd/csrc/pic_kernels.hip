@@ -1836,6 +1836,8 @@ typedef float f32x4v_t __attribute__((ext_vector_type(4)));
 //
 // TREE (AT = TreeArgs): the rows are drafted tokens; keys from the span's start on are seen
 // by the bits of the row's mask instead of by order, so every row tile runs to the span's end.
+// One-wave instances of D 128 need more than the 256 registers of two waves per SIMD (with a table or
+// computed angles 52 and 16 bytes of a lane would go to scratch memory, which no kernel here uses).
 template <int D, int STYLE, bool ROPE, bool TABLE, int NW, typename AT>
 __global__ void __launch_bounds__(NW * 64, (NW == 1 && std::is_same<AT, TreeArgs>::value ? 1 : 2)) attn_f32(const Plan plan, const AT a) {
     constexpr bool TREE = std::is_same<AT, TreeArgs>::value;

@@ -632,8 +632,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
 
     const Group g = group_of<false>(plan, blockIdx.x);
     const int G = a.group, n_rt = g.n_rt;
-    const int li = blockIdx.x - g.item_base;
-    if (li >= a.hkv * g.n_split * n_rt) return;
+    const int li = blockIdx.x - g.item_base;   // (a call's items are not padded: below the group's count)
     const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
     const int rows_total = g.n_tok * G, row_lo = ic.rt * 16 * CB;
     Keys keys(lds, a, g, ic);
@@ -939,8 +938,7 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG>
 
     const Group g = group_of<false>(plan, blockIdx.x);
     const int G = a.group, n_rt = g.n_rt;
-    const int li = blockIdx.x - g.item_base;
-    if (li >= a.hkv * g.n_split * n_rt) return;
+    const int li = blockIdx.x - g.item_base;   // (a call's items are not padded: below the group's count)
     const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
     Keys keys(lds, a, g, ic);
     const int lane = keys.lane, wave = keys.wave, nt = keys.nt;
@@ -1245,10 +1243,8 @@ template <int D, int NG, int U>
 __global__ void __launch_bounds__(kMergeRows * D / 4) tree_merge(const PlanOf<NG> plan, const TreeMergeArgs a) {
     constexpr int TPR = D / 4;
     const Group g = group_of<true>(plan, blockIdx.x);
-    if (g.n_split <= 1) return;
     const int n_rt = g.n_rt, chunks = a.tile_rows / kMergeRows;
-    int li = blockIdx.x - g.merge_base;
-    if (li >= a.hkv * n_rt * chunks) return;
+    int li = blockIdx.x - g.merge_base;   // (only groups with splits have blocks here, and no more than they need)
     const int r = (li % chunks) * kMergeRows + (int)threadIdx.x / TPR, c4 = (int)threadIdx.x % TPR;
     li /= chunks;
     const int kvh = li / n_rt, rt = li - kvh * n_rt, G = a.group;
