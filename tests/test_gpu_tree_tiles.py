@@ -83,7 +83,7 @@ class Tiled(G.Drafts):
             if self.edges <= r < len(self.lens) - 2:
                 row, off = row + n, off + L
                 continue
-            pick = np.arange(n) if r < self.edges else np.unique(np.r_[0, n // 3, n - 2, n - 1])
+            pick = np.arange(n) if r < self.edges else np.unique(np.r_[0, n // 3, max(0, n - 2), n - 1])
             j = torch.arange(w, L, device="cuda")
             blk = torch.from_numpy(self.table[r].astype(np.int64)).cuda()[j // 16]
             k, v = (G.f64(p[blk, :, j % 16]) for p in (self.k_pool, self.v_pool))
@@ -127,6 +127,22 @@ def test_lengths(tile, hq, hkv, d):
     for i, ctx in enumerate((0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 700)):
         b = Tiled([(ctx, n) for n in nodes], tile, None, hq, hkv, d, style=i % 2, seed=ctx)
         b.check(b.run(), f"tile {tile} ctx {ctx}")
+
+
+@pytest.mark.parametrize("tile", [None] + TILES)
+@pytest.mark.parametrize("hq,hkv,d", [(8, 8, 64), (24, 8, 128), (32, 16, 64), (5, 1, 128), (128, 1, 64), (12, 12, 128)])
+def test_heads(tile, hq, hkv, d):
+    """Every way of laying a span's workgroups out over the dies (8 KV heads, 8 key splits, neither)."""
+    g = hq // hkv
+    edges = [(2500, 40 // g + 1), (130, 1), (700, 130 // g + 1), (3000, max(1, 16 // g), 1001), (0, 2)]
+    if tile is not None:
+        b = Tiled(edges, tile, None, hq, hkv, d, seed=hq)
+        b.check(b.run(), f"tile {tile}")
+        return
+    for dtype in (torch.bfloat16, torch.float32):   # (as the call itself chooses)
+        for lens in (edges, edges[:1]):
+            b = G.Drafts(lens, hq, hkv, d, dtype, seed=hq)
+            b.check(b.run(), str(dtype))
 
 
 @pytest.mark.parametrize("tile", TILES)
