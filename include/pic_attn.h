@@ -258,8 +258,9 @@ pic_status pic_attn_decode_noalloc(const pic_config* cfg, const pic_batch_host* 
  *  q_out        DEVICE [n][Hq][D], dense; may be q itself if that is dense, else it must not
  *               overlap q, k_new or v_new.
  * Strides are at least a row and multiples of 16 bytes: the three inputs may be slices of one
- * fused output.  cos/sin come from the exact phase, computed once per row and pair for all
- * heads in float32; results are rounded once to cfg->dtype.  n < 2^24 per call. */
+ * fused output.  cos/sin come from the exact phase rounded to 24 bits (angles within 2^-21), computed
+ * once per row and pair for all heads in float32; results are rounded once to cfg->dtype.
+ * n < 2^24 per call. */
 pic_status pic_kv_append(const pic_config* cfg, void* k_pool, void* v_pool, int32_t num_blocks, const void* q,
                          int64_t q_stride, void* q_out, const void* k_new, int64_t k_stride, const void* v_new,
                          int64_t v_stride, const int32_t* positions, const int32_t* slot_mapping, int32_t n,
@@ -291,6 +292,15 @@ pic_status pic_tree_workspace_size(const pic_config* cfg, const pic_batch_host* 
  * (its own bit included: a token sees itself only if its mask says so; bits past the span are
  * ignored).  A token that sees nothing gets zeros.  Keys and values of tokens that a query
  * does not see, infinities and NaN included, do not change its output.
+ * How exact: float32 calls compute in float32.  In bf16 sums and softmax statistics are float32, and
+ * besides the result's own rounding
+ *  - turned keys and queries are rounded to 11 bits (exact without rotation), at angles within 2^-17:
+ *    those of a run of positions advance from one another, so that also at position 0 a sine is 0 up
+ *    to that only;
+ *  - probabilities have 16 bits where a call's trees have few rows (tokens x query heads of a KV head)
+ *    and 8 bits, as in prefill, where they have many; the choice is the call's, by its shapes.
+ *  Outputs of normally distributed inputs are off by 1.7e-3 of their norm, as by their rounding alone,
+ *  or 2.4e-3.
  *  rope      read in float32 only: in bf16 cos/sin are computed, whether a table is given or not;
  *  tree_mask DEVICE [total_q][mask_words], 8-byte aligned; mask_words * 64 must be at least
  *            every query span's length. */

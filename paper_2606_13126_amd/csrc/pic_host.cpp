@@ -167,17 +167,20 @@ bool short_items(const pic_config* c, const HostPlan& hp) {
 }
 
 // Row tiles and key splits of a call with drafted tokens in bf16.  A compute unit holds one
-// workgroup, and an item costs a start and its steps (of 128 keys with 16 or 32 query rows, of
-// 64 with 128 or 256).  Per tile, looked at are no splits and the longest splits that make no
+// workgroup at head_dim 128, and an item costs a start and its steps (of 128 keys with 16 or 32 query
+// rows, of 64 with 128 or 256).  Per tile, looked at are no splits and the longest splits that make no
 // more than 1, 2, 3 or 4 items per compute unit (at least 128 keys); taken is what ends first
 // by the costs below.  They were fitted to 78,000 calls of 2,720 batches (1 to 48 requests
 // of 1 to 100 tokens over 100 to 24,000 keys, equal and ragged, 1 to 8 KV heads of 4 to 16 query
-// heads, D 128), which they describe within 8%.  On 2,705 other batches the choice takes 1.03
-// times the best of all tiles and splits (1.10 at the 90th percentile).  Tiles by the number of rows alone
-// and splits of the average work per compute unit took 1.2 to 1.3 times (1.5): few tokens over
-// short contexts want small tiles, which fill the chip (a tree of 64 tokens, 256 rows, over 1,537
-// keys 19.9 us in tiles of 32, 30.9 in one), and a few items more than compute units end late (5
-// trees of 16 over 30,000 keys 148 us against 222).
+// heads, D 128, keys turned in the call), which they describe within 8%.  On 2,705 other batches the
+// choice takes 1.03 times the best of all tiles and splits (1.10 at the 90th percentile).  Tiles by
+// the number of rows alone and splits of the average work per compute unit took 1.2 to 1.3 times (1.5):
+// few tokens over short contexts want small tiles, which fill the chip (a tree of 64 tokens, 256 rows,
+// over 1,537 keys 19.9 us in tiles of 32, 30.9 in one), and a few items more than compute units end late
+// (5 trees of 16 over 30,000 keys 148 us against 222).
+// For head_dim 64 and for keys turned before the call the same costs are taken, not measured: steps are
+// cheaper there, and two workgroups of tree_many fit a compute unit at head_dim 64 without rotation, and
+// with GPT-J pairs in tiles of 128.
 struct TreeSplit {
     int tile = 0;
     int64_t chunk = 0;    // steps per split

@@ -24,7 +24,10 @@ typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
 // thread's units lie on the same pairs of different heads, so it computes their cos/sin
 // once, in float32 from the exact phase.  Bound by memory: every element is read once and
 // written once, four units (128 bytes) of a thread in flight.  16,384 rows of 64 + 2 x 8 heads of
-// 128 (671 MB) 121 us, 5.5 TB/s (a copy of 2 GiB 4.9); 528 rows of 32 + 2 x 8 (13 MB) 5.9 us.
+// 128 (671 MB) 121 us, 5.5 TB/s (a copy of 2 GiB 4.9); 8,192 such rows in float32 125 us, and 16,384
+// that do not turn 124.  Few rows are bound by latency: the slot, which only the stores need, is waited
+// for before a row is read, and the position asked for after it: 528 rows of 32 + 2 x 8 (13 MB) 5.4
+// to 5.8 us, 2.6 at the copy's rate.
 // ---------------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
 
@@ -611,8 +614,8 @@ __device__ __forceinline__ float back_scale(float scale, int ex) { return fmaxf(
 // After the scores lane l holds row l%16 of each block and keys 4 (l/16) + {0..3}, the B
 // operand of the output product.
 // With keys of their own bound by memory (32 requests of 8 tokens over 8,192 keys, 8 KV heads of
-// 128: 196 us, 5.5 TB/s; the vector unit, which turns the keys, is busy 48%, the matrix cores
-// 11%), with few keys by an item's start: about 6 us with 16 rows, 7 with 32, and 1.5 or 1.7 per step.
+// 128: 191 to 196 us, 5.5 to 5.6 TB/s; the vector unit, which turns the keys, is busy 45%, the matrix
+// cores 11%), with few keys by an item's start: about 6 us with 16 rows, 7 with 32, and 1.5 or 1.7 per step.
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, bool ROPE, int CB, int NG>
 __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> plan, const TreeArgs a) {
@@ -916,10 +919,12 @@ __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_few(const PlanOf<NG> 
 // After the scores lane l holds row l%32 and keys 8 (j/4) + 4 (l/32) + j%4, the B operand of
 // the output product.  A wave turns its
 // keys of the next step beside the products of the scores.
-// Bound by power: matrix cores busy 34%, vector unit 45%, at a clock of 1.75 to 1.95 GHz (32 requests
-// of 64 tokens of 32 heads over 8,192 keys 388 to 440 us, 625 to 708 TFLOP/s; keys turned already
-// 311 to 358).  Half a step between the two waves of a SIMD, so that one's products
-// run beside the other's softmax, changed nothing (387 against 388 us).
+// Bound by products and vector work that hardly overlap, although a SIMD has two waves: matrix cores
+// busy 35% of the cycles and the vector unit 42% (keys turned already: 49% and 27%), 77% in all; a
+// wave waits for data or the others a third of its time, and for its turn 22% (30%).  The clock is
+// 1.75 to 2.0 GHz.  32 requests of 64 tokens of 32 heads over 8,192 keys 376 to 440 us by the card, 625
+// to 730 TFLOP/s; keys turned already 302 to 358.  Half a step between the two waves of a SIMD, so
+// that one's products run beside the other's softmax, changed nothing (387 against 388 us).
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, bool ROPE, int WR, int NG>
 __global__ void __launch_bounds__(kTreeWaves * 64, 2) tree_many(const PlanOf<NG> plan, const TreeArgs a) {
