@@ -178,9 +178,11 @@ bool short_items(const pic_config* c, const HostPlan& hp) {
 // few tokens over short contexts want small tiles, which fill the chip (a tree of 64 tokens, 256 rows,
 // over 1,537 keys 19.9 us in tiles of 32, 30.9 in one), and a few items more than compute units end late
 // (5 trees of 16 over 30,000 keys 148 us against 222).
-// For head_dim 64 and for keys turned before the call the same costs are taken, not measured: steps are
-// cheaper there, and two workgroups of tree_many fit a compute unit at head_dim 64 without rotation, and
-// with GPT-J pairs in tiles of 128.
+// The same costs serve head_dim 64 and keys turned before the call, where steps are cheaper and where two
+// workgroups of tree_many fit a compute unit (head_dim 64 without rotation, and with GPT-J pairs in tiles
+// of 128).  On batches of the same ranges the choice takes there, times the best of the four tiles and of
+// splits from 128 keys on, in the mean and at the 90th percentile: D 128 1.02 and 1.06 (1,360 batches), on
+// turned keys 1.05 and 1.16 (1,915); D 64 1.02 and 1.07 (1,866), on turned keys 1.07 and 1.21 (2,602).
 struct TreeSplit {
     int tile = 0;
     int64_t chunk = 0;    // steps per split
