@@ -322,6 +322,93 @@ pic_status pic_kv_keep(const pic_config* cfg, void* k_pool, void* v_pool, int32_
                        const int32_t* slot_mapping, const int32_t* cu_rows, int32_t n_trees, int32_t total_rows,
                        const int32_t* path, int32_t max_path, const int32_t* path_len, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * A cache held in 8 bits.  A pool of codes, one byte per element, in the layout of the other pools, with
+ * one scale for the keys and one for the values of every block and KV head: an element is its code times
+ * its scale.  Keys are unrotated or rotated as cfg->k_prerotated says (unrotated, a block and its scale
+ * serve any position).  A step normalises its projection's queries and keys where the model does
+ * (pic_qk_norm), stores keys and values (pic_kv8_write) and attends (pic_attn8_prefill,
+ * pic_attn8_decode); pic_kv8_read returns rows as numbers.  cfg->dtype is the type of q, o and of rows;
+ * the pool's is pool->code.
+ * ---------------------------------------------------------------------------------- */
+#define PIC_KV8_E4M3 0 /* OCP e4m3: 3 bits behind the first, largest 448, no infinities */
+#define PIC_KV8_INT8 1 /* signed integers -127 .. 127 */
+
+typedef struct pic_kv8_pool {
+    void* k;            /* DEVICE [num_blocks][Hkv][16][D] codes */
+    void* v;            /* DEVICE [num_blocks][Hkv][16][D] codes */
+    float* scale;       /* DEVICE [num_blocks][Hkv][2]: of the block's keys and of its values, 8-byte aligned.
+                           pic_kv8_write's are powers of two; the readers take any finite scale >= 0 (so also
+                           codes that another program quantised).  Codes are numbers: not e4m3's NaN. */
+    int32_t num_blocks;
+    int32_t code;       /* PIC_KV8_E4M3 or PIC_KV8_INT8 */
+} pic_kv8_pool;
+
+/* Root-mean-square norm of every query and key head, and the position rotation in the same pass:
+ *   q_out[i][h] <- R_p (q[i][h] / sqrt(mean(q[i][h]^2) + eps) * q_weight), the same of k,
+ * with R_p, p = positions[i], where cfg->k_prerotated = 1 (the pool holds turned keys); with
+ * k_prerotated = 0 nothing turns (attention turns) and positions may be NULL.
+ *  q, k       DEVICE rows of [Hq][D] / [Hkv][D] dense elements, row i at i * stride elements: they may be
+ *             slices of one fused output.  q may be NULL together with q_out, or k with k_out.
+ *  q_out, k_out  DEVICE rows likewise; either may be its own input (same address and stride), else it
+ *             must share no memory with an input or the other output.
+ *  q_weight, k_weight  DEVICE [D] in cfg->dtype, or NULL (ones).
+ * Strides are at least a row and multiples of 16 bytes.  Computed in float32 and rounded once to
+ * cfg->dtype; a row's squares are summed in float32 (elements of 2^60 and more may pass its range).  cos/sin are
+ * those of pic_kv_append.  eps > 0, n < 2^24 per call. */
+pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                       const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, const void* q_weight,
+                       const void* k_weight, float eps, const int32_t* positions, int32_t n, void* stream);
+
+/* Quantise key and value rows into the pool.  Row i < n goes to slot slot_mapping[i] (block slot / 16,
+ * offset slot % 16), all KV heads; slots below 0 or at num_blocks * 16 and above store nothing.  Per
+ * block, head, and keys or values, with M the code's largest number (448 or 127):
+ *  - the rows' scale is the smallest power of two s with max|x| <= M s, the maximum over the finite
+ *    elements that the call stores there (2^-126 at least; at most 2^119 (e4m3) or 2^121 (int8), past which
+ *    elements saturate);
+ *  - a call that stores the block's offset 0 starts the block: s becomes its scale and its other rows,
+ *    unless the call stores them too, become 0.  Any other call keeps the block's rows, and its scale becomes
+ *    max(s, the scale that it had): where it grows, the rows kept are rounded to it once more
+ *    (after any number of growths an element of a row is off by less than one step of the last scale);
+ *  - an element's code is x / s rounded to nearest, ties to even (off by at most half a step;
+ *    exactly x times the float32 reciprocal of s, which for a power of two is the same); infinities
+ *    become the largest number of their sign and a NaN 0.
+ * Rows of one block must follow one another in the call (a request's tokens in order do; a row of another
+ * block or a padding row between them makes the call a race); of rows of one slot the last counts.  A block that is
+ * not started by its offset 0 needs a scale in the pool: 0 where nothing was stored before.
+ *  k_new, v_new  DEVICE rows of [Hkv][D] dense elements of cfg->dtype, row i at i * stride elements
+ *                (strides as in pic_kv_append).
+ * n < 2^24 per call. */
+pic_status pic_kv8_write(const pic_config* cfg, const pic_kv8_pool* pool, const void* k_new, int64_t k_stride,
+                         const void* v_new, int64_t v_stride, const int32_t* slot_mapping, int32_t n, void* stream);
+
+/* Rows of the pool as numbers: k_out[i][h][:], v_out[i][h][:] (DEVICE [n][Hkv][D], cfg->dtype) <- code times
+ * scale of slot slot_mapping[i], rounded once to cfg->dtype (exact for pic_kv8_write's scales).  Rows whose slot lies
+ * outside the pool are left as they are.  The outputs must not overlap the pool.  n < 2^24 per call. */
+pic_status pic_kv8_read(const pic_config* cfg, const pic_kv8_pool* pool, const int32_t* slot_mapping, int32_t n,
+                        void* k_out, void* v_out, void* stream);
+
+/* Workspace bytes of pic_attn8_prefill (is_decode = 0) or pic_attn8_decode (1) for this batch, as
+ * pic_workspace_size (float32 partial results are optional). */
+pic_status pic_attn8_workspace_size(const pic_config* cfg, const pic_batch_host* batch, int32_t is_decode, size_t* bytes);
+
+/* pic_attn_prefill and pic_attn_decode over a pool of 8-bit codes: the same batch, masks, q, o and
+ * workspace rules.  cos/sin are computed in the kernel (no table).
+ * How exact: codes and scales enter exactly; sums and softmax statistics are float32.  float32 calls compute in
+ * float32.  In bf16, besides the result's own rounding: turned queries are rounded to 11 bits; cos/sin of keys, their
+ * products and the turned keys to 11 bits each, at angles within 2^-17 (as in pic_attn_tree); without
+ * rotation both are exact; probabilities (times their block's scale of values) have 16 bits where a call's row tiles
+ * hold at most 32 rows (query tokens x query heads of a KV head) and 8 bits where they hold more.
+ * Values times 2^8 must stay within float32. */
+pic_status pic_attn8_prefill(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev, const void* q,
+                             void* o, const pic_kv8_pool* pool, void* workspace, size_t workspace_bytes, void* stream);
+pic_status pic_attn8_decode(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev, const void* q,
+                            void* o, const pic_kv8_pool* pool, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Test hook: pic_plan_debug of a pic_attn8_prefill or pic_attn8_decode call. */
+pic_status pic_attn8_plan_debug(const pic_config* cfg, const pic_batch_host* batch, int32_t is_decode, int32_t* items,
+                                int32_t capacity, int32_t* n_items);
+
 /* Test hook: pic_plan_debug of a pic_attn_tree call. */
 pic_status pic_tree_plan_debug(const pic_config* cfg, const pic_batch_host* batch, int32_t* items, int32_t capacity,
                                int32_t* n_items);

@@ -20,6 +20,7 @@ PIC_OK, PIC_EINVAL, PIC_EUNSUPPORTED, PIC_EHIP, PIC_EWORKSPACE = range(5)
 PIC_BF16, PIC_F32 = 0, 1
 PIC_ROPE_NEOX, PIC_ROPE_GPTJ = 0, 1
 PIC_SSEP, PIC_PDEP, PIC_QUERY = 1, 2, 4
+PIC_KV8_E4M3, PIC_KV8_INT8 = 0, 1
 
 
 class PicError(RuntimeError):
@@ -47,6 +48,10 @@ class pic_batch_dev(ctypes.Structure):
 
 class pic_rope_table(ctypes.Structure):
     _fields_ = [("data", c_void_p), ("len", c_int32)]
+
+
+class pic_kv8_pool(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("scale", c_void_p), ("num_blocks", c_int32), ("code", c_int32)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -86,6 +91,18 @@ _sig = {
     "pic_kv_keep": (c_int32, [_P(pic_config), c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
                               c_int32, c_void_p, c_void_p]),
     "pic_tree_plan_debug": (c_int32, [_P(pic_config), _P(pic_batch_host), _P(c_int32), c_int32, _P(c_int32)]),
+    # the cache held in 8 bits
+    "pic_qk_norm": (c_int32, [_P(pic_config), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                              c_void_p, c_float, c_void_p, c_int32, c_void_p]),
+    "pic_kv8_write": (c_int32, [_P(pic_config), _P(pic_kv8_pool), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int32,
+                                c_void_p]),
+    "pic_kv8_read": (c_int32, [_P(pic_config), _P(pic_kv8_pool), c_void_p, c_int32, c_void_p, c_void_p, c_void_p]),
+    "pic_attn8_workspace_size": (c_int32, [_P(pic_config), _P(pic_batch_host), c_int32, _P(c_size_t)]),
+    "pic_attn8_prefill": (c_int32, [_P(pic_config), _P(pic_batch_host), _P(pic_batch_dev), c_void_p, c_void_p, _P(pic_kv8_pool),
+                                    c_void_p, c_size_t, c_void_p]),
+    "pic_attn8_decode": (c_int32, [_P(pic_config), _P(pic_batch_host), _P(pic_batch_dev), c_void_p, c_void_p, _P(pic_kv8_pool),
+                                   c_void_p, c_size_t, c_void_p]),
+    "pic_attn8_plan_debug": (c_int32, [_P(pic_config), _P(pic_batch_host), c_int32, _P(c_int32), c_int32, _P(c_int32)]),
     # span cache (include/pic_cache.h): host only
     "pic_sha256": (c_int32, [c_void_p, c_size_t, c_void_p]),
     "pic_block_hashes": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p]),
@@ -325,6 +342,90 @@ def pic_tree_plan_debug(cfg: pic_config, batch: HostBatch) -> np.ndarray:
     out = np.zeros((max(n.value, 1), 8), dtype=np.int32)
     _check(_lib.pic_tree_plan_debug(ctypes.byref(cfg), ctypes.byref(batch.c), out.ctypes.data_as(POINTER(c_int32)), n.value,
                                     ctypes.byref(n)))
+    return out[: n.value]
+
+
+# ------------------------------------------------------------------------------------
+# the cache held in 8 bits: norms of a projection's queries and keys, rows into and out of the
+# pool, attention over it
+# ------------------------------------------------------------------------------------
+
+class Kv8Pool:
+    """A pool of codes: k, v one-byte tensors [blocks][Hkv][16][D] and scale float32 [blocks][Hkv][2], all dense;
+    code is PIC_KV8_E4M3 or PIC_KV8_INT8.  Keeps the tensors alive."""
+
+    def __init__(self, k, v, scale, code: int):
+        for t, what, size in ((k, "k", 1), (v, "v", 1), (scale, "scale", 4)):
+            if t.element_size() != size or not t.is_contiguous():
+                raise ValueError(f"{what} must be dense, of {size}-byte elements")
+        if k.dim() != 4 or v.shape != k.shape or tuple(scale.shape) != (k.shape[0], k.shape[1], 2):
+            raise ValueError("k and v must be [blocks][Hkv][16][D] and scale [blocks][Hkv][2]")
+        self.k, self.v, self.scale = k, v, scale
+        self.c = pic_kv8_pool(k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.size(0), int(code))
+
+    def _of(self, cfg):
+        if self.k.size(1) != cfg.num_kv_heads or self.k.size(2) != cfg.block_size or self.k.size(3) != cfg.head_dim:
+            raise ValueError("the pool's shape is not the config's")
+        return ctypes.byref(self.c)
+
+
+def pic_qk_norm(cfg: pic_config, q, k, q_weight, k_weight, eps: float, positions=None, q_out=None, k_out=None, stream=None) -> None:
+    """q [n][Hq][D] and k [n][Hkv][D] (either may be None) may be views of one projection's output, the outputs too;
+    without an output the norm is taken in place.  Weights [D] or None; positions may be None for an unrotated pool."""
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    (qp, qs), (kp, ks), (qo, qos), (ko, kos) = _rows(q, "q"), _rows(k, "k"), _rows(q_out, "q_out"), _rows(k_out, "k_out")
+    for t, o in ((q, q_out), (k, k_out)):
+        if (t is None) != (o is None) or (t is not None and t.shape != o.shape):
+            raise ValueError("an output must have its input's shape")
+    n = [t.size(0) for t in (q, k) if t is not None]
+    if len(set(n)) != 1:
+        raise ValueError("q and k must have the same rows")
+    _check(_lib.pic_qk_norm(ctypes.byref(cfg), qp, qs, qo, qos, kp, ks, ko, kos, _ptr(q_weight), _ptr(k_weight), eps, _ptr(positions),
+                            n[0], _stream(stream)))
+
+
+def pic_kv8_write(cfg: pic_config, pool: Kv8Pool, k_new, v_new, slot_mapping, stream=None) -> None:
+    """k_new, v_new [n][Hkv][D] may be views of one projection's output (rows dense, any row stride)."""
+    (kp, ks), (vp, vs) = _rows(k_new, "k_new"), _rows(v_new, "v_new")
+    _check(_lib.pic_kv8_write(ctypes.byref(cfg), pool._of(cfg), kp, ks, vp, vs, slot_mapping.data_ptr(), k_new.size(0), _stream(stream)))
+
+
+def pic_kv8_read(cfg: pic_config, pool: Kv8Pool, slot_mapping, k_out, v_out, stream=None) -> None:
+    """k_out, v_out: dense [n][Hkv][D]."""
+    if not k_out.is_contiguous() or not v_out.is_contiguous():
+        raise ValueError("k_out and v_out must be dense")
+    _check(_lib.pic_kv8_read(ctypes.byref(cfg), pool._of(cfg), slot_mapping.data_ptr(), slot_mapping.size(0), k_out.data_ptr(),
+                             v_out.data_ptr(), _stream(stream)))
+
+
+def pic_attn8_workspace_size(cfg: pic_config, batch: HostBatch, is_decode: bool) -> int:
+    out = c_size_t(0)
+    _check(_lib.pic_attn8_workspace_size(ctypes.byref(cfg), ctypes.byref(batch.c), int(is_decode), ctypes.byref(out)))
+    return out.value
+
+
+def _attn8(call, cfg, batch, block_tables, positions, q, o, pool, workspace, stream):
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(call(ctypes.byref(cfg), ctypes.byref(batch.c), ctypes.byref(_dev(block_tables, positions)), _ptr(q), _ptr(o), pool._of(cfg),
+                _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def pic_attn8_prefill(cfg: pic_config, batch: HostBatch, block_tables, positions, q, o, pool: Kv8Pool, workspace=None, stream=None) -> None:
+    """pic_attn_prefill over a pool of 8-bit codes."""
+    _attn8(_lib.pic_attn8_prefill, cfg, batch, block_tables, positions, q, o, pool, workspace, stream)
+
+
+def pic_attn8_decode(cfg: pic_config, batch: HostBatch, block_tables, positions, q, o, pool: Kv8Pool, workspace=None, stream=None) -> None:
+    """pic_attn_decode over a pool of 8-bit codes."""
+    _attn8(_lib.pic_attn8_decode, cfg, batch, block_tables, positions, q, o, pool, workspace, stream)
+
+
+def pic_attn8_plan_debug(cfg: pic_config, batch: HostBatch, is_decode: bool) -> np.ndarray:
+    n = c_int32(0)
+    _check(_lib.pic_attn8_plan_debug(ctypes.byref(cfg), ctypes.byref(batch.c), int(is_decode), None, 0, ctypes.byref(n)))
+    out = np.zeros((max(n.value, 1), 8), dtype=np.int32)
+    _check(_lib.pic_attn8_plan_debug(ctypes.byref(cfg), ctypes.byref(batch.c), int(is_decode), out.ctypes.data_as(POINTER(c_int32)),
+                                     n.value, ctypes.byref(n)))
     return out[: n.value]
 
 

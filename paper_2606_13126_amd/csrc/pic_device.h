@@ -320,6 +320,30 @@ __device__ __forceinline__ float sum_xor16(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// cos/sin by the hardware's sine of a fraction of a revolution (its error, about 2^-20, is far
+// below the 2^-12 to which the attention rounds what they turn)
+__device__ __forceinline__ void rope_cs_fast(int64_t pos, uint64_t step, float& c, float& s) {
+    const uint64_t ph = (uint64_t)pos * step;
+    const float r = (float)(int32_t)(ph >> 32) * 0x1p-32f;
+    c = __builtin_amdgcn_cosf(r);
+    s = __builtin_amdgcn_sinf(r);
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)lo, (_Float16)hi});
+}
+
+// max over the 8 lanes l & ~7 .. l | 7
+__device__ __forceinline__ float max_of8(float x) {
+    auto dpp = [&](auto ctrl) {
+        return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(x), __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    x = dpp(Idx<0xB1>{});    // lane ^ 1
+    x = dpp(Idx<0x4E>{});    // lane ^ 2
+    return dpp(Idx<0x141>{});   // lane ^ 7 (half rows mirrored)
+}
+
 // Bits of keys idx .. idx + 31 of a drafted token's mask row: keys before the span (idx < 0)
 // are seen, keys past the row's words are not.
 __device__ __forceinline__ uint32_t tree_bits(const uint32_t* __restrict__ row, int words, int idx) {

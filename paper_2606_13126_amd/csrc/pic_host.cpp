@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <exception>
 #include <limits>
 #include <string>
 #include <vector>
@@ -29,9 +30,12 @@ static_assert(sizeof(pic::Plan) + sizeof(pic::Args) <= 4096, "kernel arguments m
 static_assert(sizeof(pic::KeyPlan) + sizeof(pic::Args) <= 4096, "kernel arguments must stay within 4 KB");
 static_assert(sizeof(pic::PlanUpload) <= 4096, "kernel arguments must stay within 4 KB");
 static_assert(sizeof(pic::Plan) + sizeof(pic::TreeArgs) <= 4096, "kernel arguments must stay within 4 KB");
+static_assert(sizeof(pic::Plan) + sizeof(pic::Kv8Args) <= 4096, "kernel arguments must stay within 4 KB");
 
 // The attention calls: what a plan is made for.
-enum class Call { kPrefill, kDecode, kTree };
+enum class Call { kPrefill, kDecode, kTree, kPrefill8, kDecode8 };
+
+bool over_codes(Call call) { return call == Call::kPrefill8 || call == Call::kDecode8; }
 
 thread_local std::string g_error;
 
@@ -128,7 +132,8 @@ struct HostPlan {
     int f32_waves = 0;         // waves per workgroup of the float32 kernel (float32 only)
     bool short_items = false;  // prefill of rotated keys: without the alternating kernel
     bool tree = false;         // attention of drafted tokens
-    int tree_rows = 0;         // its query rows per workgroup (bf16 only)
+    bool kv8 = false;          // attention over a pool of 8-bit codes
+    int tree_rows = 0;         // query rows per workgroup of either (bf16 only)
     pic::KeyPlan keys{};       // the rotated key copy (n = 0: keys are rotated in the attention kernel)
     bool keys_from_table = true;   // whether the copy also pays where a cos/sin table makes rotation cheap
     int tile_rows() const { return f32_waves ? 16 * f32_waves : tree_rows ? tree_rows : pic::kTileRows; }
@@ -255,14 +260,35 @@ TreeSplit tree_split(HostPlan& hp, int G, int hkv) {
     return best;
 }
 
+// Row tiles and key splits of a call over 8-bit codes in bf16: tiles of 16 rows where every (span, KV head)
+// has no more, else of 32; chunks of about the average work per compute unit, at least one step of keys.
+void kv8_split(HostPlan& hp, int G, int hkv) {
+    int64_t most = 0;
+    for (auto& g : hp.groups) most = std::max<int64_t>(most, (int64_t)g.n_tok * G);
+    hp.tree_rows = most <= 16 ? 16 : 32;
+    const int64_t tr = hp.tree_rows, tk = pic::kv8_keys(hp.tree_rows);
+    int64_t total = 0;
+    for (auto& g : hp.groups)
+        for (int64_t rt = 0; rt < pic::row_tiles(g, G, (int32_t)tr); ++rt)
+            total += ((int64_t)g.tok0 + (std::min((rt + 1) * tr, (int64_t)g.n_tok * G) - 1) / G - g.win + tk) / tk * hkv;
+    const int64_t chunk = std::min<int64_t>(std::max<int64_t>(1, (total + pic::kTargetCUs - 1) / pic::kTargetCUs), (1 << 30) / tk);
+    for (auto& g : hp.groups) {
+        const int64_t steps = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
+        const int64_t n_split = (steps + chunk - 1) / chunk, each = (steps + n_split - 1) / n_split;
+        g.n_split = (int32_t)((steps + each - 1) / each);   // none of them is empty
+        g.split_keys = (int32_t)std::min<int64_t>(each * tk, INT32_MAX);
+    }
+}
+
 // Groups, their split policy and bases.  Prefill and float32 groups hold (row tile,
 // KV head, split) items.  `lean` (for a workspace without room for the rest) keeps
 // float32 keys unsplit and gives every query head of a decode merge one thread row.
 pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bool lean, HostPlan& hp) {
-    const bool decode = call == Call::kDecode;
+    const bool decode = call == Call::kDecode || call == Call::kDecode8;
     hp.groups.clear();
     hp.n_parts = 0;
     hp.tree = call == Call::kTree;
+    hp.kv8 = over_codes(call);
     const int G = c->num_q_heads / c->num_kv_heads;
     std::vector<int32_t> w;
     int64_t pos_off = 0, q_row = 0;
@@ -298,7 +324,7 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
     }
     if (q_row > INT32_MAX / 2) return fail(PIC_EINVAL, "too many query rows");
 
-    hp.dec_kernel = decode && c->dtype == PIC_BF16 && G <= pic::kDecMaxG;
+    hp.dec_kernel = call == Call::kDecode && c->dtype == PIC_BF16 && G <= pic::kDecMaxG;
     if (hp.dec_kernel) {
         // Decode items are (request, key split, group of KV heads).  A wide workgroup
         // holds a CU (narrow ones share it three or two ways), so cut the keys into
@@ -364,6 +390,11 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
         std::stable_sort(hp.groups.begin(), hp.groups.end(), [](const pic::Group& x, const pic::Group& y) {
             return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
         });
+    } else if (hp.kv8) {
+        kv8_split(hp, G, c->num_kv_heads);
+        std::stable_sort(hp.groups.begin(), hp.groups.end(), [](const pic::Group& x, const pic::Group& y) {
+            return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
+        });
     } else if (hp.tree) {
         const TreeSplit sp = tree_split(hp, G, c->num_kv_heads);
         hp.tree_rows = sp.tile;
@@ -425,7 +456,7 @@ pic_status assign_bases(const pic_config* c, HostPlan& hp) {
         const int64_t n = items_of(c, hp, g);
         // (drafted tokens: padding would leave compute units of the last XCDs idle, 44 trees of 4 KV
         // heads without splits half of them)
-        const int64_t n_pad = hp.dec_kernel || hp.tree ? n : round_up(n, 8);
+        const int64_t n_pad = hp.dec_kernel || hp.tree || (hp.kv8 && c->dtype == PIC_BF16) ? n : round_up(n, 8);
         g.item_base = (int32_t)item;
         g.part_base = (int32_t)part;
         g.merge_base = (int32_t)merge;
@@ -513,7 +544,7 @@ WsLayout ws_layout(const pic_config* c, const HostPlan& hp) {
 // over 131,072 keys, the most: 2,271 against 1,853 us).
 void plan_keys(const pic_config* c, HostPlan& hp) {
     hp.keys.n = 0;
-    if (c->dtype != PIC_BF16 || c->k_prerotated || hp.dec_kernel || hp.tree) return;
+    if (c->dtype != PIC_BF16 || c->k_prerotated || hp.dec_kernel || hp.tree || hp.kv8) return;
     const int G = c->num_q_heads / c->num_kv_heads;
     struct Run {
         int32_t req, lo, hi, pos_off;
@@ -648,6 +679,20 @@ uint64_t chunk_map(const pic_config* c) {
     return m;
 }
 
+// f(), with a host that has no room for what it plans as an error like any other
+template <typename F>
+pic_status within_memory(F f) noexcept {
+    try {
+        return f();
+    } catch (const std::exception&) {
+        try {
+            return fail(PIC_EINVAL, "out of host memory");
+        } catch (const std::exception&) {
+            return PIC_EINVAL;   // (the message needs memory too)
+        }
+    }
+}
+
 pic_status hip_status(int e, const char* what) {
     if (e != hipSuccess) return fail(PIC_EHIP, std::string(what) + ": " + hipGetErrorString((hipError_t)e));
     return PIC_OK;
@@ -656,7 +701,7 @@ pic_status hip_status(int e, const char* what) {
 pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic_batch_dev* dv,
                          const pic_rope_table* rope, const void* q, void* o, const void* k_pool, const void* v_pool,
                          int32_t num_blocks, void* ws, size_t ws_bytes, void* stream, Call call,
-                         const uint64_t* tree_mask = nullptr, int32_t mask_words = 0) {
+                         const uint64_t* tree_mask = nullptr, int32_t mask_words = 0, const pic_kv8_pool* codes = nullptr) {
     pic_status st = check_config(c);
     if (st) return st;
     if ((st = check_batch(b))) return st;
@@ -759,6 +804,16 @@ pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic
         (st = hip_status(pic::launch_rope_keys(c->rope_style, c->head_dim, hp.keys, a, stream), "key rotation launch")))
         return st;
     const bool rope_on = c->k_prerotated == 0;
+    if (hp.kv8) {
+        pic::Kv8Args k{};
+        static_cast<pic::Args&>(k) = a;
+        k.scale = codes->scale;
+        k.code = codes->code;
+        k.tile_rows = hp.tile_rows();
+        return hip_status(c->dtype == PIC_F32 ? pic::launch_kv8_f32(hp.f32_waves, c->rope_style, c->head_dim, rope_on, p, k, stream)
+                                              : pic::launch_kv8(c->rope_style, c->head_dim, rope_on, p, k, stream),
+                          "attention launch");
+    }
     if (hp.tree)
         return hip_status(c->dtype == PIC_F32 ? pic::launch_tree_f32(hp.f32_waves, c->rope_style, c->head_dim, rope_on, p, a, stream)
                                               : pic::launch_tree(c->rope_style, c->head_dim, rope_on, p, a, stream),
@@ -1055,6 +1110,183 @@ pic_status pic_kv_keep(const pic_config* cfg, void* k_pool, void* v_pool, int32_
                                           (int64_t)num_blocks * pic::kBlock, slot_mapping, cu_rows, path, path_len, n_trees,
                                           max_path, total_rows, stream),
                       "kv_keep launch");
+}
+
+// Element offsets of rows by stride stay in range, rows hold what they should, chunks of 16 bytes.
+static pic_status check_rows(const char* what, const void* p, int64_t stride, int64_t row, int64_t n, int64_t es) {
+    if (stride < row || stride > INT64_MAX / 2 / es / n)
+        return fail(PIC_EINVAL, std::string(what) + ": the row stride must hold a row (and its offsets 64 bits)");
+    if (misaligned(p, 16) || stride * es % 16) return fail(PIC_EINVAL, std::string(what) + " must have 16-byte aligned rows");
+    return PIC_OK;
+}
+
+// Some row of p and some row of q (n rows each, sizes and strides in bytes) share a byte.  Rows of one stride may
+// be slices of one allocation.
+static bool rows_overlap(const void* p, int64_t p_row, int64_t p_stride, const void* q, int64_t q_row, int64_t q_stride, int64_t n) {
+    if (p == nullptr || q == nullptr || !overlap(p, (n - 1) * p_stride + p_row, q, (n - 1) * q_stride + q_row)) return false;
+    if (p_stride != q_stride) return true;
+    const intptr_t d = reinterpret_cast<intptr_t>(q) - reinterpret_cast<intptr_t>(p);
+    const int64_t m = ((int64_t)d % p_stride + p_stride) % p_stride;   // where q's rows begin in p's
+    return m < p_row || m + q_row > p_stride;
+}
+
+pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k,
+                       int64_t k_stride, void* k_out, int64_t k_out_stride, const void* q_weight, const void* k_weight, float eps,
+                       const int32_t* positions, int32_t n, void* stream) {
+    pic_status st = check_config(cfg);
+    if (st) return st;
+    if (n < 0) return fail(PIC_EINVAL, "n must be >= 0");
+    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(PIC_EINVAL, "eps must be positive and finite");
+    if (n >= (1 << 24)) return fail(PIC_EINVAL, "n must be < 2^24 rows per call");
+    if (n == 0) return PIC_OK;
+    if ((q == nullptr) != (q_out == nullptr)) return fail(PIC_EINVAL, "q and q_out must both be given or both be NULL");
+    if ((k == nullptr) != (k_out == nullptr)) return fail(PIC_EINVAL, "k and k_out must both be given or both be NULL");
+    if (!q && !k) return fail(PIC_EINVAL, "neither q nor k is given");
+    if (cfg->k_prerotated && positions == nullptr) return fail(PIC_EINVAL, "positions must not be NULL");
+    if (misaligned(positions, 4) || misaligned(q_weight, 16) || misaligned(k_weight, 16))
+        return fail(PIC_EINVAL, "weights must be 16-byte aligned, positions 4-byte aligned");
+    const int64_t es = cfg->dtype == PIC_F32 ? 4 : 2, q_row = (int64_t)cfg->num_q_heads * cfg->head_dim,
+                  k_row = (int64_t)cfg->num_kv_heads * cfg->head_dim;
+    if (q && ((st = check_rows("q", q, q_stride, q_row, n, es)) || (st = check_rows("q_out", q_out, q_out_stride, q_row, n, es)))) return st;
+    if (k && ((st = check_rows("k", k, k_stride, k_row, n, es)) || (st = check_rows("k_out", k_out, k_out_stride, k_row, n, es)))) return st;
+    const int64_t qb = q_row * es, kb = k_row * es, qs = q_stride * es, ks = k_stride * es, qos = q_out_stride * es, kos = k_out_stride * es;
+    const bool q_here = q == q_out && q_stride == q_out_stride, k_here = k == k_out && k_stride == k_out_stride;
+    if ((!q_here && rows_overlap(q, qb, qs, q_out, qb, qos, n)) || (!k_here && rows_overlap(k, kb, ks, k_out, kb, kos, n)) ||
+        rows_overlap(q, qb, qs, k_out, kb, kos, n) || rows_overlap(k, kb, ks, q_out, qb, qos, n) || rows_overlap(q_out, qb, qos, k_out, kb, kos, n))
+        return fail(PIC_EINVAL, "an output overlaps an input or the other output (it may only be its own input)");
+    pic::NormArgs a{};
+    if (cfg->k_prerotated) {
+        phase_steps(cfg, a.fstep);
+        a.rot_half = (cfg->rotary_dim ? cfg->rotary_dim : cfg->head_dim) / 2;
+    }
+    a.q = q;
+    a.k = k;
+    a.q_out = q_out;
+    a.k_out = k_out;
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    a.positions = positions;
+    a.q_stride = qs / 16;
+    a.k_stride = ks / 16;
+    a.q_out_stride = qos / 16;
+    a.k_out_stride = kos / 16;
+    a.eps = eps;
+    a.hq = q ? cfg->num_q_heads : 0;
+    a.hkv = k ? cfg->num_kv_heads : 0;
+    return hip_status(pic::launch_qk_norm(cfg->dtype, cfg->rope_style, cfg->head_dim, n, a, stream), "qk_norm launch");
+}
+
+static pic_status check_pool(const pic_kv8_pool* p) {
+    if (p == nullptr) return fail(PIC_EINVAL, "pool is NULL");
+    if (p->code != PIC_KV8_E4M3 && p->code != PIC_KV8_INT8) return fail(PIC_EUNSUPPORTED, "pool->code must be PIC_KV8_E4M3 or PIC_KV8_INT8");
+    if (p->num_blocks < 0) return fail(PIC_EINVAL, "pool->num_blocks must be >= 0");
+    return PIC_OK;
+}
+
+// ... of a call that touches it
+static pic_status check_pool_memory(const pic_kv8_pool* p) {
+    if (!p->k || !p->v || !p->scale) return fail(PIC_EINVAL, "the pool's codes and scales must not be NULL");
+    if (p->num_blocks == 0) return fail(PIC_EINVAL, "empty pool");
+    if (misaligned(p->k, 16) || misaligned(p->v, 16) || misaligned(p->scale, 8))
+        return fail(PIC_EINVAL, "the pool's codes must be 16-byte aligned, its scales 8-byte aligned");
+    return PIC_OK;
+}
+
+pic_status pic_kv8_write(const pic_config* cfg, const pic_kv8_pool* pool, const void* k_new, int64_t k_stride, const void* v_new,
+                         int64_t v_stride, const int32_t* slot_mapping, int32_t n, void* stream) {
+    pic_status st = check_config(cfg);
+    if (st) return st;
+    if ((st = check_pool(pool))) return st;
+    if (n < 0) return fail(PIC_EINVAL, "n must be >= 0");
+    if (n >= (1 << 24)) return fail(PIC_EINVAL, "n must be < 2^24 rows per call");
+    if (n == 0) return PIC_OK;
+    if ((st = check_pool_memory(pool))) return st;
+    if (!k_new || !v_new || !slot_mapping) return fail(PIC_EINVAL, "NULL buffer");
+    if (misaligned(slot_mapping, 4)) return fail(PIC_EINVAL, "slot_mapping must be 4-byte aligned");
+    const int64_t es = cfg->dtype == PIC_F32 ? 4 : 2, row = (int64_t)cfg->num_kv_heads * cfg->head_dim;
+    if ((st = check_rows("k_new", k_new, k_stride, row, n, es)) || (st = check_rows("v_new", v_new, v_stride, row, n, es))) return st;
+    if (cfg->num_kv_heads > 4096) return fail(PIC_EUNSUPPORTED, "more than 4096 KV heads");
+    pic::Kv8WriteArgs a{};
+    a.k = k_new;
+    a.v = v_new;
+    a.k_pool = static_cast<uint8_t*>(pool->k);
+    a.v_pool = static_cast<uint8_t*>(pool->v);
+    a.scale = pool->scale;
+    a.slots = slot_mapping;
+    a.k_stride = k_stride * es / 16;
+    a.v_stride = v_stride * es / 16;
+    a.n_slots = (int64_t)pool->num_blocks * pic::kBlock;
+    a.n = n;
+    a.hkv = cfg->num_kv_heads;
+    a.range = n <= 1024 ? 1 : pic::kBlock;
+    return hip_status(pic::launch_kv8_write(cfg->dtype, pool->code, cfg->head_dim, a, stream), "kv8_write launch");
+}
+
+pic_status pic_kv8_read(const pic_config* cfg, const pic_kv8_pool* pool, const int32_t* slot_mapping, int32_t n, void* k_out,
+                        void* v_out, void* stream) {
+    pic_status st = check_config(cfg);
+    if (st) return st;
+    if ((st = check_pool(pool))) return st;
+    if (n < 0) return fail(PIC_EINVAL, "n must be >= 0");
+    if (n >= (1 << 24)) return fail(PIC_EINVAL, "n must be < 2^24 rows per call");
+    if (n == 0) return PIC_OK;
+    if ((st = check_pool_memory(pool))) return st;
+    if (!k_out || !v_out || !slot_mapping) return fail(PIC_EINVAL, "NULL buffer");
+    if (misaligned(slot_mapping, 4) || misaligned(k_out, 16) || misaligned(v_out, 16))
+        return fail(PIC_EINVAL, "k_out and v_out must be 16-byte aligned, slot_mapping 4-byte aligned");
+    const int64_t out = (int64_t)n * cfg->num_kv_heads * cfg->head_dim * (cfg->dtype == PIC_F32 ? 4 : 2),
+                  codes = (int64_t)pool->num_blocks * cfg->num_kv_heads * pic::kBlock * cfg->head_dim,
+                  scales = (int64_t)pool->num_blocks * cfg->num_kv_heads * 8;
+    if (overlap(k_out, out, v_out, out)) return fail(PIC_EINVAL, "k_out and v_out overlap");
+    for (const void* o : {k_out, v_out})
+        if (overlap(o, out, pool->k, codes) || overlap(o, out, pool->v, codes) || overlap(o, out, pool->scale, scales))
+            return fail(PIC_EINVAL, "an output overlaps the pool");
+    return hip_status(pic::launch_kv8_read(cfg->dtype, pool->code, cfg->head_dim, cfg->num_kv_heads, static_cast<const uint8_t*>(pool->k),
+                                           static_cast<const uint8_t*>(pool->v), pool->scale, (int64_t)pool->num_blocks * pic::kBlock,
+                                           slot_mapping, n, k_out, v_out, stream),
+                      "kv8_read launch");
+}
+
+pic_status pic_attn8_workspace_size(const pic_config* cfg, const pic_batch_host* batch, int32_t is_decode, size_t* bytes) {
+    return within_memory([&]() -> pic_status {
+        pic_status st = check_config(cfg);
+        if (st) return st;
+        if ((st = check_batch(batch))) return st;
+        if (bytes == nullptr) return fail(PIC_EINVAL, "bytes is NULL");
+        HostPlan hp;
+        if ((st = build_plan(cfg, batch, is_decode != 0 ? Call::kDecode8 : Call::kPrefill8, hp))) return st;
+        *bytes = ws_layout(cfg, hp).total;
+        return PIC_OK;
+    });
+}
+
+static pic_status attn8(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev, const void* q, void* o,
+                        const pic_kv8_pool* pool, void* workspace, size_t workspace_bytes, void* stream, Call call) {
+    return within_memory([&]() -> pic_status {
+        pic_status st = check_config(cfg);
+        if (st) return st;
+        if ((st = check_pool(pool))) return st;
+        if ((st = check_batch(batch))) return st;
+        if (batch->num_reqs == 0) return PIC_OK;
+        if ((st = check_pool_memory(pool))) return st;
+        return run_attention(cfg, batch, dev, nullptr, q, o, pool->k, pool->v, pool->num_blocks, workspace, workspace_bytes, stream, call,
+                             nullptr, 0, pool);
+    });
+}
+
+pic_status pic_attn8_prefill(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev, const void* q, void* o,
+                             const pic_kv8_pool* pool, void* workspace, size_t workspace_bytes, void* stream) {
+    return attn8(cfg, batch, dev, q, o, pool, workspace, workspace_bytes, stream, Call::kPrefill8);
+}
+
+pic_status pic_attn8_decode(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev, const void* q, void* o,
+                            const pic_kv8_pool* pool, void* workspace, size_t workspace_bytes, void* stream) {
+    return attn8(cfg, batch, dev, q, o, pool, workspace, workspace_bytes, stream, Call::kDecode8);
+}
+
+pic_status pic_attn8_plan_debug(const pic_config* cfg, const pic_batch_host* batch, int32_t is_decode, int32_t* items, int32_t capacity,
+                                int32_t* n_items) {
+    return within_memory([&] { return plan_items(cfg, batch, is_decode != 0 ? Call::kDecode8 : Call::kPrefill8, items, capacity, n_items); });
 }
 
 pic_status pic_plan_debug(const pic_config* cfg, const pic_batch_host* batch, int32_t is_decode, int32_t* items,

@@ -234,6 +234,50 @@ struct AppendArgs {
     int32_t rot_half;    // pairs that turn (0: none)
 };
 
+// Attention over a pool of 8-bit codes
+struct Kv8Args : Args {
+    const float* scale;       // [blocks][hkv][2]: of a block's keys and values
+    int32_t code;             // kCodeE4m3 or kCodeInt8
+    int32_t tile_rows;        // query rows per workgroup
+};
+constexpr int kCodeE4m3 = 0, kCodeInt8 = 1;
+
+// Its bf16 workgroups: eight waves.  With 16 or 32 query rows the waves all hold the same ones and take
+// different cache blocks.
+constexpr int kKv8Waves = 8;
+constexpr int kv8_keys(int rows) { return rows <= 32 ? kKv8Waves * kBlock : 64; }   // keys that they take at a time
+
+// Rows of qk_norm: strides in 16-byte chunks
+struct NormArgs {
+    uint64_t fstep[64];
+    const void* q;
+    const void* k;
+    void* q_out;
+    void* k_out;
+    const void* q_weight;     // or null: ones
+    const void* k_weight;
+    const int32_t* positions;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+    float eps;
+    int32_t hq, hkv;          // 0: no queries, no keys
+    int32_t rot_half;         // pairs that turn (0: none)
+};
+
+// Rows of kv8_write (strides in 16-byte chunks)
+struct Kv8WriteArgs {
+    const void* k;
+    const void* v;
+    uint8_t* k_pool;
+    uint8_t* v_pool;
+    float* scale;
+    const int32_t* slots;
+    int64_t k_stride, v_stride;
+    int64_t n_slots;
+    int32_t n;
+    int32_t hkv;
+    int32_t range;            // rows whose blocks a workgroup looks for
+};
+
 // Records msg as the thread's last error (pic_last_error) and returns st.
 int32_t host_fail(int32_t st, const char* msg);
 
@@ -258,6 +302,14 @@ int launch_kv_append(int dtype, int style, int d, int n, const AppendArgs& args,
 int launch_kv_keep(int dtype, int hkv, int d, void* k_pool, void* v_pool, int64_t n_slots, const int32_t* slots,
                    const int32_t* cu_rows, const int32_t* path, const int32_t* path_len, int n_trees, int max_path, int total_rows,
                    void* stream);
+
+int launch_kv8_f32(int f32_waves, int style, int d, bool rope, const Plan& plan, const Kv8Args& args, void* stream);
+// Launchers implemented in pic_kv8.hip
+int launch_qk_norm(int dtype, int style, int d, int n, const NormArgs& args, void* stream);
+int launch_kv8_write(int dtype, int code, int d, const Kv8WriteArgs& args, void* stream);
+int launch_kv8_read(int dtype, int code, int d, int hkv, const uint8_t* k_pool, const uint8_t* v_pool, const float* scale,
+                    int64_t n_slots, const int32_t* slots, int n, void* k_out, void* v_out, void* stream);
+int launch_kv8(int style, int d, bool rope, const Plan& plan, const Kv8Args& args, void* stream);
 
 // Device scratch of the no-allocation entry point: kScratchBytes on each device,
 // shared by every call on that device.  scratch_region returns the current

@@ -1833,14 +1833,25 @@ __global__ void __launch_bounds__(ROWS * D / 4) decode_merge(const Plan plan, co
 // ---------------------------------------------------------------------------------
 typedef float f32x4v_t __attribute__((ext_vector_type(4)));
 
+// the four codes of a word as numbers
+__device__ __forceinline__ f32x4v_t decode4(int32_t code, uint32_t w) {
+    if (code == kCodeE4m3) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+        return f32x4v_t{lo[0], lo[1], hi[0], hi[1]};
+    }
+    return f32x4v_t{(float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(int8_t)(w >> 24)};
+}
+
 //
 // TREE (AT = TreeArgs): the rows are drafted tokens; keys from the span's start on are seen
 // by the bits of the row's mask instead of by order, so every row tile runs to the span's end.
+// KV8 (AT = Kv8Args): the pool holds 8-bit codes, which the staging thread turns into numbers.
 // One-wave instances of D 128 need more than the 256 registers of two waves per SIMD (with a table or
 // computed angles 52 and 16 bytes of a lane would go to scratch memory, which no kernel here uses).
 template <int D, int STYLE, bool ROPE, bool TABLE, int NW, typename AT>
-__global__ void __launch_bounds__(NW * 64, (NW == 1 && std::is_same<AT, TreeArgs>::value ? 1 : 2)) attn_f32(const Plan plan, const AT a) {
+__global__ void __launch_bounds__(NW * 64, (NW == 1 && !std::is_same<AT, Args>::value ? 1 : 2)) attn_f32(const Plan plan, const AT a) {
     constexpr bool TREE = std::is_same<AT, TreeArgs>::value;
+    constexpr bool KV8 = std::is_same<AT, Kv8Args>::value;
     constexpr int TK = f32_tile_keys(NW);
     constexpr int HALF = D / 2;
     constexpr int KC = D / 16;            // 16-dim contraction steps of 4 products each
@@ -1972,21 +1983,43 @@ __global__ void __launch_bounds__(NW * 64, (NW == 1 && std::is_same<AT, TreeArgs
         if (ROPE) m_pos = a.positions[g.pos_off + j];
     };
     f32x4v_t kr[KU][2], vr[VU];
+    uint32_t kw[KU][2], vw[VU];     // KV8: four codes each, and their scales
+    float2 kvs;
     float cr[KU][4], sr[KU][4];
     auto load_tile = [&]() {
         const size_t base = (((size_t)m_blk * a.hkv + ic.kvh) * kBlock + m_row) * D;
+        if constexpr (KV8) {
+            const uint8_t* kc = static_cast<const uint8_t*>(a.k_pool) + base;
+            const uint8_t* vc = static_cast<const uint8_t*>(a.v_pool) + base;
 #pragma unroll
-        for (int u = 0; u < KU; ++u) {
-            kr[u][0] = *reinterpret_cast<const f32x4v_t*>(kpool + base + k_el[u][0]);
-            kr[u][1] = *reinterpret_cast<const f32x4v_t*>(kpool + base + k_el[u][1]);
+            for (int u = 0; u < KU; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) kw[u][h] = *reinterpret_cast<const uint32_t*>(kc + k_el[u][h]);
+#pragma unroll
+            for (int u = 0; u < VU; ++u) vw[u] = *reinterpret_cast<const uint32_t*>(vc + 4 * (sub + u * TPK));
+            kvs = *reinterpret_cast<const float2*>(a.scale + ((size_t)m_blk * a.hkv + ic.kvh) * 2);
+        } else {
+#pragma unroll
+            for (int u = 0; u < KU; ++u) {
+                kr[u][0] = *reinterpret_cast<const f32x4v_t*>(kpool + base + k_el[u][0]);
+                kr[u][1] = *reinterpret_cast<const f32x4v_t*>(kpool + base + k_el[u][1]);
+            }
+#pragma unroll
+            for (int u = 0; u < VU; ++u) vr[u] = *reinterpret_cast<const f32x4v_t*>(vpool + base + 4 * (sub + u * TPK));
         }
-#pragma unroll
-        for (int u = 0; u < VU; ++u) vr[u] = *reinterpret_cast<const f32x4v_t*>(vpool + base + 4 * (sub + u * TPK));
         if (ROPE)
 #pragma unroll
             for (int u = 0; u < KU; ++u) cs4(m_pos, 4 * (sub + u * TPK), cr[u], sr[u]);
     };
     auto store_tile = [&](int t) {
+        if constexpr (KV8) {
+#pragma unroll
+            for (int u = 0; u < KU; ++u)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) kr[u][h] = decode4(a.code, kw[u][h]) * kvs.x;
+#pragma unroll
+            for (int u = 0; u < VU; ++u) vr[u] = decode4(a.code, vw[u]) * kvs.y;
+        }
 #pragma unroll
         for (int u = 0; u < KU; ++u) {
             const int un = sub + u * TPK;
@@ -2304,6 +2337,18 @@ hipError_t launch_tree_f32_d(int f32_waves, bool rope, const Plan& plan, const T
 }
 
 template <int D, int STYLE>
+hipError_t launch_kv8_f32_d(int f32_waves, bool rope, const Plan& plan, const Kv8Args& a, hipStream_t st) {
+    auto go = [&](auto r) {
+        constexpr bool R = decltype(r)::value;
+        return f32_waves == 1 ? launch_f32_t<D, STYLE, R, false, 1, Kv8Args>(plan, a, st)
+                              : launch_f32_t<D, STYLE, R, false, kF32Waves, Kv8Args>(plan, a, st);
+    };
+    if constexpr (STYLE == kNeox)   // (without rotation the pairing makes no difference)
+        if (!rope) return go(std::false_type{});
+    return go(std::true_type{});
+}
+
+template <int D, int STYLE>
 hipError_t launch_attn_d(int dtype, int f32_waves, bool short_items, bool rope, const Plan& plan, const Args& a, hipStream_t st) {
     const bool table = a.rope_table != nullptr && a.rope_len > 0;
     if (!rope) return launch_attn_t<D, STYLE, false, false>(dtype, f32_waves, short_items, plan, a, st);
@@ -2445,6 +2490,16 @@ int launch_tree_f32(int f32_waves, int style, int d, bool rope, const Plan& plan
                                        : launch_tree_f32_d<64, 1>(f32_waves, rope, plan, args, st);
     return style == kNeox || !rope ? launch_tree_f32_d<128, 0>(f32_waves, rope, plan, args, st)
                                    : launch_tree_f32_d<128, 1>(f32_waves, rope, plan, args, st);
+}
+
+int launch_kv8_f32(int f32_waves, int style, int d, bool rope, const Plan& plan, const Kv8Args& args, void* stream) {
+    if (plan.n_items == 0) return hipSuccess;
+    hipStream_t st = (hipStream_t)stream;
+    if (d == 64)
+        return style == kNeox || !rope ? launch_kv8_f32_d<64, 0>(f32_waves, rope, plan, args, st)
+                                       : launch_kv8_f32_d<64, 1>(f32_waves, rope, plan, args, st);
+    return style == kNeox || !rope ? launch_kv8_f32_d<128, 0>(f32_waves, rope, plan, args, st)
+                                   : launch_kv8_f32_d<128, 1>(f32_waves, rope, plan, args, st);
 }
 
 }  // namespace pic

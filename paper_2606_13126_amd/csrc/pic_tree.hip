@@ -205,20 +205,6 @@ __global__ void __launch_bounds__(256) kv_keep_kernel(u32x4_t* __restrict__ k_po
     }
 }
 
-// cos/sin by the hardware's sine of a fraction of a revolution (its error, about 2^-20, is far
-// below the 2^-12 to which the attention rounds what they turn)
-__device__ __forceinline__ void rope_cs_fast(int64_t pos, uint64_t step, float& c, float& s) {
-    const uint64_t ph = (uint64_t)pos * step;
-    const float r = (float)(int32_t)(ph >> 32) * 0x1p-32f;
-    c = __builtin_amdgcn_cosf(r);
-    s = __builtin_amdgcn_sinf(r);
-}
-
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, f16x2_t{(_Float16)lo, (_Float16)hi});
-}
-
 // ---------------------------------------------------------------------------------
 // Attention of drafted tokens in bf16: tree_few and tree_many
 //
@@ -246,16 +232,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 // operations a pair, renewed every kRenew steps), else they are computed.
 // ---------------------------------------------------------------------------------
 constexpr int kRenew = 32;
-
-// max over the 8 lanes l & ~7 .. l | 7
-__device__ __forceinline__ float max_of8(float x) {
-    auto dpp = [&](auto ctrl) {
-        return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(x), __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false)));
-    };
-    x = dpp(Idx<0xB1>{});    // lane ^ 1
-    x = dpp(Idx<0x4E>{});    // lane ^ 2
-    return dpp(Idx<0x141>{});   // lane ^ 7 (half rows mirrored)
-}
 
 // Sizes of the two kernels' steps (SHARED: tree_many)
 template <int D, bool SHARED>

@@ -1,0 +1,527 @@
+"""The cache held in 8 bits on the GPU against plain float64: norms, the store, reading back and
+attention, at the sizes, masks and values where they can go wrong, and a step of all of them."""
+import numpy as np
+import pytest
+import torch
+
+from tests import kv8_util as K8
+from tests import tree_util as T
+from tests.gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+B = pytest.importorskip("paper_2606_13126_amd._binding")
+HALF_STEP = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}   # of a rounding, relative
+# cos/sin in float32: the phase rounded to 24 bits (pi 2^-24), the sine of it to a few units, and in
+# the bf16 attention 32 advances of at most 2^-22 each
+ANGLE, ANGLE_ADVANCED = 2.0 ** -21, 2.0 ** -17
+DTYPES = [torch.bfloat16, torch.float32]
+CODES = [K8.E4M3, K8.INT8]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def cfg_of(hq, hkv, d, dtype, style=0, rot=0, prerotated=0, theta=1e4, scale=0.0, inv_freq=None):
+    return B.make_config(hq, hkv, d, dtype=B.PIC_F32 if dtype == torch.float32 else B.PIC_BF16, rope_theta=theta, rope_style=style,
+                         rotary_dim=rot, k_prerotated=prerotated, softmax_scale=scale, inv_freq=inv_freq)
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def pool_of(codes_k, codes_v, scale, code):
+    """A pool of host bytes [blocks][H][16][D] and scales [blocks][H][2]."""
+    return B.Kv8Pool(dev(codes_k), dev(codes_v), dev(np.asarray(scale, np.float32)), code)
+
+
+def random_pool(rng, nb, hkv, d, code, powers=True):
+    """Full blocks of normally distributed rows, the sizes of whose blocks differ."""
+    out, scale = [], np.zeros((nb, hkv, 2), np.float32)
+    for i in range(2):
+        x = rng.standard_normal((nb, hkv, 16, d)) * np.exp2(rng.integers(-2, 3, (nb, hkv)))[:, :, None, None]
+        size = np.abs(x).max((2, 3))
+        s = np.vectorize(lambda m: K8.scale_of(m, code))(size) if powers else (size / K8.MOST[code]).astype(np.float32).astype(np.float64)
+        scale[..., i] = s
+        out.append(K8.encode(x / s[:, :, None, None], code))
+    return out[0], out[1], scale
+
+
+# ------------------------------------------------------------------------------------
+# pic_qk_norm
+# ------------------------------------------------------------------------------------
+
+def check_norm(got, x, w, pos, cfg_kw, rotate, eps, what):
+    """A head's sum of D squares is off by D 2^-24 of itself, so its root by half of that; root, division, product with
+    the weight and the turn round a few times more; angles are within ANGLE of a pair's size; the result rounds once."""
+    d = x.shape[-1]
+    ref = K8.norm(f64(x), None if w is None else f64(w), eps)
+    size = np.abs(ref)
+    if rotate:
+        rot = cfg_kw.get("rot") or d
+        style = cfg_kw.get("style", 0)
+        half = rot // 2
+        a, b = (ref[..., :half], ref[..., half:rot]) if style == 0 else (ref[..., 0:rot:2], ref[..., 1:rot:2])
+        pair = np.hypot(a, b)
+        size = np.abs(ref).copy()
+        if style == 0:
+            size[..., :half] = size[..., half:rot] = pair
+        else:
+            size[..., 0:rot:2] = size[..., 1:rot:2] = pair
+        ref = T.rotate(ref, pos, rot, 1e4, style)
+    tol = size * ((d / 2 + 12) * 2.0 ** -24 + (ANGLE if rotate else 0)) + HALF_STEP[got.dtype] * np.abs(ref) * 1.001
+    off = np.abs(f64(got) - ref)
+    assert (off <= tol + 1e-38).all(), (what, float((off / (tol + 1e-38)).max()))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d,style,rot", [(128, 0, 0), (64, 0, 0), (128, 1, 0), (64, 1, 34), (128, 0, 32), (64, 0, 16), (64, 1, 2)])
+@pytest.mark.parametrize("rotate", [0, 1])
+def test_qk_norm(dtype, d, style, rot, rotate):
+    for n, hq, hkv in ((1, 1, 1), (7, 8, 2), (33, 28, 4), (5, 64, 8)):
+        g = torch.Generator(device="cuda").manual_seed(n)
+        qkv = torch.randn(n, hq + 2 * hkv, d, generator=g, device="cuda")
+        qkv *= torch.exp2(torch.randint(-12, 12, (n, hq + 2 * hkv, 1), generator=g, device="cuda").float())
+        qkv = qkv.to(dtype)
+        before = qkv.clone()
+        q, k = qkv[:, :hq], qkv[:, hq:hq + hkv]
+        wq, wk = (torch.randn(d, generator=g, device="cuda").to(dtype) for _ in range(2))
+        pos = dev(np.random.default_rng(n).integers(-2**31, 2**31 - 1, n).astype(np.int32))
+        cfg = cfg_of(hq, hkv, d, dtype, style, rot, prerotated=rotate)
+        qo, ko = torch.full_like(q.contiguous(), float("nan")), torch.full_like(k.contiguous(), float("nan"))
+        B.pic_qk_norm(cfg, q, k, wq, wk, 1e-6, pos if rotate else None, q_out=qo, k_out=ko)
+        assert torch.equal(qkv, before)
+        kw = dict(style=style, rot=rot)
+        check_norm(qo, q, wq, f64(pos), kw, rotate, 1e-6, "q")
+        check_norm(ko, k, wk, f64(pos), kw, rotate, 1e-6, "k")
+        # in place inside the fused rows, without weights, and one of the two alone: the same bits
+        B.pic_qk_norm(cfg, q, k, wq, wk, 1e-6, pos if rotate else None)
+        assert torch.equal(q, qo) and torch.equal(k, ko) and torch.equal(qkv[:, hq + hkv:], before[:, hq + hkv:])
+        alone = torch.empty_like(ko)
+        B.pic_qk_norm(cfg, None, before[:, hq:hq + hkv], None, wk, 1e-6, pos, k_out=alone)
+        assert torch.equal(alone, ko)
+        plain = torch.empty_like(qo)
+        B.pic_qk_norm(cfg, before[:, :hq], None, None, None, 0.5, pos, q_out=plain)
+        check_norm(plain, before[:, :hq], None, f64(pos), kw, rotate, 0.5, "no weight")
+
+
+def test_qk_norm_of_zeros_and_large_rows():
+    cfg = cfg_of(2, 1, 64, torch.float32)
+    q = torch.zeros(2, 2, 64, device="cuda")
+    q[1] = 2.0 ** 59
+    k = torch.full((2, 1, 64), 2.0 ** -70, device="cuda")
+    B.pic_qk_norm(cfg, q, k, None, None, 1e-6)
+    assert torch.equal(q[0], torch.zeros(2, 64, device="cuda"))
+    assert (q[1] - 1).abs().max() < 1e-5
+    assert torch.allclose(k.double(), torch.full_like(k, 2.0 ** -70).double() * 1e3, rtol=1e-5)   # 1 / sqrt(eps)
+
+
+# ------------------------------------------------------------------------------------
+# pic_kv8_write, pic_kv8_read
+# ------------------------------------------------------------------------------------
+
+class Store:
+    """A pool on the device beside its model on the host."""
+
+    def __init__(self, nb, hkv, d, code, dtype, seed=0, scale=0.0):
+        self.rng = np.random.default_rng(seed)
+        self.nb, self.hkv, self.d, self.code, self.dtype = nb, hkv, d, code, dtype
+        self.cfg = cfg_of(hkv, hkv, d, dtype)
+        self.codes = [self.rng.integers(0, 127, (nb, hkv, 16, d)).astype(np.uint8) for _ in range(2)]
+        self.scale = np.full((nb, hkv, 2), scale, np.float64)
+        self.pool = pool_of(self.codes[0], self.codes[1], self.scale, code)
+
+    def rows(self, n, size=1.0):
+        return [torch.from_numpy(self.rng.standard_normal((n, self.hkv, self.d)) * size).to(self.dtype) for _ in range(2)]
+
+    def put(self, slots, kv, fused=False):
+        slots = np.asarray(slots, np.int32)
+        n = len(slots)
+        on = [t.cuda() for t in kv]
+        if fused:   # slices of one projection behind a query
+            all_ = torch.cat([torch.full((n, 1, self.d), float("nan"), dtype=self.dtype, device="cuda"), *on], 1)
+            on = [all_[:, 1:1 + self.hkv], all_[:, 1 + self.hkv:]]
+        B.pic_kv8_write(self.cfg, self.pool, on[0], on[1], dev(slots))
+        for i in range(2):
+            s = self.scale[..., i]
+            K8.write(self.codes[i], s, f64(kv[i]), slots, self.code)
+        self.same()
+
+    def same(self):
+        torch.cuda.synchronize()
+        assert np.array_equal(self.pool.scale.cpu().numpy().astype(np.float64), self.scale)
+        for t, c in zip((self.pool.k, self.pool.v), self.codes):
+            got = t.cpu().numpy()
+            if not np.array_equal(got, c):
+                at = np.argwhere(got != c)[0]
+                raise AssertionError((at, got[tuple(at)], c[tuple(at)], int((got != c).sum())))
+
+    def check_read(self, slots):
+        slots = np.asarray(slots, np.int32)
+        out = [torch.full((len(slots), self.hkv, self.d), 7.0, dtype=self.dtype, device="cuda") for _ in range(2)]
+        B.pic_kv8_read(self.cfg, self.pool, dev(slots), out[0], out[1])
+        for i in range(2):
+            x = K8.decode(self.codes[i], self.code) * self.scale[..., i][:, :, None, None]
+            ref = np.full((len(slots), self.hkv, self.d), 7.0)
+            for r, s in enumerate(slots):
+                if 0 <= s < self.nb * 16:
+                    ref[r] = x[s // 16, :, s % 16]
+            want = torch.from_numpy(ref).to(torch.float32).to(self.dtype)   # (exact in float32)
+            assert torch.equal(out[i].cpu(), want)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("hkv,d", [(1, 64), (2, 128), (5, 128), (12, 64)])
+def test_write_blocks_that_start(code, dtype, hkv, d):
+    st = Store(9, hkv, d, code, dtype, seed=hkv)
+    for i, n in enumerate((1, 2, 15, 16)):
+        st.put(16 * i + np.arange(n), st.rows(n, 2.0 ** (3 * i)), fused=i % 2 == 1)
+    st.put(64 + np.arange(63), st.rows(63))   # several blocks, the last of them not full
+    st.check_read([0, 1, 33, 64, 126, 143, -1, 144, 70, 70])
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("hkv,d", [(3, 64), (2, 128)])
+def test_write_token_by_token(code, dtype, hkv, d):
+    """Every token behind the others: scales grow, and the rows kept are rounded to them."""
+    st = Store(6, hkv, d, code, dtype, seed=d)
+    order = st.rng.permutation(6)
+    slots = np.concatenate([order[b] * 16 + np.arange(16) for b in range(6)])
+    size = np.exp2(st.rng.integers(-6, 7, len(slots)))
+    for i, s in enumerate(slots[:70]):
+        st.put([s], st.rows(1, size[i]), fused=i % 3 == 0)
+    st.put(slots[70:], st.rows(len(slots) - 70, 100.0))
+    st.check_read(slots)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_write_a_step_of_many_requests(code, dtype):
+    """One token each, blocks in any order, padding rows among them; some start their block."""
+    st = Store(80, 4, 128, code, dtype, seed=3, scale=2.0 ** -5)
+    blocks = st.rng.permutation(80)[:70]
+    slots = blocks * 16 + st.rng.integers(0, 16, 70)
+    slots[::9] = -1
+    slots[5] = 80 * 16
+    slots[6] = 2**31 - 1
+    slots[7] = -2**31
+    st.put(slots, st.rows(70, 3.0))
+    st.check_read(slots)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("hkv,d", [(1, 128), (2, 64)])
+def test_write_long_prompts(code, hkv, d):
+    """More rows than one workgroup looks through, from the middle of blocks on, and padding."""
+    st = Store(160, hkv, d, code, torch.bfloat16, seed=5, scale=0.25)
+    order = st.rng.permutation(160)
+    flat = np.concatenate([order[b] * 16 + np.arange(16) for b in range(160)])
+    slots = np.concatenate([flat[5:1100], [-1, -1, -1], flat[1100 + 4:2400], [-7]])
+    st.put(slots, st.rows(len(slots), 2.0))
+    st.check_read(flat)
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_write_what_is_no_number(code, dtype):
+    """Infinities saturate, NaN is 0, and neither moves a scale; a block of zeros has the smallest."""
+    st = Store(4, 2, 64, code, dtype, seed=1)
+    k, v = st.rows(20)
+    k[3, 0, 5], k[3, 0, 6], k[4, 1, 7] = float("inf"), -float("inf"), float("nan")
+    v[:, 1] = float("nan")
+    v[0, 0] = float("inf")
+    k[16:] = 0.0
+    st.put(np.arange(20), [k, v])
+    st.check_read(np.arange(32))
+    st.put([20], st.rows(1, 1e-3))
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_write_at_the_ends_of_the_type(code, dtype):
+    big = float(torch.finfo(dtype).max)
+    st = Store(8, 1, 64, code, dtype, seed=2)
+    for i, s in enumerate((big, 2.0 ** 120, 448.0, 127.0, 2.0 ** -120, 2.0 ** -126, 1e-39)):
+        k, v = st.rows(3)
+        k = (k.double() / k.double().abs().max() * s).to(dtype)
+        v = torch.full_like(v, s)
+        st.put(16 * i + np.arange(3), [k, v])
+        assert torch.isfinite(st.pool.scale).all()
+    st.check_read(np.arange(8 * 16)[:100])
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_write_ties_go_to_even(code):
+    """Halfway between two codes, with a scale of 1 and with a smaller one."""
+    st = Store(4, 1, 128, code, torch.float32)
+    vals = K8.E4M3_VALUES if code == K8.E4M3 else np.arange(128.0)
+    mid = (vals[1:] + vals[:-1]) / 2
+    row = np.zeros(128)
+    row[:len(mid)] = mid * np.where(np.arange(len(mid)) % 2, 1, -1)
+    row[127] = K8.MOST[code]
+    for b, s in enumerate((1.0, 2.0 ** -7)):
+        x = torch.from_numpy(row * s).float().view(1, 1, 128)
+        st.put([16 * b], [x, -x])
+    assert st.scale[0, 0, 0] == 1.0 and st.scale[1, 0, 1] == 2.0 ** -7
+
+
+def test_write_of_a_slot_twice():
+    """Of rows that follow one another in one slot the last counts (also of more than a wave looks at)."""
+    for n in (2, 5, 64, 65, 200):
+        st = Store(2, 2, 64, K8.INT8, torch.bfloat16, scale=1.0)
+        kv = st.rows(n + 2)
+        st.put(np.concatenate([[17], np.full(n, 18), [19]]), kv)
+
+
+def test_write_keeps_a_scale_that_is_no_power_of_two():
+    """Scales of another program: a call that does not pass them keeps them and the codes."""
+    st = Store(1, 1, 64, K8.INT8, torch.float32, scale=0.3)
+    before = st.pool.k.clone()
+    k, v = st.rows(1)
+    B.pic_kv8_write(st.cfg, st.pool, k.cuda(), v.cuda(), dev(np.array([5], np.int32)))
+    assert (st.pool.scale == np.float32(0.3)).all()
+    other = [o for o in range(16) if o != 5]
+    assert torch.equal(st.pool.k[:, :, other], before[:, :, other])
+    got = st.pool.k[0, 0, 5].cpu().numpy().view(np.int8)
+    assert (np.abs(got * np.float64(np.float32(0.3)) - f64(k)[0, 0]) <= 0.15 * (1 + 1e-5)).all()
+    # ... and a larger row replaces them: half a step of rounding for the row, and one more for those kept
+    B.pic_kv8_write(st.cfg, st.pool, k.cuda() * 1000, v.cuda() * 1000, dev(np.array([6], np.int32)))
+    s = float(st.pool.scale[0, 0, 0])
+    assert s == K8.scale_of(float(k.abs().max() * 1000), K8.INT8)
+    kept = st.pool.k[0, 0, 5].cpu().numpy().view(np.int8) * s
+    assert (np.abs(kept - got * 0.3) <= s / 2 * (1 + 1e-5)).all()
+
+
+# ------------------------------------------------------------------------------------
+# attention
+# ------------------------------------------------------------------------------------
+
+class Batch:
+    """Requests of (cached tokens, new tokens, window start) over a pool of blocks in random order.  Decode: one new
+    token each."""
+
+    def __init__(self, lens, hq=8, hkv=2, d=128, dtype=torch.bfloat16, code=K8.E4M3, style=0, rot=0, prerotated=0, seed=0, positions=None,
+                 inv_freq=None, theta=1e4, powers=True, qscale=1.0, decode=False, flags=None, softmax=0.0):
+        rng = self.rng = np.random.default_rng(seed)
+        self.lens = [(l + (0,))[:3] for l in lens]
+        self.hq, self.hkv, self.d, self.dtype, self.code, self.style, self.rot = hq, hkv, d, dtype, code, style, rot
+        self.prerotated, self.inv_freq, self.theta, self.decode, self.softmax = prerotated, inv_freq, theta, decode, softmax
+        self.cfg = cfg_of(hq, hkv, d, dtype, style, rot, prerotated, theta, softmax, inv_freq)
+        seq, cu, start, fl, win = [], [0], [], [], []
+        for ctx, n, w in self.lens:
+            if ctx:
+                start.append(0), fl.append(B.PIC_PDEP), win.append(-1)
+            start.append(ctx), fl.append(B.PIC_PDEP | B.PIC_QUERY), win.append(w)
+            seq.append(ctx + n)
+            cu.append(len(start))
+        self.host = B.HostBatch(seq, cu, start, fl, win)
+        need = [-(-s // 16) for s in seq]
+        self.nb = sum(need) + 2
+        table = np.full((len(seq), max(need) + 1), 2**30, np.int32)   # (past a request's blocks: never read)
+        ids = rng.permutation(self.nb)
+        for r, k in enumerate(need):
+            table[r, :k], ids = ids[:k], ids[k:]
+        self.table, self.spare = table, ids
+        self.pos = (np.concatenate([np.arange(s) + rng.integers(0, 3000) for s in seq]) if positions is None
+                    else positions(rng, sum(seq))).astype(np.int32)
+        rows = sum(n for _, n, _ in self.lens)
+        self.q = torch.from_numpy(rng.standard_normal((rows, hq, d)) * qscale).to(dtype).cuda()
+        self.set_pool(*random_pool(rng, self.nb, hkv, d, code, powers))
+        self.block_tables, self.positions = dev(table), dev(self.pos)
+        self.ws = torch.empty(max(1, B.pic_attn8_workspace_size(self.cfg, self.host, decode)), dtype=torch.uint8, device="cuda")
+
+    def set_pool(self, k, v, scale):
+        self.k_codes, self.v_codes, self.scale = k, v, np.asarray(scale, np.float32)
+        self.pool = pool_of(k, v, self.scale, self.code)
+
+    def run(self, o=None, stream=None, ws=None, pool=None):
+        o = torch.full_like(self.q, float("nan")) if o is None else o
+        call = B.pic_attn8_decode if self.decode else B.pic_attn8_prefill
+        call(self.cfg, self.host, self.block_tables, self.positions, self.q, o, pool or self.pool, workspace=self.ws if ws is None else ws,
+             stream=stream)
+        return o
+
+    def check(self, got, what=""):
+        """Every output within what its roundings can do.
+
+        A score q.k is off by at most |q||k| scale times the relative errors of q and k as vectors, and by D 2^-24 of
+        the same for its sum.  float32: angles, and one rounding each.  bf16 with rotation: q rounds once to 11
+        bits.  A pair (x, y) of codes, of size n, is turned in 11-bit arithmetic as x c - (y s), y c + (x s): c and s round,
+        the second product rounds, the result rounds: with u = 2^-11 the errors are at most u (|x c| + 2 |y s|) and u (|y c|
+        + 2 |x s|), a vector of at most u n (|c| + 2 |s|) <= sqrt(5) u n, and u n for the results; what rounds below
+        2^-14 (a cos or sin, 2^-25 times 634 at most) less than 2^-15 steps of the code, which is at least 2^-9: the term
+        `low` beside n.  Without rotation q and codes are exact.
+        A relative error e of every probability moves an output by at most e / (1 - e) sum p |v - o|.  Probabilities
+        are rounded to 8 bits at least, outputs to their type.  Both sums over n keys are in 32 bits: n additions, each
+        rounding at most sum p |v| <= |o| + sum p |v - o| to 24 bits; exp2 and joins a few roundings more."""
+        rot = self.rot or self.d
+        k_all, v_all = (K8.decode(c, self.code) * self.scale[..., i].astype(np.float64)[:, :, None, None]
+                        for i, c in enumerate((self.k_codes, self.v_codes)))
+        q, got = f64(self.q), f64(got)
+        row, off, worst, err, norm = 0, 0, 0.0, 0.0, 0.0
+        scale = self.softmax or self.d ** -0.5
+        bf = self.dtype == torch.bfloat16
+        for r, (ctx, n, w) in enumerate(self.lens):
+            L = ctx + n
+            j = np.arange(w, L)
+            k, v = (p[self.table[r, j // 16], :, j % 16] for p in (k_all, v_all))
+            ks = self.scale[self.table[r, j // 16], :, 0].astype(np.float64)
+            qq = q[row:row + n]
+            if not self.prerotated:
+                k = T.rotate(k, self.pos[off + w:off + L], rot, self.theta, self.style, self.inv_freq)
+                qq = T.rotate(qq, self.pos[off + ctx:off + L], rot, self.theta, self.style, self.inv_freq)
+            see = j <= np.arange(ctx, L)[:, None]
+            o, spread = T.attention(qq, k, v, see, scale)
+            low = 0.0
+            if self.prerotated:
+                eq = ek = 0.0 if bf else 2.0 ** -24   # (float32: code times scale, q times the softmax scale)
+            elif bf:
+                eq = 2.0 ** -11 + self.d ** 0.5 * 2.0 ** -24 + ANGLE
+                ek = (5 ** 0.5 + 1) * 2.0 ** -11 + ANGLE_ADVANCED
+                low = self.d ** 0.5 * 2.0 ** -15 * float(ks.max())
+            else:
+                eq = ek = 4 * 2.0 ** -24 + ANGLE
+            nq, nk = np.linalg.norm(qq, axis=-1).max(), np.linalg.norm(k, axis=-1).max() + low
+            ds = nq * nk * scale * (eq + ek + eq * ek + self.d * 2.0 ** -24) + nq * low * scale
+            e = np.expm1(ds) + (2.0 ** -8 if bf else 0.0) + 2.0 ** -20
+            assert e < 0.5, "inputs too large for the bound"
+            sums = (2 * len(j) + 16) * 2.0 ** -24
+            tol = e / (1 - e) * spread + (HALF_STEP[self.dtype] * 1.01 + sums) * (np.abs(o) + spread) + 1e-30
+            d = np.abs(got[row:row + n] - o)
+            assert np.isfinite(got[row:row + n]).all(), (what, r)
+            worst = max(worst, float((d / tol).max()))
+            assert (d <= tol).all(), (what, r, float((d / tol).max()), float(d.max()))
+            err, norm = err + float((d * d).sum()), norm + float((o * o).sum())
+            row, off = row + n, off + L
+        rel = (err / norm) ** 0.5
+        say(f"  {what}: at most {worst:.2f} of the bound, {rel:.2e} of the norm")
+        return rel
+
+
+LENGTHS = [0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 700]
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 64), (16, 1, 128), (7, 1, 64)])
+@pytest.mark.parametrize("ctx", LENGTHS)
+def test_prefill_lengths(hq, hkv, d, dtype, code, ctx):
+    g = hq // hkv
+    # rows that fill, overfill and underfill every size of row tile
+    nodes = sorted({1, 2, max(1, 16 // g), 16 // g + 1, max(1, 32 // g), 32 // g + 1, max(1, 128 // g), 128 // g + 1})
+    for n in nodes:
+        b = Batch([(ctx, n)], hq, hkv, d, dtype, code, style=n % 2, seed=ctx * 131 + n)
+        b.check(b.run(), f"ctx {ctx} new {n}")
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (4, 4, 64), (16, 1, 128), (28, 4, 128), (40, 1, 64), (17, 1, 128)])
+def test_decode_lengths(hq, hkv, d, dtype, code):
+    for ctx in LENGTHS + [3000]:
+        b = Batch([(ctx, 1)], hq, hkv, d, dtype, code, style=ctx % 2, seed=ctx + 7, decode=True)
+        b.check(b.run(), f"ctx {ctx}")
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("style,rot,prerotated", [(0, 0, 0), (1, 0, 0), (0, 32, 0), (0, 16, 0), (1, 34, 0), (1, 2, 0), (0, 0, 1), (0, 64, 1)])
+@pytest.mark.parametrize("d,nodes", [(128, 5), (128, 40), (64, 9), (64, 70)])
+def test_rotations(dtype, style, rot, prerotated, d, nodes, decode):
+    n = (1, 1, 1) if decode else (nodes, 3, 1)
+    b = Batch([(150, n[0]), (290, n[1]), (16, n[2])], 8, 2, d, dtype, K8.E4M3 if nodes % 2 else K8.INT8, style, rot, prerotated, seed=nodes,
+              decode=decode)
+    b.check(b.run(), "rotation")
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+def test_ragged_batches_with_windows(dtype, code, decode):
+    rng = np.random.default_rng(9)
+    for many in (3, 20, 70):   # more spans than the short and the long arguments hold
+        lens = []
+        for _ in range(many):
+            ctx, n = int(rng.integers(0, 400)), 1 if decode else int(rng.integers(1, 90))
+            lens.append((ctx, n, int(rng.integers(0, ctx + 1)) if rng.random() < 0.5 else 0))
+        b = Batch(lens, 12, 4, 64, dtype, code, style=1, seed=many, decode=decode)
+        b.check(b.run(), f"{many} requests")
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_positions_anywhere(dtype, decode):
+    n = 1 if decode else 40
+    far = lambda rng, m: np.arange(m) + 2**31 - 1 - m   # noqa: E731
+    for what, positions in (("random", lambda rng, m: rng.integers(-2**31, 2**31, m)), ("far", far), ("negative", lambda rng, m: -np.arange(m)),
+                            ("jumps", lambda rng, m: np.arange(m) // 48 * 1000 + np.arange(m)), ("one", lambda rng, m: np.full(m, 5)),
+                            ("around", lambda rng, m: np.where(np.arange(m) < 300, 2**31 - 300 + np.arange(m), np.arange(m) - 300 - 2**31))):
+        for d, style in ((128, 0), (64, 1)):
+            b = Batch([(600, n), (128, n)], 8, 2, d, dtype, K8.INT8, style, seed=3, positions=positions, decode=decode)
+            b.check(b.run(), what)
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+def test_scales_of_another_program(dtype, code, decode):
+    """Scales that are no powers of two, zeros among them, and blocks of very different sizes."""
+    n = 1 if decode else 50
+    b = Batch([(260, n), (33, n)], 8, 2, 128, dtype, code, seed=4, powers=False, decode=decode)
+    b.check(b.run(), "any scale")
+    scale = b.scale.copy()
+    scale[::3] = 0.0
+    b.set_pool(b.k_codes, b.v_codes, scale)
+    b.check(b.run(), "zero scales")
+    scale = np.exp2(b.rng.integers(-100, -6, scale.shape)).astype(np.float32)
+    scale[..., 1] = np.exp2(b.rng.integers(-40, 40, scale.shape[:2]))
+    b.set_pool(b.k_codes, b.v_codes, scale)
+    b.check(b.run(), "sizes apart")
+
+
+@pytest.mark.parametrize("decode", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_nothing_else_is_read(dtype, d, decode):
+    """What lies outside the windows holds NaN, in codes and scales, and rows behind a request's last token too."""
+    n = 1 if decode else 45
+    lens = [(200, n, 70), (37, n, 0), (96, n, 96), (500, n, 333)]
+    b = Batch(lens, 8, 2, d, dtype, K8.E4M3, seed=8, decode=decode)
+    want = b.run()
+    b.check(want, "clean")
+    k, v, scale = b.k_codes.copy(), b.v_codes.copy(), b.scale.copy()
+    used = np.zeros((b.nb, 16), bool)
+    for r, (ctx, m, w) in enumerate(lens):
+        j = np.arange(w, ctx + m)
+        used[b.table[r, j // 16], j % 16] = True
+    for c in (k, v):
+        c.swapaxes(1, 2)[~used] = 0x7f
+    scale[~used.any(1)] = np.nan
+    got = b.run(pool=pool_of(k, v, scale, b.code))
+    assert torch.equal(got, want)
+
+
+def test_long_context_and_splits():
+    for hq, hkv, n, decode in ((8, 1, 1, True), (32, 8, 1, True), (8, 1, 3, False), (16, 2, 40, False)):
+        b = Batch([(20000, n)], hq, hkv, 128, torch.bfloat16, K8.INT8, seed=n, decode=decode)
+        b.check(b.run(), f"20,000 keys, {n} new")
+
+
+def test_spread_of_a_large_softmax_scale():
+    """Row maxima that move again and again."""
+    for decode, n in ((True, 1), (False, 60)):
+        b = Batch([(900, n)], 8, 2, 128, torch.float32, K8.INT8, seed=6, softmax=2.0, decode=decode, qscale=0.5)
+        b.check(b.run(), "float32")
+        b = Batch([(900, n)], 8, 2, 128, torch.bfloat16, K8.INT8, prerotated=1, seed=6, softmax=2.0, decode=decode, qscale=0.5)
+        b.check(b.run(), "bf16")
