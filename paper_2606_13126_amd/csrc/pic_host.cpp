@@ -261,11 +261,11 @@ TreeSplit tree_split(HostPlan& hp, int G, int hkv) {
 }
 
 // Row tiles and key splits of a call over 8-bit codes in bf16: tiles of 16 rows where every (span, KV head)
-// has no more, else of 32; chunks of about the average work per compute unit, at least one step of keys.
+// has no more, of 32 and 128 likewise, else of 256; chunks of about the average work per compute unit, at least one step of keys.
 void kv8_split(HostPlan& hp, int G, int hkv) {
     int64_t most = 0;
     for (auto& g : hp.groups) most = std::max<int64_t>(most, (int64_t)g.n_tok * G);
-    hp.tree_rows = most <= 16 ? 16 : 32;
+    hp.tree_rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 128 ? 128 : 256;
     const int64_t tr = hp.tree_rows, tk = pic::kv8_keys(hp.tree_rows);
     int64_t total = 0;
     for (auto& g : hp.groups)

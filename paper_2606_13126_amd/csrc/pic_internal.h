@@ -243,7 +243,7 @@ struct Kv8Args : Args {
 constexpr int kCodeE4m3 = 0, kCodeInt8 = 1;
 
 // Its bf16 workgroups: eight waves.  With 16 or 32 query rows the waves all hold the same ones and take
-// different cache blocks.
+// different cache blocks; with 128 or 256 they hold 32 each and share keys, 64 at a time.
 constexpr int kKv8Waves = 8;
 constexpr int kv8_keys(int rows) { return rows <= 32 ? kKv8Waves * kBlock : 64; }   // keys that they take at a time
 

@@ -4,7 +4,7 @@
 //               pool holds turned keys.
 //  * kv8_write  key and value rows into the pool as codes and a scale per block and head.
 //  * kv8_read   rows of the pool as numbers.
-//  * kv8_few    attention over the codes in bf16; kv8_merge joins its key splits.  (float32: attn_f32
+//  * kv8_few, kv8_many  attention over the codes in bf16; kv8_merge joins their key splits.  (float32: attn_f32
 //               over Kv8Args, in pic_kernels.hip)
 //
 // Pools: codes [num_blocks][Hkv][16][D], one byte each, and scales [num_blocks][Hkv][2].  An
@@ -37,17 +37,38 @@ __device__ __forceinline__ float sum_of(float x) {
 // ---------------------------------------------------------------------------------
 // qk_norm: one workgroup per row; a unit is two 16-byte chunks of a head, NeoX the two runs whose
 // elements pair up, GPT-J (and what does not turn) two neighbours.  The lanes of a head are
-// neighbours, so its squares meet by lane permutes; a thread's units lie on the same pairs of
-// different heads, so it computes their cos/sin and reads their weights once.
+// neighbours, so its squares meet by lane permutes.  The row's threads put its cos/sin and the weights into
+// LDS once, while its first units are on their way.
 // Bound by memory: every element is read and written once.
 // ---------------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
 
+// the elements of a 16-byte chunk as float32, and back (rounded to nearest even)
+template <typename T>
+__device__ __forceinline__ void unpack_chunk(const u32x4_t& w, float* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t u = w[i];
+        if constexpr (sizeof(T) == 4) {
+            f[i] = __uint_as_float(u);
+        } else {
+            f[2 * i] = bf_lo(u);
+            f[2 * i + 1] = bf_hi(u);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ u32x4_t pack_chunk(const float* f) {
+    u32x4_t w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(f[i]) : pack_bf16(f[2 * i], f[2 * i + 1]);
+    return w;
+}
+
 template <typename T, int D, int STYLE, bool ROT>
 __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a) {
     constexpr int PP = 16 / sizeof(T);     // elements per chunk, pairs per unit
-    constexpr int CH = D / PP, UPH = CH / 2, U = 4;
-    typedef T vec_t __attribute__((ext_vector_type(PP)));
+    constexpr int CH = D / PP, UPH = CH / 2, U = 3;
     const int64_t row = blockIdx.x;
     const int unit = (int)threadIdx.x % UPH, step = (int)blockDim.x / UPH;
     const int rc = a.rot_half / PP;        // chunks of a half that turns (NeoX: rot_half is a multiple of 8)
@@ -55,37 +76,39 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a)
     // a turning unit's chunks, and any other's
     const int c0 = STYLE == kNeox ? (turns ? unit : 2 * rc + 2 * (unit - rc)) : 2 * unit;
     const int c1 = STYLE == kNeox && turns ? unit + rc : c0 + 1;
-    const vec_t* qr = static_cast<const vec_t*>(a.q) + row * a.q_stride;
-    const vec_t* kr = static_cast<const vec_t*>(a.k) + row * a.k_stride;
-    vec_t* qo = static_cast<vec_t*>(a.q_out) + row * a.q_out_stride;
-    vec_t* ko = static_cast<vec_t*>(a.k_out) + row * a.k_out_stride;
+    const u32x4_t* qr = static_cast<const u32x4_t*>(a.q) + row * a.q_stride;
+    const u32x4_t* kr = static_cast<const u32x4_t*>(a.k) + row * a.k_stride;
+    u32x4_t* qo = static_cast<u32x4_t*>(a.q_out) + row * a.q_out_stride;
+    u32x4_t* ko = static_cast<u32x4_t*>(a.k_out) + row * a.k_out_stride;
     const int heads = a.hq + a.hkv;
-    float c[PP], s[PP];
-    vec_t w[2][2];                         // weights of q and k
+    __shared__ __attribute__((aligned(16))) float weight[2][D];
+    __shared__ float2 cs[ROT ? D / 2 : 1];
     bool first = true;
     // (whole groups of UPH lanes take the same turns, so the lanes of a head are all there)
-    for (int h0 = (int)threadIdx.x / UPH; h0 < heads; h0 += U * step) {
-        vec_t x[U], y[U];
+    for (int h0 = (int)threadIdx.x / UPH; first || h0 < heads; h0 += U * step) {
+        u32x4_t x[U], y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * step;
-            if (h >= heads) break;
-            const vec_t* src = h < a.hq ? qr + h * CH : kr + (h - a.hq) * CH;
+            const int h = min(h0 + u * step, heads - 1);   // (past the last head: read, not stored)
+            const u32x4_t* src = h < a.hq ? qr + h * CH : kr + (h - a.hq) * CH;
             x[u] = src[c0];
             y[u] = src[c1];
         }
         if (first) {
-            const vec_t* from[2] = {static_cast<const vec_t*>(a.q_weight), static_cast<const vec_t*>(a.k_weight)};
+            for (int i = threadIdx.x; i < 2 * CH; i += blockDim.x) {
+                const u32x4_t* from = static_cast<const u32x4_t*>(i < CH ? a.q_weight : a.k_weight);
+                float f[PP];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                w[i][0] = from[i] ? from[i][c0] : vec_t((T)1.f);
-                w[i][1] = from[i] ? from[i][c1] : vec_t((T)1.f);
+                for (int k = 0; k < PP; ++k) f[k] = 1.f;
+                if (from != nullptr) unpack_chunk<T>(from[i % CH], f);
+#pragma unroll
+                for (int k = 0; k < PP; ++k) weight[i / CH][i % CH * PP + k] = f[k];
             }
-            if (turns) {
+            if (ROT) {
                 const int32_t pos = a.positions[row];
-#pragma unroll
-                for (int k = 0; k < PP; ++k) rope_cs(pos, a.fstep[unit * PP + k], c[k], s[k]);
+                for (int i = threadIdx.x; i < a.rot_half; i += blockDim.x) rope_cs(pos, a.fstep[i], cs[i].x, cs[i].y);
             }
+            barrier_keep_vmem();
             first = false;
         }
 #pragma unroll
@@ -93,33 +116,28 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a)
             const int h = h0 + u * step;
             if (h >= heads) break;
             float f[2 * PP], sum = 0.f;
+            unpack_chunk<T>(x[u], f);
+            unpack_chunk<T>(y[u], f + PP);
 #pragma unroll
-            for (int k = 0; k < 2 * PP; ++k) {
-                f[k] = (float)(k < PP ? x[u][k] : y[u][k - PP]);
-                sum = __builtin_fmaf(f[k], f[k], sum);
-            }
-            const float r = 1.f / sqrtf(sum_of<UPH>(sum) * (1.f / D) + a.eps);
-            const int i = h < a.hq ? 0 : 1;
+            for (int k = 0; k < 2 * PP; ++k) sum = __builtin_fmaf(f[k], f[k], sum);
+            const float r = __builtin_amdgcn_rsqf(fmaxf(sum_of<UPH>(sum) * (1.f / D) + a.eps, 0x1p-126f));   // (within an ulp; not of a denormal)
+            const float* w = weight[h < a.hq ? 0 : 1];
 #pragma unroll
-            for (int k = 0; k < 2 * PP; ++k) f[k] *= r * (float)(i ? w[1][k / PP][k % PP] : w[0][k / PP][k % PP]);
+            for (int k = 0; k < 2 * PP; ++k) f[k] *= r * w[(k < PP ? c0 : c1) * PP + k % PP];
             if (turns)
 #pragma unroll
                 for (int k = 0; k < PP; ++k) {
                     if (STYLE != kNeox && unit * PP + k >= a.rot_half) break;
+                    const float2 t = cs[unit * PP + k];
                     float& p = f[STYLE == kNeox ? k : 2 * k];
-                    float& t = f[STYLE == kNeox ? PP + k : 2 * k + 1];
-                    const float e = p, g = t;
-                    p = __builtin_fmaf(e, c[k], -(g * s[k]));
-                    t = __builtin_fmaf(e, s[k], g * c[k]);
+                    float& s = f[STYLE == kNeox ? PP + k : 2 * k + 1];
+                    const float p0 = p, s0 = s;
+                    p = __builtin_fmaf(p0, t.x, -(s0 * t.y));
+                    s = __builtin_fmaf(p0, t.y, s0 * t.x);
                 }
-#pragma unroll
-            for (int k = 0; k < PP; ++k) {
-                x[u][k] = (T)f[k];
-                y[u][k] = (T)f[PP + k];
-            }
-            vec_t* dst = h < a.hq ? qo + h * CH : ko + (h - a.hq) * CH;
-            dst[c0] = x[u];
-            dst[c1] = y[u];
+            u32x4_t* dst = h < a.hq ? qo + h * CH : ko + (h - a.hq) * CH;
+            dst[c0] = pack_chunk<T>(f);
+            dst[c1] = pack_chunk<T>(f + PP);
         }
     }
 }
@@ -167,21 +185,27 @@ struct Code {
         }
     }
     // ... as two words of float16 (exact)
-    static __device__ __forceinline__ u32x2_t halves(uint32_t w) {
+    static __device__ __forceinline__ uint32_t halves_lo(uint32_t w) { return half2_of<false>(w); }
+    static __device__ __forceinline__ uint32_t halves_hi(uint32_t w) { return half2_of<true>(w); }
+    template <bool HI>
+    static __device__ __forceinline__ uint32_t half2_of(uint32_t w) {
         if constexpr (CODE == kCodeE4m3) {
-            const f16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true);
-            return u32x2_t{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+            const f16x2_t x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, HI);
+            return __builtin_bit_cast(uint32_t, x);
         } else {
             // 0x64uu is 1024 + u: with u = code + 128, less 1152
-            const uint32_t u = w ^ 0x80808080u;
             const f16x2_t off = {(_Float16)-1152.f, (_Float16)-1152.f};
-            const f16x2_t lo = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
-            const f16x2_t hi = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
-            return u32x2_t{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+            const uint32_t u = __builtin_amdgcn_perm(0x64646464u, w ^ 0x80808080u, HI ? 0x04030402u : 0x04010400u);
+            const f16x2_t x = __builtin_bit_cast(f16x2_t, u) + off;
+            return __builtin_bit_cast(uint32_t, x);
         }
     }
     // ... as two words of bf16 (exact: an upper half of a float32 holds 8 bits)
     static __device__ __forceinline__ u32x2_t bf16s(uint32_t w) {
+        if constexpr (CODE == kCodeE4m3) {
+            const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true);
+            return u32x2_t{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        }
         const f32x4_t x = decode(w);
         return u32x2_t{__builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u),
                        __builtin_amdgcn_perm(__float_as_uint(x[3]), __float_as_uint(x[2]), 0x07060302u)};
@@ -323,11 +347,11 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
             const int64_t i = i0 + u * step;
             in[u] = false;
             if (i >= n_units) break;
-            const int64_t rh = i / CPR;
-            const int32_t slot = slots[rh / hkv];
+            const int64_t rh = i / CPR, row = rh <= UINT32_MAX ? (uint32_t)rh / (uint32_t)hkv : rh / hkv;
+            const int32_t slot = slots[row];
             if (slot < 0 || slot >= n_slots) continue;
             in[u] = true;
-            const int64_t page = (int64_t)(slot >> 4) * hkv + rh % hkv;
+            const int64_t page = (int64_t)(slot >> 4) * hkv + (rh - row * hkv);
             const int64_t at = (page * kBlock + (slot & 15)) * D + (i % CPR) * V;
             w[u][0] = *reinterpret_cast<const word_t*>(k_pool + at);
             w[u][1] = *reinterpret_cast<const word_t*>(v_pool + at);
@@ -370,7 +394,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
 // ---------------------------------------------------------------------------------
 constexpr int kKv8Renew = 32;
 
-template <int D>
+template <int D, int CB>
 struct Kv8Few {
     static constexpr int NW = kKv8Waves, TK = kBlock;
     static constexpr int STEP = NW * TK;         // keys of all waves
@@ -378,15 +402,18 @@ struct Kv8Few {
     static constexpr int CPR = D / 16;           // 16-byte chunks per row
     static constexpr int KPC = 64 / CPR;         // keys of a copy (64 chunks)
     static constexpr int NC = TK / KPC;          // copies of a step, each of K and V
-    static constexpr int NST = 4;                // steps in LDS
+    static constexpr int NST = D == 64 || CB > 1 ? 4 : 2;   // steps in LDS
+    static constexpr int WAVES = CB > 1 ? 2 : 4; // per SIMD
     static constexpr int LPS = 2 * NC + 1;       // copies per lane per step
     static constexpr int META = 20;              // a step's positions (16) and its two scales
 };
 
-template <int D>
+template <int D, int CB>
 struct __attribute__((aligned(16))) Kv8FewLds {
-    typedef Kv8Few<D> S;
+    typedef Kv8Few<D, CB> S;
     uint8_t stages[S::NST][S::NW][2][S::TILE];
+    uint16_t q[CB][D / 32][64][8];               // B operands: words of 4 pairs of the lanes, x then y
+    float qs[16 * CB];
     float2 stride_cs[D / 2];                     // cos/sin of STEP positions
     uint64_t fstep[D / 2];
     int32_t meta[S::NW][S::NST][S::META];
@@ -404,15 +431,15 @@ __device__ __forceinline__ int vswz(int key) { return D == 128 ? ((key >> 1) & 3
 __device__ __forceinline__ int query_exponent(float big) { return big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0; }
 
 template <int D, int STYLE, bool ROPE, int CODE, int CB, int NG>
-__global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> plan, const Kv8Args a) {
-    typedef Kv8Few<D> S;
+__global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_few(const PlanOf<NG> plan, const Kv8Args a) {
+    typedef Kv8Few<D, CB> S;
     typedef Code<CODE> C;
     constexpr int KD = D / 32;             // 16x16x32 contraction steps of QK^T; words of 4 pairs of a lane
     constexpr int DB = D / 32;             // 32-dim blocks of O^T
     constexpr int TK = S::TK, NW = S::NW, NST = S::NST, HALF = D / 2, PL = 4 * KD;
     static_assert(S::TILE * 2 * NST >= CB * 2 * DB * 1024, "a wave's outputs fit its stages");
 
-    __shared__ Kv8FewLds<D> lds;
+    __shared__ Kv8FewLds<D, CB> lds;
     __shared__ float2 mls[NW][16 * CB];
 
     const Group g = group_of<false>(plan, blockIdx.x);
@@ -442,20 +469,31 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
     // the wave's copies of step u into stage st: a lane's 16 bytes are one chunk of one key, and a key outside
     // the range stands for the nearest one inside, so that nothing outside it is read (its score is masked)
     auto near_key = [&](int k) { return min(max(k, k_lo), k_hi - 1); };
+    int k_from[S::NC], v_from[S::NC];
+#pragma unroll
+    for (int i = 0; i < S::NC; ++i) {
+        const int key = i * S::KPC + lane / S::CPR, c = lane % S::CPR;
+        k_from[i] = key * D + ((c ^ kswz<D>(key)) << 4);
+        v_from[i] = key * D + ((c ^ vswz<D>(key)) << 4);
+    }
     auto issue = [&](int u, int st, int blk) {
         const int k0 = u * S::STEP + wave * TK;
         const uint32_t to = stages_at + (uint32_t)((st * NW + wave) * 2 * S::TILE);
         __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));   // the stage's last reads have returned
         const size_t at = (size_t)(uint32_t)blk * a.hkv * page;
+        const bool whole = k0 >= k_lo && k0 + TK <= k_hi;   // the tile needs no nearest keys
 #pragma unroll
         for (int i = 0; i < S::NC; ++i) {
-            const int key = i * S::KPC + lane / S::CPR, c = lane % S::CPR;
-            const int row = (near_key(k0 + key)) & (TK - 1);
-            copy_lds16(kpool + at, (uint32_t)(row * D + ((c ^ kswz<D>(key)) << 4)), to + i * 1024);
-            copy_lds16(vpool + at, (uint32_t)(row * D + ((c ^ vswz<D>(key)) << 4)), to + S::TILE + i * 1024);
+            int moved = 0;
+            if (!whole) {
+                const int key = k0 + i * S::KPC + lane / S::CPR;
+                moved = ((near_key(key) & (TK - 1)) - (key & (TK - 1))) * D;
+            }
+            copy_lds16(kpool + at, (uint32_t)(k_from[i] + moved), to + i * 1024);
+            copy_lds16(vpool + at, (uint32_t)(v_from[i] + moved), to + S::TILE + i * 1024);
         }
         if (lane < 18) {
-            const void* src = lane < 16 ? (const void*)(posv + near_key(k0 + lane))
+            const void* src = lane < 16 ? (const void*)(posv + (whole ? k0 + lane : near_key(k0 + lane)))
                                         : (const void*)(a.scale + ((size_t)(uint32_t)blk * a.hkv + ic.kvh) * 2 + (lane - 16));
             copy_lds4(src, meta_at + (uint32_t)(st * S::META * 4));
         }
@@ -470,72 +508,90 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
             lds.fstep[i] = a.fstep[i];
             rope_cs_fast(S::STEP, a.fstep[i], lds.stride_cs[i].x, lds.stride_cs[i].y);
         }
-    __syncthreads();   // phase steps staged
 
-    // pair e of word i of the lane's (4 pairs each); its elements as they come from the chunks of a row
-    auto pair_of = [&](int i, int e) { return STYLE == kNeox ? 8 * ((i / 2) * 4 + q4) + 4 * (i % 2) + e : 4 * (i * 4 + q4) + e; };
+    // the lane's pair i (words of 4 pairs): pair0 + pair_at(i)
+    const int pair0 = (STYLE == kNeox ? 8 : 4) * q4;
+    auto pair_at = [](int i) { return STYLE == kNeox ? i / 8 * 32 + i % 8 : i / 4 * 16 + i % 4; };
+    const uint64_t* fs = lds.fstep + pair0;
+    const float2* ahead = lds.stride_cs + pair0;
 
-    // ---- queries: B operand, turned at their tokens' positions
-    u32x4_t qb[CB][KD];
-    float qs[CB];     // scores are the products times this and the block's scale (log2 units)
+    // ---- queries: the waves turn 2 CB rows each, LPR lanes a row, and leave the B operands of all in LDS
+    // (from where every tile reads them: in registers they would leave room for two waves per SIMD only)
     int last[CB];     // last key that the lane's row sees, from kt0
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
         const int row = row_lo + 16 * cb + c16;
+        last[cb] = min(k_hi - 1, g.tok0 + (row < rows_total ? row / G : 0) - kt0);
+    }
+    {
+        constexpr int LPR = 32 / CB, PP = HALF / LPR;   // lanes of a row, pairs of a lane
+        static_assert(NW * 64 == 16 * CB * LPR && PP <= 4, "every lane has a part of a row");
+        typedef uint16_t part_t __attribute__((ext_vector_type(PP)));
+        const int r = (wave * 64 + lane) / LPR, p0 = lane % LPR * PP, row = row_lo + r;
         const bool valid = row < rows_total;
         const int to = valid ? row / G : 0, hl = valid ? row - to * G : 0;
-        last[cb] = min(k_hi - 1, g.tok0 + to - kt0);
+        // two runs of PP elements: NeoX the pairs' x and y, GPT-J one after the other
+        const int e[2] = {STYLE == kNeox ? p0 : 2 * p0, STYLE == kNeox ? p0 + HALF : 2 * p0 + PP};
         const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + to) * a.hq + (size_t)ic.kvh * G + hl) * D;
-        u32x4_t raw[KD];
+        uint16_t in[2 * PP];
 #pragma unroll
-        for (int kd = 0; kd < KD; ++kd) {
-            raw[kd] = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, kd * 4 + q4) * 8);
-            if (!valid) raw[kd] = u32x4_t{0, 0, 0, 0};
-        }
-        float x[PL], y[PL], big = 0.f;
+        for (int h = 0; h < 2; ++h) {
+            const part_t w = *reinterpret_cast<const part_t*>(qp + model_chunk(a.chunk_map, e[h] >> 3) * 8 + (e[h] & 7));
 #pragma unroll
-        for (int i = 0; i < KD; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                auto el = [&](int kd, int k) { return k % 2 ? bf_hi(raw[kd][k / 2]) : bf_lo(raw[kd][k / 2]); };
-                x[4 * i + e] = STYLE == kNeox ? el(i / 2, 4 * (i % 2) + e) : el(i, 2 * e);
-                y[4 * i + e] = STYLE == kNeox ? el(KD / 2 + i / 2, 4 * (i % 2) + e) : el(i, 2 * e + 1);
+            for (int k = 0; k < PP; ++k) {
+                if constexpr (PP == 1) in[h] = w[0];
+                else in[h * PP + k] = w[k];
             }
-        qs[cb] = a.scale_log2;
+        }
+        const int32_t pos = ROPE ? a.positions[g.pos_off + g.tok0 + to] : 0;
+        __syncthreads();   // phase steps staged
+        float x[PP], y[PP], big = 0.f;
+#pragma unroll
+        for (int k = 0; k < PP; ++k) {
+            x[k] = valid ? __uint_as_float((uint32_t)in[STYLE == kNeox ? k : 2 * k] << 16) : 0.f;
+            y[k] = valid ? __uint_as_float((uint32_t)in[STYLE == kNeox ? PP + k : 2 * k + 1] << 16) : 0.f;
+        }
+        float scale = a.scale_log2;
+        int ex = 0;
         if (ROPE) {
-            const int32_t pos = a.positions[g.pos_off + g.tok0 + to];
 #pragma unroll
-            for (int i = 0; i < KD; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float c, s;
-                    rope_cs_fast(pos, lds.fstep[pair_of(i, e)], c, s);
-                    float& u = x[4 * i + e];
-                    float& v = y[4 * i + e];
-                    const float u0 = u, v0 = v;
-                    u = u0 * c - v0 * s;
-                    v = v0 * c + u0 * s;
-                    big = fmaxf(big, fmaxf(fabsf(u), fabsf(v)));
-                }
-            const int ex = query_exponent(max_xor32(max_xor16(big)));
-            qs[cb] = ldexpf(qs[cb], ex);
-#pragma unroll
-            for (int i = 0; i < PL; ++i) {
-                x[i] = ldexpf(x[i], -ex);
-                y[i] = ldexpf(y[i], -ex);
+            for (int k = 0; k < PP; ++k) {
+                float c, s;
+                rope_cs_fast(pos, lds.fstep[p0 + k], c, s);
+                const float x0 = x[k], y0 = y[k];
+                x[k] = x0 * c - y0 * s;
+                y[k] = y0 * c + x0 * s;
+                big = fmaxf(big, fmaxf(fabsf(x[k]), fabsf(y[k])));
             }
+            big = max_of8(big);
+            big = fmaxf(big, __shfl_xor(big, 8));
+            if (LPR == 32) big = max_xor16(big);
+            ex = query_exponent(big);
+            scale = ldexpf(scale, ex);
         }
+        part_t xo, yo;
 #pragma unroll
-        for (int i = 0; i < KD; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                qb[cb][i][h] = ROPE ? pack_f16(x[4 * i + 2 * h], x[4 * i + 2 * h + 1]) : pack_bf16(x[4 * i + 2 * h], x[4 * i + 2 * h + 1]);
-                qb[cb][i][2 + h] = ROPE ? pack_f16(y[4 * i + 2 * h], y[4 * i + 2 * h + 1]) : pack_bf16(y[4 * i + 2 * h], y[4 * i + 2 * h + 1]);
-            }
+        for (int k = 0; k < PP; ++k) {
+            const uint16_t xb = ROPE ? __builtin_bit_cast(uint16_t, (_Float16)ldexpf(x[k], -ex)) : (uint16_t)(__float_as_uint(x[k]) >> 16);
+            const uint16_t yb = ROPE ? __builtin_bit_cast(uint16_t, (_Float16)ldexpf(y[k], -ex)) : (uint16_t)(__float_as_uint(y[k]) >> 16);
+            xo[k] = xb;
+            yo[k] = yb;
+        }
+        // pairs p0 .. p0 + PP - 1 belong to word i of the lanes 16 qq ..
+        const int i = STYLE == kNeox ? (p0 >> 5) * 2 + ((p0 >> 2) & 1) : p0 >> 4, qq = STYLE == kNeox ? (p0 >> 3) & 3 : (p0 >> 2) & 3;
+        uint16_t* to_lds = &lds.q[r >> 4][i][16 * qq + (r & 15)][p0 & 3];
+        *reinterpret_cast<part_t*>(to_lds) = xo;
+        *reinterpret_cast<part_t*>(to_lds + 4) = yo;
+        if (lane % LPR == 0) lds.qs[r] = scale;
     }
+    barrier_keep_vmem();
+    float qs[CB];     // scores are the products times this and the block's scale (log2 units)
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) qs[cb] = lds.qs[16 * cb + c16];
 
     // per-lane byte offsets within a tile: the K operand's 8 codes of each chunk, the V operand's pieces
-    int k_off[KD], v_off[DB];
+    // (of block db of the dimensions: by xor)
+    int k_off[KD], v_off;
 #pragma unroll
     for (int kd = 0; kd < KD; ++kd) {
         const int c8 = model_chunk(a.chunk_map, kd * 4 + q4);
@@ -543,9 +599,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
     }
     {
         const int key = 4 * q4 + (c16 >> 2);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-            v_off[db] = S::TILE + key * D + (((2 * db + ((c16 >> 1) & 1)) ^ vswz<D>(key)) << 4) + (c16 & 1) * 8;
+        v_off = S::TILE + key * D + ((((c16 >> 1) & 1) ^ vswz<D>(key)) << 4) + (c16 & 1) * 8;
     }
 
     f32x4_t acc[CB][2 * DB];   // even and odd dimensions of each block
@@ -579,18 +633,21 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
 #pragma unroll
         for (int kd = 0; kd < KD; ++kd) kw[kd] = *reinterpret_cast<const u32x2_t*>(tile + k_off[kd]);
         const float ks = __int_as_float(meta[16]), vs = __int_as_float(meta[17]);
-        u32x4_t kf[KD];
+        f32x4_t sc[CB];
         if constexpr (ROPE) {
             const int32_t pos = meta[c16];
             // (STEP on, and not past the type's end)
             if (renew == 0 || __builtin_amdgcn_ballot_w64((uint32_t)pos != (uint32_t)cs_pos + S::STEP || pos < cs_pos) != 0) {
 #pragma unroll
-                for (int i = 0; i < PL; ++i) rope_cs_fast(pos, lds.fstep[pair_of(i / 4, i % 4)], rc[i], rs[i]);
+                for (int i = 0; i < PL; ++i) {
+                    rope_cs_fast(pos, fs[pair_at(i)], rc[i], rs[i]);
+                    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (side by side they would take more registers than there are)
+                }
                 renew = kKv8Renew;
             } else {
 #pragma unroll
                 for (int i = 0; i < PL; ++i) {
-                    const float2 d = lds.stride_cs[pair_of(i / 4, i % 4)];
+                    const float2 d = ahead[pair_at(i)];
                     const float c = rc[i], s = rs[i];
                     rc[i] = c * d.x - s * d.y;
                     rs[i] = s * d.x + c * d.y;
@@ -602,6 +659,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
 #pragma unroll
         for (int i = 0; i < KD; ++i) {
             uint32_t xw, yw;   // codes of the x and y of 4 pairs
+            u32x4_t kf;
             if (STYLE == kNeox) {
                 xw = kw[i / 2][i % 2];
                 yw = kw[KD / 2 + i / 2][i % 2];
@@ -610,32 +668,30 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
                 yw = __builtin_amdgcn_perm(kw[i][1], kw[i][0], 0x07050301u);
             }
             if constexpr (ROPE) {
-                const u32x2_t xh = C::halves(xw), yh = C::halves(yw);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t xb = xh[h], yb = yh[h];   // (a bit cast of a vector's element would read its first)
+                    const uint32_t xb = h ? C::halves_hi(xw) : C::halves_lo(xw), yb = h ? C::halves_hi(yw) : C::halves_lo(yw);
                     const f16x2_t x = __builtin_bit_cast(f16x2_t, xb), y = __builtin_bit_cast(f16x2_t, yb);
                     const int p = 4 * i + 2 * h;
                     const f16x2_t c = __builtin_bit_cast(f16x2_t, pack_f16(rc[p], rc[p + 1])), s = __builtin_bit_cast(f16x2_t, pack_f16(rs[p], rs[p + 1]));
-                    kf[i][h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, c, -(y * s)));
-                    kf[i][2 + h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, c, x * s));
+                    kf[h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, c, -(y * s)));
+                    kf[2 + h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, c, x * s));
                 }
             } else {
                 const u32x2_t xb = C::bf16s(xw), yb = C::bf16s(yw);
-                kf[i] = u32x4_t{xb[0], xb[1], yb[0], yb[1]};
+                kf = u32x4_t{xb[0], xb[1], yb[0], yb[1]};
             }
-        }
-        f32x4_t sc[CB];
-#pragma unroll
-        for (int i = 0; i < KD; ++i)
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
                 const f32x4_t from = i == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[cb];
+                const u32x4_t qb = *reinterpret_cast<const u32x4_t*>(lds.q[cb][i][lane]);
                 if (ROPE)
-                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kf[i]), __builtin_bit_cast(f16x8_t, qb[cb][i]), from, 0, 0, 0);
+                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kf), __builtin_bit_cast(f16x8_t, qb), from, 0, 0, 0);
                 else
-                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), __builtin_bit_cast(bf16x8_t, qb[cb][i]), from, 0, 0, 0);
+                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qb), from, 0, 0, 0);
             }
+            if (CB == 1) __builtin_amdgcn_sched_barrier(0);   // (side by side the words would take more registers than there are)
+        }
         const bool masked = k0 < k_lo || k0 + TK > min(k_hi, g.tok0 + row_lo / G + 1 - kt0);   // some row may not see some key
         float mx[CB];
         bool moves = false;
@@ -650,7 +706,6 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
                 }
             }
             mx[cb] = fmaxf(fmaxf(sc[cb][0], sc[cb][1]), fmaxf(sc[cb][2], sc[cb][3]));
-            mx[cb] = max_xor32(max_xor16(mx[cb]));
             moves |= mx[cb] > m_run[cb] + 8.f;
         }
         // the reference maximum only moves when some row's maximum grows by more than 8
@@ -658,7 +713,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
         if (__builtin_amdgcn_ballot_w64(moves) != 0) {
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                const float m_new = fmaxf(m_run[cb], mx[cb]);
+                const float m_new = fmaxf(m_run[cb], max_xor32(max_xor16(mx[cb])));
                 const float alpha = __builtin_amdgcn_exp2f(m_run[cb] - m_new);
                 l_run[cb] *= alpha;
 #pragma unroll
@@ -684,7 +739,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
         }
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-            const u32x2_t both = __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(tile + v_off[db])));
+            const u32x2_t both = __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(tile + (v_off ^ (32 * db)))));
 #pragma unroll
             for (int odd = 0; odd < 2; ++odd) {
                 const u32x2_t v = C::bf16s(__builtin_amdgcn_perm(both[1], both[0], odd ? 0x07050301u : 0x06040200u));
@@ -749,6 +804,465 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_few(const PlanOf<NG> pl
     }
 }
 
+// ---------------------------------------------------------------------------------
+// kv8_many: attention in bf16, 32 WR query rows (128 or 256) per workgroup of eight waves, in steps of 64
+// keys that all waves share: WR row groups of KG = 8 / WR waves, which take 32 keys of a step at a time.
+//   S^T (32 keys x 32 rows) = K Q^T       v_mfma_f32_32x32x16_f16 (bf16 without rotation)
+//   O^T (32 dims x 32 rows) += V^T P^T    v_mfma_f32_32x32x16_bf16, V^T by ds_read_b64_tr_b16
+// After the scores lane l holds row l%32 and keys 8 (j/4) + 4 (l/32) + j%4, the B operand of the
+// output product.  A wave loads the codes of eight keys of a step into registers, a step and a half ahead, and
+// turns them into float16 (keys) and bf16 (values) in LDS one step ahead, beside the products of the scores;
+// two LDS buffers, one barrier per step.  LDS rows hold the x of all pairs, then the y, in either pairing.
+//
+// The scales cost a few operations a step: the scores of a block's keys are multiplied in the addition that
+// the exponential needs anyway, and the values' scale joins its exponent: p' = 2^(s - m + log2 v).
+// The row sum adds the p' of a block, rounded to bf16 as they are multiplied, times 1 / v.
+// ---------------------------------------------------------------------------------
+constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
+
+template <int D>
+struct __attribute__((aligned(2 * D))) Kv8ManyLds {
+    uint16_t kv[2][2][64 * D];   // [buffer][keys, values], 16-byte chunks swizzled by key
+    float2 stride_cs[D / 2];     // cos/sin of 64 positions
+    uint64_t fstep[D / 2];
+    float4 sc[2][4];             // per block of a step: its keys' scale, log2 and inverse of its values' scale
+};
+
+template <int D, int STYLE, bool ROPE, int CODE, int WR, int NG>
+__global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> plan, const Kv8Args a) {
+    typedef Code<CODE> C;
+    constexpr int NW = kKv8Waves, KG = NW / WR, STEP = 64, HALF = D / 2;
+    constexpr int KD = D / 16;             // 32x32x16 contraction steps of QK^T
+    constexpr int DB = D / 32;             // 32-dim blocks of O^T
+    constexpr int PL = D / 16;             // pairs that a lane turns
+    constexpr int KW = PL / 4, VW = D / 32;   // words of codes of a lane: either run of its key, its value
+    static_assert(KG == 1 || KG == 2, "a step has two times 32 keys");
+
+    __shared__ Kv8ManyLds<D> lds;
+    __shared__ float2 mls[NW][32];
+    static_assert(sizeof(lds.kv) >= NW * 16 * HALF * 8, "the queries' angles pass through the buffers");
+    static_assert(sizeof(lds.kv) >= NW * DB * 2 * 64 * 16, "the outputs meet in the buffers");
+
+    const Group g = group_of<false>(plan, blockIdx.x);
+    const int G = a.group, n_rt = g.n_rt;
+    const int li = blockIdx.x - g.item_base;   // (a call's items are not padded: below the group's count)
+    const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
+    const int rt = n_rt - 1 - ic.rt;           // the longest first
+    const int rows_total = g.n_tok * G, tile_lo = rt * 32 * WR;
+    const int t_last = g.tok0 + (min(tile_lo + 32 * WR, rows_total) - 1) / G;
+    const int kv_lo = g.win + ic.split * g.split_keys;
+    if (kv_lo > t_last) return;                // (the row tile's splits end before this one)
+    // (no sum below passes the last key: a request may have 2^31 - 1 of them)
+    const int kv_hi = g.split_keys < t_last + 1 - kv_lo ? kv_lo + g.split_keys : t_last + 1;
+    const int kt0 = kv_lo & ~(kBlock - 1);
+    const int k_lo = kv_lo - kt0, k_hi = kv_hi - kt0;   // the range from the start of its first block
+    const int nt = (k_hi - 1) / STEP + 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rg = wave / KG, kg = wave % KG, l32 = lane & 31, hi = lane >> 5;
+    const int row_lo = tile_lo + rg * 32;
+    const int32_t* btab = a.block_tables + (size_t)g.req * a.max_blocks + (kt0 >> 4);
+    const int32_t* posv = a.positions + g.pos_off + kt0;
+    const size_t page = (size_t)kBlock * D;
+    const uint8_t* kpool = static_cast<const uint8_t*>(a.k_pool) + ic.kvh * page;
+    const uint8_t* vpool = static_cast<const uint8_t*>(a.v_pool) + ic.kvh * page;
+
+    // ---- the lane's part of a step's codes: of key own (of the step) pairs pair0 .. pair0 + PL - 1, and the values
+    // of chunks sub and (D 128) sub + 8.  (The keys' order lets 16 neighbouring lanes write all LDS banks: at D 128
+    // the rows of keys that differ in bit 1 lie in different halves of the swizzled chunks.)
+    const int l8 = lane >> 3, sub = lane & 7, pair0 = sub * PL;
+    const int own = wave * 8 + (D == 128 ? (l8 & 4) | ((l8 & 1) << 1) | ((l8 >> 1) & 1) : l8);
+    int k_el[2];   // bytes of its two runs in a row: NeoX its x and its y, GPT-J one after the other
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e = STYLE == kNeox ? pair0 + h * HALF : 2 * pair0 + h * PL;
+        k_el[h] = model_chunk(a.chunk_map, e >> 3) * 8 + (e & 7);
+    }
+    typedef uint32_t run_t __attribute__((ext_vector_type(KW)));
+    struct Raw {
+        uint32_t k[2][KW], v[VW];
+        int32_t pos;
+        float ks, vs;
+    } raw;
+    auto block_at = [&](int u) { return scalar_load(btab, min(u * STEP + wave * 8, k_hi - 1) >> 4); };
+    int blk = block_at(0);
+    const int own_row = (wave * 8 & (kBlock - 1)) + own - wave * 8;   // of the key in its block
+    const size_t blk_stride = (size_t)a.hkv * page;
+    auto load = [&](int u) {
+        if (u >= nt) return;
+        Raw& r = raw;
+        // a key outside the range stands for the nearest one inside, so that nothing outside it is read
+        int k = u * STEP + own, to_row = own_row * D;
+        if (u * STEP < k_lo || (u + 1) * STEP > k_hi) {
+            k = min(max(k, k_lo), k_hi - 1);
+            to_row = (k & (kBlock - 1)) * D;
+        }
+        const size_t at = (size_t)(uint32_t)blk * blk_stride;
+        const uint8_t* kp = kpool + at;
+        const uint8_t* vp = vpool + at;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const run_t w = *reinterpret_cast<const run_t*>(kp + (uint32_t)(to_row + k_el[h]));
+#pragma unroll
+            for (int i = 0; i < KW; ++i) {
+                if constexpr (KW == 1) r.k[h][i] = w[0];
+                else r.k[h][i] = w[i];
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < VW / 2; ++h) {
+            const u32x2_t w = *reinterpret_cast<const u32x2_t*>(vp + (uint32_t)(to_row + (sub + 8 * h) * 8));
+            r.v[2 * h] = w[0];
+            r.v[2 * h + 1] = w[1];
+        }
+        if (ROPE) r.pos = posv[(uint32_t)k];
+        const int32_t* sp = reinterpret_cast<const int32_t*>(a.scale) + ((size_t)(uint32_t)blk * a.hkv + ic.kvh) * 2;
+        r.ks = __int_as_float(scalar_load(sp, 0));
+        r.vs = __int_as_float(scalar_load(sp, 1));
+        if (u + 1 < nt) blk = block_at(u + 1);
+    };
+    load(0);
+    if (ROPE)
+        for (int i = threadIdx.x; i < HALF; i += NW * 64) {
+            lds.fstep[i] = a.fstep[i];
+            rope_cs_fast(STEP, a.fstep[i], lds.stride_cs[i].x, lds.stride_cs[i].y);
+        }
+
+    // ---- queries.  The cos/sin of their tokens (a token's heads share them) pass through the wave's
+    // part of the buffers, which holds 16 tokens: more take two times 16 rows.
+    const int row = row_lo + l32;
+    const bool valid = row < rows_total;
+    const int toff = valid ? row / G : 0, hl = valid ? row - toff * G : 0;
+    const int last = min(k_hi - 1, g.tok0 + toff - kt0);   // last key that the row sees, from kt0
+    u32x4_t qb[KD];
+    float qs = a.scale_log2;   // the products times this and the block's scale are scores (log2 units)
+    {
+        const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((size_t)(g.q_row0 + toff) * a.hq + (size_t)ic.kvh * G + hl) * D;
+        u32x4_t in[KD / 2][2];   // chunks 2 kd + hi of the pairs
+#pragma unroll
+        for (int kd = 0; kd < KD / 2; ++kd)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int c = 2 * kd + hi;
+                in[kd][h] = *reinterpret_cast<const u32x4_t*>(qp + model_chunk(a.chunk_map, STYLE == kNeox ? c + h * (D / 16) : 2 * c + h) * 8);
+                if (!valid) in[kd][h] = u32x4_t{0, 0, 0, 0};
+            }
+        __syncthreads();  // phase steps staged
+        float x[HALF / 2], y[HALF / 2];   // of pairs 8 c .. 8 c + 7, c = 2 kd + hi for kd < KD / 2
+#pragma unroll
+        for (int kd = 0; kd < KD / 2; ++kd) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t wx = STYLE == kNeox ? in[kd][0][e / 2] : in[kd][e / 4][e % 4], wy = STYLE == kNeox ? in[kd][1][e / 2] : wx;
+                x[8 * kd + e] = STYLE == kNeox && e % 2 ? bf_hi(wx) : bf_lo(wx);
+                y[8 * kd + e] = STYLE == kNeox && e % 2 == 0 ? bf_lo(wy) : bf_hi(wy);
+            }
+        }
+        if (ROPE) {
+            float2* cs = reinterpret_cast<float2*>(&lds.kv[0][0][0]) + wave * 16 * HALF;
+            float big = 0.f;
+            const int each = min(row_lo + 31, rows_total - 1) / G - min(row_lo, rows_total - 1) / G < 16 ? 32 : 16;
+#pragma unroll 1
+            for (int h = 0; h < 32; h += each) {
+                const int t0 = min(row_lo + h, rows_total - 1) / G, t1 = min(row_lo + h + each - 1, rows_total - 1) / G;
+                const int32_t pos = a.positions[g.pos_off + g.tok0 + min(t0 + (lane & 15), t1)];   // of token t0 + lane
+                const uint64_t step = lds.fstep[lane % HALF];
+                for (int i = lane; i < (t1 - t0 + 1) * HALF; i += 64) {
+                    float c, s;
+                    rope_cs_fast(__shfl(pos, i / HALF), step, c, s);
+                    cs[i] = make_float2(c, s);
+                }
+                __atomic_signal_fence(__ATOMIC_SEQ_CST);
+                if (l32 >= h && l32 < h + each) {
+                    const float2* tc = cs + (valid ? toff - t0 : 0) * HALF;
+#pragma unroll
+                    for (int i = 0; i < HALF / 2; ++i) {
+                        const float2 t = tc[(2 * (i / 8) + hi) * 8 + i % 8];
+                        const float x0 = x[i], y0 = y[i];
+                        x[i] = x0 * t.x - y0 * t.y;
+                        y[i] = y0 * t.x + x0 * t.y;
+                        big = fmaxf(big, fmaxf(fabsf(x[i]), fabsf(y[i])));
+                    }
+                }
+                __atomic_signal_fence(__ATOMIC_SEQ_CST);
+            }
+            const int ex = query_exponent(max_xor32(big));
+            qs = ldexpf(qs, ex);
+#pragma unroll
+            for (int i = 0; i < HALF / 2; ++i) {
+                x[i] = ldexpf(x[i], -ex);
+                y[i] = ldexpf(y[i], -ex);
+            }
+        }
+#pragma unroll
+        for (int kd = 0; kd < KD / 2; ++kd)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const int i = 8 * kd + 2 * m;
+                qb[kd][m] = ROPE ? pack_f16(x[i], x[i + 1]) : pack_bf16(x[i], x[i + 1]);
+                qb[kd + KD / 2][m] = ROPE ? pack_f16(y[i], y[i + 1]) : pack_bf16(y[i], y[i + 1]);
+            }
+    }
+    barrier_keep_vmem();   // the angles have been read: the buffers may be filled
+
+    // ---- codes into an LDS buffer, in parts that stand beside other work
+    float rc[PL], rs[PL];      // cos/sin of the lane's pairs at position cs_pos
+    int32_t cs_pos = 0;
+    int renew = 0;             // steps until they are computed again
+    const int t_chunk[2] = {(pair0 >> 3), (pair0 >> 3) + HALF / 8};   // of the turned runs, x and y
+    auto at_lds = [&](int kv, int buf, int chunk) { return &lds.kv[buf][kv][own * D + ((chunk ^ dswz<D>(own & 15)) << 3)]; };
+    constexpr int PARTS = PL / 2 + VW / 2;
+    uint32_t turned[2][PL / 2];
+    auto angles = [&]() {
+        if (!ROPE) return;
+        const int32_t pos = raw.pos;
+        // (STEP on, and not past the type's end)
+        if (renew == 0 || __builtin_amdgcn_ballot_w64((uint32_t)pos != (uint32_t)cs_pos + STEP || pos < cs_pos) != 0) {
+#pragma unroll
+            for (int i = 0; i < PL; ++i) rope_cs_fast((int64_t)pos - STEP, lds.fstep[pair0 + i], rc[i], rs[i]);
+            renew = kKv8Renew;
+        }
+        --renew;
+        cs_pos = pos;
+    };
+    auto part = [&](int buf, int i) {
+        const Raw& r = raw;
+        if (i < PL / 2) {   // pairs 2 i and 2 i + 1
+            const int w = i / 2, h = i % 2;
+            uint32_t xw, yw;
+            if (STYLE == kNeox) {
+                xw = r.k[0][w];
+                yw = r.k[1][w];
+            } else {   // neighbours: word 2 w and 2 w + 1 of the lane's words
+                const uint32_t a0 = r.k[2 * w / KW][2 * w % KW], a1 = r.k[(2 * w + 1) / KW][(2 * w + 1) % KW];
+                xw = __builtin_amdgcn_perm(a1, a0, 0x06040200u);
+                yw = __builtin_amdgcn_perm(a1, a0, 0x07050301u);
+            }
+            if constexpr (ROPE) {
+#pragma unroll
+                for (int p = 2 * i; p < 2 * i + 2; ++p) {
+                    const float2 d = lds.stride_cs[pair0 + p];
+                    const float c = rc[p], s = rs[p];
+                    rc[p] = c * d.x - s * d.y;
+                    rs[p] = s * d.x + c * d.y;
+                }
+                const uint32_t xb = h ? C::halves_hi(xw) : C::halves_lo(xw), yb = h ? C::halves_hi(yw) : C::halves_lo(yw);
+                const f16x2_t x = __builtin_bit_cast(f16x2_t, xb), y = __builtin_bit_cast(f16x2_t, yb);
+                const f16x2_t c = __builtin_bit_cast(f16x2_t, pack_f16(rc[2 * i], rc[2 * i + 1])), s = __builtin_bit_cast(f16x2_t, pack_f16(rs[2 * i], rs[2 * i + 1]));
+                turned[0][i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, c, -(y * s)));
+                turned[1][i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, c, x * s));
+            } else {
+                const u32x2_t xb = C::bf16s(xw), yb = C::bf16s(yw);
+                turned[0][i] = xb[h];
+                turned[1][i] = yb[h];
+            }
+            if (i == PL / 2 - 1) {
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    typedef uint32_t out_t __attribute__((ext_vector_type(PL / 2)));
+                    out_t o;
+#pragma unroll
+                    for (int j = 0; j < PL / 2; ++j) o[j] = turned[z][j];
+                    *reinterpret_cast<out_t*>(at_lds(0, buf, t_chunk[z]) + (pair0 & 7)) = o;
+                }
+                if (lane == 0 && (wave & 1) == 0) {
+                    const float v = fmaxf(r.vs, kLeastValueScale);
+                    lds.sc[buf][wave >> 1] = make_float4(r.ks, __builtin_amdgcn_logf(v), 1.f / v, 0.f);
+                }
+            }
+        } else {   // a chunk of values
+            const int h = i - PL / 2;
+            const u32x2_t lo = C::bf16s(r.v[2 * h]), hi2 = C::bf16s(r.v[2 * h + 1]);
+            *reinterpret_cast<u32x4_t*>(at_lds(1, buf, sub + 8 * h)) = u32x4_t{lo[0], lo[1], hi2[0], hi2[1]};
+        }
+    };
+
+    f32x16_t acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) acc[db] = f32x16_t{};
+    float m_run = kNegBig, l_run = 0.f;
+    // per-lane byte offsets: the K operand's row among 32 keys, the V^T operand's among 8 (chunk c,
+    // and the row 8 keys on, by xor)
+    constexpr int kSw8 = D == 128 ? 1 : 4;
+    uint32_t k_at = (uint32_t)(l32 * D + ((hi ^ dswz<D>(l32 & 15)) << 3)) * 2, v_at;
+    {
+        const int key = 4 * hi + ((lane & 15) >> 2), d = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+        v_at = (uint32_t)(64 * D + key * D + (((d >> 3) ^ dswz<D>(key)) << 3) + (d & 7)) * 2;
+    }
+    const uint32_t lds_at = lds_addr(&lds.kv[0][0][0]);
+    const int first_row_last = min(k_hi - 1, g.tok0 + min(row_lo, rows_total - 1) / G - kt0);   // last key that every row sees
+    typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
+
+    constexpr int NT = 2 / KG;     // times 32 keys of a step
+    constexpr int TAKEN = KD * NT;
+    // ---- step s, in buffer P = s % 2, and the codes of the next step
+    auto step = [&](int s, int P) {
+        // (the offsets are not kept apart for every chunk: registers are short)
+        asm volatile("" : "+v"(k_at), "+v"(v_at));
+        const uint32_t at = lds_at + (uint32_t)(P * 128 * D + 32 * kg * D) * 2, kt = at + k_at, vt = at + v_at;
+        constexpr int kAhead = 5;                 // K reads in flight
+        u32x4_t kf[TAKEN];
+        auto read_k = [&](int i) { kf[i] = *(lds_u32x4_t*)(uintptr_t)((kt ^ (32 * (i / NT))) + 64 * (i % NT) * D); };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read_k(i);
+        float4 bs[2 * NT];
+        if (s + 1 < nt) angles();
+        f32x16_t sc[NT];
+        __builtin_amdgcn_sched_barrier(0);
+        // Every few vector instructions follow a product that they do not wait for, in the order written (past
+        // the last step they turn what the registers hold, into a buffer that is not read again)
+#pragma unroll
+        for (int i = 0; i < TAKEN; ++i) {
+            const int kd = i / NT, n = i % NT;
+            const f32x16_t from = kd == 0 ? f32x16_t{} : sc[n];
+            if (ROPE)
+                sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, kf[i]), __builtin_bit_cast(f16x8_t, qb[kd]), from, 0, 0, 0);
+            else
+                sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), __builtin_bit_cast(bf16x8_t, qb[kd]), from, 0, 0, 0);
+            if (i + kAhead < TAKEN) read_k(i + kAhead);
+#pragma unroll
+            for (int j = i * PARTS / TAKEN; j < (i + 1) * PARTS / TAKEN; ++j) part(1 - P, j);
+            if (i == TAKEN - 2)
+#pragma unroll
+                for (int b = 0; b < 2 * NT; ++b) bs[b] = lds.sc[P][2 * kg + b];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        load(s + 2);
+        float mul[2 * NT], add[2 * NT];   // of a block's scores and of their exponents
+        float mx = kNegBig;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int k0 = s * STEP + 32 * (kg + n);
+            if (k0 < k_lo || k0 + 31 > first_row_last) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int key = k0 + 8 * (j >> 2) + 4 * hi + (j & 3);
+                    if (key < k_lo || key > last) sc[n][j] = -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float bm = sc[n][8 * h];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) bm = fmaxf(bm, sc[n][8 * h + j]);
+                mul[2 * n + h] = fmaxf(qs * bs[2 * n + h].x, 0x1p-149f);   // (not 0, with which a masked -Inf would be NaN)
+                mx = fmaxf(mx, bm * mul[2 * n + h]);
+            }
+        }
+        // the reference maximum only moves when some row's maximum grows by more than 8
+        // (probabilities stay below 2^8), so most steps skip rescaling
+        if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.f) != 0) {
+            const float m_new = fmaxf(m_run, max_xor32(mx));
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+            m_run = m_new;
+        }
+#pragma unroll
+        for (int b = 0; b < 2 * NT; ++b) add[b] = bs[b].y - m_run;
+        // ---- outputs, 16 keys (a block) at a time, with the next 16's probabilities and V reads beside
+        constexpr int NH = 2 * NT;
+        u32x4_t pw[2];               // probabilities times the values' scale, in bf16; the row sum adds exactly those
+        u32x2_t af[2][2 * DB];
+        float bsum = 0.f;
+        // part i of DB of the probabilities of block h
+        auto prob = [&](int h, int i) {
+            constexpr int E = 8 / DB;
+            if (i == 0) bsum = 0.f;
+#pragma unroll
+            for (int r = i * E; r < (i + 1) * E; r += 2) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h / 2][8 * (h % 2) + r], mul[h], add[h]));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h / 2][8 * (h % 2) + r + 1], mul[h], add[h]));
+                const uint32_t w = pack_bf16(x, y);
+                pw[h % 2][r / 2] = w;
+                bsum = sum2_bf16(w, bsum);
+            }
+            if (i == DB - 1) l_run = __builtin_fmaf(bsum, bs[h].z, l_run);
+        };
+        // V reads of block i of the dimensions
+        auto read_v = [&](int h, int i) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {   // 8 keys each
+                const uint32_t off = (vt ^ (uint32_t)(64 * i) ^ (e ? 16u * kSw8 : 0u)) + 32 * h * D + (e ? 16 * D : 0);
+                af[h % 2][2 * i + e] = __builtin_bit_cast(u32x2_t, lds_read_tr((lds_u16_t*)(uintptr_t)off));
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            read_v(0, i);
+            prob(0, i);
+        }
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                const u32x4_t v = {af[h % 2][2 * i][0], af[h % 2][2 * i][1], af[h % 2][2 * i + 1][0], af[h % 2][2 * i + 1][1]};
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, pw[h % 2]), acc[i], 0, 0, 0);
+                if (h + 1 < NH) {
+                    read_v(h + 1, i);
+                    prob(h + 1, i);
+                }
+            }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // the codes of step u alone (also: of a wave without rows)
+    auto only_codes = [&](int u, int buf) {
+        if (u < nt) {
+            angles();
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) part(buf, i);
+        }
+        load(u + 1);
+    };
+    only_codes(0, 0);
+    barrier_keep_vmem();
+    const bool rows = row_lo < rows_total;
+    for (int s = 0; s < nt; ++s) {
+        if (rows) step(s, s & 1);
+        else only_codes(s + 1, (s + 1) & 1);
+        barrier_keep_vmem();
+    }
+
+    // ---- the results of a row group's waves meet: rows by their common maximum, outputs through the buffers
+    float den = sum_xor32(l_run), M = m_run, mine = 1.f;
+    if constexpr (KG > 1) {
+        if (hi == 0) mls[wave][l32] = make_float2(m_run, den);
+        __syncthreads();
+        const float2 other = mls[wave ^ 1][l32];
+        M = fmaxf(m_run, other.x);
+        mine = __builtin_amdgcn_exp2f(m_run - M);
+        den = den * mine + other.y * __builtin_amdgcn_exp2f(other.x - M);
+    }
+    f32x4_t* meet = reinterpret_cast<f32x4_t*>(&lds.kv[0][0][0]);
+    f32x4_t out[DB * 4];   // dims 8 c + 4 (l/32) + {0..3}
+#pragma unroll
+    for (int c = 0; c < DB * 4; ++c) {
+        const f32x4_t x = {acc[c / 4][4 * (c % 4)], acc[c / 4][4 * (c % 4) + 1], acc[c / 4][4 * (c % 4) + 2], acc[c / 4][4 * (c % 4) + 3]};
+        out[c] = x * mine;
+    }
+    if constexpr (KG > 1) {   // a wave leaves the half of its outputs that the other one joins
+#pragma unroll
+        for (int c = 0; c < DB * 4; ++c)
+            if (c % 2 != kg) meet[(wave * DB * 2 + c / 2) * 64 + lane] = out[c];
+        __syncthreads();
+    }
+    if (row >= rows_total) return;
+    const size_t prow = ((size_t)g.part_base + (size_t)ic.cluster * n_rt + rt) * (32 * WR) + rg * 32 + l32;
+    const float inv = 1.f / den;
+    uint16_t* op = static_cast<uint16_t*>(a.o) + ((size_t)(g.q_row0 + toff) * a.hq + (size_t)ic.kvh * G + hl) * D;
+#pragma unroll
+    for (int c = 0; c < DB * 4; ++c) {
+        if (KG > 1 && c % 2 != kg) continue;
+        f32x4_t x = out[c];
+        if (KG > 1) x += meet[((wave ^ 1) * DB * 2 + c / 2) * 64 + lane];
+        const int d = 8 * c + 4 * hi;
+        if (g.n_split > 1) *reinterpret_cast<f32x4_t*>(a.part_o + prow * D + d) = x;
+        else *reinterpret_cast<u32x2_t*>(op + d) = u32x2_t{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
+    }
+    if (g.n_split > 1 && kg == 0 && hi == 0) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(M, den);
+}
+
 // Joins key splits: one block per kMergeRows rows of a (row tile, KV head), one float4 of a row per
 // thread, U splits' loads in flight.  A row tile has splits up to its last token's.
 struct Kv8MergeArgs {
@@ -802,12 +1316,18 @@ __global__ void __launch_bounds__(kMergeRows * D / 4) kv8_merge(const PlanOf<NG>
 template <int D, int STYLE, bool ROPE, int CODE, int NG>
 hipError_t launch_kv8_n(const PlanOf<NG>& plan, const Kv8Args& a, hipStream_t st) {
     const dim3 grid(plan.n_items), block(kKv8Waves * 64);
-    if (a.tile_rows == 16) hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 1, NG>), grid, block, 0, st, plan, a);
-    else hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 2, NG>), grid, block, 0, st, plan, a);
+    switch (a.tile_rows) {
+    case 16: hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 1, NG>), grid, block, 0, st, plan, a); break;
+    case 32: hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 2, NG>), grid, block, 0, st, plan, a); break;
+    case 128: hipLaunchKernelGGL((kv8_many<D, STYLE, ROPE, CODE, 4, NG>), grid, block, 0, st, plan, a); break;
+    default: hipLaunchKernelGGL((kv8_many<D, STYLE, ROPE, CODE, 8, NG>), grid, block, 0, st, plan, a); break;
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.n_merge == 0) return e;
     const Kv8MergeArgs m = {a.part_o, a.part_ml, a.o, a.tile_rows, a.hq, a.hkv, a.group};
-    hipLaunchKernelGGL((kv8_merge<D, NG, 8>), dim3(plan.n_merge), dim3(kMergeRows * D / 4), 0, st, plan, m);
+    const dim3 merges(plan.n_merge), threads(kMergeRows * D / 4);
+    if (a.tile_rows <= 32) hipLaunchKernelGGL((kv8_merge<D, NG, 8>), merges, threads, 0, st, plan, m);
+    else hipLaunchKernelGGL((kv8_merge<D, NG, 4>), merges, threads, 0, st, plan, m);
     return hipGetLastError();
 }
 
