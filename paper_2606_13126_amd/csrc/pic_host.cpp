@@ -260,18 +260,112 @@ TreeSplit tree_split(HostPlan& hp, int G, int hkv) {
     return best;
 }
 
-// Row tiles and key splits of a call over 8-bit codes in bf16: tiles of 16 rows where every (span, KV head)
-// has no more, of 32 and 128 likewise, else of 256; chunks of about the average work per compute unit, at least one step of keys.
-void kv8_split(HostPlan& hp, int G, int hkv) {
+// Row tiles and key splits of a call over 8-bit codes in bf16, chosen together: per tile, looked at are no
+// splits and chunks of which the call has about 1/2, 1, 2, 3, 4 and 6 items per compute unit; taken is what ends first by
+// these costs (us): an item's start, a step of 128 keys (tiles of 16 and 32 rows) or 64, by the rows
+// that a tile holds, and the join of the splits.  Two workgroups with 16 rows share a compute unit: their steps
+// cost `shared` once there are more items than units.  Fitted to 20,000 calls each of head_dim 128 and 64
+// (1 to 256 requests of 1 to 2,048 tokens over up to 131,072 keys, equal and ragged, 1 to 12 KV heads of 1 to 16
+// query heads, keys turned in the call), which they describe within 11%.  On 26,000 batches the choice takes, times
+// the best of all that were timed, in the mean 1.005 (decode) and 1.015 (prefill), and 1.007 and 1.023 on turned keys.
+// Tiles by the number of rows alone and chunks of the average work per unit: 1.05 and 1.35.
+struct Kv8Costs {
+    float start[4];       // tiles of 16, 32, 128 and 256 rows
+    float step[4][4];     // ... of up to 64, 128, 192 and more rows (16 and 32: of any)
+    float shared;
+    float join, join_split, join_row;
+    float bytes_per_us;   // of codes
+};
+constexpr Kv8Costs kKv8Costs[2] = {
+    {{5.8f, 6.7f, 10.2f, 11.3f},
+     {{1.33f, 1.33f, 1.33f, 1.33f}, {1.75f, 1.75f, 1.75f, 1.75f}, {1.19f, 1.62f, 1.62f, 1.62f}, {1.51f, 1.57f, 2.14f, 2.28f}},
+     2.31f, 4.3f, 0.15f, 1e-4f, 4.6e6f},
+    {{5.0f, 4.9f, 7.6f, 8.1f},
+     {{0.92f, 0.92f, 0.92f, 0.92f}, {1.09f, 1.09f, 1.09f, 1.09f}, {0.86f, 1.20f, 1.20f, 1.20f}, {1.10f, 1.13f, 1.56f, 1.64f}},
+     1.51f, 3.6f, 0.13f, 1e-4f, 4.0e6f},
+};
+
+void kv8_split(HostPlan& hp, int G, int hkv, int head_dim) {
+    const Kv8Costs& cost = kKv8Costs[head_dim == 128 ? 0 : 1];
+    constexpr float kCUs = pic::kTargetCUs;
     int64_t most = 0;
-    for (auto& g : hp.groups) most = std::max<int64_t>(most, (int64_t)g.n_tok * G);
-    hp.tree_rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 128 ? 128 : 256;
-    const int64_t tr = hp.tree_rows, tk = pic::kv8_keys(hp.tree_rows);
-    int64_t total = 0;
-    for (auto& g : hp.groups)
-        for (int64_t rt = 0; rt < pic::row_tiles(g, G, (int32_t)tr); ++rt)
-            total += ((int64_t)g.tok0 + (std::min((rt + 1) * tr, (int64_t)g.n_tok * G) - 1) / G - g.win + tk) / tk * hkv;
-    const int64_t chunk = std::min<int64_t>(std::max<int64_t>(1, (total + pic::kTargetCUs - 1) / pic::kTargetCUs), (1 << 30) / tk);
+    double keys = 0;
+    for (auto& g : hp.groups) {
+        most = std::max<int64_t>(most, (int64_t)g.n_tok * G);
+        keys += (double)g.tok0 + g.n_tok - g.win;
+    }
+    const float bytes_us = (float)(keys * hkv * head_dim * 2 / cost.bytes_per_us);
+    struct Span {
+        uint32_t steps;   // of the last row tile
+        float tiles, last;   // row tiles x KV heads; cost of a step of the first of them
+        float rows;
+    };
+    std::vector<Span> spans(hp.groups.size());
+    float best_us = 0;
+    int best_tile = 0;
+    int64_t best_chunk = 0;
+    for (int i = 0; i < 4; ++i) {
+        const int tile = i < 2 ? 16 << i : 128 << (i - 2);
+        // (far from where they are best: never taken)
+        if ((i > 0 && most <= 16) || (i == 3 && most <= 64) || (i < 2 && most > 1024)) continue;
+        const int64_t tk = pic::kv8_keys(tile), least = 128 / tk;
+        const auto step_us = [&](int64_t rows) { return cost.step[i][rows <= 64 ? 0 : rows <= 128 ? 1 : rows <= 192 ? 2 : 3]; };
+        double work = 0, total = 0, unsplit = 0;
+        int64_t longest = 1;
+        for (size_t k = 0; k < spans.size(); ++k) {
+            const pic::Group& g = hp.groups[k];
+            const int64_t rows = (int64_t)g.n_tok * G, full = (rows - 1) / tile, end = (int64_t)g.tok0 + g.n_tok - g.win;
+            const int64_t steps = (end + tk - 1) / tk, mean = full ? (end - g.n_tok / 2 + tk - 1) / tk : 0;   // (row tiles end at their own tokens)
+            spans[k] = Span{(uint32_t)steps, (float)((full + 1) * hkv), step_us(std::min<int64_t>(rows, tile)), (float)(rows * hkv)};
+            work += hkv * ((double)(full * mean) * step_us(tile) + (double)steps * step_us(rows - full * tile));
+            total += (double)hkv * (full * mean + steps);
+            unsplit += (double)(full + 1) * hkv;
+            longest = std::max(longest, steps);
+        }
+        const float slots = i == 0 ? 2 * kCUs : kCUs, slower = i == 0 ? cost.shared / cost.step[0][0] : 1.f;
+        if (best_tile != 0 && work * slower / slots > best_us) continue;
+        const auto look = [&](int64_t chunk) {
+            float one = 0, last = 1e30f, split_rows = 0, items = 0;
+            uint32_t splits = 1;
+            for (const Span& s : spans) {
+                const uint32_t n = (s.steps + (uint32_t)chunk - 1) / (uint32_t)chunk, each = n == 1 ? s.steps : (s.steps + n - 1) / n;
+                const float us = (float)each * s.last;
+                one = std::max(one, us);
+                last = std::min(last, us);
+                items += s.tiles * (float)n;
+                splits = std::max(splits, n);
+                if (n > 1) split_rows += (float)n * s.rows;
+            }
+            const float slow = items > kCUs ? slower : 1.f;
+            float us = cost.start[i] + one * slow;
+            if (items > slots) {
+                // in rounds, or (items of several lengths, the long ones first) near the average
+                const float rounds = std::ceil(items / slots) * us,
+                            average = (float)((items * cost.start[i] + work * slow) / slots) + 0.5f * (cost.start[i] + last * slow);
+                us = std::max(us, std::min(rounds, average));
+            }
+            us = std::max(us, bytes_us + 0.7f * cost.start[i]);
+            if (splits > 1) us += cost.join + cost.join_split * (float)splits + cost.join_row * split_rows;
+            if (best_tile == 0 || us < best_us) {
+                best_us = us;
+                best_tile = tile;
+                best_chunk = chunk;
+            }
+        };
+        look(longest);
+        int64_t before = longest;
+        for (const double per : {0.5, 1.0, 2.0, 3.0, 4.0, 6.0}) {
+            const double want = per * kCUs;
+            if (unsplit > want) continue;
+            const int64_t chunk = std::max(least, (int64_t)std::ceil(total / want));
+            if (chunk >= before) continue;
+            look(chunk);
+            before = chunk;
+            if (chunk <= least) break;
+        }
+    }
+    hp.tree_rows = best_tile;
+    const int64_t tk = pic::kv8_keys(best_tile), chunk = std::min<int64_t>(best_chunk, (1 << 30) / tk);   // (keys of a split, counted from its start, stay in 31 bits)
     for (auto& g : hp.groups) {
         const int64_t steps = ((int64_t)g.tok0 + g.n_tok - g.win + tk - 1) / tk;
         const int64_t n_split = (steps + chunk - 1) / chunk, each = (steps + n_split - 1) / n_split;
@@ -391,7 +485,7 @@ pic_status make_plan(const pic_config* c, const pic_batch_host* b, Call call, bo
             return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
         });
     } else if (hp.kv8) {
-        kv8_split(hp, G, c->num_kv_heads);
+        kv8_split(hp, G, c->num_kv_heads, c->head_dim);
         std::stable_sort(hp.groups.begin(), hp.groups.end(), [](const pic::Group& x, const pic::Group& y) {
             return std::min(x.split_keys, x.tok0 + x.n_tok - x.win) > std::min(y.split_keys, y.tok0 + y.n_tok - y.win);
         });

@@ -469,13 +469,10 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
     // the wave's copies of step u into stage st: a lane's 16 bytes are one chunk of one key, and a key outside
     // the range stands for the nearest one inside, so that nothing outside it is read (its score is masked)
     auto near_key = [&](int k) { return min(max(k, k_lo), k_hi - 1); };
-    int k_from[S::NC], v_from[S::NC];
-#pragma unroll
-    for (int i = 0; i < S::NC; ++i) {
-        const int key = i * S::KPC + lane / S::CPR, c = lane % S::CPR;
-        k_from[i] = key * D + ((c ^ kswz<D>(key)) << 4);
-        v_from[i] = key * D + ((c ^ vswz<D>(key)) << 4);
-    }
+    // the lane's bytes of a page in the first copy; the second one (D 128: 8 keys on) swizzles keys by another bit
+    const int c_key = lane / S::CPR, k_from = c_key * D + (((lane % S::CPR) ^ kswz<D>(c_key)) << 4),
+              v_from = c_key * D + (((lane % S::CPR) ^ vswz<D>(c_key)) << 4);
+    static_assert(S::NC == 1 || D == 128, "one copy of a page, or two");
     auto issue = [&](int u, int st, int blk) {
         const int k0 = u * S::STEP + wave * TK;
         const uint32_t to = stages_at + (uint32_t)((st * NW + wave) * 2 * S::TILE);
@@ -489,8 +486,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
                 const int key = k0 + i * S::KPC + lane / S::CPR;
                 moved = ((near_key(key) & (TK - 1)) - (key & (TK - 1))) * D;
             }
-            copy_lds16(kpool + at, (uint32_t)(k_from[i] + moved), to + i * 1024);
-            copy_lds16(vpool + at, (uint32_t)(v_from[i] + moved), to + S::TILE + i * 1024);
+            copy_lds16(kpool + at, (uint32_t)((k_from ^ (i << 6)) + i * S::KPC * D + moved), to + i * 1024);
+            copy_lds16(vpool + at, (uint32_t)(v_from + i * S::KPC * D + moved), to + S::TILE + i * 1024);
         }
         if (lane < 18) {
             const void* src = lane < 16 ? (const void*)(posv + (whole ? k0 + lane : near_key(k0 + lane)))
