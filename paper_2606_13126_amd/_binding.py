@@ -358,42 +358,70 @@ class Kv8Pool:
         for t, what, size in ((k, "k", 1), (v, "v", 1), (scale, "scale", 4)):
             if t.element_size() != size or not t.is_contiguous():
                 raise ValueError(f"{what} must be dense, of {size}-byte elements")
-        if k.dim() != 4 or v.shape != k.shape or tuple(scale.shape) != (k.shape[0], k.shape[1], 2):
+        if k.dim() != 4 or k.shape[2] != 16 or v.shape != k.shape or tuple(scale.shape) != (k.shape[0], k.shape[1], 2):
             raise ValueError("k and v must be [blocks][Hkv][16][D] and scale [blocks][Hkv][2]")
         self.k, self.v, self.scale = k, v, scale
+        self._heads, self._dim = k.size(1), k.size(3)
         self.c = pic_kv8_pool(k.data_ptr(), v.data_ptr(), scale.data_ptr(), k.size(0), int(code))
+        self._ref = ctypes.byref(self.c)
 
     def _of(self, cfg):
-        if self.k.size(1) != cfg.num_kv_heads or self.k.size(2) != cfg.block_size or self.k.size(3) != cfg.head_dim:
+        if self._heads != cfg.num_kv_heads or self._dim != cfg.head_dim:
             raise ValueError("the pool's shape is not the config's")
-        return ctypes.byref(self.c)
+        return self._ref
+
+
+def _rows_of(t, what: str, heads: int, dim: int):
+    """_rows of a tensor that must have these heads, and its number of rows."""
+    p, stride = _rows(t, what)
+    n, h, d = t.size()
+    if h != heads or d != dim:
+        raise ValueError(f"{what} must be [n][{heads}][{dim}]")
+    return p, stride, n
+
+
+def _norm_rows(t, out, what: str, heads: int, dim: int):
+    """Addresses and strides of one input of pic_qk_norm and its output, and the rows."""
+    if t is None:
+        if out is not None:
+            raise ValueError(f"{what}_out without {what}")
+        return 0, None, 0, None, 0
+    p, stride, n = _rows_of(t, what, heads, dim)
+    if out is None:
+        return n, p, stride, p, stride
+    if out.size() != t.size():
+        raise ValueError(f"{what}_out must have the shape of {what}")
+    if out.is_contiguous():
+        return n, p, stride, out.data_ptr(), heads * dim
+    return n, p, stride, *_rows(out, what + "_out")
 
 
 def pic_qk_norm(cfg: pic_config, q, k, q_weight, k_weight, eps: float, positions=None, q_out=None, k_out=None, stream=None) -> None:
     """q [n][Hq][D] and k [n][Hkv][D] (either may be None) may be views of one projection's output, the outputs too;
     without an output the norm is taken in place.  Weights [D] or None; positions may be None for an unrotated pool."""
-    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-    (qp, qs), (kp, ks), (qo, qos), (ko, kos) = _rows(q, "q"), _rows(k, "k"), _rows(q_out, "q_out"), _rows(k_out, "k_out")
-    for t, o in ((q, q_out), (k, k_out)):
-        if (t is None) != (o is None) or (t is not None and t.shape != o.shape):
-            raise ValueError("an output must have its input's shape")
-    n = [t.size(0) for t in (q, k) if t is not None]
-    if len(set(n)) != 1:
+    d = cfg.head_dim
+    nq, qp, qs, qo, qos = _norm_rows(q, q_out, "q", cfg.num_q_heads, d)
+    nk, kp, ks, ko, kos = _norm_rows(k, k_out, "k", cfg.num_kv_heads, d)
+    if q is not None and k is not None and nq != nk:
         raise ValueError("q and k must have the same rows")
     _check(_lib.pic_qk_norm(ctypes.byref(cfg), qp, qs, qo, qos, kp, ks, ko, kos, _ptr(q_weight), _ptr(k_weight), eps, _ptr(positions),
-                            n[0], _stream(stream)))
+                            nq or nk, _stream(stream)))
 
 
 def pic_kv8_write(cfg: pic_config, pool: Kv8Pool, k_new, v_new, slot_mapping, stream=None) -> None:
     """k_new, v_new [n][Hkv][D] may be views of one projection's output (rows dense, any row stride)."""
-    (kp, ks), (vp, vs) = _rows(k_new, "k_new"), _rows(v_new, "v_new")
-    _check(_lib.pic_kv8_write(ctypes.byref(cfg), pool._of(cfg), kp, ks, vp, vs, slot_mapping.data_ptr(), k_new.size(0), _stream(stream)))
+    h, d = cfg.num_kv_heads, cfg.head_dim
+    (kp, ks, n), (vp, vs, nv) = _rows_of(k_new, "k_new", h, d), _rows_of(v_new, "v_new", h, d)
+    if nv != n or slot_mapping.size(0) != n:
+        raise ValueError("k_new, v_new and slot_mapping must have the same rows")
+    _check(_lib.pic_kv8_write(ctypes.byref(cfg), pool._of(cfg), kp, ks, vp, vs, slot_mapping.data_ptr(), n, _stream(stream)))
 
 
 def pic_kv8_read(cfg: pic_config, pool: Kv8Pool, slot_mapping, k_out, v_out, stream=None) -> None:
     """k_out, v_out: dense [n][Hkv][D]."""
-    if not k_out.is_contiguous() or not v_out.is_contiguous():
-        raise ValueError("k_out and v_out must be dense")
+    shape = (slot_mapping.size(0), cfg.num_kv_heads, cfg.head_dim)
+    if not k_out.is_contiguous() or not v_out.is_contiguous() or k_out.size() != shape or v_out.size() != shape:
+        raise ValueError(f"k_out and v_out must be dense {list(shape)}")
     _check(_lib.pic_kv8_read(ctypes.byref(cfg), pool._of(cfg), slot_mapping.data_ptr(), slot_mapping.size(0), k_out.data_ptr(),
                              v_out.data_ptr(), _stream(stream)))
 

@@ -21,6 +21,17 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
+// Outputs of more than this go past the caches, which they would only sweep (a call's inputs then stay there for the
+// next): 33,280 rows of 8 heads read from the pool (136 MB) 30.9 us, 43.5 through the caches, 16,384 rows of 72 heads
+// normalised (302 MB) 104 and 112.  Less is likely read again from there by what follows.
+constexpr int64_t kStreamBytes = (int64_t)64 << 20;
+
+template <bool STREAMS, typename V>
+__device__ __forceinline__ void store_chunk(V* dst, const V& x) {
+    if constexpr (STREAMS) __builtin_nontemporal_store(x, dst);
+    else *dst = x;
+}
+
 // sum over the N lanes (4, 8 or 16, aligned) that hold a head
 template <int N>
 __device__ __forceinline__ float sum_of(float x) {
@@ -65,7 +76,7 @@ __device__ __forceinline__ u32x4_t pack_chunk(const float* f) {
     return w;
 }
 
-template <typename T, int D, int STYLE, bool ROT>
+template <typename T, int D, int STYLE, bool ROT, bool STREAMS>
 __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a) {
     constexpr int PP = 16 / sizeof(T);     // elements per chunk, pairs per unit
     constexpr int CH = D / PP, UPH = CH / 2, U = 3;
@@ -136,8 +147,8 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a)
                     s = __builtin_fmaf(p0, t.y, s0 * t.x);
                 }
             u32x4_t* dst = h < a.hq ? qo + h * CH : ko + (h - a.hq) * CH;
-            dst[c0] = pack_chunk<T>(f);
-            dst[c1] = pack_chunk<T>(f + PP);
+            store_chunk<STREAMS>(dst + c0, pack_chunk<T>(f));
+            store_chunk<STREAMS>(dst + c1, pack_chunk<T>(f + PP));
         }
     }
 }
@@ -231,43 +242,43 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t r0 = (int64_t)blockIdx.x * a.range;
     const int n_here = (int)min((int64_t)a.range, a.n - r0);
-    // block of row i (-1: it stores nothing)
-    auto block_of = [&](int64_t i) {
-        const int32_t s = a.slots[i];
-        return s >= 0 && s < a.n_slots ? s >> 4 : -1;
+    // the slots of 64 rows, and of the row before (a row that stores nothing: some number below 0, in no block)
+    auto slot_of = [&](int64_t i) {
+        const int32_t s = i >= 0 && i < a.n ? a.slots[i] : -1;
+        return s < a.n_slots ? s : -1;
     };
-    bool lead = false;
-    if (lane < n_here) {
-        const int b = block_of(r0 + lane);
-        lead = b >= 0 && (r0 + lane == 0 || block_of(r0 + lane - 1) != b);
-    }
-    const uint64_t leads = __builtin_amdgcn_ballot_w64(lead);
+    const int32_t mine = slot_of(r0 + lane), before = lane == 0 ? slot_of(r0 - 1) : 0;
+    int32_t prev = __shfl_up(mine, 1);
+    if (lane == 0) prev = before;
+    const uint64_t leads = __builtin_amdgcn_ballot_w64(lane < n_here && mine >= 0 && mine >> 4 != prev >> 4);
     const int per = 2 * a.hkv, units = __builtin_popcountll(leads) * per;
     const int c16 = (lane % LPO) * 16;
     for (int u = (int)blockIdx.y * kWriteWaves + wave; u < units; u += (int)gridDim.y * kWriteWaves) {
         uint64_t rest = leads;
         for (int i = u / per; i > 0; --i) rest &= rest - 1;
-        const int64_t row0 = r0 + __builtin_ctzll(rest);
+        const int first = __builtin_ctzll(rest);
         const int which = u & 1, h = (u % per) >> 1;
         // the rows of the block: of each offset the last
-        const int blk = a.slots[row0] >> 4;
+        const int blk = __builtin_amdgcn_readlane(mine, first) >> 4;
         int64_t row[P];
         bool fresh = false;
 #pragma unroll
         for (int p = 0; p < P; ++p) row[p] = -1;
-        for (int64_t from = row0;; from += 64) {
-            const int64_t i = from + lane;
-            const int32_t s = i < a.n ? a.slots[i] : -1;
-            const uint64_t others = __builtin_amdgcn_ballot_w64((s >> 4) != blk);
-            const int run = others ? __builtin_ctzll(others) : 64;
+        int32_t slot = mine;
+        uint64_t live = ~0ull << first;   // lanes whose rows come into question
+        for (int64_t from = r0;; from += 64) {
+            const uint64_t others = __builtin_amdgcn_ballot_w64((slot >> 4) != blk) & live;
+            const uint64_t run = others ? live & ((others & -others) - 1) : live;
 #pragma unroll
             for (int o = 0; o < kBlock; ++o) {
-                const uint64_t m = __builtin_amdgcn_ballot_w64(lane < run && (s & 15) == o);
+                const uint64_t m = __builtin_amdgcn_ballot_w64((slot & 15) == o) & run;
                 if (m == 0) continue;
                 if (o == 0) fresh = true;
                 if (o % OPP == lane / LPO) row[o / OPP] = from + 63 - __builtin_clzll(m);
             }
-            if (run < 64) break;
+            if (others) break;
+            live = ~0ull;   // (only rows of one slot over and over are more than a wave looks at)
+            slot = slot_of(from + 64 + lane);
         }
         const T* src = static_cast<const T*>(which ? a.v : a.k);
         const int64_t stride = (which ? a.v_stride : a.k_stride) * V;
@@ -328,7 +339,7 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
 // ---------------------------------------------------------------------------------
 // kv8_read: a thread takes the codes of 16 bytes of output (4 or 8), U of them in flight.  Bound by memory.
 // ---------------------------------------------------------------------------------
-template <typename T, int D, int CODE>
+template <typename T, int D, int CODE, bool STREAMS>
 __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool,
                                                        const float* __restrict__ scale, int64_t n_slots,
                                                        const int32_t* __restrict__ slots, int64_t n_units, int hkv,
@@ -341,12 +352,12 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
     for (int64_t i0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i0 < n_units; i0 += U * step) {
         word_t w[U][2];
         float2 sc[U];
-        bool in[U];
+        bool in[U];   // the unit exists and its slot lies in the pool
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t i = i0 + u * step;
             in[u] = false;
-            if (i >= n_units) break;
+            if (i >= n_units) continue;
             const int64_t rh = i / CPR, row = rh <= UINT32_MAX ? (uint32_t)rh / (uint32_t)hkv : rh / hkv;
             const int32_t slot = slots[row];
             if (slot < 0 || slot >= n_slots) continue;
@@ -370,7 +381,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[4 * j + e] = (T)f[e];
                 }
-                *reinterpret_cast<vec_t*>((kv ? v_out : k_out) + i * V) = y;
+                store_chunk<STREAMS>(reinterpret_cast<vec_t*>((kv ? v_out : k_out) + i * V), y);
             }
         }
     }
@@ -1342,14 +1353,14 @@ hipError_t launch_kv8_d(int style, bool rope, const Plan& plan, const Kv8Args& a
     return style == kNeox ? launch_kv8_t<D, 0, true, CODE>(plan, a, st) : launch_kv8_t<D, 1, true, CODE>(plan, a, st);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool STREAMS>
 void launch_norm_d(int style, int n, int threads, const NormArgs& a, hipStream_t st) {
     if (a.rot_half == 0)
-        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, false>), dim3(n), dim3(threads), 0, st, a);
+        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, false, STREAMS>), dim3(n), dim3(threads), 0, st, a);
     else if (style == kNeox)
-        hipLaunchKernelGGL((qk_norm_kernel<T, D, 0, true>), dim3(n), dim3(threads), 0, st, a);
+        hipLaunchKernelGGL((qk_norm_kernel<T, D, 0, true, STREAMS>), dim3(n), dim3(threads), 0, st, a);
     else
-        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, true>), dim3(n), dim3(threads), 0, st, a);
+        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, true, STREAMS>), dim3(n), dim3(threads), 0, st, a);
 }
 
 // f(type, head_dim, code) with the values as constants
@@ -1373,13 +1384,12 @@ int launch_qk_norm(int dtype, int style, int d, int n, const NormArgs& a, void* 
     hipStream_t st = (hipStream_t)stream;
     const int64_t units = (int64_t)(a.hq + a.hkv) * (d * (dtype == 1 ? 4 : 2) / 32);
     const int threads = units >= kNormThreads ? kNormThreads : (int)((units + 63) / 64) * 64;
-    if (dtype == 1) {
-        if (d == 64) launch_norm_d<float, 64>(style, n, threads, a, st);
-        else launch_norm_d<float, 128>(style, n, threads, a, st);
-    } else {
-        if (d == 64) launch_norm_d<__bf16, 64>(style, n, threads, a, st);
-        else launch_norm_d<__bf16, 128>(style, n, threads, a, st);
-    }
+    const auto go = [&](auto t, auto dim) {
+        if (32 * units * n > kStreamBytes) launch_norm_d<decltype(t), decltype(dim)::value, true>(style, n, threads, a, st);
+        else launch_norm_d<decltype(t), decltype(dim)::value, false>(style, n, threads, a, st);
+    };
+    if (dtype == 1) d == 64 ? go(float{}, Idx<64>{}) : go(float{}, Idx<128>{});
+    else d == 64 ? go(__bf16{}, Idx<64>{}) : go(__bf16{}, Idx<128>{});
     return hipGetLastError();
 }
 
@@ -1397,11 +1407,16 @@ int launch_kv8_write(int dtype, int code, int d, const Kv8WriteArgs& a, void* st
 int launch_kv8_read(int dtype, int code, int d, int hkv, const uint8_t* k_pool, const uint8_t* v_pool, const float* scale,
                     int64_t n_slots, const int32_t* slots, int n, void* k_out, void* v_out, void* stream) {
     const int64_t units = (int64_t)n * hkv * (d * (dtype == 1 ? 4 : 2) / 16);
-    const int64_t blocks = (units + 255) / 256;
+    const int64_t blocks = (units + 511) / 512;
+    const dim3 grid((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22));   // (lanes of a launch stay below 2^32)
     by_types(dtype, d, code, [&](auto t, auto dim, auto c) {
         typedef decltype(t) T;
-        hipLaunchKernelGGL((kv8_read_kernel<T, decltype(dim)::value, decltype(c)::value>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256),
-                           0, (hipStream_t)stream, k_pool, v_pool, scale, n_slots, slots, units, hkv, static_cast<T*>(k_out), static_cast<T*>(v_out));
+        const auto go = [&](auto s) {
+            hipLaunchKernelGGL((kv8_read_kernel<T, decltype(dim)::value, decltype(c)::value, decltype(s)::value>), grid, dim3(256), 0,
+                               (hipStream_t)stream, k_pool, v_pool, scale, n_slots, slots, units, hkv, static_cast<T*>(k_out), static_cast<T*>(v_out));
+        };
+        if (32 * units > kStreamBytes) go(std::true_type{});
+        else go(std::false_type{});
     });
     return hipGetLastError();
 }

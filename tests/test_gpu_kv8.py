@@ -303,6 +303,26 @@ def test_write_keeps_a_scale_that_is_no_power_of_two():
     assert (np.abs(kept - got * 0.3) <= s / 2 * (1 + 1e-5)).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [1, 3, 65, 517, 4000])
+def test_read_and_write_stay_in_their_rows(dtype, n):
+    """Outputs inside a larger buffer, and a pool between two others: what lies around them keeps its bits."""
+    nb = -(-n // 16)
+    st = Store(nb, 2, 64, K8.INT8, dtype, seed=n)
+    around = torch.full((3, nb, 2, 16, 64), 77, dtype=torch.uint8, device="cuda")
+    st.pool = B.Kv8Pool(around[1], torch.zeros_like(around[1]), st.pool.scale, K8.INT8)
+    k, v = (x.cuda() for x in st.rows(n))
+    slots = dev(np.arange(n, dtype=np.int32))
+    B.pic_kv8_write(st.cfg, st.pool, k, v, slots)
+    assert (around[0] == 77).all() and (around[2] == 77).all()
+    out = torch.full((3 * n + 128, 2, 64), 7.0, dtype=dtype, device="cuda")
+    B.pic_kv8_read(st.cfg, st.pool, slots, out[:n], out[n:2 * n])
+    assert (out[2 * n:] == 7.0).all()
+    size = st.pool.scale[slots.long() // 16]
+    for got, x, i in ((out[:n], k, 0), (out[n:2 * n], v, 1)):
+        assert (got.float() - x.float()).abs().sub(size[..., i, None] * 0.5 * (1 + 2.0 ** -7)).max() <= 0
+
+
 # ------------------------------------------------------------------------------------
 # attention
 # ------------------------------------------------------------------------------------
