@@ -387,6 +387,18 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
     }
 }
 
+// group_of for the kernels here: among groups in the arguments every lane looks at one, in one round trip
+// (kernel arguments lie in host memory, and a binary search takes up to six, one after the other).
+template <bool MERGE, int N>
+__device__ __forceinline__ Group find_group(const PlanOf<N>& plan, int bid) {
+    static_assert(N <= 64, "a lane per group");
+    if (plan.table != nullptr) return group_of<MERGE>(plan, bid);
+    if (plan.n_groups == 1) return plan.g[0];
+    const int lane = (int)threadIdx.x & 63, i = lane < plan.n_groups ? lane : 0;
+    const int base = MERGE ? plan.g[i].merge_base : plan.g[i].item_base;
+    return plan.g[__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < plan.n_groups && base <= bid)) - 1];
+}
+
 // ---------------------------------------------------------------------------------
 // kv8_few: attention in bf16, up to 16 CB query rows (query token x query head of one KV head's
 // group) per workgroup of eight waves, over one key range.  Every wave holds the rows and takes every
@@ -453,7 +465,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
     __shared__ Kv8FewLds<D, CB> lds;
     __shared__ float2 mls[NW][16 * CB];
 
-    const Group g = group_of<false>(plan, blockIdx.x);
+    const Group g = find_group<false>(plan, blockIdx.x);
     const int G = a.group, n_rt = g.n_rt;
     const int li = blockIdx.x - g.item_base;   // (a call's items are not padded: below the group's count)
     const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
@@ -851,7 +863,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     static_assert(sizeof(lds.kv) >= NW * 16 * HALF * 8, "the queries' angles pass through the buffers");
     static_assert(sizeof(lds.kv) >= NW * DB * 2 * 64 * 16, "the outputs meet in the buffers");
 
-    const Group g = group_of<false>(plan, blockIdx.x);
+    const Group g = find_group<false>(plan, blockIdx.x);
     const int G = a.group, n_rt = g.n_rt;
     const int li = blockIdx.x - g.item_base;   // (a call's items are not padded: below the group's count)
     const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
@@ -1283,7 +1295,7 @@ struct Kv8MergeArgs {
 template <int D, int NG, int U>
 __global__ void __launch_bounds__(kMergeRows * D / 4) kv8_merge(const PlanOf<NG> plan, const Kv8MergeArgs a) {
     constexpr int TPR = D / 4;
-    const Group g = group_of<true>(plan, blockIdx.x);
+    const Group g = find_group<true>(plan, blockIdx.x);
     const int n_rt = g.n_rt, chunks = a.tile_rows / kMergeRows;
     int li = blockIdx.x - g.merge_base;   // (only groups with splits have blocks here, and no more than they need)
     const int r = (li % chunks) * kMergeRows + (int)threadIdx.x / TPR, c4 = (int)threadIdx.x % TPR;

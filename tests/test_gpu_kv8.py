@@ -545,3 +545,342 @@ def test_spread_of_a_large_softmax_scale():
         b.check(b.run(), "float32")
         b = Batch([(900, n)], 8, 2, 128, torch.bfloat16, K8.INT8, prerotated=1, seed=6, softmax=2.0, decode=decode, qscale=0.5)
         b.check(b.run(), "bf16")
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_precision_of_normal_inputs(code):
+    """How far outputs are from 64 bits, by independent roundings.  A rounding to b bits is off by 2^-b / sqrt(3) / 1.39 of a
+    value in the mean square (evenly over half a step, and over mantissas).  The result's: r8 = 1.6e-3, with the spread of
+    values within a binade at most 1.07 times that.  Probabilities of 8 bits: r8 once more.  Turned keys and queries, in
+    11 bits: of a pair's element x c - (y s), with pairs of any angle, c, s, the product and the result give 1/4 + 1/4 + 1/4 +
+    1/2 of the pair's square, 1.58 of an element's size; with a query's own rounding a score is off by sqrt(1.58^2 + 1) r11 =
+    1.87 r11 of its standard deviation, which is 4 for the largest blocks here: each probability by 7.5 r11 = 0.93 r8, and
+    outputs by no more than that.  1.05 for what a sample of 10,000 and more outputs may be off by."""
+    r8 = 2.0 ** -8 / 3 ** 0.5 / 1.39
+    for n, decode in ((1, True), (2, False), (60, False), (200, False)):
+        for prerotated in (0, 1):
+            b = Batch([(2000, n)], 16, 2, 128, torch.bfloat16, code, prerotated=prerotated, seed=n, decode=decode)
+            items = B.pic_attn8_plan_debug(b.cfg, b.host, decode)
+            many = (items[:, 3] - items[:, 2]).max() > 32
+            bound = 1.05 * r8 * (1.07 ** 2 + (1.0 if many else 0.0) + (0.0 if prerotated else 0.93 ** 2)) ** 0.5
+            got = b.check(b.run(), f"{n} tokens")
+            assert got <= bound, (n, prerotated, got, bound)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_spans_as_prefill_has_them(dtype, d):
+    """Several query spans of a request, detached, inheriting and dependent ones, windows of their own: what
+    pic_attn_prefill gives on a pool of the same numbers."""
+    rng = np.random.default_rng(d)
+    hq, hkv, code = 8, 2, K8.E4M3
+    seq = [500, 61, 333]
+    cu = [0, 5, 6, 9]
+    start = [0, 100, 160, 300, 420, 0, 0, 128, 200]
+    S, P, Q = B.PIC_SSEP, B.PIC_PDEP, B.PIC_QUERY
+    flags = [S, S | Q, Q, S, P | Q, S | Q, S | Q, Q, P | Q]
+    win = [-1, -1, -1, -1, -1, -1, -1, 60, -1]
+    host = B.HostBatch(seq, cu, start, flags, win)
+    need = [-(-s // 16) for s in seq]
+    nb = sum(need)
+    ids = rng.permutation(nb).astype(np.int32)
+    table = np.zeros((3, max(need)), np.int32)
+    for r, k in enumerate(need):
+        table[r, :k], ids = ids[:k], ids[k:]
+    codes_k, codes_v, scale = random_pool(rng, nb, hkv, d, code)
+    pool = pool_of(codes_k, codes_v, scale, code)
+    dense = [dev(K8.decode(c, code) * scale[..., i][:, :, None, None]).to(dtype) for i, c in enumerate((codes_k, codes_v))]
+    cfg = cfg_of(hq, hkv, d, dtype)
+    rows = 60 + 140 + 80 + 61 + 128 + 72 + 133
+    q = torch.from_numpy(rng.standard_normal((rows, hq, d)) * 0.5).to(dtype).cuda()
+    tables, pos = dev(table), dev(np.concatenate([np.arange(s) + 50 for s in seq]).astype(np.int32))
+    o, ref = torch.full_like(q, float("nan")), torch.empty_like(q)
+    ws8 = torch.empty(max(1, B.pic_attn8_workspace_size(cfg, host, False)), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(max(1, B.pic_workspace_size(cfg, host, False)), dtype=torch.uint8, device="cuda")
+    B.pic_attn8_prefill(cfg, host, tables, pos, q, o, pool, workspace=ws8)
+    B.pic_attn_prefill(cfg, host, tables, pos, q, ref, *dense, workspace=ws)
+    # the pool's numbers are exact in either type; the prefill rounds turned keys and queries to 8 bits each where this one has 11,
+    # and probabilities to 8 bits: a few times 2^-8 of the outputs' norm (float32: of 2^-24, times its sums' lengths)
+    err = float((o.double() - ref.double()).norm() / ref.double().norm())
+    say(f"  spans: {err:.2e}")
+    assert err < (1.5e-2 if dtype == torch.bfloat16 else 5e-6)
+
+
+class Step:
+    """Decode steps of a few requests: a projection's rows are normalised, stored in 8 bits and attended."""
+
+    def __init__(self, code, dtype, prerotated, seed=0):
+        self.code, self.dtype = code, dtype
+        self.hq, self.hkv, self.d, self.r, self.most = 8, 2, 64, 5, 90
+        self.cfg = cfg_of(self.hq, self.hkv, self.d, dtype, prerotated=prerotated)
+        self.rng = np.random.default_rng(seed)
+        self.nb = self.r * 6
+        self.table = self.rng.permutation(self.nb).reshape(self.r, 6).astype(np.int32)
+        shape = (self.nb, self.hkv, 16, self.d)
+        self.pool = B.Kv8Pool(torch.full(shape, 0x7f, dtype=torch.uint8, device="cuda"), torch.full(shape, 0x7f, dtype=torch.uint8, device="cuda"),
+                              torch.full((self.nb, self.hkv, 2), float("nan"), device="cuda"), code)
+        self.wq, self.wk = (1 + 0.1 * torch.randn(self.d, generator=torch.Generator().manual_seed(i)) for i in (1, 2))
+        self.wq, self.wk = self.wq.to(dtype).cuda(), self.wk.to(dtype).cuda()
+        self.tables = dev(self.table)
+        self.keys = [[] for _ in range(self.r)]     # as normalised, float64
+        self.values = [[] for _ in range(self.r)]
+
+    def rows(self, n):
+        return torch.from_numpy(self.rng.standard_normal((n, self.hq + 2 * self.hkv, self.d))).to(self.dtype).cuda()
+
+    def put(self, qkv, at, stream=None):
+        """Rows of (request, index): norms in place, the store."""
+        q, k, v = qkv[:, :self.hq], qkv[:, self.hq:self.hq + self.hkv], qkv[:, self.hq + self.hkv:]
+        pos = dev(np.array([i for _, i in at], np.int32))
+        slots = dev(np.array([self.table[r, i // 16] * 16 + i % 16 for r, i in at], np.int32))
+        B.pic_qk_norm(self.cfg, q, k, self.wq, self.wk, 1e-6, pos, stream=stream)
+        B.pic_kv8_write(self.cfg, self.pool, k, v, slots, stream=stream)
+        return q
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("prerotated", [0, 1])
+def test_prefill_then_steps_of_all(code, dtype, prerotated):
+    """Prompts of odd lengths, then tokens one by one into pools that held NaN: attention over the pool is attention over what
+    pic_kv8_read returns from it, and that is within the codes' error of the rows stored."""
+    s = Step(code, dtype, prerotated)
+    lens = [1, 15, 16, 33, 60]
+    qkv = s.rows(sum(lens))
+    stored = [[], []]
+    at = [(r, i) for r, n in enumerate(lens) for i in range(n)]
+    q = s.put(qkv, at)
+    stored = {x: qkv[j, s.hq:].double().cpu() for j, x in enumerate(at)}
+    for step in range(20):
+        host = B.HostBatch([n + step for n in lens], range(s.r + 1), [0] * s.r, [B.PIC_PDEP | (B.PIC_QUERY if step == 0 else 0)] * s.r)
+        decode = step > 0
+        if decode:
+            new = s.rows(s.r)
+            at = [(r, n + step - 1) for r, n in enumerate(lens)]
+            q = s.put(new, at)
+            stored.update({x: new[j, s.hq:].double().cpu() for j, x in enumerate(at)})
+        q = q.contiguous()
+        total = [n + step for n in lens]
+        positions = dev(np.concatenate([np.arange(n) for n in total]).astype(np.int32))
+        o = torch.full_like(q, float("nan"))
+        ws = torch.empty(max(1, B.pic_attn8_workspace_size(s.cfg, host, decode)), dtype=torch.uint8, device="cuda")
+        (B.pic_attn8_decode if decode else B.pic_attn8_prefill)(s.cfg, host, s.tables, positions, q, o, s.pool, workspace=ws)
+        slots = dev(np.array([s.table[r, i // 16] * 16 + i % 16 for r, n in enumerate(total) for i in range(n)], np.int32))
+        k, v = (torch.empty(len(slots), s.hkv, s.d, dtype=dtype, device="cuda") for _ in range(2))
+        B.pic_kv8_read(s.cfg, s.pool, slots, k, v)
+        # half a step of rounding as it is stored, and less than another half over the growths of a block's scale
+        scale = s.pool.scale[slots.long() // 16].double().cpu()
+        ref = torch.stack([stored[r, i] for r, n in enumerate(total) for i in range(n)])
+        for i, (x, want) in enumerate(((k, ref[:, :s.hkv]), (v, ref[:, s.hkv:]))):
+            sc = scale[..., i, None]
+            unit = sc if code == K8.INT8 else torch.maximum(torch.exp2(torch.floor(torch.log2((want / sc).abs().clamp(min=2.0 ** -6))) - 3), torch.tensor(2.0 ** -9)) * sc
+            assert ((x.double().cpu() - want).abs() <= unit).all(), (step, i)
+        row, off = 0, 0
+        kk, vv, qq = f64(k), f64(v), f64(q)
+        for r, n in enumerate(total):
+            m = n if not decode else 1
+            kr, qr = kk[off:off + n], qq[row:row + m]
+            if not prerotated:
+                kr = T.rotate(kr, np.arange(n), s.d, 1e4, 0)
+                qr = T.rotate(qr, np.arange(n - m, n), s.d, 1e4, 0)
+            want, spread = T.attention(qr, kr, vv[off:off + n], np.arange(n) <= np.arange(n - m, n)[:, None], s.d ** -0.5)
+            err = np.abs(f64(o[row:row + m]) - want)
+            bound = (2.0 ** -6 if dtype == torch.bfloat16 else 2.0 ** -15) * (np.abs(want) + spread) + 1e-30
+            assert (err <= bound).all(), (step, r, float((err / bound).max()))
+            row, off = row + m, off + n
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_step_captured_and_replayed(code):
+    """A captured norm, store and attention give, on every replay, what eager ones give on the same inputs; two graphs share a
+    workspace."""
+    dtype = torch.bfloat16
+    s, e = Step(code, dtype, 0, seed=3), Step(code, dtype, 0, seed=3)
+    lens = [40, 3, 17, 64, 80]
+    first = s.rows(sum(lens))
+    at = [(r, i) for r, n in enumerate(lens) for i in range(n)]
+    for x in (s, e):
+        x.put(first.clone(), at)
+    total = [n + 1 for n in lens]
+    host = B.HostBatch(total, range(6), [0] * 5, [B.PIC_PDEP] * 5)
+    new = s.rows(5)
+    at = [(r, n) for r, n in enumerate(lens)]
+    pos = dev(np.array([i for _, i in at], np.int32))
+    slots = dev(np.array([s.table[r, i // 16] * 16 + i % 16 for r, i in at], np.int32))
+    positions = dev(np.concatenate([np.arange(n) for n in total]).astype(np.int32))
+    ws = torch.empty(max(1, B.pic_attn8_workspace_size(s.cfg, host, True)) + 4096, dtype=torch.uint8, device="cuda")
+    buf, qo = torch.empty_like(new), torch.empty(5, s.hq, s.d, dtype=dtype, device="cuda")
+
+    def run(x, buf, qo, o, stream=None):
+        q, k, v = buf[:, :x.hq], buf[:, x.hq:x.hq + x.hkv], buf[:, x.hq + x.hkv:]
+        B.pic_qk_norm(x.cfg, q, k, x.wq, x.wk, 1e-6, pos, q_out=qo, stream=stream)
+        B.pic_kv8_write(x.cfg, x.pool, k, v, slots, stream=stream)
+        B.pic_attn8_decode(x.cfg, host, x.tables, positions, qo, o, x.pool, workspace=ws, stream=stream)
+
+    other = Batch([(700, 30), (20, 9)], 8, 2, 64, seed=5)
+    ref = other.run()
+    other_ws = torch.empty(max(ws.numel(), other.ws.numel()), dtype=torch.uint8, device="cuda")
+    ws = other_ws
+    o, eo, oo = torch.empty_like(qo), torch.empty_like(qo), torch.empty_like(ref)
+    torch.cuda.synchronize()
+    graph, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(s, buf, qo, o, stream=torch.cuda.current_stream())
+    with torch.cuda.graph(second):
+        other.run(o=oo, ws=other_ws, stream=torch.cuda.current_stream())
+    for i in range(4):
+        rows = new * (1 + i)   # (scales grow: a replay works on the pool as it is)
+        buf.copy_(rows)
+        ebuf = rows.clone()
+        o.zero_(), oo.zero_()
+        graph.replay()
+        second.replay()
+        run(e, ebuf, torch.empty_like(qo), eo)
+        torch.cuda.synchronize()
+        assert torch.equal(o, eo) and torch.equal(oo, ref)
+        assert torch.equal(s.pool.k, e.pool.k) and torch.equal(s.pool.v, e.pool.v) and torch.equal(s.pool.scale.view(torch.int32), e.pool.scale.view(torch.int32))
+
+
+def test_calls_on_two_streams_and_repeats_agree():
+    """Calls that overlap on two streams, each with its own workspace, and repeats: bit for bit."""
+    a, b = Batch([(3000, 1)] * 7, 8, 2, 128, seed=1, decode=True), Batch([(2000, 9), (700, 70)], 8, 2, 128, seed=2)
+    ra, rb = a.run(), b.run()
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = [(torch.empty_like(ra), torch.empty_like(rb)) for _ in range(5)]
+    torch.cuda.synchronize()
+    for oa, ob in outs:
+        a.run(o=oa, stream=s)
+        b.run(o=ob, stream=t)
+    torch.cuda.synchronize()
+    for oa, ob in outs:
+        assert torch.equal(oa, ra) and torch.equal(ob, rb)
+
+
+def test_many_requests_captured_and_replayed():
+    """More spans than the kernel arguments hold: the captured call uploads its plan on every replay."""
+    rng = np.random.default_rng(11)
+    for decode in (False, True):
+        b = Batch([(int(rng.integers(1, 300)), 1 if decode else int(rng.integers(1, 20))) for _ in range(80)], 8, 2, 64, seed=12, decode=decode)
+        ref = b.run()
+        torch.cuda.synchronize()
+        o = torch.zeros_like(ref)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            b.run(o=o, stream=torch.cuda.current_stream())
+        for _ in range(3):
+            o.zero_()
+            b.ws.fill_(255)
+            graph.replay()
+            junk = torch.randn(1 << 16, device="cuda")
+            torch.cuda.synchronize()
+            assert torch.equal(o, ref) and junk.numel()
+
+
+def test_float32_in_a_small_workspace():
+    """Without room for partial results float32 keys stay unsplit: the same sums in another order."""
+    for lens, decode in (([(700, 5)], False), ([(900, 30), (64, 3)], False), ([(3000, 1)], True)):
+        b = Batch(lens, 8, 2, 64, torch.float32, K8.INT8, seed=7, decode=decode)
+        for ws in (torch.empty(0, dtype=torch.uint8, device="cuda"), torch.empty(256, dtype=torch.uint8, device="cuda")):
+            assert b.ws.numel() > ws.numel()
+            b.check(b.run(ws=ws), "small workspace")
+
+
+def test_pool_past_4_gib():
+    """The same blocks at the far end of a pool of 4.3 GiB of keys (and of values): bit for bit."""
+    for dtype, n, decode in ((torch.bfloat16, 1, True), (torch.bfloat16, 40, False), (torch.float32, 3, False)):
+        b = Batch([(130, n), (77, n)], 8, 8, 128, dtype, K8.INT8, seed=n, decode=decode)
+        want = b.run()
+        per = 8 * 16 * 128
+        nb = ((43 << 30) // 10) // per
+        k, v = (torch.empty(nb, 8, 16, 128, dtype=torch.uint8, device="cuda") for _ in range(2))
+        scale = torch.empty(nb, 8, 2, device="cuda")
+        far = nb - b.nb
+        k[far:], v[far:], scale[far:] = b.pool.k, b.pool.v, b.pool.scale
+        pool = B.Kv8Pool(k, v, scale, K8.INT8)
+        tables = b.block_tables
+        b.block_tables = torch.where(tables < b.nb, tables + far, tables)
+        assert torch.equal(b.run(pool=pool), want)
+        # rows stored and read there
+        slots = (torch.arange(40, device="cuda", dtype=torch.int32) + far * 16).contiguous()
+        rows = torch.randn(40, 8, 128, device="cuda").to(dtype)
+        near = B.Kv8Pool(torch.zeros_like(b.pool.k), torch.zeros_like(b.pool.v), torch.zeros_like(b.pool.scale), K8.INT8)
+        B.pic_kv8_write(b.cfg, pool, rows, rows * 2, slots)
+        B.pic_kv8_write(b.cfg, near, rows, rows * 2, slots - far * 16)
+        assert torch.equal(k[far:far + 3], near.k[:3]) and torch.equal(v[far:far + 3], near.v[:3]) and torch.equal(scale[far:far + 3], near.scale[:3])
+        got, ref = ([torch.empty_like(rows), torch.empty_like(rows)] for _ in range(2))
+        B.pic_kv8_read(b.cfg, pool, slots, *got)
+        B.pic_kv8_read(b.cfg, near, slots - far * 16, *ref)
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+        del k, v, scale, pool
+
+
+def tile_of(b):
+    """Row tile of a batch's plan, and whether its keys are split."""
+    items = B.pic_attn8_plan_debug(b.cfg, b.host, b.decode)
+    rows = (items[:, 3] - items[:, 2]).max()
+    return min(t for t in (16, 32, 128, 256) if rows <= t), bool((items[:, 7] >= 0).any())
+
+
+# what the plans of these batches are is asserted, so that every kernel, split and not, and every layout of heads over the
+# dies (8 KV heads and multiples, and others) is among them
+LARGE = [(32, 8, 128, [(1500, 100), (750, 91)], 128, True), (32, 8, 128, [(30, 600)], 128, False),
+         (32, 8, 128, [(900, 70)] + [(450, 61)] * 7, 256, True), (32, 8, 128, [(300, 60)] + [(150, 51)] * 23, 256, False),
+         (10, 5, 128, [(30, 600)], 128, True), (10, 5, 128, [(300, 60)] + [(150, 51)] * 23, 128, False),
+         (12, 12, 64, [(2500, 130), (1250, 121), (1250, 121)], 256, True), (12, 12, 64, [(300, 60)] + [(150, 51)] * 23, 128, False),
+         (64, 8, 128, [(30, 600)], 256, False), (6, 1, 64, [(700, 300), (350, 291)], 128, True), (6, 1, 64, [(0, 1000)], 256, True),
+         (8, 2, 64, [(0, 1000)], 128, True)]
+
+
+@pytest.mark.parametrize("case", range(len(LARGE)))
+@pytest.mark.parametrize("code", CODES)
+def test_large_row_tiles(case, code):
+    hq, hkv, d, lens, tile, split = LARGE[case]
+    b = Batch(lens, hq, hkv, d, torch.bfloat16, code, seed=case)
+    assert tile_of(b) == (tile, split)
+    b.check(b.run(), f"case {case}")
+
+
+@pytest.mark.parametrize("style,rot,prerotated", [(1, 0, 0), (0, 32, 0), (0, 16, 0), (1, 34, 0), (1, 2, 0), (0, 0, 1)])
+@pytest.mark.parametrize("case", [0, 1, 2, 3, 6, 7, 8])
+def test_large_row_tiles_and_rotations(case, style, rot, prerotated):
+    hq, hkv, d, lens, tile, split = LARGE[case]
+    b = Batch(lens[:6], hq, hkv, d, torch.bfloat16, CODES[case % 2], style, rot, prerotated, seed=case)
+    if len(lens) < 7:
+        assert tile_of(b) == (tile, split)
+    b.check(b.run(), f"case {case}")
+
+
+@pytest.mark.parametrize("what", ["positions", "jumps", "scales", "zeros", "sizes", "windows", "outside"])
+@pytest.mark.parametrize("case", [0, 1, 2, 5, 6, 11])
+def test_large_row_tiles_and_values(case, what):
+    hq, hkv, d, lens, tile, split = LARGE[case]
+    rng = np.random.default_rng(case)
+    kw = {"positions": dict(positions=lambda rng, m: rng.integers(-2**31, 2**31, m)),
+          "jumps": dict(positions=lambda rng, m: np.arange(m) // 40 * 999 + np.arange(m)), "scales": dict(powers=False)}.get(what, {})
+    if what == "windows":
+        lens = [(ctx, n, int(rng.integers(0, ctx // 8 + 1))) for ctx, n in lens]
+    b = Batch(lens, hq, hkv, d, torch.bfloat16, CODES[case % 2], seed=case, **kw)
+    if what != "windows":
+        assert tile_of(b) == (tile, split)
+    assert tile_of(b)[0] >= 128
+    scale = b.scale.copy()
+    if what == "zeros":
+        scale[::3] = 0.0
+    if what == "sizes":
+        scale = np.exp2(b.rng.integers(-100, -6, scale.shape)).astype(np.float32)
+        scale[..., 1] = np.exp2(b.rng.integers(-40, 40, scale.shape[:2]))
+    if what in ("zeros", "sizes"):
+        b.set_pool(b.k_codes, b.v_codes, scale)
+    o = b.run()
+    b.check(o, what)
+    if what == "outside":
+        used = np.zeros((b.nb, 16), bool)
+        for r, (ctx, m, w) in enumerate(b.lens):
+            j = np.arange(w, ctx + m)
+            used[b.table[r, j // 16], j % 16] = True
+        k, v = b.k_codes.copy(), b.v_codes.copy()
+        for c in (k, v):
+            c.swapaxes(1, 2)[~used] = 0x7f
+        scale[~used.any(1)] = np.nan
+        assert torch.equal(b.run(pool=pool_of(k, v, scale, b.code)), o)
