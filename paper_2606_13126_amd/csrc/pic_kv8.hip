@@ -411,11 +411,13 @@ __device__ __forceinline__ Group find_group(const PlanOf<N>& plan, int bid) {
 // neighbouring dimensions of four keys, two byte permutes part them.  The 32-deep product
 // holds the 16 keys twice, for a probability as two bf16 numbers (16 bits in all).
 //
-// RoPE: a lane holds 8 dimensions each of KD chunks of key l%16: PL pairs, whose cos/sin advance from one
-// of the wave's blocks to its next by a constant rotation where the positions do (renewed every
-// kKv8Renew steps), else are computed.  Codes turn in packed float16, two pairs at a time.
+// RoPE: with b the position of a block's first key, (R_p q).(R_(b+j) k) = (R_(-b) R_p q).(R_j k).  Where a block's
+// positions follow one another its keys turn by their place j in it, the same for every block, whose cos/sin a lane
+// holds in registers (of its 4 KD pairs of key l%16), and the queries turn back by b, whose cos/sin are 64 numbers
+// of the whole wave, one of a lane.  Other blocks' keys turn by the positions that they have, less b.  Turning is done
+// in packed float16, two pairs at a time: 16 operations of a lane for the queries of a block and 16 for its keys
+// (D 128: twice that), where angles of each key that advance from block to block cost 5 a pair beside the keys' own.
 // ---------------------------------------------------------------------------------
-constexpr int kKv8Renew = 32;
 
 template <int D, int CB>
 struct Kv8Few {
@@ -437,8 +439,9 @@ struct __attribute__((aligned(16))) Kv8FewLds {
     uint8_t stages[S::NST][S::NW][2][S::TILE];
     uint16_t q[CB][D / 32][64][8];               // B operands: words of 4 pairs of the lanes, x then y
     float qs[16 * CB];
-    float2 stride_cs[D / 2];                     // cos/sin of STEP positions
     uint64_t fstep[D / 2];
+    uint16_t places[kBlock][D / 8][8];           // cos/sin of 0 .. 15 positions: of 4 pairs, cos then sin
+    uint16_t base[S::NW][D / 8][8];              // ... of a wave's block
     int32_t meta[S::NW][S::NST][S::META];
 };
 
@@ -453,13 +456,28 @@ __device__ __forceinline__ int vswz(int key) { return D == 128 ? ((key >> 1) & 3
 // of up to 634 each, stay in range
 __device__ __forceinline__ int query_exponent(float big) { return big > 0.f && big < INFINITY ? __builtin_amdgcn_frexp_expf(big) : 0; }
 
+// Four pairs (x 0-1, x 2-3, y 0-1, y 2-3) turned by the angles of cs (cos, then sin), or back by them
+__device__ __forceinline__ u32x4_t turned(const u32x4_t& v, const u32x4_t& cs, bool back) {
+    u32x4_t out;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t xw = v[h], yw = v[2 + h], cw = cs[h], sw = cs[2 + h];   // (a bit cast of a vector's element would read its first)
+        const f16x2_t x = __builtin_bit_cast(f16x2_t, xw), y = __builtin_bit_cast(f16x2_t, yw), c = __builtin_bit_cast(f16x2_t, cw);
+        f16x2_t s = __builtin_bit_cast(f16x2_t, sw);
+        if (back) s = -s;
+        out[h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, c, -(y * s)));
+        out[2 + h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, c, x * s));
+    }
+    return out;
+}
+
 template <int D, int STYLE, bool ROPE, int CODE, int CB, int NG>
 __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_few(const PlanOf<NG> plan, const Kv8Args a) {
     typedef Kv8Few<D, CB> S;
     typedef Code<CODE> C;
     constexpr int KD = D / 32;             // 16x16x32 contraction steps of QK^T; words of 4 pairs of a lane
     constexpr int DB = D / 32;             // 32-dim blocks of O^T
-    constexpr int TK = S::TK, NW = S::NW, NST = S::NST, HALF = D / 2, PL = 4 * KD;
+    constexpr int TK = S::TK, NW = S::NW, NST = S::NST, HALF = D / 2;
     static_assert(S::TILE * 2 * NST >= CB * 2 * DB * 1024, "a wave's outputs fit its stages");
 
     __shared__ Kv8FewLds<D, CB> lds;
@@ -523,17 +541,26 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 #pragma unroll
     for (int u = 0; u < NST - 1; ++u)
         if (u < nt) issue(u, u, block_at(u));
-    if (ROPE)
-        for (int i = threadIdx.x; i < HALF; i += NW * 64) {
-            lds.fstep[i] = a.fstep[i];
-            rope_cs_fast(S::STEP, a.fstep[i], lds.stride_cs[i].x, lds.stride_cs[i].y);
+    // cos/sin of pair p to where the lanes of its word read them
+    auto put_cs = [](uint16_t (*to)[8], int p, float c, float s) {
+        to[p >> 2][p & 3] = __builtin_bit_cast(uint16_t, (_Float16)c);
+        to[p >> 2][4 + (p & 3)] = __builtin_bit_cast(uint16_t, (_Float16)s);
+    };
+    const int my_pair = lane % HALF;
+    const uint64_t my_step = ROPE ? a.fstep[my_pair] : 0;
+    if (ROPE) {
+        if (wave == 0) lds.fstep[my_pair] = my_step;
+#pragma unroll
+        for (int k = 0; k < TK; k += NW * 64 / HALF) {
+            float c, s;
+            const int place = k + (int)threadIdx.x / HALF;
+            rope_cs_fast(place, my_step, c, s);
+            put_cs(lds.places[place], my_pair, c, s);
         }
+    }
 
-    // the lane's pair i (words of 4 pairs): pair0 + pair_at(i)
-    const int pair0 = (STYLE == kNeox ? 8 : 4) * q4;
-    auto pair_at = [](int i) { return STYLE == kNeox ? i / 8 * 32 + i % 8 : i / 4 * 16 + i % 4; };
-    const uint64_t* fs = lds.fstep + pair0;
-    const float2* ahead = lds.stride_cs + pair0;
+    // the lane's words of 4 pairs: word i holds pairs 4 word_at(i) ..
+    auto word_at = [&](int i) { return STYLE == kNeox ? i / 2 * 8 + 2 * q4 + i % 2 : 4 * i + q4; };
 
     // ---- queries: the waves turn 2 CB rows each, LPR lanes a row, and leave the B operands of all in LDS
     // (from where every tile reads them: in registers they would leave room for two waves per SIMD only)
@@ -631,9 +658,10 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) acc[cb][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    float rc[PL], rs[PL];      // cos/sin of the lane's pairs at position cs_pos
-    int32_t cs_pos = 0;
-    int renew = 0;             // steps until they are computed again
+    u32x4_t place[ROPE ? KD : 1];   // cos/sin of the lane's key's place in its block, words as in lds.places
+    if constexpr (ROPE)
+#pragma unroll
+        for (int i = 0; i < KD; ++i) place[i] = *reinterpret_cast<const u32x4_t*>(lds.places[c16][word_at(i)]);
 
     int st = 0, blk = 0;
     if (NST - 1 < nt) blk = block_at(NST - 1);
@@ -654,27 +682,18 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
         for (int kd = 0; kd < KD; ++kd) kw[kd] = *reinterpret_cast<const u32x2_t*>(tile + k_off[kd]);
         const float ks = __int_as_float(meta[16]), vs = __int_as_float(meta[17]);
         f32x4_t sc[CB];
+        bool apart = false;   // the block's positions do not follow one another
+        int64_t away = 0;     // the lane's key's position less the block's
         if constexpr (ROPE) {
+            const int first = max(k_lo - k0, 0);   // (keys outside the range stand for others)
             const int32_t pos = meta[c16];
-            // (STEP on, and not past the type's end)
-            if (renew == 0 || __builtin_amdgcn_ballot_w64((uint32_t)pos != (uint32_t)cs_pos + S::STEP || pos < cs_pos) != 0) {
-#pragma unroll
-                for (int i = 0; i < PL; ++i) {
-                    rope_cs_fast(pos, fs[pair_at(i)], rc[i], rs[i]);
-                    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (side by side they would take more registers than there are)
-                }
-                renew = kKv8Renew;
-            } else {
-#pragma unroll
-                for (int i = 0; i < PL; ++i) {
-                    const float2 d = ahead[pair_at(i)];
-                    const float c = rc[i], s = rs[i];
-                    rc[i] = c * d.x - s * d.y;
-                    rs[i] = s * d.x + c * d.y;
-                }
-            }
-            --renew;
-            cs_pos = pos;
+            const int64_t b = (int64_t)__builtin_amdgcn_readlane(pos, first) - first;
+            away = pos - b;
+            apart = __builtin_amdgcn_ballot_w64(away != c16 && c16 >= first && k0 + c16 < k_hi) != 0;
+            float c, s;
+            rope_cs_fast(b, my_step, c, s);
+            put_cs(lds.base[wave], my_pair, c, s);
+            __atomic_signal_fence(__ATOMIC_SEQ_CST);
         }
 #pragma unroll
         for (int i = 0; i < KD; ++i) {
@@ -687,16 +706,18 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
                 xw = __builtin_amdgcn_perm(kw[i][1], kw[i][0], 0x06040200u);
                 yw = __builtin_amdgcn_perm(kw[i][1], kw[i][0], 0x07050301u);
             }
+            u32x4_t cs, bs;   // cos/sin of the keys' angles and of the queries'
             if constexpr (ROPE) {
+                cs = place[i];
+                if (apart) {
+                    float c[4], s[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t xb = h ? C::halves_hi(xw) : C::halves_lo(xw), yb = h ? C::halves_hi(yw) : C::halves_lo(yw);
-                    const f16x2_t x = __builtin_bit_cast(f16x2_t, xb), y = __builtin_bit_cast(f16x2_t, yb);
-                    const int p = 4 * i + 2 * h;
-                    const f16x2_t c = __builtin_bit_cast(f16x2_t, pack_f16(rc[p], rc[p + 1])), s = __builtin_bit_cast(f16x2_t, pack_f16(rs[p], rs[p + 1]));
-                    kf[h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, c, -(y * s)));
-                    kf[2 + h] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, c, x * s));
+                    for (int e = 0; e < 4; ++e) rope_cs_fast(away, lds.fstep[4 * word_at(i) + e], c[e], s[e]);
+                    cs = u32x4_t{pack_f16(c[0], c[1]), pack_f16(c[2], c[3]), pack_f16(s[0], s[1]), pack_f16(s[2], s[3])};
                 }
+                bs = *reinterpret_cast<const u32x4_t*>(lds.base[wave][word_at(i)]);
+                const u32x4_t k = {C::halves_lo(xw), C::halves_hi(xw), C::halves_lo(yw), C::halves_hi(yw)};
+                kf = turned(k, cs, false);
             } else {
                 const u32x2_t xb = C::bf16s(xw), yb = C::bf16s(yw);
                 kf = u32x4_t{xb[0], xb[1], yb[0], yb[1]};
@@ -705,8 +726,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
             for (int cb = 0; cb < CB; ++cb) {
                 const f32x4_t from = i == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : sc[cb];
                 const u32x4_t qb = *reinterpret_cast<const u32x4_t*>(lds.q[cb][i][lane]);
-                if (ROPE)
-                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kf), __builtin_bit_cast(f16x8_t, qb), from, 0, 0, 0);
+                if constexpr (ROPE)
+                    sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kf), __builtin_bit_cast(f16x8_t, turned(qb, bs, true)), from, 0, 0, 0);
                 else
                     sc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qb), from, 0, 0, 0);
             }
@@ -839,6 +860,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 // The row sum adds the p' of a block, rounded to bf16 as they are multiplied, times 1 / v.
 // ---------------------------------------------------------------------------------
 constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
+
+constexpr int kKv8Renew = 32;   // steps after which angles are computed again
 
 template <int D>
 struct __attribute__((aligned(2 * D))) Kv8ManyLds {
