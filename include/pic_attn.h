@@ -395,10 +395,12 @@ pic_status pic_attn8_workspace_size(const pic_config* cfg, const pic_batch_host*
 /* pic_attn_prefill and pic_attn_decode over a pool of 8-bit codes: the same batch, masks, q, o and
  * workspace rules.  cos/sin are computed in the kernel (no table).
  * How exact: codes and scales enter exactly; sums and softmax statistics are float32.  float32 calls compute in
- * float32.  In bf16, besides the result's own rounding: turned queries are rounded to 11 bits; cos/sin of keys, their
- * products and the turned keys to 11 bits each, at angles within 2^-17 (as in pic_attn_tree); without
- * rotation both are exact; probabilities (times their block's scale of values) have 16 bits where a call's row tiles
- * hold at most 32 rows (query tokens x query heads of a KV head) and 8 bits where they hold more.
+ * float32.  In bf16, besides the result's own rounding: turned queries are rounded to 11 bits, and cos/sin of keys, their
+ * products and the turned keys to 11 bits each.  Where a call's row tiles hold at most 32 rows (query tokens x query
+ * heads of a KV head) keys turn by their place in the block and queries back by the block's position, with the same
+ * roundings once more for the queries; probabilities (times their block's scale of values) have 16 bits.  Where
+ * they hold more, angles of keys are within 2^-17 (as in pic_attn_tree), probabilities have 8 bits, and a block's scale
+ * of values below 2^-90 counts as 2^-90.  Without rotation queries and keys are exact.
  * Values times 2^8 must stay within float32. */
 pic_status pic_attn8_prefill(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev, const void* q,
                              void* o, const pic_kv8_pool* pool, void* workspace, size_t workspace_bytes, void* stream);

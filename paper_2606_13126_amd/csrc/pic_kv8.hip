@@ -50,7 +50,8 @@ __device__ __forceinline__ float sum_of(float x) {
 // elements pair up, GPT-J (and what does not turn) two neighbours.  The lanes of a head are
 // neighbours, so its squares meet by lane permutes.  The row's threads put its cos/sin and the weights into
 // LDS once, while its first units are on their way.
-// Bound by memory: every element is read and written once.
+// Bound by memory: every element is read and written once.  16,384 rows of 64 + 8 heads of 128 (604 MB): 101 us, 5.9
+// TB/s; 64 rows of 32 + 8 heads 3.0, two latencies.
 // ---------------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
 
@@ -228,7 +229,8 @@ struct Code {
 // stores in the block give the scale (a maximum over the wave), then lane l codes 16 elements of offset
 // l / (D / 16) (and 64 / (D / 16) offsets on), so that a page leaves in whole lines.  A block belongs to the first of
 // its rows, which follow one another: a workgroup looks for blocks that begin among `range` rows.
-// Bound by memory for prompts, by its chain of loads (slots, then rows) for a step's tokens.
+// Bound by memory for prompts (104 MB, 8 heads of 128: 20.1 us, 5.2 TB/s), by its chain of loads (slots, then rows)
+// for a step's tokens (64 rows: 4.4 us).
 // ---------------------------------------------------------------------------------
 constexpr int kWriteWaves = 4;
 
@@ -337,7 +339,8 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
 }
 
 // ---------------------------------------------------------------------------------
-// kv8_read: a thread takes the codes of 16 bytes of output (4 or 8), U of them in flight.  Bound by memory.
+// kv8_read: a thread takes the codes of 16 bytes of output (4 or 8), U of them in flight.  Bound by memory: 33,280
+// rows of 8 heads of 128 (204 MB) 30.2 us, 6.8 TB/s (codes that lie in the cache among them).
 // ---------------------------------------------------------------------------------
 template <typename T, int D, int CODE, bool STREAMS>
 __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool,
@@ -416,7 +419,12 @@ __device__ __forceinline__ Group find_group(const PlanOf<N>& plan, int bid) {
 // holds in registers (of its 4 KD pairs of key l%16), and the queries turn back by b, whose cos/sin are 64 numbers
 // of the whole wave, one of a lane.  Other blocks' keys turn by the positions that they have, less b.  Turning is done
 // in packed float16, two pairs at a time: 16 operations of a lane for the queries of a block and 16 for its keys
-// (D 128: twice that), where angles of each key that advance from block to block cost 5 a pair beside the keys' own.
+// (D 128: twice that), where angles of each key that advance from block to block cost 5 a pair beside the keys' own
+// (64 requests x 8,192 keys of int8, 32 / 8 heads of 128: 204.6 us, 211.8 with those).
+//
+// Bound by memory and by the vector unit about alike where the card is full: the same call 196 us at its best, 5.5 TB/s, the
+// vector unit busy 66% of the cycles and the matrix cores 10%; 192 without rotation.  Few keys: by the chain of
+// plan, block ids, codes, products and the meeting of the waves (7.2 us over 1,025 keys).
 // ---------------------------------------------------------------------------------
 
 template <int D, int CB>
@@ -427,8 +435,10 @@ struct Kv8Few {
     static constexpr int CPR = D / 16;           // 16-byte chunks per row
     static constexpr int KPC = 64 / CPR;         // keys of a copy (64 chunks)
     static constexpr int NC = TK / KPC;          // copies of a step, each of K and V
-    static constexpr int NST = D == 64 || CB > 1 ? 4 : 2;   // steps in LDS
-    static constexpr int WAVES = CB > 1 ? 2 : 4; // per SIMD
+    // Steps in LDS, and waves per SIMD: at 16 rows of 128 dims four waves with two steps each hide more than two with four
+    // (the call above 204 against 224 us, spans that 64 requests share 141 against 174)
+    static constexpr int NST = D == 64 || CB > 1 ? 4 : 2;
+    static constexpr int WAVES = CB > 1 ? 2 : 4;
     static constexpr int LPS = 2 * NC + 1;       // copies per lane per step
     static constexpr int META = 20;              // a step's positions (16) and its two scales
 };
@@ -858,6 +868,10 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 // The scales cost a few operations a step: the scores of a block's keys are multiplied in the addition that
 // the exponential needs anyway, and the values' scale joins its exponent: p' = 2^(s - m + log2 v).
 // The row sum adds the p' of a block, rounded to bf16 as they are multiplied, times 1 / v.
+//
+// Bound by vector work and products, which hardly overlap: of about 5,100 cycles of a step of 256 rows the products are
+// 2,048 (38% of the cycles by the counters), the vector work, with quarter-rate exponentials, most of the others.
+// 2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1.32-1.36 ms, 860-888 TFLOP/s; on turned keys 1.17, 1000.
 // ---------------------------------------------------------------------------------
 constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
 

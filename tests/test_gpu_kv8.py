@@ -232,6 +232,19 @@ def test_write_long_prompts(code, hkv, d):
     st.check_read(flat)
 
 
+@pytest.mark.parametrize("n", [256, 257, 512, 513, 1024, 1025, 2048, 2049])
+def test_write_rows_and_their_workgroups(n):
+    """The numbers of rows around which a workgroup looks through twice as many: runs of 1 to 40 tokens, padding between."""
+    st = Store(n // 4 + 400, 2, 64, K8.INT8 if n % 2 else K8.E4M3, torch.bfloat16, seed=n, scale=2.0 ** -6)
+    blocks = iter(st.rng.permutation(st.nb))
+    slots = []
+    while len(slots) < n:
+        run, first = int(st.rng.integers(1, 41)) if st.rng.random() < 0.4 else 1, int(st.rng.integers(0, 16))
+        table = [next(blocks) for _ in range((first + run - 1) // 16 + 1)]
+        slots += [table[(first + i) // 16] * 16 + (first + i) % 16 for i in range(run)] + [-1] * int(st.rng.integers(0, 2))
+    st.put(np.array(slots[:n]), st.rows(n, 5.0))
+
+
 @pytest.mark.parametrize("code", CODES)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_write_what_is_no_number(code, dtype):
