@@ -355,7 +355,7 @@ typedef struct pic_kv8_pool {
  *  q_weight, k_weight  DEVICE [D] in cfg->dtype, or NULL (ones).
  * Strides are at least a row and multiples of 16 bytes.  Computed in float32 and rounded once to
  * cfg->dtype; a row's squares are summed in float32 (elements of 2^60 and more may pass its range).  cos/sin are
- * those of pic_kv_append.  eps > 0, n < 2^24 per call. */
+ * those of pic_kv_append.  eps > 0 and not denormal, n < 2^24 per call. */
 pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                        const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, const void* q_weight,
                        const void* k_weight, float eps, const int32_t* positions, int32_t n, void* stream);
@@ -377,7 +377,7 @@ pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, v
  * block or a padding row between them makes the call a race); of rows of one slot the last counts.  A block that is
  * not started by its offset 0 needs a scale in the pool: 0 where nothing was stored before.
  *  k_new, v_new  DEVICE rows of [Hkv][D] dense elements of cfg->dtype, row i at i * stride elements
- *                (strides as in pic_kv_append).
+ *                (strides as in pic_kv_append).  They must not overlap the pool.
  * n < 2^24 per call. */
 pic_status pic_kv8_write(const pic_config* cfg, const pic_kv8_pool* pool, const void* k_new, int64_t k_stride,
                          const void* v_new, int64_t v_stride, const int32_t* slot_mapping, int32_t n, void* stream);
@@ -398,8 +398,8 @@ pic_status pic_attn8_workspace_size(const pic_config* cfg, const pic_batch_host*
  * float32.  In bf16, besides the result's own rounding: turned queries are rounded to 11 bits, and cos/sin of keys, their
  * products and the turned keys to 11 bits each.  Where a call's row tiles hold at most 32 rows (query tokens x query
  * heads of a KV head) keys turn by their place in the block and queries back by the block's position, with the same
- * roundings once more for the queries; probabilities (times their block's scale of values) have 16 bits.  Where
- * they hold more, angles of keys are within 2^-17 (as in pic_attn_tree), probabilities have 8 bits, and a block's scale
+ * roundings once more for the queries; probabilities (times their block's scale of values) have 16 bits (small
+ * ones fewer where that scale is below 2^-100).  Where they hold more, angles of keys are within 2^-17 (as in pic_attn_tree), probabilities have 8 bits, and a block's scale
  * of values below 2^-90 counts as 2^-90.  Without rotation queries and keys are exact.
  * Values times 2^8 must stay within float32. */
 pic_status pic_attn8_prefill(const pic_config* cfg, const pic_batch_host* batch, const pic_batch_dev* dev, const void* q,

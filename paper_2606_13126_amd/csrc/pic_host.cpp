@@ -1230,7 +1230,7 @@ pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, v
     pic_status st = check_config(cfg);
     if (st) return st;
     if (n < 0) return fail(PIC_EINVAL, "n must be >= 0");
-    if (!(eps > 0.f) || !std::isfinite(eps)) return fail(PIC_EINVAL, "eps must be positive and finite");
+    if (!(eps >= std::numeric_limits<float>::min()) || !std::isfinite(eps)) return fail(PIC_EINVAL, "eps must be a positive normal number");
     if (n >= (1 << 24)) return fail(PIC_EINVAL, "n must be < 2^24 rows per call");
     if (n == 0) return PIC_OK;
     if ((q == nullptr) != (q_out == nullptr)) return fail(PIC_EINVAL, "q and q_out must both be given or both be NULL");
@@ -1300,6 +1300,12 @@ pic_status pic_kv8_write(const pic_config* cfg, const pic_kv8_pool* pool, const 
     const int64_t es = cfg->dtype == PIC_F32 ? 4 : 2, row = (int64_t)cfg->num_kv_heads * cfg->head_dim;
     if ((st = check_rows("k_new", k_new, k_stride, row, n, es)) || (st = check_rows("v_new", v_new, v_stride, row, n, es))) return st;
     if (cfg->num_kv_heads > 4096) return fail(PIC_EUNSUPPORTED, "more than 4096 KV heads");
+    const int64_t codes = (int64_t)pool->num_blocks * pic::kBlock * row, scales = (int64_t)pool->num_blocks * cfg->num_kv_heads * 8;
+    const int64_t k_bytes = ((n - 1) * k_stride + row) * es, v_bytes = ((n - 1) * v_stride + row) * es;
+    for (const void* to : {static_cast<const void*>(pool->k), static_cast<const void*>(pool->v), static_cast<const void*>(pool->scale)}) {
+        const int64_t bytes = to == pool->scale ? scales : codes;
+        if (overlap(k_new, k_bytes, to, bytes) || overlap(v_new, v_bytes, to, bytes)) return fail(PIC_EINVAL, "the rows overlap the pool");
+    }
     pic::Kv8WriteArgs a{};
     a.k = k_new;
     a.v = v_new;

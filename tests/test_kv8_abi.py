@@ -48,7 +48,7 @@ def norm_call(cfg, **kw):
 
 @pytest.mark.parametrize("kw,what", [
     (dict(n=-1), ">= 0"), (dict(n=1 << 24), "2^24"), (dict(eps=0.0), "eps"), (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"),
-    (dict(eps=float("inf")), "eps"), (dict(q_out=None), "both"), (dict(q=None), "both"), (dict(k=None), "both"), (dict(k_out=None), "both"),
+    (dict(eps=float("inf")), "eps"), (dict(eps=1e-39), "eps"), (dict(q_out=None), "both"), (dict(q=None), "both"), (dict(k=None), "both"), (dict(k_out=None), "both"),
     (dict(q=None, q_out=None, k=None, k_out=None), "neither"), (dict(positions=None), "positions"), (dict(q_stride=248), "stride"),
     (dict(k_stride=56), "stride"), (dict(k_out_stride=-64), "stride"), (dict(q_out_stride=1 << 62), "stride"), (dict(q_stride=260), "aligned"),
     (dict(k_out_stride=68), "aligned"), (dict(q=OK + 8), "aligned"), (dict(k_out=OK + 8), "aligned"), (dict(q_weight=OK + 8), "aligned"),
@@ -72,6 +72,8 @@ WRITE = dict(k=1 << 20, k_stride=64, v=1 << 21, v_stride=64, slots=OK, n=3)
     (dict(slots=None), {}, "NULL"), (dict(slots=OK + 2), {}, "aligned"), (dict(k_stride=56), {}, "stride"), (dict(v_stride=1 << 62), {}, "stride"),
     (dict(k_stride=68), {}, "aligned"), (dict(v=OK + 8), {}, "aligned"), ({}, dict(k=None), "NULL"), ({}, dict(scale=None), "NULL"),
     ({}, dict(num_blocks=0), "empty"), ({}, dict(num_blocks=-1), ">= 0"), ({}, dict(v=OK + 8), "aligned"), ({}, dict(scale=OK + 4), "aligned"),
+    ({}, dict(k=(1 << 20) + 256), "overlap"), ({}, dict(v=(1 << 21) - 65520), "overlap"), ({}, dict(scale=(1 << 21) - 504), "overlap"),
+    (dict(k_stride=1 << 20), dict(v=(1 << 20) + (1 << 22)), "overlap"),
 ])
 def test_kv8_write_refuses(kw, pl, what):
     rc, msg = status("pic_kv8_write", B.make_config(4, 1, 64), pool(**pl), *{**WRITE, **kw}.values(), None)
