@@ -394,6 +394,7 @@ pic_status pic_attn8_workspace_size(const pic_config* cfg, const pic_batch_host*
 
 /* pic_attn_prefill and pic_attn_decode over a pool of 8-bit codes: the same batch, masks, q, o and
  * workspace rules.  cos/sin are computed in the kernel (no table).
+ * As in pic_attn_prefill, room for a copy of the turned keys behind the rest of the workspace is optional.
  * How exact: codes and scales enter exactly; sums and softmax statistics are float32.  float32 calls compute in
  * float32.  In bf16, besides the result's own rounding: turned queries are rounded to 11 bits, and cos/sin of keys, their
  * products and the turned keys to 11 bits each.  Where a call's row tiles hold at most 32 rows (query tokens x query

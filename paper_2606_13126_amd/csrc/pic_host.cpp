@@ -31,6 +31,7 @@ static_assert(sizeof(pic::KeyPlan) + sizeof(pic::Args) <= 4096, "kernel argument
 static_assert(sizeof(pic::PlanUpload) <= 4096, "kernel arguments must stay within 4 KB");
 static_assert(sizeof(pic::Plan) + sizeof(pic::TreeArgs) <= 4096, "kernel arguments must stay within 4 KB");
 static_assert(sizeof(pic::Plan) + sizeof(pic::Kv8Args) <= 4096, "kernel arguments must stay within 4 KB");
+static_assert(sizeof(pic::KeyPlan) + sizeof(pic::Kv8Args) <= 4096, "kernel arguments must stay within 4 KB");
 
 // The attention calls: what a plan is made for.
 enum class Call { kPrefill, kDecode, kTree, kPrefill8, kDecode8 };
@@ -636,9 +637,16 @@ WsLayout ws_layout(const pic_config* c, const HostPlan& hp) {
 // Calls of more than kMaxGroups segments or kMaxKeyCopy bytes rotate in the attention
 // kernel: where a copy of them would pay has not been measured (512 queries of 64 / 8 heads
 // over 131,072 keys, the most: 2,271 against 1,853 us).
+//
+// Over 8-bit codes (row tiles of 128 and 256) the copy holds keys in float16, and saves 0.015 ns per key, row tile and KV head
+// for 0.06 ns per key and KV head and 1 us (head_dim 64: 2.5; the launch stands in for part of the starts): 2,048 tokens of 64 / 8
+// heads over 18,432 keys 1,331 against 1,204 us, 4,000 of 32 / 8 173.5 against 160.5, 2,048 of 32 / 4 heads of 64 over 10,240
+// 254 against 233.5.  Of 44 calls within 6 us of that line, both ways, copying lost 3 us at most where it copies not and
+// nothing where it does: 400 tokens of 32 / 4 heads of 64 over 8,400 keys 80 against 75 us, 250 of 32 / 8 over 5,376 48 both ways.
 void plan_keys(const pic_config* c, HostPlan& hp) {
     hp.keys.n = 0;
-    if (c->dtype != PIC_BF16 || c->k_prerotated || hp.dec_kernel || hp.tree || hp.kv8) return;
+    if (c->dtype != PIC_BF16 || c->k_prerotated || hp.dec_kernel || hp.tree || (hp.kv8 && hp.tree_rows <= 32)) return;
+    const int tile = hp.tile_rows();
     const int G = c->num_q_heads / c->num_kv_heads;
     struct Run {
         int32_t req, lo, hi, pos_off;
@@ -647,10 +655,10 @@ void plan_keys(const pic_config* c, HostPlan& hp) {
     double staged = 0.0;   // keys times the row tiles that see them
     double items = 0.0;
     for (const auto& g : hp.groups) {
-        items += (double)pic::row_tiles(g, G, pic::kTileRows) * g.n_split * c->num_kv_heads;
+        items += (double)pic::row_tiles(g, G, tile) * g.n_split * c->num_kv_heads;
         runs.push_back(Run{g.req, g.win, g.tok0 + g.n_tok, g.pos_off});
-        for (int rt = 0; rt < pic::row_tiles(g, G, pic::kTileRows); ++rt)
-            staged += (double)(g.tok0 + (std::min((int64_t)(rt + 1) * pic::kTileRows, (int64_t)g.n_tok * G) - 1) / G + 1 - g.win);
+        for (int rt = 0; rt < pic::row_tiles(g, G, tile); ++rt)
+            staged += (double)(g.tok0 + (std::min((int64_t)(rt + 1) * tile, (int64_t)g.n_tok * G) - 1) / G + 1 - g.win);
     }
     std::sort(runs.begin(), runs.end(), [](const Run& x, const Run& y) { return x.req != y.req ? x.req < y.req : x.lo < y.lo; });
     // runs of a request that overlap or touch make one segment
@@ -664,7 +672,8 @@ void plan_keys(const pic_config* c, HostPlan& hp) {
         keys += r.hi - r.lo;
         blocks += ((r.hi - 1) >> 4) - (r.lo >> 4) + 1;
     }
-    const double gain_us = c->num_kv_heads * (0.043e-3 * staged - 0.07e-3 * (double)keys) - 10.0;
+    const double gain_us = hp.kv8 ? c->num_kv_heads * (0.015e-3 * staged - 0.06e-3 * (double)keys) - (c->head_dim == 128 ? 1.0 : 2.5)
+                                  : c->num_kv_heads * (0.043e-3 * staged - 0.07e-3 * (double)keys) - 10.0;
     if (gain_us <= 0 || segs.size() > (size_t)pic::kMaxGroups || key_copy_bytes(c, blocks) > pic::kMaxKeyCopy) return;
     hp.keys_from_table = c->head_dim != 128 || c->num_kv_heads * (0.037e-3 * staged - 0.07e-3 * (double)keys) >
                                                    1.2 * items / pic::kTargetCUs + 3.3;
@@ -894,7 +903,7 @@ pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic
             if ((st = hip_status(pic::launch_plan_upload(u, stream), "plan upload launch"))) return st;
         }
     }
-    if (copy_keys &&
+    if (copy_keys && !hp.kv8 &&
         (st = hip_status(pic::launch_rope_keys(c->rope_style, c->head_dim, hp.keys, a, stream), "key rotation launch")))
         return st;
     const bool rope_on = c->k_prerotated == 0;
@@ -904,6 +913,7 @@ pic_status run_attention(const pic_config* c, const pic_batch_host* b, const pic
         k.scale = codes->scale;
         k.code = codes->code;
         k.tile_rows = hp.tile_rows();
+        if (copy_keys && (st = hip_status(pic::launch_kv8_keys(c->rope_style, c->head_dim, hp.keys, k, stream), "key rotation launch"))) return st;
         return hip_status(c->dtype == PIC_F32 ? pic::launch_kv8_f32(hp.f32_waves, c->rope_style, c->head_dim, rope_on, p, k, stream)
                                               : pic::launch_kv8(c->rope_style, c->head_dim, rope_on, p, k, stream),
                           "attention launch");

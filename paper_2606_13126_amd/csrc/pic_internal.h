@@ -309,6 +309,7 @@ int launch_qk_norm(int dtype, int style, int d, int n, const NormArgs& args, voi
 int launch_kv8_write(int dtype, int code, int d, const Kv8WriteArgs& args, void* stream);
 int launch_kv8_read(int dtype, int code, int d, int hkv, const uint8_t* k_pool, const uint8_t* v_pool, const float* scale,
                     int64_t n_slots, const int32_t* slots, int n, void* k_out, void* v_out, void* stream);
+int launch_kv8_keys(int style, int d, const KeyPlan& plan, const Kv8Args& args, void* stream);
 int launch_kv8(int style, int d, bool rope, const Plan& plan, const Kv8Args& args, void* stream);
 
 // Device scratch of the no-allocation entry point: kScratchBytes on each device,

@@ -6,6 +6,7 @@
 //  * kv8_read   rows of the pool as numbers.
 //  * kv8_few, kv8_many  attention over the codes in bf16; kv8_merge joins their key splits.  (float32: attn_f32
 //               over Kv8Args, in pic_kernels.hip)
+//  * kv8_keys   the call's turned copy of its keys, where many row tiles share them.
 //
 // Pools: codes [num_blocks][Hkv][16][D], one byte each, and scales [num_blocks][Hkv][2].  An
 // element is code x scale.  The attention multiplies codes as they are (every code is exact in float16
@@ -864,6 +865,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 // output product.  A wave loads the codes of eight keys of a step into registers, a step and a half ahead, and
 // turns them into float16 (keys) and bf16 (values) in LDS one step ahead, beside the products of the scores;
 // two LDS buffers, one barrier per step.  LDS rows hold the x of all pairs, then the y, in either pairing.
+// COPY: keys come turned from the call's copy (kv8_keys).
 //
 // The scales cost a few operations a step: the scores of a block's keys are multiplied in the addition that
 // the exponential needs anyway, and the values' scale joins its exponent: p' = 2^(s - m + log2 v).
@@ -871,7 +873,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 //
 // Bound by vector work and products, which hardly overlap: of about 5,100 cycles of a step of 256 rows the products are
 // 2,048 (38% of the cycles by the counters), the vector work, with quarter-rate exponentials, most of the others.
-// 2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1.32-1.36 ms, 860-888 TFLOP/s; on turned keys 1.17, 1000.
+// 2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1,204 us with the copy, 970 TFLOP/s, 1,331 without it; on
+// a pool of turned keys 1,141, 1,020.
 // ---------------------------------------------------------------------------------
 constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
 
@@ -885,14 +888,15 @@ struct __attribute__((aligned(2 * D))) Kv8ManyLds {
     float4 sc[2][4];             // per block of a step: its keys' scale, log2 and inverse of its values' scale
 };
 
-template <int D, int STYLE, bool ROPE, int CODE, int WR, int NG>
+template <int D, int STYLE, bool ROPE, bool COPY, int CODE, int WR, int NG>
 __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> plan, const Kv8Args a) {
     typedef Code<CODE> C;
     constexpr int NW = kKv8Waves, KG = NW / WR, STEP = 64, HALF = D / 2;
     constexpr int KD = D / 16;             // 32x32x16 contraction steps of QK^T
     constexpr int DB = D / 32;             // 32-dim blocks of O^T
     constexpr int PL = D / 16;             // pairs that a lane turns
-    constexpr int KW = PL / 4, VW = D / 32;   // words of codes of a lane: either run of its key, its value
+    constexpr int KW = PL / (COPY ? 2 : 4), VW = D / 32;   // words of a lane: either run of its key (of the copy: in float16), its value
+    static_assert(ROPE || !COPY, "a copy holds turned keys");
     static_assert(KG == 1 || KG == 2, "a step has two times 32 keys");
 
     __shared__ Kv8ManyLds<D> lds;
@@ -901,7 +905,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     static_assert(sizeof(lds.kv) >= NW * DB * 2 * 64 * 16, "the outputs meet in the buffers");
 
     const Group g = find_group<false>(plan, blockIdx.x);
-    const int G = a.group, n_rt = g.n_rt;
+    const int G = a.group, n_rt = COPY ? row_tiles(g, G, 32 * WR) : g.n_rt;
     const int li = blockIdx.x - g.item_base;   // (a call's items are not padded: below the group's count)
     const ItemCoords ic = item_coords(g, a.hkv, n_rt, li);
     const int rt = n_rt - 1 - ic.rt;           // the longest first
@@ -928,12 +932,13 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     // the rows of keys that differ in bit 1 lie in different halves of the swizzled chunks.)
     const int l8 = lane >> 3, sub = lane & 7, pair0 = sub * PL;
     const int own = wave * 8 + (D == 128 ? (l8 & 4) | ((l8 & 1) << 1) | ((l8 >> 1) & 1) : l8);
-    int k_el[2];   // bytes of its two runs in a row: NeoX its x and its y, GPT-J one after the other
+    int k_el[2];   // its two runs in a row: NeoX its x and its y, GPT-J one after the other, the copy x and y
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int e = STYLE == kNeox ? pair0 + h * HALF : 2 * pair0 + h * PL;
-        k_el[h] = model_chunk(a.chunk_map, e >> 3) * 8 + (e & 7);
+        const int e = COPY || STYLE == kNeox ? pair0 + h * HALF : 2 * pair0 + h * PL;
+        k_el[h] = COPY ? e : model_chunk(a.chunk_map, e >> 3) * 8 + (e & 7);
     }
+    const uint16_t* copy = COPY ? static_cast<const uint16_t*>(a.k_rot) + ((size_t)(g.krot0 + (kt0 >> 4)) * a.hkv + ic.kvh) * page : nullptr;
     typedef uint32_t run_t __attribute__((ext_vector_type(KW)));
     struct Raw {
         uint32_t k[2][KW], v[VW];
@@ -956,9 +961,11 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
         const size_t at = (size_t)(uint32_t)blk * blk_stride;
         const uint8_t* kp = kpool + at;
         const uint8_t* vp = vpool + at;
+        const uint16_t* cp = COPY ? copy + (size_t)(uint32_t)(min(u * STEP + wave * 8, k_hi - 1) >> 4) * blk_stride : nullptr;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const run_t w = *reinterpret_cast<const run_t*>(kp + (uint32_t)(to_row + k_el[h]));
+            const uint32_t from = (uint32_t)(to_row + k_el[h]);
+            const run_t w = *(COPY ? reinterpret_cast<const run_t*>(cp + from) : reinterpret_cast<const run_t*>(kp + from));
 #pragma unroll
             for (int i = 0; i < KW; ++i) {
                 if constexpr (KW == 1) r.k[h][i] = w[0];
@@ -971,7 +978,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
             r.v[2 * h] = w[0];
             r.v[2 * h + 1] = w[1];
         }
-        if (ROPE) r.pos = posv[(uint32_t)k];
+        if (ROPE && !COPY) r.pos = posv[(uint32_t)k];
         const int32_t* sp = reinterpret_cast<const int32_t*>(a.scale) + ((size_t)(uint32_t)blk * a.hkv + ic.kvh) * 2;
         r.ks = __int_as_float(scalar_load(sp, 0));
         r.vs = __int_as_float(scalar_load(sp, 1));
@@ -981,7 +988,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     if (ROPE)
         for (int i = threadIdx.x; i < HALF; i += NW * 64) {
             lds.fstep[i] = a.fstep[i];
-            rope_cs_fast(STEP, a.fstep[i], lds.stride_cs[i].x, lds.stride_cs[i].y);
+            if (!COPY) rope_cs_fast(STEP, a.fstep[i], lds.stride_cs[i].x, lds.stride_cs[i].y);
         }
 
     // ---- queries.  The cos/sin of their tokens (a token's heads share them) pass through the wave's
@@ -1070,7 +1077,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     constexpr int PARTS = PL / 2 + VW / 2;
     uint32_t turned[2][PL / 2];
     auto angles = [&]() {
-        if (!ROPE) return;
+        if (!ROPE || COPY) return;
         const int32_t pos = raw.pos;
         // (STEP on, and not past the type's end)
         if (renew == 0 || __builtin_amdgcn_ballot_w64((uint32_t)pos != (uint32_t)cs_pos + STEP || pos < cs_pos) != 0) {
@@ -1086,7 +1093,10 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
         if (i < PL / 2) {   // pairs 2 i and 2 i + 1
             const int w = i / 2, h = i % 2;
             uint32_t xw, yw;
-            if (STYLE == kNeox) {
+            if constexpr (COPY) {
+                xw = r.k[0][i];
+                yw = r.k[1][i];
+            } else if (STYLE == kNeox) {
                 xw = r.k[0][w];
                 yw = r.k[1][w];
             } else {   // neighbours: word 2 w and 2 w + 1 of the lane's words
@@ -1094,7 +1104,10 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
                 xw = __builtin_amdgcn_perm(a1, a0, 0x06040200u);
                 yw = __builtin_amdgcn_perm(a1, a0, 0x07050301u);
             }
-            if constexpr (ROPE) {
+            if constexpr (COPY) {
+                turned[0][i] = xw;
+                turned[1][i] = yw;
+            } else if constexpr (ROPE) {
 #pragma unroll
                 for (int p = 2 * i; p < 2 * i + 2; ++p) {
                     const float2 d = lds.stride_cs[pair0 + p];
@@ -1320,6 +1333,98 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     if (g.n_split > 1 && kg == 0 && hi == 0) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(M, den);
 }
 
+// ---------------------------------------------------------------------------------
+// kv8_keys: the call's copy of the keys that its queries see, turned, in float16: codes times cos/sin (the scales stay
+// beside the pool's blocks), rounded once, the x of all pairs of a key and then the y.  Blocks in the order of the sequences.
+// One workgroup per block: 8 lanes per key (D / 16 pairs each), every second KV head.  Bound by memory: each key read
+// once and written twice as wide.
+// ---------------------------------------------------------------------------------
+template <int D, int STYLE, int CODE>
+__global__ void __launch_bounds__(256) kv8_keys(const KeyPlan plan, const Kv8Args a) {
+    typedef Code<CODE> C;
+    constexpr int HALF = D / 2, PL = D / 16, KW = PL / 4, U = 4;
+    typedef uint32_t run_t __attribute__((ext_vector_type(KW)));
+    typedef uint32_t out_t __attribute__((ext_vector_type(PL / 2)));
+    int lo = 0, up = plan.n - 1;
+    while (lo < up) {
+        const int mid = (lo + up + 1) >> 1;
+        if (plan.seg[mid].blk0 <= (int)blockIdx.x) lo = mid;
+        else up = mid - 1;
+    }
+    const KeySegment sg = plan.seg[lo];
+    const int kb = (sg.lo >> 4) + (int)blockIdx.x - sg.blk0;   // block of the sequence
+    const int key = ((int)threadIdx.x >> 3) & 15, pair0 = ((int)threadIdx.x & 7) * PL;
+    const int64_t j = (int64_t)kb * kBlock + key;
+    if (j < sg.lo || j >= sg.hi) return;                       // no query sees it
+    const int32_t blk = a.block_tables[(size_t)sg.req * a.max_blocks + kb];
+    const int32_t pos = a.positions[sg.pos_off + j];
+    int el[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e = STYLE == kNeox ? pair0 + h * HALF : 2 * pair0 + h * PL;
+        el[h] = key * D + model_chunk(a.chunk_map, e >> 3) * 8 + (e & 7);
+    }
+    const uint8_t* kp = static_cast<const uint8_t*>(a.k_pool) + (size_t)(uint32_t)blk * a.hkv * kBlock * D;
+    uint16_t* op = static_cast<uint16_t*>(const_cast<void*>(a.k_rot)) + (size_t)blockIdx.x * a.hkv * kBlock * D + key * D + pair0;
+    float c[PL], s[PL];
+#pragma unroll
+    for (int i = 0; i < PL; ++i) rope_cs_fast(pos, a.fstep[pair0 + i], c[i], s[i]);
+    // KV heads hp, hp + 2, ..: the loads of four go out together
+    for (int h0 = (int)threadIdx.x >> 7; h0 < a.hkv; h0 += 2 * U) {
+        uint32_t w[U][2 * KW];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const run_t in = *reinterpret_cast<const run_t*>(kp + (size_t)min(h0 + 2 * u, a.hkv - 1) * kBlock * D + el[h]);
+#pragma unroll
+                for (int i = 0; i < KW; ++i) {
+                    if constexpr (KW == 1) w[u][h] = in[0];
+                    else w[u][h * KW + i] = in[i];
+                }
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (h0 + 2 * u >= a.hkv) continue;
+            out_t ox, oy;
+#pragma unroll
+            for (int i = 0; i < KW; ++i) {
+                uint32_t xw, yw;
+                if (STYLE == kNeox) {
+                    xw = w[u][i];
+                    yw = w[u][KW + i];
+                } else {
+                    xw = __builtin_amdgcn_perm(w[u][2 * i + 1], w[u][2 * i], 0x06040200u);
+                    yw = __builtin_amdgcn_perm(w[u][2 * i + 1], w[u][2 * i], 0x07050301u);
+                }
+                const f32x4_t x = C::decode(xw), y = C::decode(yw);
+                float tx[4], ty[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    tx[e] = x[e] * c[4 * i + e] - y[e] * s[4 * i + e];
+                    ty[e] = y[e] * c[4 * i + e] + x[e] * s[4 * i + e];
+                }
+                ox[2 * i] = pack_f16(tx[0], tx[1]);
+                ox[2 * i + 1] = pack_f16(tx[2], tx[3]);
+                oy[2 * i] = pack_f16(ty[0], ty[1]);
+                oy[2 * i + 1] = pack_f16(ty[2], ty[3]);
+            }
+            uint16_t* row = op + (size_t)(h0 + 2 * u) * kBlock * D;
+            *reinterpret_cast<out_t*>(row) = ox;
+            *reinterpret_cast<out_t*>(row + HALF) = oy;
+        }
+    }
+}
+
+template <int D>
+void launch_keys_d(int style, const KeyPlan& plan, const Kv8Args& a, hipStream_t st) {
+    const auto go = [&](auto s, auto c) {
+        hipLaunchKernelGGL((kv8_keys<D, decltype(s)::value, decltype(c)::value>), dim3(plan.n_blocks), dim3(256), 0, st, plan, a);
+    };
+    if (a.code == kCodeE4m3) style == kNeox ? go(Idx<0>{}, Idx<kCodeE4m3>{}) : go(Idx<1>{}, Idx<kCodeE4m3>{});
+    else style == kNeox ? go(Idx<0>{}, Idx<kCodeInt8>{}) : go(Idx<1>{}, Idx<kCodeInt8>{});
+}
+
 // Joins key splits: one block per kMergeRows rows of a (row tile, KV head), one float4 of a row per
 // thread, U splits' loads in flight.  A row tile has splits up to its last token's.
 struct Kv8MergeArgs {
@@ -1327,13 +1432,14 @@ struct Kv8MergeArgs {
     const float* part_ml;
     void* o;
     int32_t tile_rows, hq, hkv, group;
+    bool copied;   // the groups hold where their keys' copy begins
 };
 
 template <int D, int NG, int U>
 __global__ void __launch_bounds__(kMergeRows * D / 4) kv8_merge(const PlanOf<NG> plan, const Kv8MergeArgs a) {
     constexpr int TPR = D / 4;
     const Group g = find_group<true>(plan, blockIdx.x);
-    const int n_rt = g.n_rt, chunks = a.tile_rows / kMergeRows;
+    const int n_rt = a.copied ? row_tiles(g, a.group, a.tile_rows) : g.n_rt, chunks = a.tile_rows / kMergeRows;
     int li = blockIdx.x - g.merge_base;   // (only groups with splits have blocks here, and no more than they need)
     const int r = (li % chunks) * kMergeRows + (int)threadIdx.x / TPR, c4 = (int)threadIdx.x % TPR;
     li /= chunks;
@@ -1370,36 +1476,41 @@ __global__ void __launch_bounds__(kMergeRows * D / 4) kv8_merge(const PlanOf<NG>
     *reinterpret_cast<u32x2_t*>(op) = u32x2_t{pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv)};
 }
 
-template <int D, int STYLE, bool ROPE, int CODE, int NG>
+template <int D, int STYLE, bool ROPE, bool COPY, int CODE, int NG>
 hipError_t launch_kv8_n(const PlanOf<NG>& plan, const Kv8Args& a, hipStream_t st) {
     const dim3 grid(plan.n_items), block(kKv8Waves * 64);
-    switch (a.tile_rows) {
-    case 16: hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 1, NG>), grid, block, 0, st, plan, a); break;
-    case 32: hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 2, NG>), grid, block, 0, st, plan, a); break;
-    case 128: hipLaunchKernelGGL((kv8_many<D, STYLE, ROPE, CODE, 4, NG>), grid, block, 0, st, plan, a); break;
-    default: hipLaunchKernelGGL((kv8_many<D, STYLE, ROPE, CODE, 8, NG>), grid, block, 0, st, plan, a); break;
+    if (a.tile_rows <= 32) {
+        if constexpr (!COPY) {
+            if (a.tile_rows == 16) hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 1, NG>), grid, block, 0, st, plan, a);
+            else hipLaunchKernelGGL((kv8_few<D, STYLE, ROPE, CODE, 2, NG>), grid, block, 0, st, plan, a);
+        }
+    } else if (a.tile_rows == 128) {
+        hipLaunchKernelGGL((kv8_many<D, STYLE, ROPE, COPY, CODE, 4, NG>), grid, block, 0, st, plan, a);
+    } else {
+        hipLaunchKernelGGL((kv8_many<D, STYLE, ROPE, COPY, CODE, 8, NG>), grid, block, 0, st, plan, a);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.n_merge == 0) return e;
-    const Kv8MergeArgs m = {a.part_o, a.part_ml, a.o, a.tile_rows, a.hq, a.hkv, a.group};
+    const Kv8MergeArgs m = {a.part_o, a.part_ml, a.o, a.tile_rows, a.hq, a.hkv, a.group, COPY};
     const dim3 merges(plan.n_merge), threads(kMergeRows * D / 4);
     if (a.tile_rows <= 32) hipLaunchKernelGGL((kv8_merge<D, NG, 8>), merges, threads, 0, st, plan, m);
     else hipLaunchKernelGGL((kv8_merge<D, NG, 4>), merges, threads, 0, st, plan, m);
     return hipGetLastError();
 }
 
-template <int D, int STYLE, bool ROPE, int CODE>
+template <int D, int STYLE, bool ROPE, bool COPY, int CODE>
 hipError_t launch_kv8_t(const Plan& plan, const Kv8Args& a, hipStream_t st) {
-    if (plan.n_groups > kFewGroups) return launch_kv8_n<D, STYLE, ROPE, CODE, kMaxGroups>(plan, a, st);
+    if (plan.n_groups > kFewGroups) return launch_kv8_n<D, STYLE, ROPE, COPY, CODE, kMaxGroups>(plan, a, st);
     PlanOf<kFewGroups> few = {plan.n_groups, plan.n_items, plan.n_merge, plan.merge_ways, plan.table, plan.item_map, plan.merge_map, {}};
     for (int i = 0; i < plan.n_groups; ++i) few.g[i] = plan.g[i];
-    return launch_kv8_n<D, STYLE, ROPE, CODE, kFewGroups>(few, a, st);
+    return launch_kv8_n<D, STYLE, ROPE, COPY, CODE, kFewGroups>(few, a, st);
 }
 
 template <int D, int CODE>
 hipError_t launch_kv8_d(int style, bool rope, const Plan& plan, const Kv8Args& a, hipStream_t st) {
-    if (!rope) return launch_kv8_t<D, 0, false, CODE>(plan, a, st);   // (without rotation the pairing makes no difference)
-    return style == kNeox ? launch_kv8_t<D, 0, true, CODE>(plan, a, st) : launch_kv8_t<D, 1, true, CODE>(plan, a, st);
+    if (!rope) return launch_kv8_t<D, 0, false, false, CODE>(plan, a, st);   // (without rotation the pairing makes no difference)
+    if (a.k_rot != nullptr) return style == kNeox ? launch_kv8_t<D, 0, true, true, CODE>(plan, a, st) : launch_kv8_t<D, 1, true, true, CODE>(plan, a, st);
+    return style == kNeox ? launch_kv8_t<D, 0, true, false, CODE>(plan, a, st) : launch_kv8_t<D, 1, true, false, CODE>(plan, a, st);
 }
 
 template <typename T, int D, bool STREAMS>
@@ -1467,6 +1578,12 @@ int launch_kv8_read(int dtype, int code, int d, int hkv, const uint8_t* k_pool, 
         if (32 * units > kStreamBytes) go(std::true_type{});
         else go(std::false_type{});
     });
+    return hipGetLastError();
+}
+
+int launch_kv8_keys(int style, int d, const KeyPlan& plan, const Kv8Args& args, void* stream) {
+    if (d == 64) launch_keys_d<64>(style, plan, args, (hipStream_t)stream);
+    else launch_keys_d<128>(style, plan, args, (hipStream_t)stream);
     return hipGetLastError();
 }
 

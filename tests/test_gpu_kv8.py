@@ -902,3 +902,74 @@ def test_large_row_tiles_and_values(case, what):
             c.swapaxes(1, 2)[~used] = 0x7f
         scale[~used.any(1)] = np.nan
         assert torch.equal(b.run(pool=pool_of(k, v, scale, b.code)), o)
+
+
+# calls of which many row tiles share the keys: these are turned once, into a copy in the workspace
+COPIED = [(64, 1, 128, [(800, 400)], 128, False), (64, 1, 128, [(790, 230, 37), (33, 300, 16), (0, 250)], 128, False),
+          (16, 2, 64, [(1500, 900)], 128, True), (32, 1, 128, [(300, 160)] * 12, 256, False),
+          (64, 2, 64, [(700, 500, 5), (1201, 499, 37)], 256, False), (24, 12, 128, [(300, 900)], 128, False),
+          (32, 8, 128, [(600, 900)], 256, True), (64, 2, 128, [(2500, 120)], 128, True)]
+
+
+def copied_bytes(b):
+    """Workspace that a batch's turned keys take."""
+    turned = cfg_of(b.hq, b.hkv, b.d, b.dtype, prerotated=1)
+    return B.pic_attn8_workspace_size(b.cfg, b.host, b.decode) - B.pic_attn8_workspace_size(turned, b.host, b.decode)
+
+
+@pytest.mark.parametrize("case,style,rot", [(i, 0, 0) for i in range(len(COPIED))] +
+                         [(i, *r) for i in (1, 2) for r in ((1, 0), (0, 32), (1, 34))])
+def test_keys_turned_once(case, style, rot):
+    """... with the copy, and in a workspace without room for it."""
+    hq, hkv, d, lens, tile, split = COPIED[case]
+    b = Batch(lens, hq, hkv, d, torch.bfloat16, CODES[(case + style) % 2], style, rot, seed=case)
+    extra = copied_bytes(b)
+    assert extra > 0 and tile_of(b) == (tile, split)
+    got = b.run(ws=torch.full((b.ws.numel(),), 0xff, dtype=torch.uint8, device="cuda"))
+    b.check(got, f"case {case}")
+    small = b.run(ws=torch.zeros(max(1, b.ws.numel() - extra), dtype=torch.uint8, device="cuda"))
+    if case in (1, 2, 7):
+        b.check(small, f"case {case}, turned in the kernel")
+
+
+@pytest.mark.parametrize("what", ["random", "jumps", "outside", "scales"])
+@pytest.mark.parametrize("case", [1, 2])
+def test_keys_turned_once_and_values(case, what):
+    hq, hkv, d, lens, tile, split = COPIED[case]
+    kw = {"random": dict(positions=lambda rng, m: rng.integers(-2**31, 2**31, m)),
+          "jumps": dict(positions=lambda rng, m: np.arange(m) // 40 * 999 + np.arange(m)), "scales": dict(powers=False)}.get(what, {})
+    b = Batch(lens, hq, hkv, d, torch.bfloat16, CODES[case % 2], seed=case, **kw)
+    assert copied_bytes(b) > 0
+    got = b.run()
+    b.check(got, what)
+    if what == "outside":
+        k, v, scale = b.k_codes.copy(), b.v_codes.copy(), b.scale.copy()
+        used = np.zeros((b.nb, 16), bool)
+        for r, (ctx, m, w) in enumerate(b.lens):
+            j = np.arange(w, ctx + m)
+            used[b.table[r, j // 16], j % 16] = True
+        for c in (k, v):
+            c.swapaxes(1, 2)[~used] = 0x7f
+        scale[~used.any(1)] = np.nan
+        assert torch.equal(b.run(pool=pool_of(k, v, scale, b.code)), got)
+
+
+def test_keys_turned_once_captured_and_replayed():
+    """The copy is made anew on every replay, from the pool as it is then; calls on a side stream between them."""
+    hq, hkv, d, lens, _, _ = COPIED[1]
+    b = Batch(lens, hq, hkv, d, torch.bfloat16, K8.INT8, seed=1)
+    assert copied_bytes(b) > 0
+    o = torch.zeros_like(b.q)
+    b.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.run(o, stream=torch.cuda.current_stream())
+    for i in range(3):
+        b.pool.k.copy_(b.pool.k.roll(1, 0))
+        b.pool.scale.copy_(b.pool.scale.roll(1, 0))
+        o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = o.clone()
+        assert torch.equal(b.run(ws=torch.zeros_like(b.ws)), got), i
