@@ -954,6 +954,23 @@ def test_keys_turned_once_and_values(case, what):
         assert torch.equal(b.run(pool=pool_of(k, v, scale, b.code)), got)
 
 
+def test_keys_turned_once_for_many_spans():
+    """More query spans than the kernel arguments hold, of few requests: plan and copy in the workspace."""
+    lens = [(600, 350, 0), (500, 350, 21)]
+    b = Batch(lens, 64, 1, 128, torch.bfloat16, K8.INT8, seed=2)
+    n, spans = 10, 35
+    start, flags, win, cu = [], [], [], [0]
+    for ctx, m, w in lens:
+        start += [0, *range(ctx, ctx + m, n)]
+        flags += [B.PIC_PDEP] + [B.PIC_PDEP | B.PIC_QUERY] * spans
+        win += [-1] + [w] * spans
+        cu.append(len(start))
+    b.host = B.HostBatch([ctx + m for ctx, m, _ in lens], cu, start, flags, win)
+    assert copied_bytes(b) > 0
+    b.ws = torch.full((B.pic_attn8_workspace_size(b.cfg, b.host, False),), 0xff, dtype=torch.uint8, device="cuda")
+    b.check(b.run(), "70 spans")
+
+
 def test_keys_turned_once_captured_and_replayed():
     """The copy is made anew on every replay, from the pool as it is then; calls on a side stream between them."""
     hq, hkv, d, lens, _, _ = COPIED[1]
