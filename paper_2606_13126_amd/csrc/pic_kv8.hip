@@ -873,8 +873,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 //
 // Bound by vector work and products, which hardly overlap: of about 5,100 cycles of a step of 256 rows the products are
 // 2,048 (38% of the cycles by the counters), the vector work, with quarter-rate exponentials, most of the others.
-// 2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1,204 us with the copy, 970 TFLOP/s, 1,331 without it; on
-// a pool of turned keys 1,141, 1,020.
+// 2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1,204 us with the copy, 970 TFLOP/s, 1,350 without it; on
+// a pool of turned keys 1,160, 1,007.
 // ---------------------------------------------------------------------------------
 constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
 
@@ -944,14 +944,18 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
         uint32_t k[2][KW], v[VW];
         int32_t pos;
         float ks, vs;
-    } raw;
+    };
+    // Sets of codes on their way: one, a step and a half ahead, or with the copy, whose angles take no registers, two (the
+    // call above 1,224 -> 1,204 us; without rotation 1,160 -> 1,152, but 42.3 -> 43.2 for 250 tokens over 5,376 keys: one)
+    constexpr int SETS = COPY ? 2 : 1;
+    Raw raw[SETS];
     auto block_at = [&](int u) { return scalar_load(btab, min(u * STEP + wave * 8, k_hi - 1) >> 4); };
     int blk = block_at(0);
     const int own_row = (wave * 8 & (kBlock - 1)) + own - wave * 8;   // of the key in its block
     const size_t blk_stride = (size_t)a.hkv * page;
-    auto load = [&](int u) {
+    auto load = [&](int u, auto set) {
         if (u >= nt) return;
-        Raw& r = raw;
+        Raw& r = raw[decltype(set)::value];
         // a key outside the range stands for the nearest one inside, so that nothing outside it is read
         int k = u * STEP + own, to_row = own_row * D;
         if (u * STEP < k_lo || (u + 1) * STEP > k_hi) {
@@ -984,7 +988,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
         r.vs = __int_as_float(scalar_load(sp, 1));
         if (u + 1 < nt) blk = block_at(u + 1);
     };
-    load(0);
+    load(0, Idx<0>{});
+    if constexpr (SETS > 1) load(1, Idx<1>{});
     if (ROPE)
         for (int i = threadIdx.x; i < HALF; i += NW * 64) {
             lds.fstep[i] = a.fstep[i];
@@ -1078,7 +1083,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     uint32_t turned[2][PL / 2];
     auto angles = [&]() {
         if (!ROPE || COPY) return;
-        const int32_t pos = raw.pos;
+        const int32_t pos = raw[0].pos;
         // (STEP on, and not past the type's end)
         if (renew == 0 || __builtin_amdgcn_ballot_w64((uint32_t)pos != (uint32_t)cs_pos + STEP || pos < cs_pos) != 0) {
 #pragma unroll
@@ -1088,8 +1093,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
         --renew;
         cs_pos = pos;
     };
-    auto part = [&](int buf, int i) {
-        const Raw& r = raw;
+    auto part = [&](int buf, int i, auto set) {
+        const Raw& r = raw[decltype(set)::value];
         if (i < PL / 2) {   // pairs 2 i and 2 i + 1
             const int w = i / 2, h = i % 2;
             uint32_t xw, yw;
@@ -1165,7 +1170,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     constexpr int NT = 2 / KG;     // times 32 keys of a step
     constexpr int TAKEN = KD * NT;
     // ---- step s, in buffer P = s % 2, and the codes of the next step
-    auto step = [&](int s, int P) {
+    auto step = [&](int s, int P, auto set) {
         // (the offsets are not kept apart for every chunk: registers are short)
         asm volatile("" : "+v"(k_at), "+v"(v_at));
         const uint32_t at = lds_at + (uint32_t)(P * 128 * D + 32 * kg * D) * 2, kt = at + k_at, vt = at + v_at;
@@ -1190,13 +1195,13 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
                 sc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), __builtin_bit_cast(bf16x8_t, qb[kd]), from, 0, 0, 0);
             if (i + kAhead < TAKEN) read_k(i + kAhead);
 #pragma unroll
-            for (int j = i * PARTS / TAKEN; j < (i + 1) * PARTS / TAKEN; ++j) part(1 - P, j);
+            for (int j = i * PARTS / TAKEN; j < (i + 1) * PARTS / TAKEN; ++j) part(1 - P, j, set);
             if (i == TAKEN - 2)
 #pragma unroll
                 for (int b = 0; b < 2 * NT; ++b) bs[b] = lds.sc[P][2 * kg + b];
             __builtin_amdgcn_sched_barrier(0);
         }
-        load(s + 2);
+        load(s + 1 + SETS, set);
         float mul[2 * NT], add[2 * NT];   // of a block's scores and of their exponents
         float mx = kNegBig;
 #pragma unroll
@@ -1277,21 +1282,30 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
         __builtin_amdgcn_sched_barrier(0);
     };
     // the codes of step u alone (also: of a wave without rows)
-    auto only_codes = [&](int u, int buf) {
+    auto only_codes = [&](int u, int buf, auto set) {
         if (u < nt) {
             angles();
 #pragma unroll
-            for (int i = 0; i < PARTS; ++i) part(buf, i);
+            for (int i = 0; i < PARTS; ++i) part(buf, i, set);
         }
-        load(u + 1);
+        load(u + SETS, set);
     };
-    only_codes(0, 0);
+    only_codes(0, 0, Idx<0>{});
     barrier_keep_vmem();
     const bool rows = row_lo < rows_total;
-    for (int s = 0; s < nt; ++s) {
-        if (rows) step(s, s & 1);
-        else only_codes(s + 1, (s + 1) & 1);
+    // (the codes of step s + 1 are in set (s + 1) % SETS)
+    auto one = [&](int s, int P, auto set) {
+        if (rows) step(s, P, set);
+        else only_codes(s + 1, 1 - P, set);
         barrier_keep_vmem();
+    };
+    if constexpr (SETS > 1) {
+        for (int s = 0; s < nt; s += 2) {
+            one(s, 0, Idx<1>{});
+            if (s + 1 < nt) one(s + 1, 1, Idx<0>{});
+        }
+    } else {
+        for (int s = 0; s < nt; ++s) one(s, s & 1, Idx<0>{});
     }
 
     // ---- the results of a row group's waves meet: rows by their common maximum, outputs through the buffers
