@@ -871,9 +871,9 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 // the exponential needs anyway, and the values' scale joins its exponent: p' = 2^(s - m + log2 v).
 // The row sum adds the p' of a block, rounded to bf16 as they are multiplied, times 1 / v.
 //
-// Bound by vector work and products, which hardly overlap: of about 5,100 cycles of a step of 256 rows the products are
-// 2,048 (38% of the cycles by the counters), the vector work, with quarter-rate exponentials, most of the others.
-// 2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1,204 us with the copy, 970 TFLOP/s, 1,350 without it; on
+// Bound by products, vector work and LDS reads, which overlap in part: a step of 256 rows has 2,048 cycles of products and
+// 2,300 of LDS, and takes about 5,100 cycles with turning (products 38%, vector unit 48% by the counters), 4,500 with
+// the copy (45% and 37%).  2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1,204 us with the copy, 970 TFLOP/s, 1,350 without it; on
 // a pool of turned keys 1,160, 1,007.
 // ---------------------------------------------------------------------------------
 constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
@@ -1351,7 +1351,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
 // kv8_keys: the call's copy of the keys that its queries see, turned, in float16: codes times cos/sin (the scales stay
 // beside the pool's blocks), rounded once, the x of all pairs of a key and then the y.  Blocks in the order of the sequences.
 // One workgroup per block: 8 lanes per key (D / 16 pairs each), every second KV head.  Bound by memory: each key read
-// once and written twice as wide.
+// once and written twice as wide (18,432 keys of 8 heads of 128, 57 MB, in 13.0 us).
 // ---------------------------------------------------------------------------------
 template <int D, int STYLE, int CODE>
 __global__ void __launch_bounds__(256) kv8_keys(const KeyPlan plan, const Kv8Args a) {
