@@ -270,6 +270,7 @@ TreeSplit tree_split(HostPlan& hp, int G, int hkv) {
 // query heads, keys turned in the call), which they describe within 11%.  On 26,000 batches the choice takes, times
 // the best of all that were timed, in the mean 1.005 (decode) and 1.015 (prefill), and 1.007 and 1.023 on turned keys.
 // Tiles by the number of rows alone and chunks of the average work per unit: 1.05 and 1.35.
+// (Timed before calls copied turned keys (plan_keys), which choose by the same costs.)
 struct Kv8Costs {
     float start[4];       // tiles of 16, 32, 128 and 256 rows
     float step[4][4];     // ... of up to 64, 128, 192 and more rows (16 and 32: of any)
