@@ -888,11 +888,20 @@ struct __attribute__((aligned(2 * D))) Kv8ManyLds {
     float4 sc[2][4];             // per block of a step: its keys' scale, log2 and inverse of its values' scale
 };
 
+// The products of a wave's scores of a step: KD of each of its NT times 32 keys
+template <int D, int WR>
+struct Kv8Many {
+    static constexpr int KG = kKv8Waves / WR, NT = 2 / KG;
+    static constexpr int KD = D / 16;                  // 32x32x16 contraction steps of QK^T
+    static constexpr int TAKEN = KD * NT;
+    static constexpr int AHEAD = TAKEN < 5 ? TAKEN : 5;   // K reads in flight
+};
+
 template <int D, int STYLE, bool ROPE, bool COPY, int CODE, int WR, int NG>
 __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> plan, const Kv8Args a) {
     typedef Code<CODE> C;
-    constexpr int NW = kKv8Waves, KG = NW / WR, STEP = 64, HALF = D / 2;
-    constexpr int KD = D / 16;             // 32x32x16 contraction steps of QK^T
+    typedef Kv8Many<D, WR> S;
+    constexpr int NW = kKv8Waves, KG = S::KG, KD = S::KD, STEP = 64, HALF = D / 2;
     constexpr int DB = D / 32;             // 32-dim blocks of O^T
     constexpr int PL = D / 16;             // pairs that a lane turns
     constexpr int KW = PL / (COPY ? 2 : 4), VW = D / 32;   // words of a lane: either run of its key (of the copy: in float16), its value
@@ -1167,14 +1176,13 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     const int first_row_last = min(k_hi - 1, g.tok0 + min(row_lo, rows_total - 1) / G - kt0);   // last key that every row sees
     typedef __attribute__((address_space(3))) const u32x4_t lds_u32x4_t;
 
-    constexpr int NT = 2 / KG;     // times 32 keys of a step
-    constexpr int TAKEN = KD * NT;
+    constexpr int NT = S::NT, TAKEN = S::TAKEN, kAhead = S::AHEAD;
+    static_assert(kAhead >= 1 && kAhead <= TAKEN, "no read past a step's operands");
     // ---- step s, in buffer P = s % 2, and the codes of the next step
     auto step = [&](int s, int P, auto set) {
         // (the offsets are not kept apart for every chunk: registers are short)
         asm volatile("" : "+v"(k_at), "+v"(v_at));
         const uint32_t at = lds_at + (uint32_t)(P * 128 * D + 32 * kg * D) * 2, kt = at + k_at, vt = at + v_at;
-        constexpr int kAhead = 5;                 // K reads in flight
         u32x4_t kf[TAKEN];
         auto read_k = [&](int i) { kf[i] = *(lds_u32x4_t*)(uintptr_t)((kt ^ (32 * (i / NT))) + 64 * (i % NT) * D); };
 #pragma unroll
