@@ -373,9 +373,9 @@ pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, v
  *  - an element's code is x / s rounded to nearest, ties to even (off by at most half a step;
  *    exactly x times the float32 reciprocal of s, which for a power of two is the same); infinities
  *    become the largest number of their sign and a NaN 0.
- * Rows of one block must follow one another in the call (a request's tokens in order do; a row of another
- * block or a padding row between them makes the call a race); of rows of one slot the last counts.  A block that is
- * not started by its offset 0 needs a scale in the pool: 0 where nothing was stored before.
+ * Rows may stand in any order, those of one block anywhere in the call; of rows of one slot the last counts.  A
+ * block that is not started by its offset 0 needs a scale in the pool: 0 where nothing was stored before.  While a
+ * call of more than 8,192 rows runs, the signs of scales of the blocks that it stores in are not theirs.
  *  k_new, v_new  DEVICE rows of [Hkv][D] dense elements of cfg->dtype, row i at i * stride elements
  *                (strides as in pic_kv_append).  They must not overlap the pool.
  * n < 2^24 per call. */

@@ -275,8 +275,11 @@ struct Kv8WriteArgs {
     int64_t n_slots;
     int32_t n;
     int32_t hkv;
-    int32_t range;            // rows whose blocks a workgroup looks for
+    int32_t range;            // rows whose runs a workgroup looks for
+    int32_t noted;            // blocks of several runs are noted in the scales' signs
 };
+constexpr int kWriteRange = kBlock;   // the most of them
+constexpr int kWriteScan = 8192;      // the most rows of a call whose workgroups look for such blocks themselves
 
 // Records msg as the thread's last error (pic_last_error) and returns st.
 int32_t host_fail(int32_t st, const char* msg);

@@ -19,6 +19,7 @@ namespace pic {
 namespace {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
@@ -228,12 +229,41 @@ struct Code {
 // ---------------------------------------------------------------------------------
 // kv8_write.  A unit is (block, head, keys or values), taken by a wave: the rows that the call
 // stores in the block give the scale (a maximum over the wave), then lane l codes 16 elements of offset
-// l / (D / 16) (and 64 / (D / 16) offsets on), so that a page leaves in whole lines.  A block belongs to the first of
-// its rows, which follow one another: a workgroup looks for blocks that begin among `range` rows.
-// Bound by memory for prompts (104 MB, 8 heads of 128: 20.1 us, 5.2 TB/s), by its chain of loads (slots, then rows)
-// for a step's tokens (64 rows: 4.4 us).
+// l / (D / 16) (and 64 / (D / 16) offsets on), so that a page leaves in whole lines.  A workgroup looks for runs (rows of one
+// block that follow one another) that begin among `range` rows.  Where a block has one run in the call (a request's tokens
+// in order), the run is all of it.  A block of several belongs to the first of them, whose waves look through the call for
+// the others' rows; the others' leave it.  Whether a block has several, every workgroup counts for itself in calls of up
+// to kWriteScan rows (it reads all slots).  In longer ones a launch ahead notes it in the signs of the scales of the
+// block's head 0, which are not negative otherwise, and a launch behind clears them: of the keys' that a run of the
+// block is there, of the values' that another one is.  Counting costs nothing for 256 rows, 1.0 us of 8.0 for 1,024 of a
+// prompt, 2.4 of 13.9 for 8,192 and 11 of 33 for 16,876, the two launches 5.3 to 6.2 us at any number (1,024 requests of a
+// row: 2.6 of 17.4 and 5.6).
+// Bound by memory for prompts (104 MB, 8 heads of 128: 20.1 us, 5.2 TB/s, beside the two launches), by its chain of loads
+// (slots, then rows) for a step's tokens (64 rows: 4.4 us).
 // ---------------------------------------------------------------------------------
 constexpr int kWriteWaves = 4;
+constexpr uint32_t kSign = 0x80000000u;
+
+// The block in which row i of a call stores, if it begins a run; else below 0
+__device__ __forceinline__ int32_t run_block(const Kv8WriteArgs& a, int64_t i) {
+    if (i >= a.n) return -1;
+    const int32_t s = a.slots[i], p = i > 0 ? a.slots[i - 1] : -1;
+    return s < 0 || s >= a.n_slots || (p >= 0 && p < a.n_slots && p >> 4 == s >> 4) ? -1 : s >> 4;
+}
+
+// The signs of a call's blocks: set for kv8_write_kernel, or (CLEAR) taken away again
+template <bool CLEAR>
+__global__ void __launch_bounds__(256) kv8_runs_kernel(const Kv8WriteArgs a) {
+    const int32_t blk = run_block(a, (int64_t)blockIdx.x * blockDim.x + threadIdx.x);
+    if (blk < 0) return;
+    uint32_t* w = reinterpret_cast<uint32_t*>(a.scale) + (int64_t)blk * a.hkv * 2;
+    if (CLEAR) {
+        atomicAnd(w, ~kSign);
+        atomicAnd(w + 1, ~kSign);
+    } else if (atomicOr(w, kSign) & kSign) {
+        atomicOr(w + 1, kSign);
+    }
+}
 
 template <typename T, int D, int CODE>
 __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8WriteArgs a) {
@@ -254,8 +284,48 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
     int32_t prev = __shfl_up(mine, 1);
     if (lane == 0) prev = before;
     const uint64_t leads = __builtin_amdgcn_ballot_w64(lane < n_here && mine >= 0 && mine >> 4 != prev >> 4);
+    if (leads == 0) return;
     const int per = 2 * a.hkv, units = __builtin_popcountll(leads) * per;
     const int c16 = (lane % LPO) * 16;
+    // how many rows of the call store in the block of a run (by the lane of its first row)
+    __shared__ int stored[kWriteRange];
+    if (!a.noted) {
+        if (threadIdx.x < kWriteRange) stored[threadIdx.x] = 0;
+        __syncthreads();
+        constexpr int U = 4, EACH = kWriteWaves * 64 * 4;   // slots of a load of all threads
+        for (uint32_t i0 = 0; i0 < (uint32_t)a.n; i0 += U * EACH) {
+            i32x4_t s[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const uint32_t at = i0 + k * EACH + threadIdx.x * 4;
+                if (i0 + (k + 1) * EACH <= (uint32_t)a.n) {
+                    s[k] = *reinterpret_cast<const i32x4_t*>(a.slots + at);
+                } else {
+                    s[k] = i32x4_t{-1, -1, -1, -1};
+                    if (i0 + k * EACH < (uint32_t)a.n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (at + e < (uint32_t)a.n) s[k][e] = a.slots[at + e];
+                }
+            }
+            for (uint64_t rest = leads; rest; rest &= rest - 1) {
+                const int first = __builtin_ctzll(rest), blk = __builtin_amdgcn_readlane(mine, first) >> 4;
+                uint32_t least = ~0u;   // (below 16: a slot of the block; most lanes have none)
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) least = min(least, (uint32_t)(s[k][e] ^ blk << 4));
+                if (least >= kBlock) continue;
+                int of = 0;
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) of += s[k][e] >> 4 == blk;
+                atomicAdd(&stored[first], of);
+            }
+        }
+        __syncthreads();
+    }
     for (int u = (int)blockIdx.y * kWriteWaves + wave; u < units; u += (int)gridDim.y * kWriteWaves) {
         uint64_t rest = leads;
         for (int i = u / per; i > 0; --i) rest &= rest - 1;
@@ -267,21 +337,39 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
         bool fresh = false;
 #pragma unroll
         for (int p = 0; p < P; ++p) row[p] = -1;
-        int32_t slot = mine;
-        uint64_t live = ~0ull << first;   // lanes whose rows come into question
-        for (int64_t from = r0;; from += 64) {
-            const uint64_t others = __builtin_amdgcn_ballot_w64((slot >> 4) != blk) & live;
-            const uint64_t run = others ? live & ((others & -others) - 1) : live;
+        auto take = [&](int64_t from, int32_t slot, uint64_t rows) {   // rows of 64 from `from` on
 #pragma unroll
             for (int o = 0; o < kBlock; ++o) {
-                const uint64_t m = __builtin_amdgcn_ballot_w64((slot & 15) == o) & run;
+                const uint64_t m = __builtin_amdgcn_ballot_w64((slot & 15) == o) & rows;
                 if (m == 0) continue;
                 if (o == 0) fresh = true;
                 if (o % OPP == lane / LPO) row[o / OPP] = from + 63 - __builtin_clzll(m);
             }
+        };
+        int32_t slot = mine;
+        uint64_t live = ~0ull << first;   // lanes whose rows come into question
+        int here = 0;                     // rows of the run
+        for (int64_t from = r0;; from += 64) {
+            const uint64_t others = __builtin_amdgcn_ballot_w64((slot >> 4) != blk) & live;
+            const uint64_t run = others ? live & ((others & -others) - 1) : live;
+            here += __builtin_popcountll(run);
+            take(from, slot, run);
             if (others) break;
             live = ~0ull;   // (only rows of one slot over and over are more than a wave looks at)
             slot = slot_of(from + 64 + lane);
+        }
+        const uint32_t* signs = reinterpret_cast<const uint32_t*>(a.scale) + (int64_t)blk * a.hkv * 2;
+        const bool many = a.noted ? (signs[1] & kSign) != 0 : stored[first] != here;
+        if (many) {   // the block has other runs
+            bool before_it = false;
+            for (int64_t from = 0; from < r0 + first && !before_it; from += 64)
+                before_it = __builtin_amdgcn_ballot_w64(from + lane < r0 + first && slot_of(from + lane) >> 4 == blk) != 0;
+            if (before_it) continue;
+            for (int64_t from = r0 + first; from < a.n; from += 64) {
+                slot = slot_of(from + lane);
+                const uint64_t rows = __builtin_amdgcn_ballot_w64((slot >> 4) == blk);
+                if (rows) take(from, slot, rows);
+            }
         }
         const T* src = static_cast<const T*>(which ? a.v : a.k);
         const int64_t stride = (which ? a.v_stride : a.k_stride) * V;
@@ -293,7 +381,7 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
             for (int i = 0; i < NV; ++i)
                 x[p][i] = row[p] >= 0 ? *reinterpret_cast<const vec_t*>(src + row[p] * stride + h * D + c16 + i * V) : vec_t((T)0.f);
         float* sp = a.scale + ((int64_t)blk * a.hkv + h) * 2 + which;
-        const float old = fresh ? 0.f : *sp;
+        const float old = fresh ? 0.f : fabsf(*sp);
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -335,7 +423,8 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
             }
             *dst = w;
         }
-        if (lane == 0 && s != old) *sp = s;
+        // (a noted sign stays until the launch behind this one: waves of the block's other runs may still look for it)
+        if (lane == 0 && s != old) *sp = a.noted && many && h == 0 && which == 1 ? -s : s;
     }
 }
 
@@ -1579,10 +1668,13 @@ int launch_kv8_write(int dtype, int code, int d, const Kv8WriteArgs& a, void* st
     // a block's units over workgroups in y, so that a few tokens fill the chip
     const int64_t per = 2 * (int64_t)a.hkv;
     const dim3 grid((unsigned)((a.n + (int64_t)a.range - 1) / a.range), (unsigned)(per + kWriteWaves - 1 < 4 * kWriteWaves ? (per + kWriteWaves - 1) / kWriteWaves : 4));
+    const dim3 rows((unsigned)(((int64_t)a.n + 255) / 256));
+    if (a.noted) hipLaunchKernelGGL((kv8_runs_kernel<false>), rows, dim3(256), 0, (hipStream_t)stream, a);
     by_types(dtype, d, code, [&](auto t, auto dim, auto c) {
         hipLaunchKernelGGL((kv8_write_kernel<decltype(t), decltype(dim)::value, decltype(c)::value>), grid, dim3(kWriteWaves * 64), 0,
                            (hipStream_t)stream, a);
     });
+    if (a.noted) hipLaunchKernelGGL((kv8_runs_kernel<true>), rows, dim3(256), 0, (hipStream_t)stream, a);
     return hipGetLastError();
 }
 
