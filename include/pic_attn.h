@@ -354,7 +354,8 @@ typedef struct pic_kv8_pool {
  *             must share no memory with an input or the other output.
  *  q_weight, k_weight  DEVICE [D] in cfg->dtype, or NULL (ones).
  * Strides are at least a row and multiples of 16 bytes.  Computed in float32 and rounded once to
- * cfg->dtype; a row's squares are summed in float32 (elements of 2^60 and more may pass its range).  cos/sin are
+ * cfg->dtype; a row's squares are summed in float32 (elements of 2^60 and more may pass its range).  A head that
+ * holds a NaN becomes NaN; one that holds an infinity is NaN there and 0 elsewhere (before it turns).  cos/sin are
  * those of pic_kv_append.  eps > 0 and not denormal, n < 2^24 per call. */
 pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                        const void* k, int64_t k_stride, void* k_out, int64_t k_out_stride, const void* q_weight,

@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a)
             unpack_chunk<T>(y[u], f + PP);
 #pragma unroll
             for (int k = 0; k < 2 * PP; ++k) sum = __builtin_fmaf(f[k], f[k], sum);
-            const float r = __builtin_amdgcn_rsqf(fmaxf(sum_of<UPH>(sum) * (1.f / D) + a.eps, 0x1p-126f));   // (within an ulp; not of a denormal)
+            const float r = __builtin_amdgcn_rsqf(sum_of<UPH>(sum) * (1.f / D) + a.eps);   // (within an ulp; eps is normal, so is the argument)
             const float* w = weight[h < a.hq ? 0 : 1];
 #pragma unroll
             for (int k = 0; k < 2 * PP; ++k) f[k] *= r * w[(k < PP ? c0 : c1) * PP + k % PP];
