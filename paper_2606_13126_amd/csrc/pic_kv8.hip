@@ -967,7 +967,9 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 // ---------------------------------------------------------------------------------
 constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
 
-constexpr int kKv8Renew = 32;   // steps after which angles are computed again
+// Steps after which angles are computed again.  A pair's cos/sin start within 2^-22.4 (rope_cs_fast, as a vector), and an advance
+// adds the stride's own error, 2^-23.7 at most, and two roundings of each, 2^-23.5: within 2^-17.5 after 32.
+constexpr int kKv8Renew = 32;
 
 template <int D>
 struct __attribute__((aligned(2 * D))) Kv8ManyLds {
@@ -1091,7 +1093,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, 2) kv8_many(const PlanOf<NG> p
     if (ROPE)
         for (int i = threadIdx.x; i < HALF; i += NW * 64) {
             lds.fstep[i] = a.fstep[i];
-            if (!COPY) rope_cs_fast(STEP, a.fstep[i], lds.stride_cs[i].x, lds.stride_cs[i].y);
+            if (!COPY) rope_cs(STEP, a.fstep[i], lds.stride_cs[i].x, lds.stride_cs[i].y);   // (its error comes again with every advance)
         }
 
     // ---- queries.  The cos/sin of their tokens (a token's heads share them) pass through the wave's
