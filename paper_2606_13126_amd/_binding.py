@@ -8,6 +8,7 @@ import of this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 from typing import Optional
@@ -350,14 +351,29 @@ def pic_tree_plan_debug(cfg: pic_config, batch: HostBatch) -> np.ndarray:
 # pool, attention over it
 # ------------------------------------------------------------------------------------
 
+def _dense(t, what: str, dtypes) -> None:
+    """Refuses a tensor (None passes) of another type, which the library would read as one of these, or one with gaps."""
+    if t is not None and (t.dtype not in dtypes or not t.is_contiguous()):
+        raise ValueError(f"{what} must be dense, of {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+
+
+@functools.lru_cache(maxsize=None)
+def _types(which) -> tuple:
+    """torch types: of cfg.dtype's rows, of int32 arrays ("int32"), of scales ("scale") and of codes ("codes", code)."""
+    import torch
+    return {PIC_BF16: (torch.bfloat16,), PIC_F32: (torch.float32,), "int32": (torch.int32,), "scale": (torch.float32,),
+            ("codes", PIC_KV8_E4M3): (torch.float8_e4m3fn, torch.uint8), ("codes", PIC_KV8_INT8): (torch.int8, torch.uint8)}.get(which, ())
+
+
 class Kv8Pool:
-    """A pool of codes: k, v one-byte tensors [blocks][Hkv][16][D] and scale float32 [blocks][Hkv][2], all dense;
-    code is PIC_KV8_E4M3 or PIC_KV8_INT8.  Keeps the tensors alive."""
+    """A pool of codes: k, v [blocks][Hkv][16][D] of float8_e4m3fn or int8, as code (PIC_KV8_E4M3, PIC_KV8_INT8) says, or
+    their bytes (uint8), and scale float32 [blocks][Hkv][2], all dense.  Keeps the tensors alive."""
 
     def __init__(self, k, v, scale, code: int):
-        for t, what, size in ((k, "k", 1), (v, "v", 1), (scale, "scale", 4)):
-            if t.element_size() != size or not t.is_contiguous():
-                raise ValueError(f"{what} must be dense, of {size}-byte elements")
+        if code not in (PIC_KV8_E4M3, PIC_KV8_INT8):
+            raise ValueError("code must be PIC_KV8_E4M3 or PIC_KV8_INT8")
+        for t, what, types in ((k, "k", ("codes", code)), (v, "v", ("codes", code)), (scale, "scale", "scale")):
+            _dense(t, what, _types(types))
         if k.dim() != 4 or k.shape[2] != 16 or v.shape != k.shape or tuple(scale.shape) != (k.shape[0], k.shape[1], 2):
             raise ValueError("k and v must be [blocks][Hkv][16][D] and scale [blocks][Hkv][2]")
         self.k, self.v, self.scale = k, v, scale
@@ -371,26 +387,26 @@ class Kv8Pool:
         return self._ref
 
 
-def _rows_of(t, what: str, heads: int, dim: int):
-    """_rows of a tensor that must have these heads, and its number of rows."""
+def _rows_of(t, what: str, heads: int, dim: int, types):
+    """_rows of a tensor that must have these heads and one of these types, and its number of rows."""
     p, stride = _rows(t, what)
     n, h, d = t.size()
-    if h != heads or d != dim:
-        raise ValueError(f"{what} must be [n][{heads}][{dim}]")
+    if h != heads or d != dim or t.dtype not in types:
+        raise ValueError(f"{what} must be [n][{heads}][{dim}] of the config's type")
     return p, stride, n
 
 
-def _norm_rows(t, out, what: str, heads: int, dim: int):
+def _norm_rows(t, out, what: str, heads: int, dim: int, types):
     """Addresses and strides of one input of pic_qk_norm and its output, and the rows."""
     if t is None:
         if out is not None:
             raise ValueError(f"{what}_out without {what}")
         return 0, None, 0, None, 0
-    p, stride, n = _rows_of(t, what, heads, dim)
+    p, stride, n = _rows_of(t, what, heads, dim, types)
     if out is None:
         return n, p, stride, p, stride
-    if out.size() != t.size():
-        raise ValueError(f"{what}_out must have the shape of {what}")
+    if out.size() != t.size() or out.dtype != t.dtype:
+        raise ValueError(f"{what}_out must have the shape and type of {what}")
     if out.is_contiguous():
         return n, p, stride, out.data_ptr(), heads * dim
     return n, p, stride, *_rows(out, what + "_out")
@@ -399,19 +415,27 @@ def _norm_rows(t, out, what: str, heads: int, dim: int):
 def pic_qk_norm(cfg: pic_config, q, k, q_weight, k_weight, eps: float, positions=None, q_out=None, k_out=None, stream=None) -> None:
     """q [n][Hq][D] and k [n][Hkv][D] (either may be None) may be views of one projection's output, the outputs too;
     without an output the norm is taken in place.  Weights [D] or None; positions may be None for an unrotated pool."""
-    d = cfg.head_dim
-    nq, qp, qs, qo, qos = _norm_rows(q, q_out, "q", cfg.num_q_heads, d)
-    nk, kp, ks, ko, kos = _norm_rows(k, k_out, "k", cfg.num_kv_heads, d)
+    d, types = cfg.head_dim, _types(cfg.dtype)
+    nq, qp, qs, qo, qos = _norm_rows(q, q_out, "q", cfg.num_q_heads, d, types)
+    nk, kp, ks, ko, kos = _norm_rows(k, k_out, "k", cfg.num_kv_heads, d, types)
     if q is not None and k is not None and nq != nk:
         raise ValueError("q and k must have the same rows")
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        _dense(w, what, types)
+        if w is not None and w.numel() != d:
+            raise ValueError(f"{what} must have {d} elements")
+    _dense(positions, "positions", _types("int32"))
+    if positions is not None and positions.numel() < (nq or nk):
+        raise ValueError("positions must have an entry per row")
     _check(_lib.pic_qk_norm(ctypes.byref(cfg), qp, qs, qo, qos, kp, ks, ko, kos, _ptr(q_weight), _ptr(k_weight), eps, _ptr(positions),
                             nq or nk, _stream(stream)))
 
 
 def pic_kv8_write(cfg: pic_config, pool: Kv8Pool, k_new, v_new, slot_mapping, stream=None) -> None:
     """k_new, v_new [n][Hkv][D] may be views of one projection's output (rows dense, any row stride)."""
-    h, d = cfg.num_kv_heads, cfg.head_dim
-    (kp, ks, n), (vp, vs, nv) = _rows_of(k_new, "k_new", h, d), _rows_of(v_new, "v_new", h, d)
+    h, d, types = cfg.num_kv_heads, cfg.head_dim, _types(cfg.dtype)
+    (kp, ks, n), (vp, vs, nv) = _rows_of(k_new, "k_new", h, d, types), _rows_of(v_new, "v_new", h, d, types)
+    _dense(slot_mapping, "slot_mapping", _types("int32"))
     if nv != n or slot_mapping.size(0) != n:
         raise ValueError("k_new, v_new and slot_mapping must have the same rows")
     _check(_lib.pic_kv8_write(ctypes.byref(cfg), pool._of(cfg), kp, ks, vp, vs, slot_mapping.data_ptr(), n, _stream(stream)))
@@ -419,9 +443,12 @@ def pic_kv8_write(cfg: pic_config, pool: Kv8Pool, k_new, v_new, slot_mapping, st
 
 def pic_kv8_read(cfg: pic_config, pool: Kv8Pool, slot_mapping, k_out, v_out, stream=None) -> None:
     """k_out, v_out: dense [n][Hkv][D]."""
-    shape = (slot_mapping.size(0), cfg.num_kv_heads, cfg.head_dim)
-    if not k_out.is_contiguous() or not v_out.is_contiguous() or k_out.size() != shape or v_out.size() != shape:
-        raise ValueError(f"k_out and v_out must be dense {list(shape)}")
+    shape, types = (slot_mapping.size(0), cfg.num_kv_heads, cfg.head_dim), _types(cfg.dtype)
+    _dense(slot_mapping, "slot_mapping", _types("int32"))
+    for out, what in ((k_out, "k_out"), (v_out, "v_out")):
+        _dense(out, what, types)
+        if out.size() != shape:
+            raise ValueError(f"{what} must be {list(shape)}")
     _check(_lib.pic_kv8_read(ctypes.byref(cfg), pool._of(cfg), slot_mapping.data_ptr(), slot_mapping.size(0), k_out.data_ptr(),
                              v_out.data_ptr(), _stream(stream)))
 
@@ -433,6 +460,9 @@ def pic_attn8_workspace_size(cfg: pic_config, batch: HostBatch, is_decode: bool)
 
 
 def _attn8(call, cfg, batch, block_tables, positions, q, o, pool, workspace, stream):
+    types, ints = _types(cfg.dtype), _types("int32")
+    for t, what, of in ((q, "q", types), (o, "o", types), (block_tables, "block_tables", ints), (positions, "positions", ints)):
+        _dense(t, what, of)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(call(ctypes.byref(cfg), ctypes.byref(batch.c), ctypes.byref(_dev(block_tables, positions)), _ptr(q), _ptr(o), pool._of(cfg),
                 _ptr(workspace), ws_bytes, _stream(stream)))
