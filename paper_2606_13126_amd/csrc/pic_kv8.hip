@@ -23,17 +23,6 @@ typedef int32_t i32x4_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
-// Outputs of more than this go past the caches, which they would only sweep (a call's inputs then stay there for the
-// next): 33,280 rows of 8 heads read from the pool (136 MB) 30.9 us, 43.5 through the caches, 16,384 rows of 72 heads
-// normalised (302 MB) 104 and 112.  Less is likely read again from there by what follows.
-constexpr int64_t kStreamBytes = (int64_t)64 << 20;
-
-template <bool STREAMS, typename V>
-__device__ __forceinline__ void store_chunk(V* dst, const V& x) {
-    if constexpr (STREAMS) __builtin_nontemporal_store(x, dst);
-    else *dst = x;
-}
-
 // sum over the N lanes (4, 8 or 16, aligned) that hold a head
 template <int N>
 __device__ __forceinline__ float sum_of(float x) {
@@ -52,8 +41,9 @@ __device__ __forceinline__ float sum_of(float x) {
 // elements pair up, GPT-J (and what does not turn) two neighbours.  The lanes of a head are
 // neighbours, so its squares meet by lane permutes.  The row's threads put its cos/sin and the weights into
 // LDS once, while its first units are on their way.
-// Bound by memory: every element is read and written once.  16,384 rows of 64 + 8 heads of 128 (604 MB): 101 us, 5.9
-// TB/s; 64 rows of 32 + 8 heads 3.0, two latencies.
+// Bound by memory: every element is read and written once.  16,384 rows of 64 + 8 heads of 128 (604 MB): 109 us, 5.5
+// TB/s; 64 rows of 32 + 8 heads 3.0, two latencies.  Stores go through the caches, where what follows finds them: past
+// them those calls took 100 to 105 where inputs repeat, but 164 against 136 with inputs and outputs out of the caches.
 // ---------------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
 
@@ -79,7 +69,7 @@ __device__ __forceinline__ u32x4_t pack_chunk(const float* f) {
     return w;
 }
 
-template <typename T, int D, int STYLE, bool ROT, bool STREAMS>
+template <typename T, int D, int STYLE, bool ROT>
 __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a) {
     constexpr int PP = 16 / sizeof(T);     // elements per chunk, pairs per unit
     constexpr int CH = D / PP, UPH = CH / 2, U = 3;
@@ -150,8 +140,8 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(const NormArgs a)
                     s = __builtin_fmaf(p0, t.y, s0 * t.x);
                 }
             u32x4_t* dst = h < a.hq ? qo + h * CH : ko + (h - a.hq) * CH;
-            store_chunk<STREAMS>(dst + c0, pack_chunk<T>(f));
-            store_chunk<STREAMS>(dst + c1, pack_chunk<T>(f + PP));
+            dst[c0] = pack_chunk<T>(f);
+            dst[c1] = pack_chunk<T>(f + PP);
         }
     }
 }
@@ -430,9 +420,11 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
 
 // ---------------------------------------------------------------------------------
 // kv8_read: a thread takes the codes of 16 bytes of output (4 or 8), U of them in flight.  Bound by memory: 33,280
-// rows of 8 heads of 128 (204 MB) 30.2 us, 6.8 TB/s (codes that lie in the cache among them).
+// rows of 8 heads of 128 (204 MB) 41 us, 4.9 TB/s.  Stores go through the caches: past them the call took 31 us where the
+// same blocks are read over and over, but 55.5 against 57 with its inputs out of the caches, and with a copy of its outputs
+// behind it 121 against 103 (20,480 rows: 82 against 61).
 // ---------------------------------------------------------------------------------
-template <typename T, int D, int CODE, bool STREAMS>
+template <typename T, int D, int CODE>
 __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool,
                                                        const float* __restrict__ scale, int64_t n_slots,
                                                        const int32_t* __restrict__ slots, int64_t n_units, int hkv,
@@ -474,7 +466,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const uint8_t* __restrict
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[4 * j + e] = (T)f[e];
                 }
-                store_chunk<STREAMS>(reinterpret_cast<vec_t*>((kv ? v_out : k_out) + i * V), y);
+                *reinterpret_cast<vec_t*>((kv ? v_out : k_out) + i * V) = y;
             }
         }
     }
@@ -1626,14 +1618,14 @@ hipError_t launch_kv8_d(int style, bool rope, const Plan& plan, const Kv8Args& a
     return style == kNeox ? launch_kv8_t<D, 0, true, false, CODE>(plan, a, st) : launch_kv8_t<D, 1, true, false, CODE>(plan, a, st);
 }
 
-template <typename T, int D, bool STREAMS>
+template <typename T, int D>
 void launch_norm_d(int style, int n, int threads, const NormArgs& a, hipStream_t st) {
     if (a.rot_half == 0)
-        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, false, STREAMS>), dim3(n), dim3(threads), 0, st, a);
+        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, false>), dim3(n), dim3(threads), 0, st, a);
     else if (style == kNeox)
-        hipLaunchKernelGGL((qk_norm_kernel<T, D, 0, true, STREAMS>), dim3(n), dim3(threads), 0, st, a);
+        hipLaunchKernelGGL((qk_norm_kernel<T, D, 0, true>), dim3(n), dim3(threads), 0, st, a);
     else
-        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, true, STREAMS>), dim3(n), dim3(threads), 0, st, a);
+        hipLaunchKernelGGL((qk_norm_kernel<T, D, 1, true>), dim3(n), dim3(threads), 0, st, a);
 }
 
 // f(type, head_dim, code) with the values as constants
@@ -1657,10 +1649,7 @@ int launch_qk_norm(int dtype, int style, int d, int n, const NormArgs& a, void* 
     hipStream_t st = (hipStream_t)stream;
     const int64_t units = (int64_t)(a.hq + a.hkv) * (d * (dtype == 1 ? 4 : 2) / 32);
     const int threads = units >= kNormThreads ? kNormThreads : (int)((units + 63) / 64) * 64;
-    const auto go = [&](auto t, auto dim) {
-        if (32 * units * n > kStreamBytes) launch_norm_d<decltype(t), decltype(dim)::value, true>(style, n, threads, a, st);
-        else launch_norm_d<decltype(t), decltype(dim)::value, false>(style, n, threads, a, st);
-    };
+    const auto go = [&](auto t, auto dim) { launch_norm_d<decltype(t), decltype(dim)::value>(style, n, threads, a, st); };
     if (dtype == 1) d == 64 ? go(float{}, Idx<64>{}) : go(float{}, Idx<128>{});
     else d == 64 ? go(__bf16{}, Idx<64>{}) : go(__bf16{}, Idx<128>{});
     return hipGetLastError();
@@ -1687,12 +1676,8 @@ int launch_kv8_read(int dtype, int code, int d, int hkv, const uint8_t* k_pool, 
     const dim3 grid((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22));   // (lanes of a launch stay below 2^32)
     by_types(dtype, d, code, [&](auto t, auto dim, auto c) {
         typedef decltype(t) T;
-        const auto go = [&](auto s) {
-            hipLaunchKernelGGL((kv8_read_kernel<T, decltype(dim)::value, decltype(c)::value, decltype(s)::value>), grid, dim3(256), 0,
-                               (hipStream_t)stream, k_pool, v_pool, scale, n_slots, slots, units, hkv, static_cast<T*>(k_out), static_cast<T*>(v_out));
-        };
-        if (32 * units > kStreamBytes) go(std::true_type{});
-        else go(std::false_type{});
+        hipLaunchKernelGGL((kv8_read_kernel<T, decltype(dim)::value, decltype(c)::value>), grid, dim3(256), 0, (hipStream_t)stream, k_pool,
+                           v_pool, scale, n_slots, slots, units, hkv, static_cast<T*>(k_out), static_cast<T*>(v_out));
     });
     return hipGetLastError();
 }
