@@ -397,11 +397,12 @@ pic_status pic_attn8_workspace_size(const pic_config* cfg, const pic_batch_host*
  * workspace rules.  cos/sin are computed in the kernel (no table).
  * As in pic_attn_prefill, room for a copy of the turned keys behind the rest of the workspace is optional.
  * How exact: codes and scales enter exactly; sums and softmax statistics are float32.  float32 calls compute in
- * float32.  In bf16, besides the result's own rounding: turned queries are rounded to 11 bits (elements below 2^-14
- * of their row's largest to 2^-25 of that), and cos/sin of keys, their products and the turned keys to 11 bits each (cos/sin
- * below 2^-14 to 2^-25).  Where a call's row tiles hold at most 32 rows (query tokens x query heads of a KV head)
- * keys turn by their place in the block and queries back by the block's position, with the same roundings once more for
- * the queries; probabilities (times their block's scale of values) have 16 bits (small ones fewer where that scale is
+ * float32.  In bf16, besides the result's own rounding, with rotation: cos/sin of keys, their products and the turned keys
+ * are rounded to 11 bits each (cos/sin below 2^-14 to 2^-25), turned queries to 11 bits (elements below 2^-14 of their
+ * row's largest to 2^-25 of that).  Where a call's row tiles hold at most 32 rows (query tokens x query heads of a KV head)
+ * keys turn by their place in the block, and queries by the distance of the tile's first token from the block, with
+ * roundings as the keys'; queries of other tokens than the first turn by their distance from it before, and are
+ * rounded once there; probabilities (times their block's scale of values) have 16 bits (small ones fewer where that scale is
  * below 2^-100).  Where they hold more, angles of keys are within 2^-17 (those of a run of positions advance from one
  * another; keys of a copy are rounded once), probabilities have 8 bits, and a block's scale of values below
  * 2^-90 counts as 2^-90.  Without rotation queries and keys are exact.

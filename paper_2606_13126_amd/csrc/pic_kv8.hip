@@ -496,13 +496,15 @@ __device__ __forceinline__ Group find_group(const PlanOf<N>& plan, int bid) {
 // neighbouring dimensions of four keys, two byte permutes part them.  The 32-deep product
 // holds the 16 keys twice, for a probability as two bf16 numbers (16 bits in all).
 //
-// RoPE: with b the position of a block's first key, (R_p q).(R_(b+j) k) = (R_(-b) R_p q).(R_j k).  Where a block's
-// positions follow one another its keys turn by their place j in it, the same for every block, whose cos/sin a lane
-// holds in registers (of its 4 KD pairs of key l%16), and the queries turn back by b, whose cos/sin are 64 numbers
-// of the whole wave, one of a lane.  Other blocks' keys turn by the positions that they have, less b.  Turning is done
-// in packed float16, two pairs at a time: 16 operations of a lane for the queries of a block and 16 for its keys
-// (D 128: twice that), where angles of each key that advance from block to block cost 5 a pair beside the keys' own
-// (64 requests x 8,192 keys of int8, 32 / 8 heads of 128: 204.6 us, 211.8 with those).
+// RoPE: with b the position of a block's first key and r that of the row tile's first query token, (R_p q).(R_(b+j) k) =
+// (R_(r-b) R_(p-r) q).(R_j k).  Where a block's positions follow one another its keys turn by their place j in it, the same
+// for every block, whose cos/sin a lane holds in registers (of its 4 KD pairs of key l%16), and the queries turn by r - b,
+// whose cos/sin are 64 numbers of the whole wave, one of a lane.  Other blocks' keys turn by the positions that they have,
+// less b.  Turning is done in packed float16, two pairs at a time: 16 operations of a lane for the queries of a block and 16
+// for its keys (D 128: twice that), where angles of each key that advance from block to block cost 5 a pair beside the keys'
+// own (64 requests x 8,192 keys of int8, 32 / 8 heads of 128: 204.6 us, 211.8 with those).  The first token's queries
+// (all of a decode's) are rounded there alone: p = r.  Those of other tokens turn by p - r before, once, in float32, and are
+// rounded to float16.
 //
 // Bound by memory and by the vector unit about alike where the card is full: the same call 196 us at its best, 5.5 TB/s, the
 // vector unit busy 66% of the cycles and the matrix cores 10%; 192 without rotation.  Few keys: by the chain of
@@ -533,7 +535,7 @@ struct __attribute__((aligned(16))) Kv8FewLds {
     float qs[16 * CB];
     uint64_t fstep[D / 2];
     uint16_t places[kBlock][D / 8][8];           // cos/sin of 0 .. 15 positions: of 4 pairs, cos then sin
-    uint16_t base[S::NW][D / 8][8];              // ... of a wave's block
+    uint16_t base[S::NW][D / 8][8];              // ... of a wave's block, from the first token on
     int32_t meta[S::NW][S::NST][S::META];
 };
 
@@ -656,6 +658,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 
     // ---- queries: the waves turn 2 CB rows each, LPR lanes a row, and leave the B operands of all in LDS
     // (from where every tile reads them: in registers they would leave room for two waves per SIMD only)
+    const int64_t first_pos = ROPE ? a.positions[g.pos_off + g.tok0 + row_lo / G] : 0;   // of the tile's first token
     int last[CB];     // last key that the lane's row sees, from kt0
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -682,7 +685,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
                 else in[h * PP + k] = w[k];
             }
         }
-        const int32_t pos = ROPE ? a.positions[g.pos_off + g.tok0 + to] : 0;
+        const int64_t from_first = ROPE ? (int64_t)a.positions[g.pos_off + g.tok0 + to] - first_pos : 0;
         __syncthreads();   // phase steps staged
         float x[PP], y[PP], big = 0.f;
 #pragma unroll
@@ -696,7 +699,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 #pragma unroll
             for (int k = 0; k < PP; ++k) {
                 float c, s;
-                rope_cs_fast(pos, lds.fstep[p0 + k], c, s);
+                rope_cs_fast(from_first, lds.fstep[p0 + k], c, s);
                 const float x0 = x[k], y0 = y[k];
                 x[k] = x0 * c - y0 * s;
                 y[k] = y0 * c + x0 * s;
@@ -783,7 +786,7 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
             away = pos - b;
             apart = __builtin_amdgcn_ballot_w64(away != c16 && c16 >= first && k0 + c16 < k_hi) != 0;
             float c, s;
-            rope_cs_fast(b, my_step, c, s);
+            rope_cs_fast(b - first_pos, my_step, c, s);
             put_cs(lds.base[wave], my_pair, c, s);
             __atomic_signal_fence(__ATOMIC_SEQ_CST);
         }
