@@ -228,8 +228,8 @@ struct Code {
 // block is there, of the values' that another one is.  Counting costs nothing for 256 rows, 1.0 us of 8.0 for 1,024 of a
 // prompt, 2.4 of 13.9 for 8,192 and 11 of 33 for 16,876, the two launches 5.3 to 6.2 us at any number (1,024 requests of a
 // row: 2.6 of 17.4 and 5.6).
-// Bound by memory for prompts (104 MB, 8 heads of 128: 20.1 us, 5.2 TB/s, beside the two launches), by its chain of loads
-// (slots, then rows) for a step's tokens (64 rows: 4.4 us).
+// Bound by memory for prompts (104 MB, 8 heads of 128: 20.4 us, 5.1 TB/s, beside the two launches), by its chain of loads
+// (slots, then rows) for a step's tokens (64 rows: 5.0 us).
 // ---------------------------------------------------------------------------------
 constexpr int kWriteWaves = 4;
 constexpr uint32_t kSign = 0x80000000u;
@@ -508,7 +508,7 @@ __device__ __forceinline__ Group find_group(const PlanOf<N>& plan, int bid) {
 //
 // Bound by memory and by the vector unit about alike where the card is full: the same call 196 us at its best, 5.5 TB/s, the
 // vector unit busy 66% of the cycles and the matrix cores 10%; 192 without rotation.  Few keys: by the chain of
-// plan, block ids, codes, products and the meeting of the waves (7.2 us over 1,025 keys).
+// plan, block ids, codes, products and the meeting of the waves (7.2 us over 1,537 keys).
 // ---------------------------------------------------------------------------------
 
 template <int D, int CB>
@@ -961,8 +961,8 @@ __global__ void __launch_bounds__(kKv8Waves * 64, (Kv8Few<D, CB>::WAVES)) kv8_fe
 //
 // Bound by products, vector work and LDS reads, which overlap in part: a step of 256 rows has 2,048 cycles of products and
 // 2,300 of LDS, and takes about 5,100 cycles with turning (products 38%, vector unit 48% by the counters), 4,500 with
-// the copy (45% and 37%).  2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1,204 us with the copy, 970 TFLOP/s, 1,350 without it; on
-// a pool of turned keys 1,160, 1,007.
+// the copy (45% and 37%).  2,048 tokens of 64 / 8 heads of 128 over 18,432 keys of int8: 1,142 to 1,225 us by the card with the copy, 954
+// to 1,023 TFLOP/s; on one of them 1,204 with it, 1,350 without it, and 1,160 on a pool of turned keys.
 // ---------------------------------------------------------------------------------
 constexpr float kLeastValueScale = 0x1p-90f;   // (p' of 2^-36 and more stay above the type's least)
 
