@@ -376,7 +376,7 @@ pic_status pic_qk_norm(const pic_config* cfg, const void* q, int64_t q_stride, v
  *    become the largest number of their sign and a NaN 0.
  * Rows may stand in any order, those of one block anywhere in the call; of rows of one slot the last counts.  A
  * block that is not started by its offset 0 needs a scale in the pool: 0 where nothing was stored before.  While a
- * call of more than 8,192 rows runs, the signs of scales of the blocks that it stores in are not theirs.
+ * call of more than 1,024 rows runs, the signs of scales of the blocks that it stores in are not theirs.
  *  k_new, v_new  DEVICE rows of [Hkv][D] dense elements of cfg->dtype, row i at i * stride elements
  *                (strides as in pic_kv_append).  They must not overlap the pool.
  * n < 2^24 per call. */

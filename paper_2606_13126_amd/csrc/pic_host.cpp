@@ -1334,7 +1334,6 @@ pic_status pic_kv8_write(const pic_config* cfg, const pic_kv8_pool* pool, const 
     // row 7.6 us, 34 with ranges of 16; a prompt of 1,024 rows 7.4, 15.7 with ranges of 1; 1,024 requests of one row 15.8,
     // 14.4 with ranges of 1, 33.6 with 16 (before workgroups counted a block's rows, which adds up to 2.6 us there).
     for (a.range = 1; a.range < pic::kWriteRange && n > 256 * a.range;) a.range *= 2;
-    a.noted = n > pic::kWriteScan;
     return hip_status(pic::launch_kv8_write(cfg->dtype, pool->code, cfg->head_dim, a, stream), "kv8_write launch");
 }
 

@@ -276,10 +276,9 @@ struct Kv8WriteArgs {
     int32_t n;
     int32_t hkv;
     int32_t range;            // rows whose runs a workgroup looks for
-    int32_t noted;            // blocks of several runs are noted in the scales' signs
 };
 constexpr int kWriteRange = kBlock;   // the most of them
-constexpr int kWriteScan = 8192;      // the most rows of a call whose workgroups look for such blocks themselves
+constexpr int kWriteScan = 1024;      // the most rows of a call whose workgroups count them themselves
 
 // Records msg as the thread's last error (pic_last_error) and returns st.
 int32_t host_fail(int32_t st, const char* msg);

@@ -220,43 +220,52 @@ struct Code {
 // kv8_write.  A unit is (block, head, keys or values), taken by a wave: the rows that the call
 // stores in the block give the scale (a maximum over the wave), then lane l codes 16 elements of offset
 // l / (D / 16) (and 64 / (D / 16) offsets on), so that a page leaves in whole lines.  A workgroup looks for runs (rows of one
-// block that follow one another) that begin among `range` rows.  Where a block has one run in the call (a request's tokens
-// in order), the run is all of it.  A block of several belongs to the first of them, whose waves look through the call for
-// the others' rows; the others' leave it.  Whether a block has several, every workgroup counts for itself in calls of up
-// to kWriteScan rows (it reads all slots).  In longer ones a launch ahead notes it in the signs of the scales of the
-// block's head 0, which are not negative otherwise, and a launch behind clears them: of the keys' that a run of the
-// block is there, of the values' that another one is.  Counting costs nothing for 256 rows, 1.0 us of 8.0 for 1,024 of a
-// prompt, 2.4 of 13.9 for 8,192 and 11 of 33 for 16,876, the two launches 5.3 to 6.2 us at any number (1,024 requests of a
-// row: 2.6 of 17.4 and 5.6).
-// Bound by memory for prompts (104 MB, 8 heads of 128: 20.4 us, 5.1 TB/s, beside the two launches), by its chain of loads
+// block that follow one another) that begin among `range` rows, and has to know whose a block of several runs is, and
+// the others' rows:
+//  - Calls of up to kWriteScan rows: every workgroup counts its blocks' rows in the call.  Where a run is all of them (a
+//    request's tokens in order) that is all; else the block is the first run's, whose waves look for the others' rows.
+//  - More rows: a launch ahead (kv8_notes) sets the sign of the scale of the block's head 0, which is not negative
+//    otherwise, and leaves in every slot that the call writes the last of its rows.  A block is the run's that takes the sign
+//    away, and its rows are what its slots hold.  (A slot's first bytes are a note where the row that they name stores there:
+//    true of any bytes, so what was there before needs no clearing.)
+// Counting costs nothing for 256 rows, 1 us of 8.0 for 1,024 of a prompt and 2.7 of 17.6 for 1,024 requests of a row; notes
+// 4 us of 11.4 for 2,048 of a prompt, 6 of 28.0 for 16,876, and nothing for 2,048 requests of a row.  16 tokens of each of 64
+// requests, token by token, take 101 us by counting, of 128 requests 31 by notes and of 1,024 58.
+// Bound by memory for prompts (104 MB, 8 heads of 128: 20.4 us, 5.1 TB/s, beside the notes), by its chain of loads
 // (slots, then rows) for a step's tokens (64 rows: 5.0 us).
 // ---------------------------------------------------------------------------------
-constexpr int kWriteWaves = 4;
+constexpr int kWriteWaves = 4, kNotedWaves = 16;
 constexpr uint32_t kSign = 0x80000000u;
 
-// The block in which row i of a call stores, if it begins a run; else below 0
-__device__ __forceinline__ int32_t run_block(const Kv8WriteArgs& a, int64_t i) {
-    if (i >= a.n) return -1;
-    const int32_t s = a.slots[i], p = i > 0 ? a.slots[i - 1] : -1;
-    return s < 0 || s >= a.n_slots || (p >= 0 && p < a.n_slots && p >> 4 == s >> 4) ? -1 : s >> 4;
+// Row i of a call stores in slot s
+__device__ __forceinline__ bool stores_in(const Kv8WriteArgs& a, int32_t i, int32_t s) { return i >= 0 && i < a.n && a.slots[i] == s; }
+
+// The first four bytes of a slot's keys of head 0, which the call writes anyway: the last row that stores there
+template <int D>
+__device__ __forceinline__ int32_t* note_of(const Kv8WriteArgs& a, int32_t slot) {
+    return reinterpret_cast<int32_t*>(a.k_pool + ((int64_t)(slot >> 4) * a.hkv * kBlock + (slot & 15)) * D);
 }
 
-// The signs of a call's blocks: set for kv8_write_kernel, or (CLEAR) taken away again
-template <bool CLEAR>
-__global__ void __launch_bounds__(256) kv8_runs_kernel(const Kv8WriteArgs a) {
-    const int32_t blk = run_block(a, (int64_t)blockIdx.x * blockDim.x + threadIdx.x);
-    if (blk < 0) return;
-    uint32_t* w = reinterpret_cast<uint32_t*>(a.scale) + (int64_t)blk * a.hkv * 2;
-    if (CLEAR) {
-        atomicAnd(w, ~kSign);
-        atomicAnd(w + 1, ~kSign);
-    } else if (atomicOr(w, kSign) & kSign) {
-        atomicOr(w + 1, kSign);
+// Notes of a call for kv8_write_kernel
+template <int D>
+__global__ void __launch_bounds__(256) kv8_notes(const Kv8WriteArgs a) {
+    const int64_t row = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (row >= a.n) return;
+    const int32_t i = (int32_t)row, s = a.slots[i];
+    if (s < 0 || s >= a.n_slots) return;
+    const int32_t before = i > 0 ? a.slots[i - 1] : -1;
+    if (before >> 4 != s >> 4) atomicOr(reinterpret_cast<uint32_t*>(a.scale) + (int64_t)(s >> 4) * a.hkv * 2, kSign);
+    // (what no row of this slot left there is some code; a later row's note stays)
+    int32_t* note = note_of<D>(a, s);
+    for (int32_t have = *note; have < i || !stores_in(a, have, s);) {
+        const int32_t now = atomicCAS(note, have, i);
+        if (now == have) break;
+        have = now;
     }
 }
 
-template <typename T, int D, int CODE>
-__global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8WriteArgs a) {
+template <typename T, int D, int CODE, int WAVES, bool NOTED>
+__global__ void __launch_bounds__(WAVES * 64) kv8_write_kernel(const Kv8WriteArgs a) {
     typedef Code<CODE> C;
     constexpr int LPO = D / 16;            // lanes of an offset
     constexpr int OPP = 64 / LPO, P = kBlock / OPP;   // offsets per pass, passes
@@ -275,14 +284,34 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
     if (lane == 0) prev = before;
     const uint64_t leads = __builtin_amdgcn_ballot_w64(lane < n_here && mine >= 0 && mine >> 4 != prev >> 4);
     if (leads == 0) return;
-    const int per = 2 * a.hkv, units = __builtin_popcountll(leads) * per;
-    const int c16 = (lane % LPO) * 16;
-    // how many rows of the call store in the block of a run (by the lane of its first row)
-    __shared__ int stored[kWriteRange];
-    if (!a.noted) {
+    const int per = 2 * a.hkv, c16 = (lane % LPO) * 16;
+    uint64_t taken = leads;                     // the runs whose blocks are this workgroup's
+    __shared__ int rows_of[kWriteRange][kBlock];   // noted: of each block (by the lane of the run's first row), its rows or -1
+    __shared__ int stored[kWriteRange];            // else how many rows of the call store there
+    if constexpr (NOTED) {
+        __shared__ unsigned mask;
+        if (wave == 0) {
+            bool first_here = false;
+            if (leads >> lane & 1)
+                first_here = (atomicAnd(reinterpret_cast<uint32_t*>(a.scale) + (int64_t)(mine >> 4) * a.hkv * 2, ~kSign) & kSign) != 0;
+            const uint64_t m = __builtin_amdgcn_ballot_w64(first_here);
+            if (lane == 0) mask = (unsigned)m;
+        }
+        __syncthreads();
+        taken = mask;
+        if (taken == 0) return;
+        for (int i = wave; i < kWriteRange * kBlock / 64; i += WAVES) {
+            const int at = i * 64 / kBlock + lane / kBlock, slot = (__shfl(mine, at) & ~15) + lane % kBlock;
+            if (taken >> at & 1) {
+                const int32_t row = *note_of<D>(a, slot);
+                rows_of[at][lane % kBlock] = stores_in(a, row, slot) ? row : -1;
+            }
+        }
+        __syncthreads();
+    } else {
         if (threadIdx.x < kWriteRange) stored[threadIdx.x] = 0;
         __syncthreads();
-        constexpr int U = 4, EACH = kWriteWaves * 64 * 4;   // slots of a load of all threads
+        constexpr int U = 4, EACH = WAVES * 64 * 4;   // slots of a load of all threads
         for (uint32_t i0 = 0; i0 < (uint32_t)a.n; i0 += U * EACH) {
             i32x4_t s[U];
 #pragma unroll
@@ -316,8 +345,9 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
         }
         __syncthreads();
     }
-    for (int u = (int)blockIdx.y * kWriteWaves + wave; u < units; u += (int)gridDim.y * kWriteWaves) {
-        uint64_t rest = leads;
+    const int units = __builtin_popcountll(taken) * per;
+    for (int u = (int)blockIdx.y * WAVES + wave; u < units; u += (int)gridDim.y * WAVES) {
+        uint64_t rest = taken;
         for (int i = u / per; i > 0; --i) rest &= rest - 1;
         const int first = __builtin_ctzll(rest);
         const int which = u & 1, h = (u % per) >> 1;
@@ -325,40 +355,56 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
         const int blk = __builtin_amdgcn_readlane(mine, first) >> 4;
         int64_t row[P];
         bool fresh = false;
+        if constexpr (NOTED) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) row[p] = -1;
-        auto take = [&](int64_t from, int32_t slot, uint64_t rows) {   // rows of 64 from `from` on
+            for (int p = 0; p < P; ++p) row[p] = rows_of[first][p * OPP + lane / LPO];
+            fresh = rows_of[first][0] >= 0;
+        } else {
 #pragma unroll
-            for (int o = 0; o < kBlock; ++o) {
-                const uint64_t m = __builtin_amdgcn_ballot_w64((slot & 15) == o) & rows;
-                if (m == 0) continue;
-                if (o == 0) fresh = true;
-                if (o % OPP == lane / LPO) row[o / OPP] = from + 63 - __builtin_clzll(m);
+            for (int p = 0; p < P; ++p) row[p] = -1;
+            auto take = [&](int64_t from, int32_t slot, uint64_t rows) {   // rows of 64 from `from` on
+#pragma unroll
+                for (int o = 0; o < kBlock; ++o) {
+                    const uint64_t m = __builtin_amdgcn_ballot_w64((slot & 15) == o) & rows;
+                    if (m == 0) continue;
+                    if (o == 0) fresh = true;
+                    if (o % OPP == lane / LPO) row[o / OPP] = from + 63 - __builtin_clzll(m);
+                }
+            };
+            int32_t slot = mine;
+            uint64_t live = ~0ull << first;   // lanes whose rows come into question
+            int here = 0;                     // rows of the run
+            for (int64_t from = r0;; from += 64) {
+                const uint64_t others = __builtin_amdgcn_ballot_w64((slot >> 4) != blk) & live;
+                const uint64_t run = others ? live & ((others & -others) - 1) : live;
+                here += __builtin_popcountll(run);
+                take(from, slot, run);
+                if (others) break;
+                live = ~0ull;   // (only rows of one slot over and over are more than a wave looks at)
+                slot = slot_of(from + 64 + lane);
             }
-        };
-        int32_t slot = mine;
-        uint64_t live = ~0ull << first;   // lanes whose rows come into question
-        int here = 0;                     // rows of the run
-        for (int64_t from = r0;; from += 64) {
-            const uint64_t others = __builtin_amdgcn_ballot_w64((slot >> 4) != blk) & live;
-            const uint64_t run = others ? live & ((others & -others) - 1) : live;
-            here += __builtin_popcountll(run);
-            take(from, slot, run);
-            if (others) break;
-            live = ~0ull;   // (only rows of one slot over and over are more than a wave looks at)
-            slot = slot_of(from + 64 + lane);
-        }
-        const uint32_t* signs = reinterpret_cast<const uint32_t*>(a.scale) + (int64_t)blk * a.hkv * 2;
-        const bool many = a.noted ? (signs[1] & kSign) != 0 : stored[first] != here;
-        if (many) {   // the block has other runs
-            bool before_it = false;
-            for (int64_t from = 0; from < r0 + first && !before_it; from += 64)
-                before_it = __builtin_amdgcn_ballot_w64(from + lane < r0 + first && slot_of(from + lane) >> 4 == blk) != 0;
-            if (before_it) continue;
-            for (int64_t from = r0 + first; from < a.n; from += 64) {
-                slot = slot_of(from + lane);
-                const uint64_t rows = __builtin_amdgcn_ballot_w64((slot >> 4) == blk);
-                if (rows) take(from, slot, rows);
+            if (stored[first] != here) {   // the block has other runs
+                constexpr int U = 4;   // times 64 rows on their way
+                bool before_it = false;
+                for (int64_t from = 0; from < r0 + first && !before_it; from += 64 * U) {
+                    int32_t it[U];
+#pragma unroll
+                    for (int k = 0; k < U; ++k) it[k] = slot_of(from + 64 * k + lane);
+#pragma unroll
+                    for (int k = 0; k < U; ++k)
+                        before_it |= __builtin_amdgcn_ballot_w64(from + 64 * k + lane < r0 + first && it[k] >> 4 == blk) != 0;
+                }
+                if (before_it) continue;
+                for (int64_t from = r0 + first; from < a.n; from += 64 * U) {
+                    int32_t it[U];
+#pragma unroll
+                    for (int k = 0; k < U; ++k) it[k] = slot_of(from + 64 * k + lane);
+#pragma unroll
+                    for (int k = 0; k < U; ++k) {
+                        const uint64_t rows = __builtin_amdgcn_ballot_w64(it[k] >> 4 == blk);
+                        if (rows) take(from + 64 * k, it[k], rows);
+                    }
+                }
             }
         }
         const T* src = static_cast<const T*>(which ? a.v : a.k);
@@ -413,8 +459,7 @@ __global__ void __launch_bounds__(kWriteWaves * 64) kv8_write_kernel(const Kv8Wr
             }
             *dst = w;
         }
-        // (a noted sign stays until the launch behind this one: waves of the block's other runs may still look for it)
-        if (lane == 0 && s != old) *sp = a.noted && many && h == 0 && which == 1 ? -s : s;
+        if (lane == 0 && s != old) *sp = s;
     }
 }
 
@@ -1663,16 +1708,23 @@ int launch_qk_norm(int dtype, int style, int d, int n, const NormArgs& a, void* 
 }
 
 int launch_kv8_write(int dtype, int code, int d, const Kv8WriteArgs& a, void* stream) {
-    // a block's units over workgroups in y, so that a few tokens fill the chip
-    const int64_t per = 2 * (int64_t)a.hkv;
-    const dim3 grid((unsigned)((a.n + (int64_t)a.range - 1) / a.range), (unsigned)(per + kWriteWaves - 1 < 4 * kWriteWaves ? (per + kWriteWaves - 1) / kWriteWaves : 4));
-    const dim3 rows((unsigned)(((int64_t)a.n + 255) / 256));
-    if (a.noted) hipLaunchKernelGGL((kv8_runs_kernel<false>), rows, dim3(256), 0, (hipStream_t)stream, a);
+    const int per = 2 * a.hkv;   // units of a block
+    const unsigned ranges = (unsigned)(((int64_t)a.n + a.range - 1) / a.range);
     by_types(dtype, d, code, [&](auto t, auto dim, auto c) {
-        hipLaunchKernelGGL((kv8_write_kernel<decltype(t), decltype(dim)::value, decltype(c)::value>), grid, dim3(kWriteWaves * 64), 0,
-                           (hipStream_t)stream, a);
+        constexpr int D = decltype(dim)::value;
+        const auto go = [&](auto waves, auto noted, unsigned y) {
+            constexpr int W = decltype(waves)::value;
+            hipLaunchKernelGGL((kv8_write_kernel<decltype(t), D, decltype(c)::value, W, decltype(noted)::value>), dim3(ranges, y), dim3(W * 64), 0,
+                               (hipStream_t)stream, a);
+        };
+        if (a.n > kWriteScan) {
+            hipLaunchKernelGGL((kv8_notes<D>), dim3((unsigned)(((int64_t)a.n + 255) / 256)), dim3(256), 0, (hipStream_t)stream, a);
+            if (per > kWriteWaves) go(Idx<kNotedWaves>{}, std::true_type{}, 1);
+            else go(Idx<kWriteWaves>{}, std::true_type{}, 1);
+        } else {   // a block's units over workgroups in y, so that a few tokens fill the chip
+            go(Idx<kWriteWaves>{}, std::false_type{}, per <= 3 * kWriteWaves ? (unsigned)((per + kWriteWaves - 1) / kWriteWaves) : 4);
+        }
     });
-    if (a.noted) hipLaunchKernelGGL((kv8_runs_kernel<true>), rows, dim3(256), 0, (hipStream_t)stream, a);
     return hipGetLastError();
 }
 
